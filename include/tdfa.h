@@ -416,6 +416,106 @@ TDFA_API int tdfa_sample_step_at(const tdfa_table *table, const void *logits_dev
 TDFA_API int tdfa_sample_noise(int32_t batch, int32_t n_tokens, uint64_t seed, uint64_t offset,
                       float *noise_dev, void *stream);
 
+/* ---- scoring and training the constrained policy ---------------------------------------------- */
+
+/* A language model that decodes under a constraint is the policy that tdfa_sample_step draws from:
+ * in state q the softmax of logits / temperature over the tokens that q allows (Algorithm 2 with a
+ * sampler).  The calls below score and train that policy on rows of logits, one row per token: the
+ * log-probability of the row's token, its gradient, and two losses made of them.
+ *
+ * Arguments they share:
+ *   table       : the constraint, dense or packed, or NULL: every token is allowed.
+ *   logits_dev, dtype, row_stride : as tdfa_mask_step ([rows][row_stride], rows 16-byte aligned, the
+ *                 first n_tokens of each row are used, nothing behind them is read or written).
+ *   n_tokens    : >= 0; that of the table if there is one.
+ *   states_dev  : device, int32 [rows]: the state before the row's token; may be NULL without a table.
+ *   tokens_dev  : device, int32 [rows].
+ *   temperature : > 0, and log2(e) / temperature finite in binary32.
+ *   workspace_dev, workspace_bytes : device memory for the call's own use, 16-byte aligned, of at least
+ *                 tdfa_loss_workspace_bytes(rows, n_pairs) bytes (n_pairs 0 unless the call has pairs).
+ *                 It need not be cleared, and must not be used by anything else until the call's work is done.
+ * Row i has logits z, allowed set A (of states[i]), token t and c = 1 / temperature.  NaN counts as -inf, as
+ * for the draw, and a logit outside A has no effect whatever it is.  With m the largest z in A and
+ * s the sum over A of exp((z_j - m) c),
+ *     lp = (z_t - m) c - ln s,          p_j = exp((z_j - m) c) / s in A, 0 elsewhere,
+ *     d lp / d z_j = c ([j = t] - p_j) in A, 0 elsewhere.
+ * A row takes part if t is in A, z_t is above -inf and so is lp in binary32.  Of the others one with t = TDFA_NO_TOKEN (padding, a
+ * text that is complete) has lp = 0: nothing was chosen.  Any other has lp = -inf (t is not allowed or no
+ * token, z_t is -inf or NaN, lp overflows, the state is no row of the table).  Rows that take no part have a gradient of
+ * zero and add nothing to a loss.  An allowed logit of +inf makes lp and the row's gradient NaN.
+ * Sums are held in binary32 or more; a gradient is rounded once, to the type of the logits.  Results depend on
+ * the arguments only, not on the order in which anything runs.
+ * The calls enqueue on `stream` and return, allocate nothing and may be captured into a graph.
+ * Errors: INVALID_ARG, DEVICE. */
+
+/* Workspace in bytes; -1 if rows or n_pairs is negative. */
+TDFA_API int64_t tdfa_loss_workspace_bytes(int32_t rows, int32_t n_pairs);
+
+/* logprobs[i] = lp of row i.
+ *   logprobs_dev : device, float [rows], written.
+ *   stats_dev    : device, float [rows][2], or NULL: receives {m, ln s} of every row that takes part and
+ *                  {0, +inf} of the others, for tdfa_token_logprobs_backward. */
+TDFA_API int tdfa_token_logprobs(const tdfa_table *table, const void *logits_dev, int dtype, int32_t rows,
+                        int32_t n_tokens, int64_t row_stride, const int32_t *states_dev, const int32_t *tokens_dev,
+                        float temperature, float *logprobs_dev, float *stats_dev,
+                        void *workspace_dev, int64_t workspace_bytes, void *stream);
+
+/* The gradient of a loss of which d loss / d lp is known: grad[i][j] = grad_logprobs[i] * d lp_i / d z_j.
+ *   stats_dev         : as tdfa_token_logprobs has written it for the same arguments.
+ *   grad_logprobs_dev : device, float [rows].
+ *   grad_dev          : device, [rows][grad_stride] of the type of the logits, rows 16-byte aligned, the first
+ *                       n_tokens of every row are written.  May be logits_dev (with grad_stride = row_stride); the
+ *                       two must not overlap otherwise. */
+TDFA_API int tdfa_token_logprobs_backward(const tdfa_table *table, const void *logits_dev, int dtype, int32_t rows,
+                        int32_t n_tokens, int64_t row_stride, const int32_t *states_dev, const int32_t *tokens_dev,
+                        float temperature, const float *stats_dev, const float *grad_logprobs_dev,
+                        void *grad_dev, int64_t grad_stride, void *stream);
+
+/* The clipped policy loss with a KL term, and its gradient.  With w, lp, old, ref and adv those of a row,
+ *     r      = exp(lp - old)
+ *     l      = -min(r adv, clamp(r, 1 - clip_low, 1 + clip_high) adv) + kl_coef (exp(ref - lp) - (ref - lp) - 1)
+ *     loss   = the sum of w l over the rows that take part
+ *     d l / d lp = -(r adv where it is the smaller one or equal, else 0) + kl_coef (1 - exp(ref - lp))
+ * How the rows are averaged is in the weights (1 / number of tokens, say).  A row of weight 0 takes no part: its
+ * logits are not read, and its lp is reported as 0.
+ *   old_logprobs_dev : device, float [rows]: lp when the tokens were drawn.
+ *   ref_logprobs_dev : device, float [rows]: lp under a reference model; may be NULL if kl_coef is 0 (it is not read then).
+ *   advantages_dev   : device, float [rows].
+ *   weights_dev      : device, float [rows], or NULL: all 1.
+ *   clip_low         : 0 .. 1.   clip_high : >= 0, may be +inf.   kl_coef : finite.
+ *   loss_dev         : device, float [1], written (0 if there are no rows).
+ *   logprobs_dev     : device, float [rows], written: lp.
+ *   grad_dev         : as above, d loss / d logits, or NULL: not wanted. */
+TDFA_API int tdfa_policy_loss(const tdfa_table *table, const void *logits_dev, int dtype, int32_t rows,
+                        int32_t n_tokens, int64_t row_stride, const int32_t *states_dev, const int32_t *tokens_dev,
+                        float temperature, const float *old_logprobs_dev, const float *ref_logprobs_dev,
+                        const float *advantages_dev, const float *weights_dev,
+                        float clip_low, float clip_high, float kl_coef,
+                        float *loss_dev, float *logprobs_dev, void *grad_dev, int64_t grad_stride,
+                        void *workspace_dev, int64_t workspace_bytes, void *stream);
+
+/* The preference loss of paired sequences (log ratios against a reference), and its gradient.  Rows begin[k] ..
+ * begin[k + 1] - 1 are the tokens of sequence k; sequences 2 p and 2 p + 1 are the chosen and the rejected one
+ * of pair p.
+ *     reward_k = beta * the sum of lp - ref over the rows of sequence k that take part     (binary64)
+ *     g_p      = reward_{2p} - reward_{2p + 1}
+ *     loss     = the mean over the pairs of (1 - smoothing) softplus(-g) + smoothing softplus(g)
+ * where softplus(x) = ln(1 + exp(x)); with smoothing = 0 that is -ln of the logistic function of g.  A sequence may have
+ * no rows; rows that belong to no sequence have a gradient of zero.
+ *   ref_logprobs_dev : device, float [rows]: lp under the reference model (read for the rows that take part).
+ *   begin_dev        : device, int32 [2 * n_pairs + 1], not decreasing, in 0 .. rows (what lies outside is cut off there).
+ *   beta             : > 0, finite.   smoothing : 0 .. 1.   n_pairs : >= 0.
+ *   loss_dev         : device, float [1], written (0 if there are no pairs).
+ *   rewards_dev      : device, float [2 * n_pairs], written.
+ *   logprobs_dev     : device, float [rows], written.
+ *   grad_dev         : as above, d loss / d logits, or NULL: not wanted. */
+TDFA_API int tdfa_preference_loss(const tdfa_table *table, const void *logits_dev, int dtype, int32_t rows,
+                        int32_t n_tokens, int64_t row_stride, const int32_t *states_dev, const int32_t *tokens_dev,
+                        float temperature, const float *ref_logprobs_dev, const int32_t *begin_dev, int32_t n_pairs,
+                        float beta, float smoothing,
+                        float *loss_dev, float *rewards_dev, float *logprobs_dev, void *grad_dev, int64_t grad_stride,
+                        void *workspace_dev, int64_t workspace_bytes, void *stream);
+
 /* ---- terminal labels (Section 2.5.1, wildcard matching) -------------------------------------- */
 
 /* Applies terminal edges to a compiled table.  A terminal edge (state, label, target) stands for

@@ -94,6 +94,15 @@ def lib():
         L.tdfa_pda_sample_step.argtypes = [C.c_void_p, C.c_void_p, C.c_int, C.c_int32, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p,
                                            C.c_int32, C.c_float, C.c_int32, C.c_uint64, C.c_uint64, C.c_void_p, C.c_void_p, C.c_void_p,
                                            C.c_void_p]
+        rows = [C.c_void_p, C.c_void_p, C.c_int, C.c_int32, C.c_int32, C.c_int64, C.c_void_p, C.c_void_p, C.c_float]
+        work = [C.c_void_p, C.c_int64, C.c_void_p]
+        L.tdfa_loss_workspace_bytes.restype = C.c_int64
+        L.tdfa_loss_workspace_bytes.argtypes = [C.c_int32, C.c_int32]
+        L.tdfa_token_logprobs.argtypes = rows + [C.c_void_p, C.c_void_p] + work
+        L.tdfa_token_logprobs_backward.argtypes = rows + [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]
+        L.tdfa_policy_loss.argtypes = (rows + [C.c_void_p] * 4 + [C.c_float] * 3 + [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64] + work)
+        L.tdfa_preference_loss.argtypes = (rows + [C.c_void_p, C.c_void_p, C.c_int32, C.c_float, C.c_float] +
+                                           [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64] + work)
         _lib = L
     return _lib
 
@@ -366,6 +375,129 @@ def sample_noise(noise: torch.Tensor, seed: int, offset: int, stream=None) -> No
         raise ValueError("noise must be contiguous float32 [batch, n_tokens]")
     _check(lib().tdfa_sample_noise(noise.shape[0], noise.shape[1], int(seed) & (2 ** 64 - 1),
                                    int(offset) & (2 ** 64 - 1), noise.data_ptr(), _stream(stream)))
+
+
+def _vector(t, name: str, dtype, length: int, device, optional: bool = False):
+    """Address of a contiguous vector of at least `length` elements on the logits' device (None: not given)."""
+    if t is None:
+        if optional:
+            return None
+        raise ValueError(f"{name} is wanted")
+    if t.dtype != dtype or t.device != device or not t.is_contiguous() or t.numel() < length:
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of {length} elements on {device}")
+    return t.data_ptr()
+
+
+def _rows_args(table, logits, states, tokens, temperature):
+    """The leading arguments that the calls which score and train share."""
+    if logits.dtype == torch.float32:
+        dtype = F32
+    elif logits.dtype == torch.bfloat16:
+        dtype = BF16
+    else:
+        raise TypeError("logits must be float32 or bfloat16")
+    if logits.dim() != 2 or not logits.is_cuda or (logits.stride(1) != 1 and logits.shape[1] > 1):
+        raise ValueError("logits must be [rows, n] on the GPU with unit inner stride")
+    rows, n = logits.shape
+    if table is not None:
+        if n < table.n_tokens:
+            raise ValueError("logits have fewer columns than the table has tokens")
+        n = table.n_tokens
+    return (None if table is None else table._h, logits.data_ptr(), dtype, rows, n, logits.stride(0) if rows > 1 else max(logits.stride(0), n),
+            _vector(states, "states", torch.int32, rows, logits.device, table is None), _vector(tokens, "tokens", torch.int32, rows, logits.device),
+            float(temperature))
+
+
+def _grad_args(logits, grad_logits):
+    if grad_logits is None:
+        return None, 0
+    if grad_logits.dtype != logits.dtype or grad_logits.shape != logits.shape or grad_logits.device != logits.device:
+        raise ValueError("the gradient must have the type, shape and device of the logits")
+    if grad_logits.stride(1) != 1 and grad_logits.shape[1] > 1:
+        raise ValueError("the gradient must have unit inner stride")
+    return grad_logits.data_ptr(), max(grad_logits.stride(0), grad_logits.shape[1]) if grad_logits.shape[0] <= 1 else grad_logits.stride(0)
+
+
+def loss_workspace_bytes(rows: int, n_pairs: int = 0) -> int:
+    """tdfa_loss_workspace_bytes."""
+    return int(lib().tdfa_loss_workspace_bytes(rows, n_pairs))
+
+
+def _workspace(workspace, rows, n_pairs, device, stream):
+    """The caller's workspace, or one from torch's allocator, which hands it out again only behind the stream's work."""
+    if workspace is not None:
+        if not workspace.is_contiguous() or workspace.device != device:
+            raise ValueError(f"workspace must be contiguous on {device}")
+        return workspace, workspace.numel() * workspace.element_size()
+    n = lib().tdfa_loss_workspace_bytes(rows, n_pairs)
+    if stream is None:
+        return torch.empty(n, dtype=torch.uint8, device=device), n
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(int(stream), device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(n, dtype=torch.uint8, device=device), n
+
+
+def token_logprobs(table: Table | None, logits: torch.Tensor, states: torch.Tensor | None, tokens: torch.Tensor, logprobs: torch.Tensor,
+                   temperature: float = 1.0, stats: torch.Tensor | None = None, workspace: torch.Tensor | None = None, stream=None) -> None:
+    """tdfa_token_logprobs.  logits: [rows, >= n_tokens] float32 or bfloat16 on the GPU; table None: no
+    constraint, and every column is a token.  states, tokens: int32 [rows]; logprobs: float32 [rows], and
+    stats: float32 [rows, 2] if the gradient is wanted later, are written.  workspace: at least
+    loss_workspace_bytes(rows) bytes, allocated by torch if not given."""
+    a = _rows_args(table, logits, states, tokens, temperature)
+    rows, dev = a[3], logits.device
+    out = _vector(logprobs, "logprobs", torch.float32, rows, dev), _vector(stats, "stats", torch.float32, 2 * rows, dev, True)
+    ws, n = _workspace(workspace, rows, 0, dev, stream)
+    _check(lib().tdfa_token_logprobs(*a, *out, ws.data_ptr(), n, _stream(stream)))
+
+
+def token_logprobs_backward(table: Table | None, logits: torch.Tensor, states: torch.Tensor | None, tokens: torch.Tensor, stats: torch.Tensor,
+                            grad_logprobs: torch.Tensor, grad_logits: torch.Tensor, temperature: float = 1.0, stream=None) -> None:
+    """tdfa_token_logprobs_backward.  stats as token_logprobs wrote them for the same arguments;
+    grad_logits has the type and shape of logits, may be logits, and its first n_tokens columns are written."""
+    a = _rows_args(table, logits, states, tokens, temperature)
+    rows, dev = a[3], logits.device
+    if grad_logits is None:
+        raise ValueError("grad_logits is wanted")
+    _check(lib().tdfa_token_logprobs_backward(*a, _vector(stats, "stats", torch.float32, 2 * rows, dev),
+                                              _vector(grad_logprobs, "grad_logprobs", torch.float32, rows, dev),
+                                              *_grad_args(logits, grad_logits), _stream(stream)))
+
+
+def policy_loss(table: Table | None, logits: torch.Tensor, states: torch.Tensor | None, tokens: torch.Tensor, old_logprobs: torch.Tensor,
+                advantages: torch.Tensor, loss: torch.Tensor, logprobs: torch.Tensor, grad_logits: torch.Tensor | None = None,
+                ref_logprobs: torch.Tensor | None = None, weights: torch.Tensor | None = None, temperature: float = 1.0, clip=(0.2, 0.2),
+                kl_coef: float = 0.0, workspace: torch.Tensor | None = None, stream=None) -> None:
+    """tdfa_policy_loss.  Rows as token_logprobs; old_logprobs, advantages, ref_logprobs, weights: float32
+    [rows]; loss: float32 [1], logprobs: float32 [rows] and grad_logits (if given) are written.  clip: how
+    far the ratio may go below and above 1."""
+    a = _rows_args(table, logits, states, tokens, temperature)
+    rows, dev, f32 = a[3], logits.device, torch.float32
+    vectors = (_vector(old_logprobs, "old_logprobs", f32, rows, dev), _vector(ref_logprobs, "ref_logprobs", f32, rows, dev, True),
+               _vector(advantages, "advantages", f32, rows, dev), _vector(weights, "weights", f32, rows, dev, True))
+    out = _vector(loss, "loss", f32, 1, dev), _vector(logprobs, "logprobs", f32, rows, dev)
+    ws, n = _workspace(workspace, rows, 0, dev, stream)
+    _check(lib().tdfa_policy_loss(*a, *vectors, float(clip[0]), float(clip[1]), float(kl_coef), *out, *_grad_args(logits, grad_logits),
+                                  ws.data_ptr(), n, _stream(stream)))
+
+
+def preference_loss(table: Table | None, logits: torch.Tensor, states: torch.Tensor | None, tokens: torch.Tensor, ref_logprobs: torch.Tensor,
+                    begin: torch.Tensor, loss: torch.Tensor, rewards: torch.Tensor, logprobs: torch.Tensor,
+                    grad_logits: torch.Tensor | None = None, temperature: float = 1.0, beta: float = 0.1, smoothing: float = 0.0,
+                    workspace: torch.Tensor | None = None, stream=None) -> None:
+    """tdfa_preference_loss.  Rows as token_logprobs; begin: int32 [2 * pairs + 1], sequence k is rows
+    begin[k] .. begin[k + 1] - 1, chosen and rejected in turn; loss: float32 [1], rewards: float32
+    [2 * pairs], logprobs: float32 [rows] and grad_logits (if given) are written."""
+    a = _rows_args(table, logits, states, tokens, temperature)
+    rows, dev, f32 = a[3], logits.device, torch.float32
+    if begin.dim() != 1 or begin.numel() % 2 == 0:
+        raise ValueError("begin must be [2 * pairs + 1]")
+    pairs = begin.numel() // 2
+    vectors = _vector(ref_logprobs, "ref_logprobs", f32, rows, dev), _vector(begin, "begin", torch.int32, 1, dev)
+    out = (_vector(loss, "loss", f32, 1, dev), _vector(rewards, "rewards", f32, 2 * pairs, dev), _vector(logprobs, "logprobs", f32, rows, dev))
+    ws, n = _workspace(workspace, rows, pairs, dev, stream)
+    _check(lib().tdfa_preference_loss(*a, *vectors, pairs, float(beta), float(smoothing), *out, *_grad_args(logits, grad_logits),
+                                      ws.data_ptr(), n, _stream(stream)))
 
 
 def advance_tokens(table: Table, states: torch.Tensor, tokens: torch.Tensor, history: torch.Tensor,

@@ -2,6 +2,7 @@
 // packing, and kernel launches.  Every table entry, mask and token choice is computed by the
 // kernels; the host packs the vocabulary and prepares an automaton for them (plan.hip).
 #include <algorithm>
+#include <cmath>
 #include <cstdarg>
 #include <cstdio>
 #include <cstdlib>
@@ -1782,6 +1783,165 @@ int tdfa_sample_noise(int32_t batch, int32_t n_tokens, uint64_t seed, uint64_t o
     if (batch == 0 || n_tokens == 0) return TDFA_OK;
     if (!noise_dev) return fail(TDFA_E_INVALID_ARG, "noise is NULL");
     return launch_sample_noise(batch, n_tokens, seed, offset, noise_dev, static_cast<hipStream_t>(stream));
+}
+
+namespace {
+
+// Whether the bytes of two sets of rows may meet.
+bool rows_meet(const void* x, int64_t x_stride, const void* y, int64_t y_stride, int64_t rows, int64_t n_tokens, int64_t esz)
+{
+    const uintptr_t x0 = reinterpret_cast<uintptr_t>(x), y0 = reinterpret_cast<uintptr_t>(y);
+    const uintptr_t xb = (uintptr_t)(((rows - 1) * x_stride + n_tokens) * esz), yb = (uintptr_t)(((rows - 1) * y_stride + n_tokens) * esz);
+    return x0 < y0 + yb && y0 < x0 + xb;
+}
+
+// Argument checks and kernel arguments shared by the calls that score and train.
+int prepare_rows(const tdfa_table* table, const void* logits_dev, int dtype, int32_t rows, int32_t n_tokens, int64_t row_stride,
+                 const int32_t* states_dev, const int32_t* tokens_dev, float temperature, tdfa::TokenRows* a)
+{
+    if (dtype != TDFA_F32 && dtype != TDFA_BF16) return fail(TDFA_E_INVALID_ARG, "unknown dtype %d", dtype);
+    if (rows < 0 || n_tokens < 0) return fail(TDFA_E_INVALID_ARG, "rows %d or n_tokens %d is negative", rows, n_tokens);
+    if (table && table->n_tokens != n_tokens) return fail(TDFA_E_INVALID_ARG, "n_tokens %d differs from the table's %d", n_tokens, table->n_tokens);
+    if (!(temperature > 0.0f)) return fail(TDFA_E_INVALID_ARG, "temperature %g is not positive", (double)temperature);
+    const volatile float one = 1.0f;                     // divided at run time, rounded once to binary32
+    const float inv_t = one / temperature;
+    if (!(inv_t > 0.0f) || inv_t > 2.3e38f)
+        return fail(TDFA_E_INVALID_ARG, "log2(e) / temperature is not finite for temperature %g", (double)temperature);
+    if (row_stride < n_tokens) return fail(TDFA_E_INVALID_ARG, "row_stride %lld < n_tokens %d", (long long)row_stride, n_tokens);
+    const int64_t esz = dtype == TDFA_F32 ? 4 : 2;
+    if (rows > 0) {
+        if ((!logits_dev && n_tokens > 0) || !tokens_dev || (table && !states_dev))
+            return fail(TDFA_E_INVALID_ARG, "logits, tokens or states is NULL");
+        if ((reinterpret_cast<uintptr_t>(logits_dev) & 15) || (rows > 1 && ((row_stride * esz) & 15)))
+            return fail(TDFA_E_INVALID_ARG, "logits rows must be 16-byte aligned");
+    }
+    *a = tdfa::TokenRows();
+    if (table) {
+        a->allow = table->allow;
+        a->row_allowed = table->row_allowed;
+        a->n_states = table->n_rows;
+        a->row_words = table->row_words;
+    }
+    a->logits = logits_dev;
+    a->dtype = dtype;
+    a->row_stride = row_stride;
+    a->rows = rows;
+    a->n_tokens = n_tokens;
+    a->states = states_dev;
+    a->tokens = tokens_dev;
+    a->inv_t = inv_t;
+    return TDFA_OK;
+}
+
+int check_grad(const tdfa::TokenRows& a, const void* grad_dev, int64_t grad_stride)
+{
+    const int64_t esz = a.dtype == TDFA_F32 ? 4 : 2;
+    if (a.rows == 0 || a.n_tokens == 0) return TDFA_OK;
+    if (grad_stride < a.n_tokens) return fail(TDFA_E_INVALID_ARG, "grad_stride %lld < n_tokens %d", (long long)grad_stride, a.n_tokens);
+    if ((reinterpret_cast<uintptr_t>(grad_dev) & 15) || (a.rows > 1 && ((grad_stride * esz) & 15)))
+        return fail(TDFA_E_INVALID_ARG, "gradient rows must be 16-byte aligned");
+    const bool same = grad_dev == a.logits && (a.rows == 1 || grad_stride == a.row_stride);
+    if (!same && rows_meet(a.logits, a.row_stride, grad_dev, grad_stride, a.rows, a.n_tokens, esz))
+        return fail(TDFA_E_INVALID_ARG, "the gradient overlaps the logits without being the same rows");
+    return TDFA_OK;
+}
+
+int check_workspace(const void* workspace_dev, int64_t workspace_bytes, int64_t rows, int64_t n_pairs)
+{
+    const int64_t need = tdfa::loss_workspace(rows, n_pairs);
+    if (need == 0) return TDFA_OK;
+    if (!workspace_dev || workspace_bytes < need)
+        return fail(TDFA_E_INVALID_ARG, "workspace of %lld bytes, %lld are wanted", workspace_dev ? (long long)workspace_bytes : 0LL, (long long)need);
+    if (reinterpret_cast<uintptr_t>(workspace_dev) & 15) return fail(TDFA_E_INVALID_ARG, "workspace must be 16-byte aligned");
+    return TDFA_OK;
+}
+
+bool misaligned(const void* p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) != 0; }
+
+}  // namespace
+
+int64_t tdfa_loss_workspace_bytes(int32_t rows, int32_t n_pairs)
+{
+    return rows < 0 || n_pairs < 0 ? -1 : tdfa::loss_workspace(rows, n_pairs);
+}
+
+int tdfa_token_logprobs(const tdfa_table* table, const void* logits_dev, int dtype, int32_t rows, int32_t n_tokens, int64_t row_stride,
+                        const int32_t* states_dev, const int32_t* tokens_dev, float temperature, float* logprobs_dev, float* stats_dev,
+                        void* workspace_dev, int64_t workspace_bytes, void* stream)
+{
+    clear_error();
+    tdfa::TokenRows a;
+    int rc = prepare_rows(table, logits_dev, dtype, rows, n_tokens, row_stride, states_dev, tokens_dev, temperature, &a);
+    if (rc != TDFA_OK || rows == 0) return rc;
+    if (!logprobs_dev) return fail(TDFA_E_INVALID_ARG, "logprobs is NULL");
+    if (misaligned(stats_dev, 8)) return fail(TDFA_E_INVALID_ARG, "stats must be 8-byte aligned");
+    rc = check_workspace(workspace_dev, workspace_bytes, rows, 0);
+    if (rc != TDFA_OK) return rc;
+    return launch_token_logprobs(a, logprobs_dev, stats_dev, workspace_dev, static_cast<hipStream_t>(stream));
+}
+
+int tdfa_token_logprobs_backward(const tdfa_table* table, const void* logits_dev, int dtype, int32_t rows, int32_t n_tokens, int64_t row_stride,
+                                 const int32_t* states_dev, const int32_t* tokens_dev, float temperature, const float* stats_dev,
+                                 const float* grad_logprobs_dev, void* grad_dev, int64_t grad_stride, void* stream)
+{
+    clear_error();
+    tdfa::TokenRows a;
+    int rc = prepare_rows(table, logits_dev, dtype, rows, n_tokens, row_stride, states_dev, tokens_dev, temperature, &a);
+    if (rc != TDFA_OK || rows == 0 || n_tokens == 0) return rc;
+    if (!stats_dev || !grad_logprobs_dev || !grad_dev) return fail(TDFA_E_INVALID_ARG, "stats, grad_logprobs or the gradient is NULL");
+    if (misaligned(stats_dev, 8)) return fail(TDFA_E_INVALID_ARG, "stats must be 8-byte aligned");
+    rc = check_grad(a, grad_dev, grad_stride);
+    if (rc != TDFA_OK) return rc;
+    return launch_token_grad(a, stats_dev, grad_logprobs_dev, grad_dev, grad_stride, static_cast<hipStream_t>(stream));
+}
+
+int tdfa_policy_loss(const tdfa_table* table, const void* logits_dev, int dtype, int32_t rows, int32_t n_tokens, int64_t row_stride,
+                     const int32_t* states_dev, const int32_t* tokens_dev, float temperature, const float* old_logprobs_dev,
+                     const float* ref_logprobs_dev, const float* advantages_dev, const float* weights_dev, float clip_low, float clip_high,
+                     float kl_coef, float* loss_dev, float* logprobs_dev, void* grad_dev, int64_t grad_stride,
+                     void* workspace_dev, int64_t workspace_bytes, void* stream)
+{
+    clear_error();
+    tdfa::TokenRows a;
+    int rc = prepare_rows(table, logits_dev, dtype, rows, n_tokens, row_stride, states_dev, tokens_dev, temperature, &a);
+    if (rc != TDFA_OK) return rc;
+    if (!(clip_low >= 0.0f && clip_low <= 1.0f) || !(clip_high >= 0.0f))
+        return fail(TDFA_E_INVALID_ARG, "clip_low %g is not in 0 .. 1, or clip_high %g is negative", (double)clip_low, (double)clip_high);
+    if (!std::isfinite(kl_coef)) return fail(TDFA_E_INVALID_ARG, "kl_coef %g is not finite", (double)kl_coef);
+    if (!loss_dev) return fail(TDFA_E_INVALID_ARG, "loss is NULL");
+    if (rows > 0 && (!old_logprobs_dev || !advantages_dev || !logprobs_dev))
+        return fail(TDFA_E_INVALID_ARG, "old_logprobs, advantages or logprobs is NULL");
+    if (rows > 0 && kl_coef != 0.0f && !ref_logprobs_dev) return fail(TDFA_E_INVALID_ARG, "a KL term wants ref_logprobs");
+    if (grad_dev) rc = check_grad(a, grad_dev, grad_stride);
+    if (rc == TDFA_OK) rc = check_workspace(workspace_dev, workspace_bytes, rows, 0);
+    if (rc != TDFA_OK) return rc;
+    a.weights = weights_dev;
+    const tdfa::PolicyArgs p = {old_logprobs_dev, kl_coef != 0.0f ? ref_logprobs_dev : nullptr, advantages_dev, 1.0f - clip_low, 1.0f + clip_high, kl_coef};
+    return launch_policy_loss(a, p, loss_dev, logprobs_dev, n_tokens > 0 ? grad_dev : nullptr, grad_stride, workspace_dev,
+                              static_cast<hipStream_t>(stream));
+}
+
+int tdfa_preference_loss(const tdfa_table* table, const void* logits_dev, int dtype, int32_t rows, int32_t n_tokens, int64_t row_stride,
+                         const int32_t* states_dev, const int32_t* tokens_dev, float temperature, const float* ref_logprobs_dev,
+                         const int32_t* begin_dev, int32_t n_pairs, float beta, float smoothing, float* loss_dev, float* rewards_dev,
+                         float* logprobs_dev, void* grad_dev, int64_t grad_stride, void* workspace_dev, int64_t workspace_bytes, void* stream)
+{
+    clear_error();
+    tdfa::TokenRows a;
+    int rc = prepare_rows(table, logits_dev, dtype, rows, n_tokens, row_stride, states_dev, tokens_dev, temperature, &a);
+    if (rc != TDFA_OK) return rc;
+    if (n_pairs < 0) return fail(TDFA_E_INVALID_ARG, "n_pairs %d is negative", n_pairs);
+    if (!(beta > 0.0f) || !std::isfinite(beta)) return fail(TDFA_E_INVALID_ARG, "beta %g is not positive and finite", (double)beta);
+    if (!(smoothing >= 0.0f && smoothing <= 1.0f)) return fail(TDFA_E_INVALID_ARG, "smoothing %g is not in 0 .. 1", (double)smoothing);
+    if (!loss_dev) return fail(TDFA_E_INVALID_ARG, "loss is NULL");
+    if (n_pairs > 0 && (!begin_dev || !rewards_dev)) return fail(TDFA_E_INVALID_ARG, "begin or rewards is NULL");
+    if (rows > 0 && (!ref_logprobs_dev || !logprobs_dev)) return fail(TDFA_E_INVALID_ARG, "ref_logprobs or logprobs is NULL");
+    if (grad_dev) rc = check_grad(a, grad_dev, grad_stride);
+    if (rc == TDFA_OK) rc = check_workspace(workspace_dev, workspace_bytes, rows, n_pairs);
+    if (rc != TDFA_OK) return rc;
+    const tdfa::PairArgs p = {ref_logprobs_dev, begin_dev, n_pairs, beta, smoothing, rewards_dev};
+    return launch_preference_loss(a, p, loss_dev, logprobs_dev, n_tokens > 0 ? grad_dev : nullptr, grad_stride, workspace_dev,
+                                  static_cast<hipStream_t>(stream));
 }
 
 int tdfa_table_apply_terminals(tdfa_table* table, int32_t n_edges, const int32_t* edge_state_host,

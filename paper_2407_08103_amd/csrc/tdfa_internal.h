@@ -260,6 +260,46 @@ int launch_sample_noise(int32_t batch, int32_t n_tokens, uint64_t seed, uint64_t
 int launch_advance_tokens(const MaskArgs& table, int32_t batch, int32_t k, const int32_t* states, const int32_t* tokens,
                           int32_t* history, int32_t* n_valid, hipStream_t stream);
 
+// Rows of logits with a token each, under a constraint or none (loss.hip).
+struct TokenRows {
+    const uint32_t* allow;              // allowed-bit rows of the table, or NULL: every token is allowed
+    const uint32_t* row_allowed;        // [n_states] tokens each state allows, or NULL if not known
+    int64_t n_states;
+    int64_t row_words;
+    const void* logits;
+    int dtype;
+    int64_t row_stride;
+    int64_t rows;
+    int32_t n_tokens;
+    const int32_t* states;
+    const int32_t* tokens;
+    const float* weights;               // [rows] or NULL; a row of weight 0 takes no part
+    float inv_t;
+};
+struct PolicyArgs {
+    const float* old_logprobs;
+    const float* ref_logprobs;          // or NULL: no KL term
+    const float* advantages;
+    float clip_low, clip_high;          // bounds of the ratio
+    float kl_coef;
+};
+struct PairArgs {
+    const float* ref_logprobs;
+    const int32_t* begin;               // [2 n_pairs + 1]
+    int32_t n_pairs;
+    float beta, smoothing;
+    float* rewards;                     // [2 n_pairs]
+};
+// Bytes of workspace that the launchers below want (16-byte aligned).
+int64_t loss_workspace(int64_t rows, int64_t n_pairs);
+// logprobs: [rows]; stats: [rows][2] or NULL; grad: rows of the type of the logits, or NULL.
+int launch_token_logprobs(const TokenRows& a, float* logprobs, float* stats, void* workspace, hipStream_t stream);
+int launch_token_grad(const TokenRows& a, const float* stats, const float* down, void* grad, int64_t grad_stride, hipStream_t stream);
+int launch_policy_loss(const TokenRows& a, const PolicyArgs& p, float* loss, float* logprobs, void* grad, int64_t grad_stride, void* workspace,
+                       hipStream_t stream);
+int launch_preference_loss(const TokenRows& a, const PairArgs& p, float* loss, float* logprobs, void* grad, int64_t grad_stride, void* workspace,
+                           hipStream_t stream);
+
 // Between reads and writes of LDS by different lanes of one wavefront: a wavefront's LDS instructions are carried out in order, so
 // that only the compiler is to be kept from moving one past another.
 __device__ __forceinline__ void wave_lds_sync()
