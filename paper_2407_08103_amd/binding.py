@@ -21,6 +21,7 @@ PATH_AUTO, PATH_WALK, PATH_PAIRS, PATH_STAGED = 0, 1, 2, 3
 OK = 0
 
 _lib = None
+_LOGITS = {torch.float32: F32, torch.bfloat16: BF16}        # element types of logits
 
 
 class TdfaError(RuntimeError):
@@ -113,8 +114,8 @@ def _check(rc: int):
 
 
 def _stream(stream) -> int:
-    if stream is None:
-        return torch.cuda.current_stream().cuda_stream
+    if stream is None:                             # torch.cuda.current_stream().cuda_stream, without the object around it
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
@@ -377,45 +378,47 @@ def sample_noise(noise: torch.Tensor, seed: int, offset: int, stream=None) -> No
                                    int(offset) & (2 ** 64 - 1), noise.data_ptr(), _stream(stream)))
 
 
-def _vector(t, name: str, dtype, length: int, device, optional: bool = False):
+def _vector(t, name: str, dtype, length: int, device: int, optional: bool = False):
     """Address of a contiguous vector of at least `length` elements on the logits' device (None: not given)."""
     if t is None:
         if optional:
             return None
         raise ValueError(f"{name} is wanted")
-    if t.dtype != dtype or t.device != device or not t.is_contiguous() or t.numel() < length:
-        raise ValueError(f"{name} must be a contiguous {dtype} tensor of {length} elements on {device}")
+    if t.dtype is not dtype or t.get_device() != device or not t.is_contiguous() or t.numel() < length:
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of {length} elements on the logits' device")
     return t.data_ptr()
 
 
 def _rows_args(table, logits, states, tokens, temperature):
     """The leading arguments that the calls which score and train share."""
-    if logits.dtype == torch.float32:
-        dtype = F32
-    elif logits.dtype == torch.bfloat16:
-        dtype = BF16
-    else:
+    dtype = _LOGITS.get(logits.dtype)
+    if dtype is None:
         raise TypeError("logits must be float32 or bfloat16")
-    if logits.dim() != 2 or not logits.is_cuda or (logits.stride(1) != 1 and logits.shape[1] > 1):
-        raise ValueError("logits must be [rows, n] on the GPU with unit inner stride")
-    rows, n = logits.shape
+    if logits.dim() != 2 or not logits.is_cuda:
+        raise ValueError("logits must be [rows, n] on the GPU")
+    (rows, n), (stride, inner), device = logits.shape, logits.stride(), logits.get_device()
+    if inner != 1 and n > 1:
+        raise ValueError("logits must have unit inner stride")
+    if rows <= 1:
+        stride = max(stride, n)
+    handle = None
     if table is not None:
         if n < table.n_tokens:
             raise ValueError("logits have fewer columns than the table has tokens")
-        n = table.n_tokens
-    return (None if table is None else table._h, logits.data_ptr(), dtype, rows, n, logits.stride(0) if rows > 1 else max(logits.stride(0), n),
-            _vector(states, "states", torch.int32, rows, logits.device, table is None), _vector(tokens, "tokens", torch.int32, rows, logits.device),
-            float(temperature))
+        handle, n = table._h, table.n_tokens
+    return (handle, logits.data_ptr(), dtype, rows, n, stride, _vector(states, "states", torch.int32, rows, device, table is None),
+            _vector(tokens, "tokens", torch.int32, rows, device), float(temperature))
 
 
 def _grad_args(logits, grad_logits):
     if grad_logits is None:
         return None, 0
-    if grad_logits.dtype != logits.dtype or grad_logits.shape != logits.shape or grad_logits.device != logits.device:
+    if grad_logits.dtype is not logits.dtype or grad_logits.shape != logits.shape or grad_logits.get_device() != logits.get_device():
         raise ValueError("the gradient must have the type, shape and device of the logits")
-    if grad_logits.stride(1) != 1 and grad_logits.shape[1] > 1:
+    (rows, n), (stride, inner) = grad_logits.shape, grad_logits.stride()
+    if inner != 1 and n > 1:
         raise ValueError("the gradient must have unit inner stride")
-    return grad_logits.data_ptr(), max(grad_logits.stride(0), grad_logits.shape[1]) if grad_logits.shape[0] <= 1 else grad_logits.stride(0)
+    return grad_logits.data_ptr(), max(stride, n) if rows <= 1 else stride
 
 
 def loss_workspace_bytes(rows: int, n_pairs: int = 0) -> int:
@@ -423,19 +426,22 @@ def loss_workspace_bytes(rows: int, n_pairs: int = 0) -> int:
     return int(lib().tdfa_loss_workspace_bytes(rows, n_pairs))
 
 
-def _workspace(workspace, rows, n_pairs, device, stream):
-    """The caller's workspace, or one from torch's allocator, which hands it out again only behind the stream's work."""
+def _workspace(workspace, rows, n_pairs, logits, stream):
+    """Address and size of the caller's workspace, or of one from torch's allocator, which hands it out again only behind the
+    work of the stream that it was allocated on; and the tensor, to be held until the call is made."""
     if workspace is not None:
-        if not workspace.is_contiguous() or workspace.device != device:
-            raise ValueError(f"workspace must be contiguous on {device}")
-        return workspace, workspace.numel() * workspace.element_size()
-    n = lib().tdfa_loss_workspace_bytes(rows, n_pairs)
-    if stream is None:
-        return torch.empty(n, dtype=torch.uint8, device=device), n
-    if not isinstance(stream, torch.cuda.Stream):
-        stream = torch.cuda.ExternalStream(int(stream), device=device)
-    with torch.cuda.stream(stream):
-        return torch.empty(n, dtype=torch.uint8, device=device), n
+        if not workspace.is_contiguous() or workspace.device != logits.device:
+            raise ValueError("workspace must be contiguous on the logits' device")
+    else:
+        n = lib().tdfa_loss_workspace_bytes(rows, n_pairs)
+        if stream is None:
+            workspace = torch.empty(n, dtype=torch.uint8, device=logits.device)
+        else:
+            if not isinstance(stream, torch.cuda.Stream):
+                stream = torch.cuda.ExternalStream(int(stream), device=logits.device)
+            with torch.cuda.stream(stream):
+                workspace = torch.empty(n, dtype=torch.uint8, device=logits.device)
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
 
 
 def token_logprobs(table: Table | None, logits: torch.Tensor, states: torch.Tensor | None, tokens: torch.Tensor, logprobs: torch.Tensor,
@@ -445,10 +451,10 @@ def token_logprobs(table: Table | None, logits: torch.Tensor, states: torch.Tens
     stats: float32 [rows, 2] if the gradient is wanted later, are written.  workspace: at least
     loss_workspace_bytes(rows) bytes, allocated by torch if not given."""
     a = _rows_args(table, logits, states, tokens, temperature)
-    rows, dev = a[3], logits.device
+    rows, dev = a[3], logits.get_device()
     out = _vector(logprobs, "logprobs", torch.float32, rows, dev), _vector(stats, "stats", torch.float32, 2 * rows, dev, True)
-    ws, n = _workspace(workspace, rows, 0, dev, stream)
-    _check(lib().tdfa_token_logprobs(*a, *out, ws.data_ptr(), n, _stream(stream)))
+    ws, n, _held = _workspace(workspace, rows, 0, logits, stream)
+    _check(lib().tdfa_token_logprobs(*a, *out, ws, n, _stream(stream)))
 
 
 def token_logprobs_backward(table: Table | None, logits: torch.Tensor, states: torch.Tensor | None, tokens: torch.Tensor, stats: torch.Tensor,
@@ -456,7 +462,7 @@ def token_logprobs_backward(table: Table | None, logits: torch.Tensor, states: t
     """tdfa_token_logprobs_backward.  stats as token_logprobs wrote them for the same arguments;
     grad_logits has the type and shape of logits, may be logits, and its first n_tokens columns are written."""
     a = _rows_args(table, logits, states, tokens, temperature)
-    rows, dev = a[3], logits.device
+    rows, dev = a[3], logits.get_device()
     if grad_logits is None:
         raise ValueError("grad_logits is wanted")
     _check(lib().tdfa_token_logprobs_backward(*a, _vector(stats, "stats", torch.float32, 2 * rows, dev),
@@ -472,13 +478,13 @@ def policy_loss(table: Table | None, logits: torch.Tensor, states: torch.Tensor 
     [rows]; loss: float32 [1], logprobs: float32 [rows] and grad_logits (if given) are written.  clip: how
     far the ratio may go below and above 1."""
     a = _rows_args(table, logits, states, tokens, temperature)
-    rows, dev, f32 = a[3], logits.device, torch.float32
+    rows, dev, f32 = a[3], logits.get_device(), torch.float32
     vectors = (_vector(old_logprobs, "old_logprobs", f32, rows, dev), _vector(ref_logprobs, "ref_logprobs", f32, rows, dev, True),
                _vector(advantages, "advantages", f32, rows, dev), _vector(weights, "weights", f32, rows, dev, True))
     out = _vector(loss, "loss", f32, 1, dev), _vector(logprobs, "logprobs", f32, rows, dev)
-    ws, n = _workspace(workspace, rows, 0, dev, stream)
+    ws, n, _held = _workspace(workspace, rows, 0, logits, stream)
     _check(lib().tdfa_policy_loss(*a, *vectors, float(clip[0]), float(clip[1]), float(kl_coef), *out, *_grad_args(logits, grad_logits),
-                                  ws.data_ptr(), n, _stream(stream)))
+                                  ws, n, _stream(stream)))
 
 
 def preference_loss(table: Table | None, logits: torch.Tensor, states: torch.Tensor | None, tokens: torch.Tensor, ref_logprobs: torch.Tensor,
@@ -489,15 +495,15 @@ def preference_loss(table: Table | None, logits: torch.Tensor, states: torch.Ten
     begin[k] .. begin[k + 1] - 1, chosen and rejected in turn; loss: float32 [1], rewards: float32
     [2 * pairs], logprobs: float32 [rows] and grad_logits (if given) are written."""
     a = _rows_args(table, logits, states, tokens, temperature)
-    rows, dev, f32 = a[3], logits.device, torch.float32
+    rows, dev, f32 = a[3], logits.get_device(), torch.float32
     if begin.dim() != 1 or begin.numel() % 2 == 0:
         raise ValueError("begin must be [2 * pairs + 1]")
     pairs = begin.numel() // 2
     vectors = _vector(ref_logprobs, "ref_logprobs", f32, rows, dev), _vector(begin, "begin", torch.int32, 1, dev)
     out = (_vector(loss, "loss", f32, 1, dev), _vector(rewards, "rewards", f32, 2 * pairs, dev), _vector(logprobs, "logprobs", f32, rows, dev))
-    ws, n = _workspace(workspace, rows, pairs, dev, stream)
+    ws, n, _held = _workspace(workspace, rows, pairs, logits, stream)
     _check(lib().tdfa_preference_loss(*a, *vectors, pairs, float(beta), float(smoothing), *out, *_grad_args(logits, grad_logits),
-                                      ws.data_ptr(), n, _stream(stream)))
+                                      ws, n, _stream(stream)))
 
 
 def advance_tokens(table: Table, states: torch.Tensor, tokens: torch.Tensor, history: torch.Tensor,
