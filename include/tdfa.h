@@ -427,7 +427,7 @@ TDFA_API int tdfa_sample_noise(int32_t batch, int32_t n_tokens, uint64_t seed, u
  *   table       : the constraint, dense or packed, or NULL: every token is allowed.
  *   logits_dev, dtype, row_stride : as tdfa_mask_step ([rows][row_stride], rows 16-byte aligned, the
  *                 first n_tokens of each row are used, nothing behind them is read or written).
- *   n_tokens    : >= 0; that of the table if there is one.
+ *   n_tokens    : 0 .. 2^24; that of the table if there is one.
  *   states_dev  : device, int32 [rows]: the state before the row's token; may be NULL without a table.
  *   tokens_dev  : device, int32 [rows].
  *   temperature : > 0, and log2(e) / temperature finite in binary32.

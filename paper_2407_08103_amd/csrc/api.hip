@@ -1795,12 +1795,15 @@ bool rows_meet(const void* x, int64_t x_stride, const void* y, int64_t y_stride,
     return x0 < y0 + yb && y0 < x0 + xb;
 }
 
+constexpr int32_t kMaxTokens = 1 << 24;                  // of a vocabulary; the kernels reach a row by 32-bit offsets
+
 // Argument checks and kernel arguments shared by the calls that score and train.
 int prepare_rows(const tdfa_table* table, const void* logits_dev, int dtype, int32_t rows, int32_t n_tokens, int64_t row_stride,
                  const int32_t* states_dev, const int32_t* tokens_dev, float temperature, tdfa::TokenRows* a)
 {
     if (dtype != TDFA_F32 && dtype != TDFA_BF16) return fail(TDFA_E_INVALID_ARG, "unknown dtype %d", dtype);
     if (rows < 0 || n_tokens < 0) return fail(TDFA_E_INVALID_ARG, "rows %d or n_tokens %d is negative", rows, n_tokens);
+    if (n_tokens > kMaxTokens) return fail(TDFA_E_INVALID_ARG, "n_tokens %d exceeds %d", n_tokens, kMaxTokens);
     if (table && table->n_tokens != n_tokens) return fail(TDFA_E_INVALID_ARG, "n_tokens %d differs from the table's %d", n_tokens, table->n_tokens);
     if (!(temperature > 0.0f)) return fail(TDFA_E_INVALID_ARG, "temperature %g is not positive", (double)temperature);
     const volatile float one = 1.0f;                     // divided at run time, rounded once to binary32

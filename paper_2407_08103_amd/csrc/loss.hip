@@ -81,17 +81,17 @@ struct Row {
     float lp;                  // of a row that is not read
 };
 
-// (The loads do not wait for one another.)
+// (i is the same in all lanes of a wavefront.  The loads do not wait for one another.)
 __device__ __forceinline__ Row row_of(const TokenRows& a, int64_t i)
 {
-    const int32_t token = a.tokens[i], q = a.allow ? a.states[i] : 0;
+    const int32_t token = __builtin_amdgcn_readfirstlane(a.tokens[i]), q = a.allow ? __builtin_amdgcn_readfirstlane(a.states[i]) : 0;
     const float w = a.weights ? a.weights[i] : 1.0f;
     Row r = {nullptr, token, false, 0.0f};
     if (token == TDFA_NO_TOKEN || w == 0.0f) return r;
     r.lp = -INFINITY;
     if (token < 0 || token >= a.n_tokens || (a.allow && (q < 0 || q >= a.n_states))) return r;
     if (a.allow) r.bits = a.allow + (int64_t)q * a.row_words;
-    r.read = true;
+    r.read = true;                                         // (and lp is -inf if the token turns out not to be allowed)
     return r;
 }
 
@@ -107,15 +107,6 @@ __device__ __forceinline__ float token_logit(const Row& r, const E* row)
     const uint32_t word = r.bits ? r.bits[r.token >> 5] : 0xFFFFFFFFu;
     const float z = to_f32(row[r.token]);
     return (word >> (r.token & 31) & 1) && z == z ? z : -INFINITY;
-}
-
-// The allowed bits of group g, from bit 0 on.
-template <int DTYPE>
-__device__ __forceinline__ uint32_t group_bits(const uint32_t* bits, int32_t g)
-{
-    const uint8_t* b = reinterpret_cast<const uint8_t*>(bits);
-    if constexpr (DTYPE == TDFA_F32) return (uint32_t)(b[g >> 1] >> ((g & 1) * 4)) & 15u;
-    else return b[g];
 }
 
 // Masks of four 16-bit elements by their four allowed bits: an entry of 8 bytes per bit pattern.  16 entries lie in 32
@@ -141,100 +132,128 @@ __device__ __forceinline__ uint4 keep_allowed(uint4 x, uint32_t bits, const uint
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-// A group at a 32-bit offset from an address that the wavefront shares (a row is at most 2^26 bytes).  ONCE: it is not read again,
-// and leaves the caches to what is.
-template <bool ONCE>
-__device__ __forceinline__ uint4 group_at(const uint4* base, int32_t g)
+// The whole groups of a row, and their allowed bits, as buffers: a read behind the end gives 0 and a write there is dropped, both
+// without reaching the memory, so that no access needs a branch and the compiler knows how many are in flight.  (A row is at most
+// 2^26 bytes long.)
+struct RowBuffers {
+    __amdgpu_buffer_rsrc_t x, bits;
+};
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const void* base, uint32_t bytes)
 {
-    const u32x4* at = reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(base) + (uint32_t)g * 16u);
-    const u32x4 x = ONCE ? __builtin_nontemporal_load(at) : *at;
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, (int)bytes, 0x00027000);
+}
+template <int DTYPE>
+__device__ __forceinline__ RowBuffers row_buffers(const void* row, const uint32_t* bits, int32_t n_groups)
+{
+    return {buffer_of(row, (uint32_t)n_groups * 16u), buffer_of(bits, DTYPE == TDFA_F32 ? (uint32_t)(n_groups + 1) / 2u : (uint32_t)n_groups)};
+}
+constexpr uint32_t kNowhere = 0x80000000u;
+constexpr int kPastCaches = 2;             // the nt bit of an access
+// ONCE: what is read is not read again, and leaves the caches to what is.
+template <bool ONCE>
+__device__ __forceinline__ uint4 group_at(__amdgpu_buffer_rsrc_t rows, uint32_t offset)
+{
+    const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(rows, (int)offset, 0, ONCE ? kPastCaches : 0);
     return make_uint4(x.x, x.y, x.z, x.w);
 }
 // Gradients are written past the caches: 1,024 rows of 128,256 tokens in bf16 113 us, 95 so.
-__device__ __forceinline__ void set_group(uint4* base, int32_t g, uint4 x)
+__device__ __forceinline__ void set_group(__amdgpu_buffer_rsrc_t rows, int32_t g, uint4 x)
 {
     const u32x4 y = {x.x, x.y, x.z, x.w};
-    __builtin_nontemporal_store(y, reinterpret_cast<u32x4*>(reinterpret_cast<char*>(base) + (uint32_t)g * 16u));
+    __builtin_amdgcn_raw_buffer_store_b128(y, rows, g * 16, 0, kPastCaches);
 }
 // What is made of one group is finished before the next is begun: the registers of eight elements at a time, not of all.
 __device__ __forceinline__ void next_group() { __builtin_amdgcn_sched_barrier(0); }
 
-// Groups g0 + threadIdx.x + k NT of a row, k < U, with -inf where a token is not allowed or the row is at an end; groups
-// without an allowed token are not fetched.  Bit k of the result: the wavefront has an allowed token in its k-th groups.
-template <int DTYPE, int NT, int U, bool BITS, bool ONCE = false>
-__device__ __forceinline__ uint32_t fetch(const uint4* row, const uint32_t* bits, int32_t g0, int32_t n_groups, const uint2 (&masks)[16], uint4 (&x)[U])
+// The allowed bits of groups g0 + threadIdx.x + k NT of a row, k < U, and the groups; those without an allowed token are not fetched.
+template <int DTYPE, int NT, int U, bool BITS>
+__device__ __forceinline__ void fetch_bits(const RowBuffers& row, int32_t g0, uint32_t (&b)[U])
 {
-    constexpr uint32_t none = kNegInf<DTYPE>;
-    uint32_t b[U], some = 0;
     const int32_t g = g0 + (int32_t)threadIdx.x;
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+        const int32_t at = g + k * NT;
+        if constexpr (BITS) b[k] = __builtin_amdgcn_raw_buffer_load_b8(row.bits, DTYPE == TDFA_F32 ? at >> 1 : at, 0, 0);
+        else b[k] = 0;
+    }
+}
+template <int DTYPE, int NT, int U, bool BITS, bool ONCE = false>
+__device__ __forceinline__ void fetch_groups(const RowBuffers& row, int32_t g0, int32_t n_groups, uint4 (&x)[U], uint32_t (&b)[U])
+{
+    const int32_t g = g0 + (int32_t)threadIdx.x;
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+        const int32_t at = g + k * NT;
+        if constexpr (BITS && DTYPE == TDFA_F32) b[k] = at < n_groups ? b[k] >> ((at & 1) * 4) & 15u : 0u;
+        x[k] = group_at<ONCE>(row.x, BITS && b[k] == 0 ? kNowhere : (uint32_t)at * 16u);
+    }
+}
+template <int DTYPE, int NT, int U, bool BITS, bool ONCE = false>
+__device__ __forceinline__ void fetch(const RowBuffers& row, int32_t g0, int32_t n_groups, uint4 (&x)[U], uint32_t (&b)[U])
+{
+    fetch_bits<DTYPE, NT, U, BITS>(row, g0, b);
+    fetch_groups<DTYPE, NT, U, BITS, ONCE>(row, g0, n_groups, x, b);
+}
+
+// Puts -inf where a token of group g is not allowed or the row is at its end.  False: so it is in the whole wavefront.
+template <int DTYPE, bool BITS>
+__device__ __forceinline__ bool settle(uint4& x, uint32_t b, int32_t g, int32_t n_groups, const uint2 (&masks)[16])
+{
     if constexpr (BITS) {
-#pragma unroll
-        for (int k = 0; k < U; ++k) b[k] = g + k * NT < n_groups ? group_bits<DTYPE>(bits, g + k * NT) : 0u;
-    }
-#pragma unroll
-    for (int k = 0; k < U; ++k) {
-        x[k] = make_uint4(none, none, none, none);
-        if (BITS ? b[k] != 0 : g + k * NT < n_groups) x[k] = group_at<ONCE>(row + k * NT, g);
-    }
-#pragma unroll
-    for (int k = 0; k < U; ++k) {
-        if constexpr (BITS) {
-            if (!__ballot(b[k] != 0)) continue;
-            x[k] = keep_allowed<DTYPE>(x[k], b[k], masks);
-        } else if (__builtin_amdgcn_readfirstlane(g) + k * NT >= n_groups) {
-            continue;
+        if (!__ballot(b != 0)) return false;
+        x = keep_allowed<DTYPE>(x, b, masks);
+    } else {
+        const int32_t g0 = __builtin_amdgcn_readfirstlane(g);             // (lanes are in the order of their groups)
+        if (g0 >= n_groups) return false;
+        if (g0 + 63 >= n_groups && g >= n_groups) {
+            constexpr uint32_t none = kNegInf<DTYPE>;
+            x = make_uint4(none, none, none, none);
         }
-        some |= 1u << k;
-        next_group();
     }
-    return some;
+    return true;
 }
 
 // Sum of 2^(z c2 + nb), nb = -ref c2 rounded: the rounding moves all terms, the token's own among them, by the same factor.
-template <int DTYPE, int U>
-__device__ __forceinline__ float sum_of(const uint4 (&x)[U], uint32_t some, float c2, float nb)
+template <int DTYPE>
+__device__ __forceinline__ void add_group(uint4 x, float c2, float nb, float (&s)[2])
 {
-    float s[2] = {0.0f, 0.0f};
+    float z[Elem<DTYPE>::kGroup];
+    unpack<DTYPE>(x, z);
 #pragma unroll
-    for (int k = 0; k < U; ++k) {
-        if (!(some >> k & 1)) continue;
-        float z[Elem<DTYPE>::kGroup];
-        unpack<DTYPE>(x[k], z);
-#pragma unroll
-        for (int j = 0; j < Elem<DTYPE>::kGroup; ++j) s[j & 1] += __builtin_amdgcn_exp2f(fmaf(z[j], c2, nb));
-        next_group();
-    }
-    return s[0] + s[1];
+    for (int j = 0; j < Elem<DTYPE>::kGroup; ++j) s[j & 1] += __builtin_amdgcn_exp2f(fmaf(z[j], c2, nb));
 }
-
-// The same with differences taken first and NaN passed over.
-template <int DTYPE, int U>
-__device__ __forceinline__ float careful_sum_of(const uint4 (&x)[U], float c2, float ref)
+// The same with differences taken first and NaN passed over (fmaxf with a number does).
+template <int DTYPE>
+__device__ __forceinline__ void add_group_careful(uint4 x, float c2, float ref, float& s)
 {
-    float s = 0.0f;
+    float z[Elem<DTYPE>::kGroup];
+    unpack<DTYPE>(x, z);
 #pragma unroll
-    for (int k = 0; k < U; ++k) {
-        float z[Elem<DTYPE>::kGroup];
-        unpack<DTYPE>(x[k], z);
-#pragma unroll
-        for (int j = 0; j < Elem<DTYPE>::kGroup; ++j) s += z[j] == z[j] ? __builtin_amdgcn_exp2f((z[j] - ref) * c2) : 0.0f;
-        next_group();
-    }
-    return s;
+    for (int j = 0; j < Elem<DTYPE>::kGroup; ++j) s += __builtin_amdgcn_exp2f((fmaxf(z[j], -INFINITY) - ref) * c2);
 }
-
-template <int DTYPE, int U>
-__device__ __forceinline__ float max_of(const uint4 (&x)[U], float m)
+template <int DTYPE>
+__device__ __forceinline__ float max_group(uint4 x, float m)
 {
+    float z[Elem<DTYPE>::kGroup];
+    unpack<DTYPE>(x, z);
 #pragma unroll
-    for (int k = 0; k < U; ++k) {
-        float z[Elem<DTYPE>::kGroup];
-        unpack<DTYPE>(x[k], z);
-#pragma unroll
-        for (int j = 0; j < Elem<DTYPE>::kGroup; ++j) m = fmaxf(m, z[j]);          // a NaN is passed over
-        next_group();
-    }
+    for (int j = 0; j < Elem<DTYPE>::kGroup; ++j) m = fmaxf(m, z[j]);
     return m;
+}
+
+// Over fetched groups.  Bit k of `some`: the wavefront has an allowed token in its k-th groups.
+template <int DTYPE, int NT, int U, bool BITS>
+__device__ __forceinline__ void add_groups(uint4 (&x)[U], const uint32_t (&b)[U], int32_t g0, int32_t n_groups, const uint2 (&masks)[16], float c2, float nb,
+                                           float (&s)[2], uint32_t& some)
+{
+    some = 0;
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+        if (!settle<DTYPE, BITS>(x[k], b[k], g0 + (int32_t)threadIdx.x + k * NT, n_groups, masks)) continue;
+        some |= 1u << k;
+        add_group<DTYPE>(x[k], c2, nb, s);
+        next_group();
+    }
 }
 
 // The element behind the last whole group that belongs to this thread, -inf if there is none.
@@ -323,20 +342,25 @@ __device__ __forceinline__ Scored score_careful(float z, float ref, float inv_t,
 // Sum of the exponentials of a row relative to its largest logit, NaN passed over: what a row takes whose sum relative to its own
 // token is not usable.  Sets *ref to that logit.
 template <int DTYPE, int NT, int U, bool BITS>
-__device__ __forceinline__ float careful_sum(const uint4* row4, const uint32_t* bits, int32_t n_groups, float last, float c2, float* ref,
-                                          const uint2 (&masks)[16], float (&part)[NT / 64])
+__device__ __forceinline__ float careful_sum(const RowBuffers& row, int32_t n_groups, float last, float c2, float* ref, const uint2 (&masks)[16],
+                                             float (&part)[NT / 64])
 {
     uint4 x[U];
+    uint32_t b[U];
     float m = fmaxf(kLowest, last);
     for (int32_t g = 0; g < n_groups; g += NT * U) {
-        fetch<DTYPE, NT, U, BITS>(row4, bits, g, n_groups, masks, x);
-        m = max_of<DTYPE, U>(x, m);
+        fetch<DTYPE, NT, U, BITS>(row, g, n_groups, x, b);
+#pragma unroll
+        for (int k = 0; k < U; ++k)
+            if (settle<DTYPE, BITS>(x[k], b[k], g + (int32_t)threadIdx.x + k * NT, n_groups, masks)) m = max_group<DTYPE>(x[k], m);
     }
     m = block_reduce<NT, true>(m, part);
-    float s = last == last ? __builtin_amdgcn_exp2f((last - m) * c2) : 0.0f;
+    float s = __builtin_amdgcn_exp2f((fmaxf(last, -INFINITY) - m) * c2);
     for (int32_t g = 0; g < n_groups; g += NT * U) {
-        fetch<DTYPE, NT, U, BITS>(row4, bits, g, n_groups, masks, x);
-        s += careful_sum_of<DTYPE, U>(x, c2, m);
+        fetch<DTYPE, NT, U, BITS>(row, g, n_groups, x, b);
+#pragma unroll
+        for (int k = 0; k < U; ++k)
+            if (settle<DTYPE, BITS>(x[k], b[k], g + (int32_t)threadIdx.x + k * NT, n_groups, masks)) add_group_careful<DTYPE>(x[k], c2, m, s);
     }
     *ref = m;
     return block_reduce<NT, false>(s, part);
@@ -419,21 +443,108 @@ __global__ void __launch_bounds__(NT, 8) token_stats_kernel(TokenRows a, Outputs
         __syncthreads();
     }
     const E* row = static_cast<const E*>(a.logits) + i * a.row_stride;
-    const float z = r.read ? token_logit(r, row) : -INFINITY;
+    if (!r.read) {
+        if (threadIdx.x == 0) leave_out(o, i, r.lp);
+        return;
+    }
+    // the first bits are on their way together with the token's logit
+    const RowBuffers buf = row_buffers<DTYPE>(row, r.bits, n_groups);
+    uint32_t b[U];
+    fetch_bits<DTYPE, NT, U, BITS>(buf, 0, b);
+    const float z = token_logit(r, row), last = last_element<DTYPE>(a, row, r.bits);
     if (z == -INFINITY) {
         if (threadIdx.x == 0) leave_out(o, i, r.lp);
         return;
     }
-    const uint4* row4 = reinterpret_cast<const uint4*>(row);
-    const float last = last_element<DTYPE>(a, row, r.bits), nb = -z * c2;
-    float s = __builtin_amdgcn_exp2f(fmaf(last, c2, nb)), ref = z;
-    uint4 x[U];
-    for (int32_t g = 0; g < n_groups; g += NT * U)
-        s += sum_of<DTYPE, U>(x, fetch<DTYPE, NT, U, BITS>(row4, r.bits, g, n_groups, s_masks, x), c2, nb);
-    s = block_reduce<NT, false>(s, s_part);
+    const float nb = -z * c2;
+    float sum[2] = {__builtin_amdgcn_exp2f(fmaf(last, c2, nb)), 0.0f}, ref = z;
+    for (int32_t g = 0; g < n_groups; g += NT * U) {
+        uint4 x[U];
+        uint32_t some;
+        if (g) fetch_bits<DTYPE, NT, U, BITS>(buf, g, b);
+        fetch_groups<DTYPE, NT, U, BITS>(buf, g, n_groups, x, b);
+        add_groups<DTYPE, NT, U, BITS>(x, b, g, n_groups, s_masks, c2, nb, sum, some);
+    }
+    float s = block_reduce<NT, false>(sum[0] + sum[1], s_part);
     const bool careful = !usable(s);
-    if (careful) s = careful_sum<DTYPE, NT, 2, BITS>(row4, r.bits, n_groups, last, c2, &ref, s_masks, s_part);
+    if (careful) s = careful_sum<DTYPE, NT, 2, BITS>(buf, n_groups, last, c2, &ref, s_masks, s_part);
     if (threadIdx.x == 0) finish(o, i, careful ? score_careful(z, ref, a.inv_t, s) : score(z, c2, nb, s), careful, v);
+}
+
+// The largest logit and the sum relative to it of a part of a row; {kLowest, 0}: of none.
+struct Part {
+    float m, s;
+};
+
+// One workgroup per part of `span` groups of a row: few long rows are shared out, and every part finds a reference of its own.
+template <int DTYPE, int NT, int U, bool BITS>
+__global__ void __launch_bounds__(NT) part_stats_kernel(TokenRows a, Part* out, int32_t parts, int32_t span)
+{
+    using E = typename Elem<DTYPE>::type;
+    __shared__ float s_part[NT / 64];
+    __shared__ uint2 s_masks[16];
+    const int64_t w = block_index(), i = w / parts;
+    const int32_t part = (int32_t)(w - i * parts);
+    if (i >= a.rows) return;
+    const Row r = row_of(a, i);
+    if (!r.read) return;
+    const float c2 = a.inv_t * kLog2e;
+    const int32_t n_groups = a.n_tokens / Elem<DTYPE>::kGroup;
+    if (BITS && DTYPE == TDFA_BF16) {
+        fill_masks(s_masks);
+        __syncthreads();
+    }
+    const E* row = static_cast<const E*>(a.logits) + i * a.row_stride;
+    const int32_t end = min(n_groups, (part + 1) * span);
+    const RowBuffers buf = row_buffers<DTYPE>(row, r.bits, end);
+    // fmaxf with a number passes over a NaN
+    const float last = part == parts - 1 ? fmaxf(last_element<DTYPE>(a, row, r.bits), -INFINITY) : -INFINITY;
+    float m = fmaxf(kLowest, last), s = __builtin_amdgcn_exp2f((last - m) * c2);
+    for (int32_t g = part * span; g < end; g += NT * U) {
+        uint4 x[U];
+        uint32_t b[U], some = 0;
+        fetch<DTYPE, NT, U, BITS>(buf, g, end, x, b);
+        float top = m;
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            if (!settle<DTYPE, BITS>(x[k], b[k], g + (int32_t)threadIdx.x + k * NT, end, s_masks)) continue;
+            some |= 1u << k;
+            top = max_group<DTYPE>(x[k], top);
+            next_group();
+        }
+        s *= __builtin_amdgcn_exp2f((m - top) * c2);
+        m = top;
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            if (!(some >> k & 1)) continue;
+            add_group_careful<DTYPE>(x[k], c2, m, s);
+            next_group();
+        }
+    }
+    const float top = block_reduce<NT, true>(m, s_part);
+    s = block_reduce<NT, false>(s * __builtin_amdgcn_exp2f((m - top) * c2), s_part);
+    if (threadIdx.x == 0) out[i * parts + part] = {top, s};
+}
+
+// A wavefront per row joins its parts, at most 64.
+template <int DTYPE>
+__global__ void __launch_bounds__(kThreads) join_parts_kernel(TokenRows a, Outputs o, const Part* in, int32_t parts)
+{
+    using E = typename Elem<DTYPE>::type;
+    const int64_t i = block_index() * (kThreads / 64) + threadIdx.x / 64;
+    if (i >= a.rows) return;
+    const int lane = threadIdx.x & 63;
+    const Row r = row_of(a, i);
+    const PolicyRow v = o.each ? policy_row(a, o.policy, i) : PolicyRow{};
+    const float z = r.read ? token_logit(r, static_cast<const E*>(a.logits) + i * a.row_stride) : -INFINITY;
+    if (z == -INFINITY) {
+        if (lane == 0) leave_out(o, i, r.lp);
+        return;
+    }
+    const float c2 = a.inv_t * kLog2e;
+    const Part mine = lane < parts ? in[i * parts + lane] : Part{kLowest, 0.0f};
+    const float top = wave_max(mine.m), s = wave_sum(mine.s * __builtin_amdgcn_exp2f((mine.m - top) * c2));
+    if (lane == 0) finish(o, i, score_careful(z, top, a.inv_t, s), true, v);
 }
 
 // What a row's gradient is made of: g_j = -d p_j, and d more at the token.
@@ -454,46 +565,53 @@ __device__ __forceinline__ Slope slope_of(float d, float ref, float ls, float c2
 __device__ __forceinline__ float shared_by_wave(float x) { return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(x))); }
 __device__ __forceinline__ Slope shared_by_wave(Slope q) { return {shared_by_wave(q.d), shared_by_wave(q.ref), shared_by_wave(q.k2), shared_by_wave(q.fold)}; }
 
-// Gradient of groups g + k NT, g = g0 + threadIdx.x, of a row.
-template <int DTYPE, int NT, int U>
-__device__ __forceinline__ void write_gradient(uint4* out4, int32_t g0, int32_t n_groups, const uint4 (&x)[U], uint32_t some, Slope q, float c2, int32_t token)
+// Gradient of one group; own: the token is in it.
+template <int DTYPE>
+__device__ __forceinline__ uint4 gradient_of(uint4 x, bool some, Slope q, float c2, bool folds, uint32_t sign, bool own, int32_t token)
 {
     constexpr int G = Elem<DTYPE>::kGroup;
-    const int32_t g = g0 + (int32_t)threadIdx.x;
-    const bool folds = DTYPE == TDFA_BF16 && q.fold == q.fold;
-    const uint32_t sign = q.d > 0.0f ? 0x80008000u : 0u;
+    if (!some) return make_uint4(0, 0, 0, 0);
+    float z[G];
+    unpack<DTYPE>(x, z);
+    if (folds) {
 #pragma unroll
-    for (int k = 0; k < U; ++k) {
-        uint4 y = make_uint4(0, 0, 0, 0);
-        if (some >> k & 1) {
-            float z[G];
-            unpack<DTYPE>(x[k], z);
-            if (folds) {
+        for (int j = 0; j < G; ++j) z[j] = __builtin_amdgcn_exp2f(fmaf(z[j], c2, q.fold));
+        if (own) {
 #pragma unroll
-                for (int j = 0; j < G; ++j) z[j] = __builtin_amdgcn_exp2f(fmaf(z[j], c2, q.fold));
-                if (g + k * NT == token / G) {
-#pragma unroll
-                    for (int j = 0; j < G; ++j) z[j] -= j == token % G ? fabsf(q.d) : 0.0f;
-                }
-                y = pack<DTYPE>(z);
-                y = make_uint4(y.x ^ sign, y.y ^ sign, y.z ^ sign, y.w ^ sign);
-            } else {
-#pragma unroll
-                for (int j = 0; j < G; ++j) {
-                    const float e = __builtin_amdgcn_exp2f(fmaf(z[j] - q.ref, c2, q.k2));
-                    z[j] = z[j] == z[j] ? -q.d * e : 0.0f;
-                }
-                if (g + k * NT == token / G) {
-#pragma unroll
-                    for (int j = 0; j < G; ++j) z[j] += j == token % G ? q.d : 0.0f;
-                }
-                y = pack<DTYPE>(z);
-            }
+            for (int j = 0; j < G; ++j) z[j] -= j == token % G ? fabsf(q.d) : 0.0f;
         }
-        if (g + k * NT < n_groups) set_group(out4 + k * NT, g, y);
+        const uint4 y = pack<DTYPE>(z);
+        return make_uint4(y.x ^ sign, y.y ^ sign, y.z ^ sign, y.w ^ sign);
+    }
+#pragma unroll
+    for (int j = 0; j < G; ++j) {
+        const float e = __builtin_amdgcn_exp2f(fmaf(z[j] - q.ref, c2, q.k2));
+        z[j] = z[j] == z[j] ? -q.d * e : 0.0f;
+    }
+    if (own) {
+#pragma unroll
+        for (int j = 0; j < G; ++j) z[j] += j == token % G ? q.d : 0.0f;
+    }
+    return pack<DTYPE>(z);
+}
+
+// What the gradients of all groups of a row share.
+template <int DTYPE>
+struct Writer {
+    Slope q;
+    float c2;
+    int32_t token;
+    bool folds;
+    uint32_t sign;
+    __device__ __forceinline__ Writer(Slope q, float c2, int32_t token)
+        : q(q), c2(c2), token(token), folds(DTYPE == TDFA_BF16 && q.fold == q.fold), sign(q.d > 0.0f ? 0x80008000u : 0u) {}
+    // some: the wavefront has an allowed token in its groups
+    __device__ __forceinline__ void write(__amdgpu_buffer_rsrc_t out, int32_t g, uint4 x, bool some) const
+    {
+        set_group(out, g, gradient_of<DTYPE>(x, some, q, c2, folds, sign, g == token / Elem<DTYPE>::kGroup, token));
         next_group();
     }
-}
+};
 // The same for an element behind the last whole group.
 __device__ __forceinline__ float last_gradient(float z, Slope q, float c2, bool own)
 {
@@ -558,24 +676,31 @@ __global__ void __launch_bounds__(NT) token_grad_kernel(TokenRows a, const float
     const Slope q = shared_by_wave(slope_of<DTYPE>(r.read && st.y != INFINITY ? slope * a.inv_t : 0.0f, st.x, fabsf(st.y), c2, signbit(st.y)));
     const E* row = static_cast<const E*>(a.logits) + i * a.row_stride;
     E* out = static_cast<E*>(grad) + i * grad_stride;
-    uint4* out4 = reinterpret_cast<uint4*>(out);
+    const __amdgpu_buffer_rsrc_t to = buffer_of(out, (uint32_t)n_groups * 16u);
     const int32_t g0 = part * (NT * U), g = g0 + (int32_t)threadIdx.x;
     const int32_t behind = n_groups * G + (int32_t)threadIdx.x;
     if (q.d == 0.0f) {
 #pragma unroll
-        for (int k = 0; k < U; ++k)
-            if (g + k * NT < n_groups) set_group(out4 + k * NT, g, make_uint4(0, 0, 0, 0));
+        for (int k = 0; k < U; ++k) set_group(to, g + k * NT, make_uint4(0, 0, 0, 0));
         if (part == parts - 1 && behind < a.n_tokens) store_rounded(out + behind, 0.0f);
         return;
     }
     const float last = part == parts - 1 ? last_element<DTYPE>(a, row, r.bits) : -INFINITY;
     uint4 x[U];
-    const uint32_t some = fetch<DTYPE, NT, U, BITS, true>(reinterpret_cast<const uint4*>(row), r.bits, g0, n_groups, s_masks, x);
-    write_gradient<DTYPE, NT, U>(out4, g0, n_groups, x, some, q, c2, r.token);
+    uint32_t b[U];
+    fetch<DTYPE, NT, U, BITS, true>(row_buffers<DTYPE>(row, r.bits, n_groups), g0, n_groups, x, b);
+    const Writer<DTYPE> writer(q, c2, r.token);
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+        const bool some = settle<DTYPE, BITS>(x[k], b[k], g + k * NT, n_groups, s_masks);
+        writer.write(to, g + k * NT, x[k], some);
+    }
     if (part == parts - 1 && behind < a.n_tokens) store_rounded(out + behind, last_gradient(last, q, c2, behind == r.token));
 }
 
 constexpr int64_t kWholeGroups = 1024 * 16;
+constexpr int kMaxParts = 64;
+constexpr int64_t kPartRows = 384;
 
 // One workgroup per row: the sum, the row's term, the gradient.  The row stays in registers between the sum and the gradient, R groups
 // to a thread: 1,024 threads hold 256 KB, half of a compute unit's registers, and the row is read once.
@@ -598,23 +723,36 @@ __global__ void __launch_bounds__(NT, 4) policy_row_kernel(TokenRows a, PolicyAr
         __syncthreads();
     }
     const E* row = static_cast<const E*>(a.logits) + i * a.row_stride;
-    const uint4* row4 = reinterpret_cast<const uint4*>(row);
+    const RowBuffers buf = row_buffers<DTYPE>(row, r.bits, n_groups);
     Slope q = {0.0f, 0.0f, 0.0f, 0.0f};
     float last = -INFINITY;
     uint4 x[R];
     uint32_t some = 0;
-    const float z = r.read ? token_logit(r, row) : -INFINITY;
-    if (z > -INFINITY) {
+    uint32_t b[R];
+    float z = -INFINITY;
+    if (r.read) {                                          // the bits are on their way together with the token's logit
+        fetch_bits<DTYPE, NT, R, BITS>(buf, 0, b);
+        z = token_logit(r, row);
         last = last_element<DTYPE>(a, row, r.bits);
+    }
+    if (z > -INFINITY) {
+        fetch_groups<DTYPE, NT, R, BITS, true>(buf, 0, n_groups, x, b);
         const float nb = -z * c2;
-        some = fetch<DTYPE, NT, R, BITS, true>(row4, r.bits, 0, n_groups, s_masks, x);
-        float s = __builtin_amdgcn_exp2f(fmaf(last, c2, nb)) + sum_of<DTYPE, R>(x, some, c2, nb), ref = z;
-        s = block_reduce<NT, false>(s, s_part);
+        float sum[2] = {__builtin_amdgcn_exp2f(fmaf(last, c2, nb)), 0.0f}, ref = z;
+        add_groups<DTYPE, NT, R, BITS>(x, b, 0, n_groups, s_masks, c2, nb, sum, some);
+        float s = block_reduce<NT, false>(sum[0] + sum[1], s_part);
         const bool careful = !usable(s);
         if (careful) {
-            ref = block_reduce<NT, true>(max_of<DTYPE, R>(x, fmaxf(kLowest, last)), s_part);
-            s = last == last ? __builtin_amdgcn_exp2f((last - ref) * c2) : 0.0f;
-            s = block_reduce<NT, false>(s + careful_sum_of<DTYPE, R>(x, c2, ref), s_part);
+            ref = fmaxf(kLowest, last);
+#pragma unroll
+            for (int k = 0; k < R; ++k)
+                if (some >> k & 1) ref = max_group<DTYPE>(x[k], ref);
+            ref = block_reduce<NT, true>(ref, s_part);
+            s = __builtin_amdgcn_exp2f((fmaxf(last, -INFINITY) - ref) * c2);
+#pragma unroll
+            for (int k = 0; k < R; ++k)
+                if (some >> k & 1) add_group_careful<DTYPE>(x[k], c2, ref, s);
+            s = block_reduce<NT, false>(s, s_part);
         }
         if (threadIdx.x < 64) {
             const Scored sc = careful ? score_careful(z, ref, a.inv_t, s) : score(z, c2, nb, s);
@@ -635,14 +773,16 @@ __global__ void __launch_bounds__(NT, 4) policy_row_kernel(TokenRows a, PolicyAr
     }
     if (!grad) return;
     E* out = static_cast<E*>(grad) + i * grad_stride;
-    uint4* out4 = reinterpret_cast<uint4*>(out);
+    const __amdgpu_buffer_rsrc_t to = buffer_of(out, (uint32_t)n_groups * 16u);
     const int32_t behind = n_groups * G + (int32_t)threadIdx.x;
     if (q.d == 0.0f) {
-        for (int32_t g = threadIdx.x; g < n_groups; g += NT) set_group(out4, g, make_uint4(0, 0, 0, 0));
+        for (int32_t g = threadIdx.x; g < n_groups; g += NT) set_group(to, g, make_uint4(0, 0, 0, 0));
         if (behind < a.n_tokens) store_rounded(out + behind, 0.0f);
         return;
     }
-    write_gradient<DTYPE, NT, R>(out4, 0, n_groups, x, some, q, c2, r.token);
+    const Writer<DTYPE> writer(q, c2, r.token);
+#pragma unroll
+    for (int k = 0; k < R; ++k) writer.write(to, (int32_t)threadIdx.x + k * NT, x[k], some >> k & 1);
     if (behind < a.n_tokens) store_rounded(out + behind, last_gradient(last, q, c2, behind == r.token));
 }
 
@@ -694,18 +834,40 @@ template <int DTYPE, bool BITS>
 int stats_launch(const TokenRows& a, const Outputs& o, hipStream_t stream)
 {
     const int32_t n_groups = a.n_tokens / Elem<DTYPE>::kGroup;
-#define ROWS(NT) token_stats_kernel<DTYPE, NT, 4, BITS><<<grid_for(a.rows), NT, 0, stream>>>(a, o)
-    if (n_groups <= 64 * 8) ROWS(64);
-    else if (n_groups <= 256 * 16) ROWS(256);
-    else if (n_groups <= 512 * 16) ROWS(512);
-    else ROWS(1024);
+    // Two rows or more to a compute unit, so that one is fetched while another is summed.
+#define ROWS(NT, U) token_stats_kernel<DTYPE, NT, U, BITS><<<grid_for(a.rows), NT, 0, stream>>>(a, o)
+    if (n_groups <= 64 * 4) ROWS(64, 4);
+    else if (n_groups <= 256 * 16) ROWS(256, 8);
+    else if (n_groups <= 512 * 16) ROWS(512, 8);
+    else ROWS(1024, 8);
 #undef ROWS
     TDFA_HIP(hipGetLastError());
     return TDFA_OK;
 }
 
-int stats_of(const TokenRows& a, const Outputs& o, hipStream_t stream)
+template <int DTYPE, bool BITS>
+int parts_launch(const TokenRows& a, const Outputs& o, Part* out, hipStream_t stream)
 {
+    const int32_t n_groups = a.n_tokens / Elem<DTYPE>::kGroup, round = 256 * 8;
+    const int32_t span = (n_groups + kMaxParts * round - 1) / (kMaxParts * round) * round, parts = (n_groups + span - 1) / span;
+    part_stats_kernel<DTYPE, 256, 8, BITS><<<grid_for(a.rows * parts), 256, 0, stream>>>(a, out, parts, span);
+    TDFA_HIP(hipGetLastError());
+    join_parts_kernel<DTYPE><<<grid_for((a.rows + kThreads / 64 - 1) / (kThreads / 64)), kThreads, 0, stream>>>(a, o, out, parts);
+    TDFA_HIP(hipGetLastError());
+    return TDFA_OK;
+}
+
+int64_t groups_of(const TokenRows& a) { return a.n_tokens / (a.dtype == TDFA_F32 ? Elem<TDFA_F32>::kGroup : Elem<TDFA_BF16>::kGroup); }
+
+// parts: workspace for kMaxParts parts of each of the first kPartRows rows.  Few rows that are longer than a workgroup's registers are
+// shared out by parts, which a second launch joins: 1 row of 256,000 tokens in fp32 14.5 us by one workgroup, 6.8 so; 64 rows 34.5 and
+// 14.9, 300 rows 60.6 and 44.5; of 128,256 tokens 19.8 and 12.1, 28.7 and 24.9; 512 rows 38.1 and 37.9, in bf16 of 256,000 36.6 and 40.6.
+int stats_of(const TokenRows& a, const Outputs& o, Part* parts, hipStream_t stream)
+{
+    if (a.rows <= kPartRows && groups_of(a) > kWholeGroups) {
+        if (a.dtype == TDFA_F32) return a.allow ? parts_launch<TDFA_F32, true>(a, o, parts, stream) : parts_launch<TDFA_F32, false>(a, o, parts, stream);
+        return a.allow ? parts_launch<TDFA_BF16, true>(a, o, parts, stream) : parts_launch<TDFA_BF16, false>(a, o, parts, stream);
+    }
     if (a.dtype == TDFA_F32) return a.allow ? stats_launch<TDFA_F32, true>(a, o, stream) : stats_launch<TDFA_F32, false>(a, o, stream);
     return a.allow ? stats_launch<TDFA_BF16, true>(a, o, stream) : stats_launch<TDFA_BF16, false>(a, o, stream);
 }
@@ -717,8 +879,8 @@ int grad_launch(const TokenRows& a, const float2* stats, const float* down, void
     if (n_groups <= 256) {
         token_grad_kernel<DTYPE, 64, 4, BITS><<<grid_for(a.rows + more), 64, 0, stream>>>(a, stats, down, grad, grad_stride, 1, sum);
     } else {
-        const int32_t parts = (n_groups + 256 * 4 - 1) / (256 * 4);
-        token_grad_kernel<DTYPE, 256, 4, BITS><<<grid_for(a.rows * parts + more), 256, 0, stream>>>(a, stats, down, grad, grad_stride, parts, sum);
+        const int32_t parts = (n_groups + 256 * 8 - 1) / (256 * 8);
+        token_grad_kernel<DTYPE, 256, 8, BITS><<<grid_for(a.rows * parts + more), 256, 0, stream>>>(a, stats, down, grad, grad_stride, parts, sum);
     }
     TDFA_HIP(hipGetLastError());
     return TDFA_OK;
@@ -728,12 +890,11 @@ int grad_launch(const TokenRows& a, const float2* stats, const float* down, void
 
 int launch_token_logprobs(const TokenRows& a, float* logprobs, float* stats, void* workspace, hipStream_t stream)
 {
-    (void)workspace;
     if (a.rows == 0) return TDFA_OK;
     Outputs o = {};
     o.logprobs = logprobs;
     o.stats = reinterpret_cast<float2*>(stats);
-    return stats_of(a, o, stream);
+    return stats_of(a, o, static_cast<Part*>(workspace), stream);
 }
 
 static int grad_of(const TokenRows& a, const float2* stats, const float* down, void* grad, int64_t grad_stride, const LossSum& sum, hipStream_t stream)
@@ -751,8 +912,10 @@ int launch_token_grad(const TokenRows& a, const float* stats, const float* down,
     return grad_of(a, reinterpret_cast<const float2*>(stats), down, grad, grad_stride, LossSum{}, stream);
 }
 
-// Workspace: double [rows] (lp, or the rows' losses), double [n_pairs] losses of the pairs, float2 [rows] statistics, float [rows] d loss / d lp.
-int64_t loss_workspace(int64_t rows, int64_t n_pairs) { return 8 * n_pairs + 20 * rows; }
+// Workspace: Part [kMaxParts] of each of the first kPartRows rows, double [rows] (lp, or the rows' losses), double [n_pairs] losses of the
+// pairs, float2 [rows] statistics, float [rows] d loss / d lp.
+static int64_t parts_bytes(int64_t rows) { return (rows < kPartRows ? rows : kPartRows) * kMaxParts * (int64_t)sizeof(Part); }
+int64_t loss_workspace(int64_t rows, int64_t n_pairs) { return parts_bytes(rows) + 8 * n_pairs + 20 * rows; }
 
 template <int DTYPE, bool BITS>
 static int policy_launch(const TokenRows& a, const PolicyArgs& p, float* logprobs, double* each, void* grad, int64_t grad_stride, hipStream_t stream)
@@ -774,14 +937,15 @@ static int policy_launch(const TokenRows& a, const PolicyArgs& p, float* logprob
 // a workgroup's registers (300 rows of 256,000 in fp32 117 us, 167 with half of every row read twice by one launch).
 bool one_launch(const TokenRows& a)
 {
-    const int64_t n_groups = a.n_tokens / (a.dtype == TDFA_F32 ? Elem<TDFA_F32>::kGroup : Elem<TDFA_BF16>::kGroup);
+    const int64_t n_groups = groups_of(a);
     return n_groups <= kWholeGroups && (a.rows > 32 || n_groups <= 2048);
 }
 
 int launch_policy_loss(const TokenRows& a, const PolicyArgs& p, float* loss, float* logprobs, void* grad, int64_t grad_stride, void* workspace,
                        hipStream_t stream)
 {
-    double* each = static_cast<double*>(workspace);
+    Part* parts = static_cast<Part*>(workspace);
+    double* each = reinterpret_cast<double*>(static_cast<char*>(workspace) + parts_bytes(a.rows));
     if (a.rows && one_launch(a)) {
         const int rc = a.dtype == TDFA_F32 ? (a.allow ? policy_launch<TDFA_F32, true>(a, p, logprobs, each, grad, grad_stride, stream)
                                                       : policy_launch<TDFA_F32, false>(a, p, logprobs, each, grad, grad_stride, stream))
@@ -797,7 +961,7 @@ int launch_policy_loss(const TokenRows& a, const PolicyArgs& p, float* loss, flo
             o.stats = reinterpret_cast<float2*>(each + a.rows);
             o.down = reinterpret_cast<float*>(o.stats + a.rows);
         }
-        const int rc = stats_of(a, o, stream);
+        const int rc = stats_of(a, o, parts, stream);
         if (rc != TDFA_OK || grad) return rc != TDFA_OK ? rc : grad_of(a, o.stats, o.down, grad, grad_stride, LossSum{each, a.rows, 1.0, loss}, stream);
     }
     loss_sum_kernel<<<1, 1024, 0, stream>>>(LossSum{each, a.rows, 1.0, loss});
@@ -808,7 +972,8 @@ int launch_policy_loss(const TokenRows& a, const PolicyArgs& p, float* loss, flo
 int launch_preference_loss(const TokenRows& a, const PairArgs& p, float* loss, float* logprobs, void* grad, int64_t grad_stride, void* workspace,
                            hipStream_t stream)
 {
-    double* exact = static_cast<double*>(workspace);
+    Part* parts = static_cast<Part*>(workspace);
+    double* exact = reinterpret_cast<double*>(static_cast<char*>(workspace) + parts_bytes(a.rows));
     double* each = exact + a.rows;
     Outputs o = {};
     o.logprobs = logprobs;
@@ -816,7 +981,7 @@ int launch_preference_loss(const TokenRows& a, const PairArgs& p, float* loss, f
     o.stats = reinterpret_cast<float2*>(each + p.n_pairs);
     o.down = reinterpret_cast<float*>(o.stats + a.rows);                   // zero, for the rows of no sequence
     if (a.rows) {
-        const int rc = stats_of(a, o, stream);
+        const int rc = stats_of(a, o, parts, stream);
         if (rc != TDFA_OK) return rc;
     }
     if (p.n_pairs) {
