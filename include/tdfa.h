@@ -434,6 +434,7 @@ TDFA_API int tdfa_sample_noise(int32_t batch, int32_t n_tokens, uint64_t seed, u
  *   workspace_dev, workspace_bytes : device memory for the call's own use, 16-byte aligned, of at least
  *                 tdfa_loss_workspace_bytes(rows, n_pairs) bytes (n_pairs 0 unless the call has pairs).
  *                 It need not be cleared, and must not be used by anything else until the call's work is done.
+ *                 tdfa_token_logprobs takes NULL too where a row of logits is at most 256 KiB long.
  * Row i has logits z, allowed set A (of states[i]), token t and c = 1 / temperature.  NaN counts as -inf, as
  * for the draw, and a logit outside A has no effect whatever it is.  With m the largest z in A and
  * s the sum over A of exp((z_j - m) c),

@@ -453,7 +453,10 @@ def token_logprobs(table: Table | None, logits: torch.Tensor, states: torch.Tens
     a = _rows_args(table, logits, states, tokens, temperature)
     rows, dev = a[3], logits.get_device()
     out = _vector(logprobs, "logprobs", torch.float32, rows, dev), _vector(stats, "stats", torch.float32, 2 * rows, dev, True)
-    ws, n, _held = _workspace(workspace, rows, 0, logits, stream)
+    if workspace is None and a[4] * logits.element_size() <= 1 << 18:
+        ws, n, _held = None, 0, None                   # such rows want none
+    else:
+        ws, n, _held = _workspace(workspace, rows, 0, logits, stream)
     _check(lib().tdfa_token_logprobs(*a, *out, ws, n, _stream(stream)))
 
 

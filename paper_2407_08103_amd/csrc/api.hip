@@ -1878,7 +1878,7 @@ int tdfa_token_logprobs(const tdfa_table* table, const void* logits_dev, int dty
     if (rc != TDFA_OK || rows == 0) return rc;
     if (!logprobs_dev) return fail(TDFA_E_INVALID_ARG, "logprobs is NULL");
     if (misaligned(stats_dev, 8)) return fail(TDFA_E_INVALID_ARG, "stats must be 8-byte aligned");
-    rc = check_workspace(workspace_dev, workspace_bytes, rows, 0);
+    if (workspace_dev || token_logprobs_want_workspace(a)) rc = check_workspace(workspace_dev, workspace_bytes, rows, 0);
     if (rc != TDFA_OK) return rc;
     return launch_token_logprobs(a, logprobs_dev, stats_dev, workspace_dev, static_cast<hipStream_t>(stream));
 }

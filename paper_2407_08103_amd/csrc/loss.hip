@@ -17,6 +17,7 @@
 #include "tdfa_internal.h"
 
 #include <cmath>
+#include <tuple>
 
 namespace tdfa {
 namespace {
@@ -81,13 +82,18 @@ struct Row {
     float lp;                  // of a row that is not read
 };
 
-// (i is the same in all lanes of a wavefront.  The loads do not wait for one another.)
+// (i is the same in all lanes of a wavefront.)  The loads do not wait for one another: what there is none of is read from the tokens,
+// and all three values are wanted before any of them is looked at.
 __device__ __forceinline__ Row row_of(const TokenRows& a, int64_t i)
 {
-    const int32_t token = __builtin_amdgcn_readfirstlane(a.tokens[i]), q = a.allow ? __builtin_amdgcn_readfirstlane(a.states[i]) : 0;
-    const float w = a.weights ? a.weights[i] : 1.0f;
+    int32_t token = a.tokens[i], q = (a.allow ? a.states : a.tokens)[i];
+    int32_t w = (a.weights ? reinterpret_cast<const int32_t*>(a.weights) : a.tokens)[i];
+    asm volatile("" : "+v"(token), "+v"(q), "+v"(w));
+    token = __builtin_amdgcn_readfirstlane(token);
+    q = __builtin_amdgcn_readfirstlane(q);
+    w = __builtin_amdgcn_readfirstlane(w);
     Row r = {nullptr, token, false, 0.0f};
-    if (token == TDFA_NO_TOKEN || w == 0.0f) return r;
+    if (token == TDFA_NO_TOKEN || (a.weights && __int_as_float(w) == 0.0f)) return r;
     r.lp = -INFINITY;
     if (token < 0 || token >= a.n_tokens || (a.allow && (q < 0 || q >= a.n_states))) return r;
     if (a.allow) r.bits = a.allow + (int64_t)q * a.row_words;
@@ -104,8 +110,9 @@ __device__ __forceinline__ bool allowed(const uint32_t* bits, int32_t t)
 template <typename E>
 __device__ __forceinline__ float token_logit(const Row& r, const E* row)
 {
-    const uint32_t word = r.bits ? r.bits[r.token >> 5] : 0xFFFFFFFFu;
-    const float z = to_f32(row[r.token]);
+    uint32_t word = r.bits ? r.bits[r.token >> 5] : 0xFFFFFFFFu;
+    float z = to_f32(row[r.token]);
+    asm volatile("" : "+v"(word), "+v"(z));                // both are on their way before either is looked at
     return (word >> (r.token & 31) & 1) && z == z ? z : -INFINITY;
 }
 
@@ -826,6 +833,18 @@ pair_kernel(PairArgs p, int64_t rows, const double* exact, const float2* stats, 
     }
 }
 
+// A launch that reports its own error (asking for the last one afterwards costs the host 0.4 us more).
+template <typename... Params, typename... Args>
+int launch(void (*kernel)(Params...), dim3 grid, unsigned threads, hipStream_t stream, Args... args)
+{
+    std::tuple<Params...> params(args...);
+    return std::apply([&](Params&... p) -> int {
+        void* at[] = {&p...};
+        TDFA_HIP(hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, dim3(threads), at, 0, stream));
+        return TDFA_OK;
+    }, params);
+}
+
 unsigned blocks_for(int64_t n) { return (unsigned)(n < 1 << 20 ? n : 1 << 20); }
 // At least n workgroups, whose threads stay below 2^32 in each dimension.
 dim3 grid_for(int64_t n) { return n <= 1 << 21 ? dim3((unsigned)n) : dim3(1u << 21, (unsigned)((n + (1 << 21) - 1) >> 21)); }
@@ -835,14 +854,10 @@ int stats_launch(const TokenRows& a, const Outputs& o, hipStream_t stream)
 {
     const int32_t n_groups = a.n_tokens / Elem<DTYPE>::kGroup;
     // Two rows or more to a compute unit, so that one is fetched while another is summed.
-#define ROWS(NT, U) token_stats_kernel<DTYPE, NT, U, BITS><<<grid_for(a.rows), NT, 0, stream>>>(a, o)
-    if (n_groups <= 64 * 4) ROWS(64, 4);
-    else if (n_groups <= 256 * 16) ROWS(256, 8);
-    else if (n_groups <= 512 * 16) ROWS(512, 8);
-    else ROWS(1024, 8);
-#undef ROWS
-    TDFA_HIP(hipGetLastError());
-    return TDFA_OK;
+    if (n_groups <= 64 * 4) return launch(token_stats_kernel<DTYPE, 64, 4, BITS>, grid_for(a.rows), 64, stream, a, o);
+    if (n_groups <= 256 * 16) return launch(token_stats_kernel<DTYPE, 256, 8, BITS>, grid_for(a.rows), 256, stream, a, o);
+    if (n_groups <= 512 * 16) return launch(token_stats_kernel<DTYPE, 512, 8, BITS>, grid_for(a.rows), 512, stream, a, o);
+    return launch(token_stats_kernel<DTYPE, 1024, 8, BITS>, grid_for(a.rows), 1024, stream, a, o);
 }
 
 template <int DTYPE, bool BITS>
@@ -850,21 +865,21 @@ int parts_launch(const TokenRows& a, const Outputs& o, Part* out, hipStream_t st
 {
     const int32_t n_groups = a.n_tokens / Elem<DTYPE>::kGroup, round = 256 * 8;
     const int32_t span = (n_groups + kMaxParts * round - 1) / (kMaxParts * round) * round, parts = (n_groups + span - 1) / span;
-    part_stats_kernel<DTYPE, 256, 8, BITS><<<grid_for(a.rows * parts), 256, 0, stream>>>(a, out, parts, span);
-    TDFA_HIP(hipGetLastError());
-    join_parts_kernel<DTYPE><<<grid_for((a.rows + kThreads / 64 - 1) / (kThreads / 64)), kThreads, 0, stream>>>(a, o, out, parts);
-    TDFA_HIP(hipGetLastError());
-    return TDFA_OK;
+    const int rc = launch(part_stats_kernel<DTYPE, 256, 8, BITS>, grid_for(a.rows * parts), 256, stream, a, out, parts, span);
+    if (rc != TDFA_OK) return rc;
+    return launch(join_parts_kernel<DTYPE>, grid_for((a.rows + kThreads / 64 - 1) / (kThreads / 64)), kThreads, stream, a, o, out, parts);
 }
 
 int64_t groups_of(const TokenRows& a) { return a.n_tokens / (a.dtype == TDFA_F32 ? Elem<TDFA_F32>::kGroup : Elem<TDFA_BF16>::kGroup); }
+
+bool in_parts(const TokenRows& a) { return a.rows <= kPartRows && groups_of(a) > kWholeGroups; }
 
 // parts: workspace for kMaxParts parts of each of the first kPartRows rows.  Few rows that are longer than a workgroup's registers are
 // shared out by parts, which a second launch joins: 1 row of 256,000 tokens in fp32 14.5 us by one workgroup, 6.8 so; 64 rows 34.5 and
 // 14.9, 300 rows 60.6 and 44.5; of 128,256 tokens 19.8 and 12.1, 28.7 and 24.9; 512 rows 38.1 and 37.9, in bf16 of 256,000 36.6 and 40.6.
 int stats_of(const TokenRows& a, const Outputs& o, Part* parts, hipStream_t stream)
 {
-    if (a.rows <= kPartRows && groups_of(a) > kWholeGroups) {
+    if (in_parts(a)) {
         if (a.dtype == TDFA_F32) return a.allow ? parts_launch<TDFA_F32, true>(a, o, parts, stream) : parts_launch<TDFA_F32, false>(a, o, parts, stream);
         return a.allow ? parts_launch<TDFA_BF16, true>(a, o, parts, stream) : parts_launch<TDFA_BF16, false>(a, o, parts, stream);
     }
@@ -876,17 +891,15 @@ template <int DTYPE, bool BITS>
 int grad_launch(const TokenRows& a, const float2* stats, const float* down, void* grad, int64_t grad_stride, const LossSum& sum, hipStream_t stream)
 {
     const int32_t n_groups = a.n_tokens / Elem<DTYPE>::kGroup, more = sum.each ? 1 : 0;
-    if (n_groups <= 256) {
-        token_grad_kernel<DTYPE, 64, 4, BITS><<<grid_for(a.rows + more), 64, 0, stream>>>(a, stats, down, grad, grad_stride, 1, sum);
-    } else {
-        const int32_t parts = (n_groups + 256 * 8 - 1) / (256 * 8);
-        token_grad_kernel<DTYPE, 256, 8, BITS><<<grid_for(a.rows * parts + more), 256, 0, stream>>>(a, stats, down, grad, grad_stride, parts, sum);
-    }
-    TDFA_HIP(hipGetLastError());
-    return TDFA_OK;
+    if (n_groups <= 256)
+        return launch(token_grad_kernel<DTYPE, 64, 4, BITS>, grid_for(a.rows + more), 64, stream, a, stats, down, grad, grad_stride, 1, sum);
+    const int32_t parts = (n_groups + 256 * 8 - 1) / (256 * 8);
+    return launch(token_grad_kernel<DTYPE, 256, 8, BITS>, grid_for(a.rows * parts + more), 256, stream, a, stats, down, grad, grad_stride, parts, sum);
 }
 
 }  // namespace
+
+bool token_logprobs_want_workspace(const TokenRows& a) { return in_parts(a); }
 
 int launch_token_logprobs(const TokenRows& a, float* logprobs, float* stats, void* workspace, hipStream_t stream)
 {
@@ -921,14 +934,10 @@ template <int DTYPE, bool BITS>
 static int policy_launch(const TokenRows& a, const PolicyArgs& p, float* logprobs, double* each, void* grad, int64_t grad_stride, hipStream_t stream)
 {
     const int32_t n_groups = a.n_tokens / Elem<DTYPE>::kGroup;
-#define ROWS(NT, R) policy_row_kernel<DTYPE, NT, R, BITS><<<grid_for(a.rows), NT, 0, stream>>>(a, p, logprobs, each, grad, grad_stride)
-    if (n_groups <= 64 * 8) ROWS(64, 8);
-    else if (n_groups <= 256 * 16) ROWS(256, 16);
-    else if (n_groups <= 512 * 16) ROWS(512, 16);
-    else ROWS(1024, 16);
-#undef ROWS
-    TDFA_HIP(hipGetLastError());
-    return TDFA_OK;
+    if (n_groups <= 64 * 8) return launch(policy_row_kernel<DTYPE, 64, 8, BITS>, grid_for(a.rows), 64, stream, a, p, logprobs, each, grad, grad_stride);
+    if (n_groups <= 256 * 16) return launch(policy_row_kernel<DTYPE, 256, 16, BITS>, grid_for(a.rows), 256, stream, a, p, logprobs, each, grad, grad_stride);
+    if (n_groups <= 512 * 16) return launch(policy_row_kernel<DTYPE, 512, 16, BITS>, grid_for(a.rows), 512, stream, a, p, logprobs, each, grad, grad_stride);
+    return launch(policy_row_kernel<DTYPE, 1024, 16, BITS>, grid_for(a.rows), 1024, stream, a, p, logprobs, each, grad, grad_stride);
 }
 
 // Whether a policy loss is scored and its gradient written by one launch, a workgroup per row that reads it once, or by two, which read
@@ -964,9 +973,7 @@ int launch_policy_loss(const TokenRows& a, const PolicyArgs& p, float* loss, flo
         const int rc = stats_of(a, o, parts, stream);
         if (rc != TDFA_OK || grad) return rc != TDFA_OK ? rc : grad_of(a, o.stats, o.down, grad, grad_stride, LossSum{each, a.rows, 1.0, loss}, stream);
     }
-    loss_sum_kernel<<<1, 1024, 0, stream>>>(LossSum{each, a.rows, 1.0, loss});
-    TDFA_HIP(hipGetLastError());
-    return TDFA_OK;
+    return launch(loss_sum_kernel, dim3(1), 1024, stream, LossSum{each, a.rows, 1.0, loss});
 }
 
 int launch_preference_loss(const TokenRows& a, const PairArgs& p, float* loss, float* logprobs, void* grad, int64_t grad_stride, void* workspace,
@@ -985,14 +992,12 @@ int launch_preference_loss(const TokenRows& a, const PairArgs& p, float* loss, f
         if (rc != TDFA_OK) return rc;
     }
     if (p.n_pairs) {
-        pair_kernel<<<blocks_for(p.n_pairs), kThreads, 0, stream>>>(p, a.rows, exact, o.stats, o.down, each);
-        TDFA_HIP(hipGetLastError());
+        const int rc = launch(pair_kernel, dim3(blocks_for(p.n_pairs)), kThreads, stream, p, a.rows, exact, o.stats, o.down, each);
+        if (rc != TDFA_OK) return rc;
     }
     const LossSum sum = {each, p.n_pairs, p.n_pairs ? 1.0 / (double)p.n_pairs : 0.0, loss};
     if (grad && a.rows) return grad_of(a, o.stats, o.down, grad, grad_stride, sum, stream);
-    loss_sum_kernel<<<1, 1024, 0, stream>>>(sum);
-    TDFA_HIP(hipGetLastError());
-    return TDFA_OK;
+    return launch(loss_sum_kernel, dim3(1), 1024, stream, sum);
 }
 
 }  // namespace tdfa

@@ -293,6 +293,7 @@ struct PairArgs {
 // Bytes of workspace that the launchers below want (16-byte aligned).
 int64_t loss_workspace(int64_t rows, int64_t n_pairs);
 // logprobs: [rows]; stats: [rows][2] or NULL; grad: rows of the type of the logits, or NULL.
+bool token_logprobs_want_workspace(const TokenRows& a);       // otherwise it may be NULL
 int launch_token_logprobs(const TokenRows& a, float* logprobs, float* stats, void* workspace, hipStream_t stream);
 int launch_token_grad(const TokenRows& a, const float* stats, const float* down, void* grad, int64_t grad_stride, hipStream_t stream);
 int launch_policy_loss(const TokenRows& a, const PolicyArgs& p, float* loss, float* logprobs, void* grad, int64_t grad_stride, void* workspace,
