@@ -674,7 +674,8 @@ __global__ void __launch_bounds__(NT) token_grad_kernel(TokenRows a, const float
         sum_losses<NT>(sum, s_part);
         return;
     }
-    const int64_t i = w / parts;
+    // (there are less than 2^32 parts of rows: a part is 16 KB or a row)
+    const int64_t i = (uint32_t)w / (uint32_t)parts;
     const int32_t part = (int32_t)(w - i * parts);
     if (i >= a.rows) return;
     const Row r = row_of(a, i);
@@ -855,6 +856,9 @@ int stats_launch(const TokenRows& a, const Outputs& o, hipStream_t stream)
     const int32_t n_groups = a.n_tokens / Elem<DTYPE>::kGroup;
     // Two rows or more to a compute unit, so that one is fetched while another is summed.
     if (n_groups <= 64 * 4) return launch(token_stats_kernel<DTYPE, 64, 4, BITS>, grid_for(a.rows), 64, stream, a, o);
+    // Rows too few to fill the card are shared by more wavefronts each: 24 rows of 32,000 tokens in bf16 6.0 -> 5.1 us, 400 rows 8.2 -> 7.7;
+    // of 8,000 tokens 4.1 either way, 400 rows 4.5 -> 5.4.
+    if (a.rows <= 512 && n_groups > 256 * 8 && n_groups <= 512 * 16) return launch(token_stats_kernel<DTYPE, 1024, 4, BITS>, grid_for(a.rows), 1024, stream, a, o);
     if (n_groups <= 256 * 16) return launch(token_stats_kernel<DTYPE, 256, 8, BITS>, grid_for(a.rows), 256, stream, a, o);
     if (n_groups <= 512 * 16) return launch(token_stats_kernel<DTYPE, 512, 8, BITS>, grid_for(a.rows), 512, stream, a, o);
     return launch(token_stats_kernel<DTYPE, 1024, 8, BITS>, grid_for(a.rows), 1024, stream, a, o);
@@ -893,8 +897,11 @@ int grad_launch(const TokenRows& a, const float2* stats, const float* down, void
     const int32_t n_groups = a.n_tokens / Elem<DTYPE>::kGroup, more = sum.each ? 1 : 0;
     if (n_groups <= 256)
         return launch(token_grad_kernel<DTYPE, 64, 4, BITS>, grid_for(a.rows + more), 64, stream, a, stats, down, grad, grad_stride, 1, sum);
-    const int32_t parts = (n_groups + 256 * 8 - 1) / (256 * 8);
-    return launch(token_grad_kernel<DTYPE, 256, 8, BITS>, grid_for(a.rows * parts + more), 256, stream, a, stats, down, grad, grad_stride, parts, sum);
+    // Few rows in parts of half the size: gradients of 128 rows of 32,000 tokens in bf16 7 -> 6 us; 2,048 of 128,256 107 -> 112.
+    const bool few = a.rows <= 128;
+    const int32_t span = few ? 256 * 4 : 256 * 8, parts = (n_groups + span - 1) / span;
+    return launch(few ? token_grad_kernel<DTYPE, 256, 4, BITS> : token_grad_kernel<DTYPE, 256, 8, BITS>, grid_for(a.rows * parts + more), 256, stream, a, stats,
+                  down, grad, grad_stride, parts, sum);
 }
 
 }  // namespace
@@ -934,20 +941,23 @@ template <int DTYPE, bool BITS>
 static int policy_launch(const TokenRows& a, const PolicyArgs& p, float* logprobs, double* each, void* grad, int64_t grad_stride, hipStream_t stream)
 {
     const int32_t n_groups = a.n_tokens / Elem<DTYPE>::kGroup;
+    // The more wavefronts share a row, the sooner it is read: 1,500 rows of 32,000 tokens in bf16 34.4 us by 1,024 threads of 4 groups,
+    // 38.5 by 256 of 16; 24 rows 9.1 and 10.4 (of 20,000 tokens, 1,500 rows 27.6 and 26.3).
     if (n_groups <= 64 * 8) return launch(policy_row_kernel<DTYPE, 64, 8, BITS>, grid_for(a.rows), 64, stream, a, p, logprobs, each, grad, grad_stride);
-    if (n_groups <= 256 * 16) return launch(policy_row_kernel<DTYPE, 256, 16, BITS>, grid_for(a.rows), 256, stream, a, p, logprobs, each, grad, grad_stride);
-    if (n_groups <= 512 * 16) return launch(policy_row_kernel<DTYPE, 512, 16, BITS>, grid_for(a.rows), 512, stream, a, p, logprobs, each, grad, grad_stride);
+    if (n_groups <= 256 * 8) return launch(policy_row_kernel<DTYPE, 256, 8, BITS>, grid_for(a.rows), 256, stream, a, p, logprobs, each, grad, grad_stride);
+    if (n_groups <= 1024 * 4) return launch(policy_row_kernel<DTYPE, 1024, 4, BITS>, grid_for(a.rows), 1024, stream, a, p, logprobs, each, grad, grad_stride);
+    if (n_groups <= 1024 * 8) return launch(policy_row_kernel<DTYPE, 1024, 8, BITS>, grid_for(a.rows), 1024, stream, a, p, logprobs, each, grad, grad_stride);
     return launch(policy_row_kernel<DTYPE, 1024, 16, BITS>, grid_for(a.rows), 1024, stream, a, p, logprobs, each, grad, grad_stride);
 }
 
 // Whether a policy loss is scored and its gradient written by one launch, a workgroup per row that reads it once, or by two, which read
-// it twice but share the second out by parts of rows.  Two are faster where few long rows leave compute units idle (16 rows of
-// 128,256 tokens in bf16 14.3 us against 18.0, of 32,000 10.7 against 11.2; 64 rows 20.8 against 19.2) and where a row does not fit
+// it twice but share the second out by parts of rows.  Two are faster where few long rows leave compute units idle (24 rows of
+// 128,256 tokens in bf16 14.9 us against 18.4, of 64,000 11.0 against 12.1; 96 rows 21.8 against 20.1) and where a row does not fit
 // a workgroup's registers (300 rows of 256,000 in fp32 117 us, 167 with half of every row read twice by one launch).
 bool one_launch(const TokenRows& a)
 {
     const int64_t n_groups = groups_of(a);
-    return n_groups <= kWholeGroups && (a.rows > 32 || n_groups <= 2048);
+    return n_groups <= kWholeGroups && (a.rows > 32 || n_groups <= 1024 * 4);
 }
 
 int launch_policy_loss(const TokenRows& a, const PolicyArgs& p, float* loss, float* logprobs, void* grad, int64_t grad_stride, void* workspace,

@@ -56,7 +56,8 @@ def policy(lp, live, old, ref, adv, weights, low, high, kl):
         down = down + kl * (1.0 - e)
         size = size + abs(kl) * (e + 1.0 + np.abs(ref - x))
     w = np.where(live, weights, 0.0)
-    return float((w * np.where(live, each, 0.0)).sum()), w * down, np.abs(w) * size
+    each, down, size = (np.where(live, a, 0.0) for a in (each, down, size))       # (exp of the others may overflow)
+    return float((w * each).sum()), w * down, np.abs(w) * size
 
 
 def preference(lp, live, ref, begin, beta, smoothing):

@@ -169,6 +169,36 @@ def test_uniform_and_extreme_rows(T, dtype, v, fill):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,v", [(5, 300), (40, 5000), (3, 40001), (140, 9000), (2, 140001)])
+def test_low_temperatures(T, dtype, n, v):
+    """Tokens whose probability is far below what a sum of exponentials relative to them can hold (lp below -87)."""
+    _check_logprobs(T, Case(T, n, v, dtype, 31, sigma=3.0), 0.02)
+    _run_policy(T, Case(T, n, v, dtype, 32, sigma=3.0), 0.02, (0.2, 0.2), 0.05)
+    _run_policy(T, Case(T, n, v, dtype, 33, constrained=False, sigma=3.0), 0.02, (0.2, 0.2), 0.05)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("groups", [255, 256, 257, 512, 513, 2048, 2049, 4096, 4097, 8192, 8193, 16384, 16385])
+def test_rows_at_the_edges_of_launch_shapes(T, dtype, groups):
+    """Whole numbers of 16-byte groups, and an element or two more, around every length at which another launch shape is taken."""
+    v = groups * (4 if dtype == "f32" else 8) + groups % 3
+    for n in (3, 40):
+        if n * v > 3_000_000:
+            n = 34
+        c = Case(T, n, v, dtype, 34)
+        _check_logprobs(T, c, 1.0)
+        _run_policy(T, Case(T, n, v, dtype, 35), 1.0, (0.2, 0.2), 0.05)
+    _run_preference(T, Case(T, 4, v, dtype, 36), 1.0, 0.3, 0.0, [0, 1, 4])
+
+
+@pytest.mark.parametrize("n,v", [(129, 16400), (513, 9000), (385, 65601), (384, 65601)])
+def test_many_rows_at_the_edges_of_launch_shapes(T, n, v):
+    c = Case(T, n, v, "f32", 37)
+    _check_logprobs(T, c, 1.0)
+    _run_policy(T, c, 1.0, (0.2, 0.2), 0.05)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_infinite_logit_is_loud(T, dtype):
     c = Case(T, 3, 2000, dtype, 5, False)
     c.x[1, 77] = math.inf
@@ -519,6 +549,17 @@ def test_refusals(T):
         (ValueError, lambda: T.token_logprobs_backward(c.table, c.logits, c.states, c.tokens, stats, ones, None)),
         (T.TdfaError, lambda: T.token_logprobs_backward(c.table, x[:2, :100], c.states, c.tokens, stats, ones, x[1:3, :100])),
     ]
+    lib, addr = T.lib(), [x.data_ptr(), c.states.data_ptr(), c.tokens.data_ptr(), lp.data_ptr()]
+    assert lib.tdfa_token_logprobs(None, addr[0], 1, 4, (1 << 24) + 1, 1 << 25, None, addr[2], 1.0, addr[3], None, None, 0, None) == -1
+    assert lib.tdfa_token_logprobs(c.table._h, addr[0], 1, 4, 99, 128, addr[1], addr[2], 1.0, addr[3], None, None, 0, None) == -1
+    assert lib.tdfa_token_logprobs(c.table._h, addr[0], 2, 4, 100, 128, addr[1], addr[2], 1.0, addr[3], None, None, 0, None) == -1
+    assert lib.tdfa_token_logprobs(c.table._h, addr[0], 1, -1, 100, 128, addr[1], addr[2], 1.0, addr[3], None, None, 0, None) == -1
+    assert lib.tdfa_token_logprobs(c.table._h, None, 1, 4, 100, 128, addr[1], addr[2], 1.0, addr[3], None, None, 0, None) == -1
+    assert lib.tdfa_token_logprobs(None, addr[0], 1, 1, 1 << 20, 1 << 20, None, addr[2], 1.0, addr[3], None, None, 0, None) == -1      # wants a workspace
+    assert lib.tdfa_policy_loss(None, addr[0], 1, 4, 100, 128, None, addr[2], 1.0, addr[3], None, addr[3], None, 0.2, 0.2, 0.0, loss.data_ptr(),
+                                addr[3], None, 0, None, 0, None) == -1
+    assert b"workspace" in lib.tdfa_last_error()
+    assert lib.tdfa_loss_workspace_bytes(-1, 0) == -1 and lib.tdfa_loss_workspace_bytes(0, -1) == -1
     for k, (error, call) in enumerate(refused):
         with pytest.raises(error):
             call()
