@@ -24,7 +24,6 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr float kLog2e = 1.44269504088896341f;
-constexpr float kLn2 = 0.693147180559945309f;
 constexpr float kLowest = -3.402823466e38f;
 
 // Logits are read and gradients written in groups of 16 bytes.
