@@ -16,6 +16,7 @@
 // alone (0: no token was chosen; -inf: probability zero), so that their logits are not read.
 #include "tdfa_internal.h"
 
+#include <algorithm>
 #include <cmath>
 #include <tuple>
 
@@ -625,12 +626,105 @@ __device__ __forceinline__ float last_gradient(float z, Slope q, float c2, bool 
     return own ? g + q.d : g;
 }
 
+// Sums of lp - ref over the rows of the two sequences of pair k, as far as `lane` of `width` lanes has them.  A sequence that reaches
+// outside the rows is cut there.
+__device__ __forceinline__ void add_pair(const PairArgs& p, int64_t rows, const double* exact, const float2* stats, int64_t k, int lane, int width, double (&sum)[2])
+{
+    const int64_t b0 = p.begin[2 * k], b1 = p.begin[2 * k + 1], b2 = p.begin[2 * k + 2];
+#pragma unroll
+    for (int side = 0; side < 2; ++side) {
+        const int64_t from = max(side ? b1 : b0, (int64_t)0), to = min(side ? b2 : b1, rows);
+        for (int64_t i = from + lane; i < to; i += width) {
+            const double lp = exact[i], ref = (double)p.ref_logprobs[i];
+            if (stats[i].y != INFINITY) sum[side] += lp - ref;
+        }
+    }
+}
+// softplus(x) = max(x, 0) + log1p(exp(-|x|)); binary32 from the difference of the rewards on.
+__device__ __forceinline__ float pair_loss(const PairArgs& p, float gap)
+{
+    const float tail = log1pf(expf(-fabsf(gap)));
+    return (1.0f - p.smoothing) * (fmaxf(-gap, 0.0f) + tail) + p.smoothing * (fmaxf(gap, 0.0f) + tail);
+}
+// d loss / d lp of a row of the pair's first sequence.
+__device__ __forceinline__ float pair_slope(const PairArgs& p, float gap)
+{
+    return (p.smoothing / (1.0f + expf(-gap)) - (1.0f - p.smoothing) / (1.0f + expf(gap))) * (p.beta / (float)p.n_pairs);
+}
+
+// All pairs by one workgroup, 16 lanes to a pair: the rewards and the loss.
+template <int NT>
+__device__ __forceinline__ void sum_pairs(const PairArgs& p, int64_t rows, const double* exact, const float2* stats, float* loss, double (&part)[NT / 64])
+{
+    double total = 0.0;
+    const int lane = threadIdx.x & 15;
+    for (int64_t k0 = 0; k0 < p.n_pairs; k0 += NT / 16) {
+        const int64_t k = k0 + threadIdx.x / 16;
+        double sum[2] = {0.0, 0.0};
+        if (k < p.n_pairs) add_pair(p, rows, exact, stats, k, lane, 16, sum);
+#pragma unroll
+        for (int d = 8; d; d >>= 1) {
+            sum[0] += __shfl_xor(sum[0], d);
+            sum[1] += __shfl_xor(sum[1], d);
+        }
+        if (lane == 0 && k < p.n_pairs) {
+            const double chosen = (double)p.beta * sum[0], rejected = (double)p.beta * sum[1];
+            p.rewards[2 * k] = (float)chosen;
+            p.rewards[2 * k + 1] = (float)rejected;
+            total += (double)pair_loss(p, (float)(chosen - rejected));
+        }
+    }
+#pragma unroll
+    for (int d = 32; d; d >>= 1) total += __shfl_xor(total, d);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = total;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < NT / 64; ++w) total += part[w];
+        *loss = (float)(total / (double)p.n_pairs);
+    }
+}
+
+// d loss / d lp of row i, by the whole workgroup: its sequence is looked for and the pair's rewards are summed again.  Of few rows and
+// pairs this costs less than a launch that hands it on.
+template <int NT>
+__device__ __forceinline__ float slope_of_row(const PairArgs& p, int64_t rows, const double* exact, const float2* stats, int64_t i, int& found, double (&part)[2][NT / 64])
+{
+    if (threadIdx.x == 0) found = -1;
+    __syncthreads();
+    for (int k = threadIdx.x; k < 2 * p.n_pairs; k += NT)
+        if (p.begin[k] <= i && i < p.begin[k + 1]) found = k;
+    __syncthreads();
+    const int k = __builtin_amdgcn_readfirstlane(found);
+    if (k < 0) return 0.0f;
+    double sum[2] = {0.0, 0.0};
+    add_pair(p, rows, exact, stats, k / 2, threadIdx.x, NT, sum);
+#pragma unroll
+    for (int d = 32; d; d >>= 1) {
+        sum[0] += __shfl_xor(sum[0], d);
+        sum[1] += __shfl_xor(sum[1], d);
+    }
+    if ((threadIdx.x & 63) == 0) {
+        part[0][threadIdx.x >> 6] = sum[0];
+        part[1][threadIdx.x >> 6] = sum[1];
+    }
+    __syncthreads();
+    sum[0] = part[0][0];
+    sum[1] = part[1][0];
+#pragma unroll
+    for (int w = 1; w < NT / 64; ++w) {
+        sum[0] += part[0][w];
+        sum[1] += part[1][w];
+    }
+    const float slope = pair_slope(p, (float)((double)p.beta * sum[0] - (double)p.beta * sum[1]));
+    return k & 1 ? -slope : slope;
+}
+
 // loss = scale * the sum of each, by one workgroup, in an order that depends on nothing but n and NT.
 struct LossSum {
-    const double* each;        // or NULL: no sum is wanted
+    const double* each;
     int64_t n;
     double scale;
-    float* loss;
+    float* loss;               // or NULL: no sum is wanted
 };
 template <int NT>
 __device__ __forceinline__ void sum_losses(const LossSum& q, double (&part)[NT / 64])
@@ -654,9 +748,11 @@ __global__ void __launch_bounds__(1024) loss_sum_kernel(LossSum q)
 
 // grad[i][j] = down[i] c ([j = t] - p_j) over A, 0 elsewhere; 0 throughout in a row that takes no part.  A workgroup
 // takes NT U groups of one row; the last of a row takes the elements behind the last whole group too.  One more workgroup, the first,
-// sums the losses that an earlier launch has left, if that is wanted.
-template <int DTYPE, int NT, int U, bool BITS>
-__global__ void __launch_bounds__(NT) token_grad_kernel(TokenRows a, const float2* stats, const float* down, void* grad, int64_t grad_stride, int32_t parts, LossSum sum)
+// sums the losses that an earlier launch has left, if that is wanted.  PAIRS: d loss / d lp is worked out here (slope_of_row), and that first
+// workgroup does what the pairs' own launch would.
+template <int DTYPE, int NT, int U, bool BITS, bool PAIRS>
+__global__ void __launch_bounds__(NT)
+token_grad_kernel(TokenRows a, const float2* stats, const float* down, void* grad, int64_t grad_stride, int32_t parts, LossSum sum, PairArgs pairs, const double* exact)
 {
     using E = typename Elem<DTYPE>::type;
     constexpr int G = Elem<DTYPE>::kGroup;
@@ -668,9 +764,10 @@ __global__ void __launch_bounds__(NT) token_grad_kernel(TokenRows a, const float
     const float c2 = a.inv_t * kLog2e;
     const int32_t n_groups = a.n_tokens / G;
     int64_t w = block_index();
-    if (sum.each && w-- == 0) {
+    if (sum.loss && w-- == 0) {
         __shared__ double s_part[NT / 64];
-        sum_losses<NT>(sum, s_part);
+        if constexpr (PAIRS) sum_pairs<NT>(pairs, a.rows, exact, stats, sum.loss, s_part);
+        else sum_losses<NT>(sum, s_part);
         return;
     }
     // (there are less than 2^32 parts of rows: a part is 16 KB or a row)
@@ -679,7 +776,14 @@ __global__ void __launch_bounds__(NT) token_grad_kernel(TokenRows a, const float
     if (i >= a.rows) return;
     const Row r = row_of(a, i);
     const float2 st = stats[i];
-    const float slope = down[i];
+    float slope;
+    if constexpr (PAIRS) {
+        __shared__ int s_found;
+        __shared__ double s_sums[2][NT / 64];
+        slope = slope_of_row<NT>(pairs, a.rows, exact, stats, i, s_found, s_sums);
+    } else {
+        slope = down[i];
+    }
     const Slope q = shared_by_wave(slope_of<DTYPE>(r.read && st.y != INFINITY ? slope * a.inv_t : 0.0f, st.x, fabsf(st.y), c2, signbit(st.y)));
     const E* row = static_cast<const E*>(a.logits) + i * a.row_stride;
     E* out = static_cast<E*>(grad) + i * grad_stride;
@@ -793,42 +897,44 @@ __global__ void __launch_bounds__(NT, 4) policy_row_kernel(TokenRows a, PolicyAr
     if (behind < a.n_tokens) store_rounded(out + behind, last_gradient(last, q, c2, behind == r.token));
 }
 
-// One workgroup per pair, half of it to a sequence: the two rewards, the pair's loss, and d loss / d lp of every row of the pair.
-// Bound by its chain of reads.
+// One workgroup per pair: the two rewards, the pair's loss, and d loss / d lp of every row of the pair.  Bound by its chain of reads.
 __global__ void __launch_bounds__(kThreads)
 pair_kernel(PairArgs p, int64_t rows, const double* exact, const float2* stats, float* down, double* each)
 {
-    __shared__ double s_part[kThreads / 64];
-    const int half = threadIdx.x / (kThreads / 2), lane = threadIdx.x % (kThreads / 2);
+    __shared__ double s_part[2][kThreads / 64];
     for (int64_t k = blockIdx.x; k < p.n_pairs; k += gridDim.x) {
-        // a sequence that reaches outside the rows is cut there
-        const int64_t from = max((int64_t)p.begin[2 * k + half], (int64_t)0), to = min((int64_t)p.begin[2 * k + half + 1], rows);
-        double sum = 0.0;
-        for (int64_t i = from + lane; i < to; i += kThreads / 2) {
-            const double lp = exact[i], ref = (double)p.ref_logprobs[i];
-            if (stats[i].y != INFINITY) sum += lp - ref;
-        }
+        double sum[2] = {0.0, 0.0};
+        add_pair(p, rows, exact, stats, k, threadIdx.x, kThreads, sum);
 #pragma unroll
-        for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
-        __syncthreads();
-        if ((threadIdx.x & 63) == 0) s_part[threadIdx.x >> 6] = sum;
-        __syncthreads();
-        constexpr int W = kThreads / 128;                  // wavefronts to a sequence
-        double reward[2] = {s_part[0], s_part[W]};
-#pragma unroll
-        for (int w = 1; w < W; ++w) {
-            reward[0] += s_part[w];
-            reward[1] += s_part[W + w];
+        for (int d = 32; d; d >>= 1) {
+            sum[0] += __shfl_xor(sum[0], d);
+            sum[1] += __shfl_xor(sum[1], d);
         }
-        reward[0] *= (double)p.beta;
-        reward[1] *= (double)p.beta;
-        // softplus(x) = max(x, 0) + log1p(exp(-|x|)); binary32 from here on
-        const float gap = (float)(reward[0] - reward[1]), eps = p.smoothing, tail = log1pf(expf(-fabsf(gap)));
-        if (lane == 0) p.rewards[2 * k + half] = (float)reward[half];
-        if (threadIdx.x == 0) each[k] = (double)((1.0f - eps) * (fmaxf(-gap, 0.0f) + tail) + eps * (fmaxf(gap, 0.0f) + tail));
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) {
+            s_part[0][threadIdx.x >> 6] = sum[0];
+            s_part[1][threadIdx.x >> 6] = sum[1];
+        }
+        __syncthreads();
+        sum[0] = s_part[0][0];
+        sum[1] = s_part[1][0];
+#pragma unroll
+        for (int w = 1; w < kThreads / 64; ++w) {
+            sum[0] += s_part[0][w];
+            sum[1] += s_part[1][w];
+        }
+        const double chosen = (double)p.beta * sum[0], rejected = (double)p.beta * sum[1];
+        const float gap = (float)(chosen - rejected);
+        if (threadIdx.x == 0) {
+            p.rewards[2 * k] = (float)chosen;
+            p.rewards[2 * k + 1] = (float)rejected;
+            each[k] = (double)pair_loss(p, gap);
+        }
         if (down) {
-            const float slope = (eps / (1.0f + expf(-gap)) - (1.0f - eps) / (1.0f + expf(gap))) * (p.beta / (float)p.n_pairs);
-            for (int64_t i = from + lane; i < to; i += kThreads / 2) down[i] = half ? -slope : slope;
+            const float slope = pair_slope(p, gap);
+            const int64_t b0 = p.begin[2 * k], b1 = p.begin[2 * k + 1], b2 = p.begin[2 * k + 2];
+            for (int64_t i = max(b0, (int64_t)0) + threadIdx.x; i < min(b1, rows); i += kThreads) down[i] = slope;
+            for (int64_t i = max(b1, (int64_t)0) + threadIdx.x; i < min(b2, rows); i += kThreads) down[i] = -slope;
         }
     }
 }
@@ -890,17 +996,27 @@ int stats_of(const TokenRows& a, const Outputs& o, Part* parts, hipStream_t stre
     return a.allow ? stats_launch<TDFA_BF16, true>(a, o, stream) : stats_launch<TDFA_BF16, false>(a, o, stream);
 }
 
-template <int DTYPE, bool BITS>
-int grad_launch(const TokenRows& a, const float2* stats, const float* down, void* grad, int64_t grad_stride, const LossSum& sum, hipStream_t stream)
+// What the gradient of a preference loss of few rows and pairs is made of; exact NULL: not that.
+struct FewPairs {
+    PairArgs pairs;
+    const double* exact;
+};
+
+template <int DTYPE, bool BITS, bool PAIRS>
+int grad_launch(const TokenRows& a, const float2* stats, const float* down, void* grad, int64_t grad_stride, const LossSum& sum, const FewPairs& few_pairs,
+                hipStream_t stream)
 {
-    const int32_t n_groups = a.n_tokens / Elem<DTYPE>::kGroup, more = sum.each ? 1 : 0;
-    if (n_groups <= 256)
-        return launch(token_grad_kernel<DTYPE, 64, 4, BITS>, grid_for(a.rows + more), 64, stream, a, stats, down, grad, grad_stride, 1, sum);
+    const int32_t n_groups = a.n_tokens / Elem<DTYPE>::kGroup, more = sum.loss ? 1 : 0;
+    if constexpr (!PAIRS) {
+        if (n_groups <= 256)
+            return launch(token_grad_kernel<DTYPE, 64, 4, BITS, false>, grid_for(a.rows + more), 64, stream, a, stats, down, grad, grad_stride, 1, sum,
+                          few_pairs.pairs, few_pairs.exact);
+    }
     // Few rows in parts of half the size: gradients of 128 rows of 32,000 tokens in bf16 7 -> 6 us; 2,048 of 128,256 107 -> 112.
     const bool few = a.rows <= 128;
-    const int32_t span = few ? 256 * 4 : 256 * 8, parts = (n_groups + span - 1) / span;
-    return launch(few ? token_grad_kernel<DTYPE, 256, 4, BITS> : token_grad_kernel<DTYPE, 256, 8, BITS>, grid_for(a.rows * parts + more), 256, stream, a, stats,
-                  down, grad, grad_stride, parts, sum);
+    const int32_t span = few ? 256 * 4 : 256 * 8, parts = std::max(1, (n_groups + span - 1) / span);
+    return launch(few ? token_grad_kernel<DTYPE, 256, 4, BITS, PAIRS> : token_grad_kernel<DTYPE, 256, 8, BITS, PAIRS>, grid_for(a.rows * parts + more), 256,
+                  stream, a, stats, down, grad, grad_stride, parts, sum, few_pairs.pairs, few_pairs.exact);
 }
 
 }  // namespace
@@ -916,19 +1032,21 @@ int launch_token_logprobs(const TokenRows& a, float* logprobs, float* stats, voi
     return stats_of(a, o, static_cast<Part*>(workspace), stream);
 }
 
-static int grad_of(const TokenRows& a, const float2* stats, const float* down, void* grad, int64_t grad_stride, const LossSum& sum, hipStream_t stream)
+template <bool PAIRS>
+static int grad_of(const TokenRows& a, const float2* stats, const float* down, void* grad, int64_t grad_stride, const LossSum& sum, const FewPairs& few,
+                   hipStream_t stream)
 {
     if (a.dtype == TDFA_F32)
-        return a.allow ? grad_launch<TDFA_F32, true>(a, stats, down, grad, grad_stride, sum, stream)
-                       : grad_launch<TDFA_F32, false>(a, stats, down, grad, grad_stride, sum, stream);
-    return a.allow ? grad_launch<TDFA_BF16, true>(a, stats, down, grad, grad_stride, sum, stream)
-                   : grad_launch<TDFA_BF16, false>(a, stats, down, grad, grad_stride, sum, stream);
+        return a.allow ? grad_launch<TDFA_F32, true, PAIRS>(a, stats, down, grad, grad_stride, sum, few, stream)
+                       : grad_launch<TDFA_F32, false, PAIRS>(a, stats, down, grad, grad_stride, sum, few, stream);
+    return a.allow ? grad_launch<TDFA_BF16, true, PAIRS>(a, stats, down, grad, grad_stride, sum, few, stream)
+                   : grad_launch<TDFA_BF16, false, PAIRS>(a, stats, down, grad, grad_stride, sum, few, stream);
 }
 
 int launch_token_grad(const TokenRows& a, const float* stats, const float* down, void* grad, int64_t grad_stride, hipStream_t stream)
 {
     if (a.rows == 0) return TDFA_OK;
-    return grad_of(a, reinterpret_cast<const float2*>(stats), down, grad, grad_stride, LossSum{}, stream);
+    return grad_of<false>(a, reinterpret_cast<const float2*>(stats), down, grad, grad_stride, LossSum{}, FewPairs{}, stream);
 }
 
 // Workspace: Part [kMaxParts] of each of the first kPartRows rows, double [rows] (lp, or the rows' losses), double [n_pairs] losses of the
@@ -980,7 +1098,7 @@ int launch_policy_loss(const TokenRows& a, const PolicyArgs& p, float* loss, flo
             o.down = reinterpret_cast<float*>(o.stats + a.rows);
         }
         const int rc = stats_of(a, o, parts, stream);
-        if (rc != TDFA_OK || grad) return rc != TDFA_OK ? rc : grad_of(a, o.stats, o.down, grad, grad_stride, LossSum{each, a.rows, 1.0, loss}, stream);
+        if (rc != TDFA_OK || grad) return rc != TDFA_OK ? rc : grad_of<false>(a, o.stats, o.down, grad, grad_stride, LossSum{each, a.rows, 1.0, loss}, FewPairs{}, stream);
     }
     return launch(loss_sum_kernel, dim3(1), 1024, stream, LossSum{each, a.rows, 1.0, loss});
 }
@@ -1000,12 +1118,16 @@ int launch_preference_loss(const TokenRows& a, const PairArgs& p, float* loss, f
         const int rc = stats_of(a, o, parts, stream);
         if (rc != TDFA_OK) return rc;
     }
+    // Few rows and pairs without the launch between the other two: 90 rows of 32,000 tokens in bf16 in 4 pairs 13.9 -> 12.2 us, 1,000 rows
+    // in 64 pairs 34.4 -> 32.5 (of 1,000 tokens 11.6 -> 13.0), and 3.3 us less of the host; 300 rows in 128 pairs 10.7 -> 16.8.
+    if (grad && a.rows && a.rows <= 1024 && p.n_pairs && p.n_pairs <= 64)
+        return grad_of<true>(a, o.stats, nullptr, grad, grad_stride, LossSum{nullptr, 0, 0.0, loss}, FewPairs{p, exact}, stream);
     if (p.n_pairs) {
         const int rc = launch(pair_kernel, dim3(blocks_for(p.n_pairs)), kThreads, stream, p, a.rows, exact, o.stats, o.down, each);
         if (rc != TDFA_OK) return rc;
     }
     const LossSum sum = {each, p.n_pairs, p.n_pairs ? 1.0 / (double)p.n_pairs : 0.0, loss};
-    if (grad && a.rows) return grad_of(a, o.stats, o.down, grad, grad_stride, sum, stream);
+    if (grad && a.rows) return grad_of<false>(a, o.stats, o.down, grad, grad_stride, sum, FewPairs{}, stream);
     return launch(loss_sum_kernel, dim3(1), 1024, stream, sum);
 }
 
