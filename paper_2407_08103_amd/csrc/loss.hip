@@ -113,6 +113,8 @@ __device__ __forceinline__ float token_logit(const Row& r, const E* row)
     uint32_t word = r.bits ? r.bits[r.token >> 5] : 0xFFFFFFFFu;
     float z = to_f32(row[r.token]);
     asm volatile("" : "+v"(word), "+v"(z));                // both are on their way before either is looked at
+    word = __builtin_amdgcn_readfirstlane(word);
+    z = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(z)));
     return (word >> (r.token & 31) & 1) && z == z ? z : -INFINITY;
 }
 
@@ -209,6 +211,7 @@ __device__ __forceinline__ bool settle(uint4& x, uint32_t b, int32_t g, int32_t 
     if constexpr (BITS) {
         if (!__ballot(b != 0)) return false;
         x = keep_allowed<DTYPE>(x, b, masks);
+        asm volatile("" : "+v"(x.x), "+v"(x.y), "+v"(x.z), "+v"(x.w));      // masked once, not again in every element
     } else {
         const int32_t g0 = __builtin_amdgcn_readfirstlane(g);             // (lanes are in the order of their groups)
         if (g0 >= n_groups) return false;
@@ -891,7 +894,8 @@ __global__ void __launch_bounds__(NT, 4) policy_row_kernel(TokenRows a, PolicyAr
         if (behind < a.n_tokens) store_rounded(out + behind, 0.0f);
         return;
     }
-    const Writer<DTYPE> writer(q, c2, r.token);
+    some = __builtin_amdgcn_readfirstlane(some);
+    const Writer<DTYPE> writer(shared_by_wave(q), c2, r.token);
 #pragma unroll
     for (int k = 0; k < R; ++k) writer.write(to, (int32_t)threadIdx.x + k * NT, x[k], some >> k & 1);
     if (behind < a.n_tokens) store_rounded(out + behind, last_gradient(last, q, c2, behind == r.token));
