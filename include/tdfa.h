@@ -454,8 +454,9 @@ TDFA_API int64_t tdfa_loss_workspace_bytes(int32_t rows, int32_t n_pairs);
 
 /* logprobs[i] = lp of row i.
  *   logprobs_dev : device, float [rows], written.
- *   stats_dev    : device, float [rows][2], or NULL: receives {m, ln s} of every row that takes part and
- *                  {0, +inf} of the others, for tdfa_token_logprobs_backward. */
+ *   stats_dev    : device, float [rows][2], or NULL: receives, for tdfa_token_logprobs_backward, what the sum of
+ *                  every row that takes part was taken relative to and its logarithm (with a sign of the
+ *                  library's own), and {0, +inf} of the others. */
 TDFA_API int tdfa_token_logprobs(const tdfa_table *table, const void *logits_dev, int dtype, int32_t rows,
                         int32_t n_tokens, int64_t row_stride, const int32_t *states_dev, const int32_t *tokens_dev,
                         float temperature, float *logprobs_dev, float *stats_dev,
