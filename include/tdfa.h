@@ -426,7 +426,8 @@ TDFA_API int tdfa_sample_noise(int32_t batch, int32_t n_tokens, uint64_t seed, u
  * Arguments they share:
  *   table       : the constraint, dense or packed, or NULL: every token is allowed.
  *   logits_dev, dtype, row_stride : as tdfa_mask_step ([rows][row_stride], rows 16-byte aligned, the
- *                 first n_tokens of each row are used, nothing behind them is read or written).
+ *                 first n_tokens of each row are used, nothing behind them is read or written; rows less than 2^36
+ *                 bytes apart).
  *   n_tokens    : 0 .. 2^24; that of the table if there is one.
  *   states_dev  : device, int32 [rows]: the state before the row's token; may be NULL without a table.
  *   tokens_dev  : device, int32 [rows].
@@ -435,6 +436,7 @@ TDFA_API int tdfa_sample_noise(int32_t batch, int32_t n_tokens, uint64_t seed, u
  *                 tdfa_loss_workspace_bytes(rows, n_pairs) bytes (n_pairs 0 unless the call has pairs).
  *                 It need not be cleared, and must not be used by anything else until the call's work is done.
  *                 tdfa_token_logprobs takes NULL too where a row of logits is at most 256 KiB long.
+ * What a call writes must not overlap anything else that it reads or writes, but for a gradient in place of the logits.
  * Row i has logits z, allowed set A (of states[i]), token t and c = 1 / temperature.  NaN counts as -inf, as
  * for the draw, and a logit outside A has no effect whatever it is.  With m the largest z in A and
  * s the sum over A of exp((z_j - m) c),

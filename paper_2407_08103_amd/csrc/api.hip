@@ -1796,6 +1796,7 @@ bool rows_meet(const void* x, int64_t x_stride, const void* y, int64_t y_stride,
 }
 
 constexpr int32_t kMaxTokens = 1 << 24;                  // of a vocabulary; the kernels reach a row by 32-bit offsets
+constexpr int64_t kMaxRowBytes = (int64_t)UINT32_MAX * 16;      // between the beginnings of two rows
 
 // Argument checks and kernel arguments shared by the calls that score and train.
 int prepare_rows(const tdfa_table* table, const void* logits_dev, int dtype, int32_t rows, int32_t n_tokens, int64_t row_stride,
@@ -1812,6 +1813,7 @@ int prepare_rows(const tdfa_table* table, const void* logits_dev, int dtype, int
         return fail(TDFA_E_INVALID_ARG, "log2(e) / temperature is not finite for temperature %g", (double)temperature);
     if (row_stride < n_tokens) return fail(TDFA_E_INVALID_ARG, "row_stride %lld < n_tokens %d", (long long)row_stride, n_tokens);
     const int64_t esz = dtype == TDFA_F32 ? 4 : 2;
+    if (rows > 1 && row_stride > kMaxRowBytes / esz) return fail(TDFA_E_INVALID_ARG, "row_stride %lld is too large", (long long)row_stride);
     if (rows > 0) {
         if ((!logits_dev && n_tokens > 0) || !tokens_dev || (table && !states_dev))
             return fail(TDFA_E_INVALID_ARG, "logits, tokens or states is NULL");
@@ -1821,9 +1823,7 @@ int prepare_rows(const tdfa_table* table, const void* logits_dev, int dtype, int
     *a = tdfa::TokenRows();
     if (table) {
         a->allow = table->allow;
-        a->row_allowed = table->row_allowed;
         a->n_states = table->n_rows;
-        a->row_words = table->row_words;
     }
     a->logits = logits_dev;
     a->dtype = dtype;
@@ -1841,11 +1841,23 @@ int check_grad(const tdfa::TokenRows& a, const void* grad_dev, int64_t grad_stri
     const int64_t esz = a.dtype == TDFA_F32 ? 4 : 2;
     if (a.rows == 0 || a.n_tokens == 0) return TDFA_OK;
     if (grad_stride < a.n_tokens) return fail(TDFA_E_INVALID_ARG, "grad_stride %lld < n_tokens %d", (long long)grad_stride, a.n_tokens);
+    if (a.rows > 1 && grad_stride > kMaxRowBytes / esz) return fail(TDFA_E_INVALID_ARG, "grad_stride %lld is too large", (long long)grad_stride);
     if ((reinterpret_cast<uintptr_t>(grad_dev) & 15) || (a.rows > 1 && ((grad_stride * esz) & 15)))
         return fail(TDFA_E_INVALID_ARG, "gradient rows must be 16-byte aligned");
     const bool same = grad_dev == a.logits && (a.rows == 1 || grad_stride == a.row_stride);
     if (!same && rows_meet(a.logits, a.row_stride, grad_dev, grad_stride, a.rows, a.n_tokens, esz))
         return fail(TDFA_E_INVALID_ARG, "the gradient overlaps the logits without being the same rows");
+    return TDFA_OK;
+}
+
+// The log-probabilities of a loss must not lie over what is read of its rows: later launches read that again.
+int check_logprobs(const float* logprobs_dev, int64_t rows, std::initializer_list<const void*> inputs)
+{
+    const uintptr_t p = reinterpret_cast<uintptr_t>(logprobs_dev), bytes = (uintptr_t)rows * 4;
+    for (const void* input : inputs) {
+        const uintptr_t q = reinterpret_cast<uintptr_t>(input);
+        if (q && p < q + bytes && q < p + bytes) return fail(TDFA_E_INVALID_ARG, "logprobs overlaps an input");
+    }
     return TDFA_OK;
 }
 
@@ -1917,6 +1929,7 @@ int tdfa_policy_loss(const tdfa_table* table, const void* logits_dev, int dtype,
     if (rows > 0 && kl_coef != 0.0f && !ref_logprobs_dev) return fail(TDFA_E_INVALID_ARG, "a KL term wants ref_logprobs");
     if (grad_dev) rc = check_grad(a, grad_dev, grad_stride);
     if (rc == TDFA_OK) rc = check_workspace(workspace_dev, workspace_bytes, rows, 0);
+    if (rc == TDFA_OK) rc = check_logprobs(logprobs_dev, rows, {a.states, tokens_dev, old_logprobs_dev, kl_coef != 0.0f ? ref_logprobs_dev : nullptr, advantages_dev, weights_dev});
     if (rc != TDFA_OK) return rc;
     a.weights = weights_dev;
     const tdfa::PolicyArgs p = {old_logprobs_dev, kl_coef != 0.0f ? ref_logprobs_dev : nullptr, advantages_dev, 1.0f - clip_low, 1.0f + clip_high, kl_coef};
@@ -1941,6 +1954,7 @@ int tdfa_preference_loss(const tdfa_table* table, const void* logits_dev, int dt
     if (rows > 0 && (!ref_logprobs_dev || !logprobs_dev)) return fail(TDFA_E_INVALID_ARG, "ref_logprobs or logprobs is NULL");
     if (grad_dev) rc = check_grad(a, grad_dev, grad_stride);
     if (rc == TDFA_OK) rc = check_workspace(workspace_dev, workspace_bytes, rows, n_pairs);
+    if (rc == TDFA_OK) rc = check_logprobs(logprobs_dev, rows, {a.states, tokens_dev, ref_logprobs_dev});
     if (rc != TDFA_OK) return rc;
     const tdfa::PairArgs p = {ref_logprobs_dev, begin_dev, n_pairs, beta, smoothing, rewards_dev};
     return launch_preference_loss(a, p, loss_dev, logprobs_dev, n_tokens > 0 ? grad_dev : nullptr, grad_stride, workspace_dev,

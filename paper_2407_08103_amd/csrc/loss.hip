@@ -19,6 +19,7 @@
 #include <algorithm>
 #include <cmath>
 #include <tuple>
+#include <type_traits>
 
 namespace tdfa {
 namespace {
@@ -70,9 +71,67 @@ __device__ __forceinline__ uint4 pack(const float (&g)[Elem<DTYPE>::kGroup])
 
 template <int DTYPE> constexpr uint32_t kNegInf = DTYPE == TDFA_F32 ? 0xFF800000u : 0xFF80FF80u;
 
-// Workgroups are numbered over both dimensions of a grid (grid_for).  A workgroup does one thing and ends: a loop over rows would
+// What the kernels are handed.  A launch whose arguments take at most 112 bytes, and whose kernel asks for nothing else (the size of its
+// grid, say), costs the host 2.6 us, a larger one 3.3; so strides are in units of 16 bytes, rows are numbered by the workgroups of a grid
+// that has no others, and what a call keeps of a row lies together.  A workgroup does one thing and ends: a loop over rows would
 // have the compiler keep every group's address and bounds in registers from one row to the next.
-__device__ __forceinline__ int64_t block_index() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
+struct RowArgs {
+    const uint32_t* allow;     // or NULL: every token is allowed
+    const void* logits;
+    const int32_t* states;
+    const int32_t* tokens;
+    uint32_t stride16;
+    int32_t n_states, n_tokens;
+    float inv_t;
+};
+// What a loss keeps of a row between its launches.
+struct RowWork {
+    double value;              // preference loss: lp; policy loss: the row's part of the loss
+    float2 stats;
+    float down;                // d loss / d lp
+    float unused;
+};
+// Log-probabilities and statistics for the caller, or for the preference loss.
+struct ScoreArgs : RowArgs {
+    float* logprobs;
+    float2* stats;             // or NULL
+};
+struct PairScoreArgs : RowArgs {
+    float* logprobs;
+    RowWork* work;
+};
+// What a row of the policy loss has beside its logits.
+struct PolicyTerms : RowArgs {
+    const float* old_logprobs;
+    const float* ref_logprobs;
+    const float* advantages;
+    const float* weights;
+    float* logprobs;
+    float clip_low, clip_high, kl_coef;
+    uint32_t grad_stride16;
+};
+struct PolicyScoreArgs : PolicyTerms {
+    RowWork* work;
+};
+struct PolicyRowArgs : PolicyTerms {
+    void* grad;
+};
+static_assert(sizeof(PolicyScoreArgs) <= 112 && sizeof(PolicyRowArgs) <= 112, "see above");
+
+template <int DTYPE>
+__device__ __forceinline__ const typename Elem<DTYPE>::type* row_at(const void* rows, uint32_t i, uint32_t stride16)
+{
+    return reinterpret_cast<const typename Elem<DTYPE>::type*>(static_cast<const char*>(rows) + (uint64_t)i * stride16 * 16u);
+}
+template <int DTYPE>
+__device__ __forceinline__ typename Elem<DTYPE>::type* row_at(void* rows, uint32_t i, uint32_t stride16)
+{
+    return reinterpret_cast<typename Elem<DTYPE>::type*>(static_cast<char*>(rows) + (uint64_t)i * stride16 * 16u);
+}
+__device__ __forceinline__ const uint32_t* bits_of(const uint32_t* allow, int32_t q, int32_t n_tokens)
+{
+    return allow + (int64_t)q * ((((int64_t)n_tokens + 31) / 32 + 3) / 4 * 4);
+}
 
 // What is known about a row before its logits are read.
 struct Row {
@@ -84,19 +143,19 @@ struct Row {
 
 // (i is the same in all lanes of a wavefront.)  The loads do not wait for one another: what there is none of is read from the tokens,
 // and all three values are wanted before any of them is looked at.
-__device__ __forceinline__ Row row_of(const TokenRows& a, int64_t i)
+__device__ __forceinline__ Row row_of(const RowArgs& a, const float* weights, uint32_t i)
 {
     int32_t token = a.tokens[i], q = (a.allow ? a.states : a.tokens)[i];
-    int32_t w = (a.weights ? reinterpret_cast<const int32_t*>(a.weights) : a.tokens)[i];
+    int32_t w = (weights ? reinterpret_cast<const int32_t*>(weights) : a.tokens)[i];
     asm volatile("" : "+v"(token), "+v"(q), "+v"(w));
     token = __builtin_amdgcn_readfirstlane(token);
     q = __builtin_amdgcn_readfirstlane(q);
     w = __builtin_amdgcn_readfirstlane(w);
     Row r = {nullptr, token, false, 0.0f};
-    if (token == TDFA_NO_TOKEN || (a.weights && __int_as_float(w) == 0.0f)) return r;
+    if (token == TDFA_NO_TOKEN || (weights && __int_as_float(w) == 0.0f)) return r;
     r.lp = -INFINITY;
     if (token < 0 || token >= a.n_tokens || (a.allow && (q < 0 || q >= a.n_states))) return r;
-    if (a.allow) r.bits = a.allow + (int64_t)q * a.row_words;
+    if (a.allow) r.bits = bits_of(a.allow, q, a.n_tokens);
     r.read = true;                                         // (and lp is -inf if the token turns out not to be allowed)
     return r;
 }
@@ -268,10 +327,10 @@ __device__ __forceinline__ void add_groups(uint4 (&x)[U], const uint32_t (&b)[U]
 
 // The element behind the last whole group that belongs to this thread, -inf if there is none.
 template <int DTYPE>
-__device__ __forceinline__ float last_element(const TokenRows& a, const typename Elem<DTYPE>::type* row, const uint32_t* bits)
+__device__ __forceinline__ float last_element(int32_t n_tokens, const typename Elem<DTYPE>::type* row, const uint32_t* bits)
 {
-    const int32_t t = a.n_tokens / Elem<DTYPE>::kGroup * Elem<DTYPE>::kGroup + (int32_t)threadIdx.x;
-    return t < a.n_tokens && allowed(bits, t) ? to_f32(row[t]) : -INFINITY;
+    const int32_t t = n_tokens / Elem<DTYPE>::kGroup * Elem<DTYPE>::kGroup + (int32_t)threadIdx.x;
+    return t < n_tokens && allowed(bits, t) ? to_f32(row[t]) : -INFINITY;
 }
 
 // Over the 64 lanes of a wavefront, all of them active, by data-parallel primitives (no LDS); the result is uniform.
@@ -376,98 +435,101 @@ __device__ __forceinline__ float careful_sum(const RowBuffers& row, int32_t n_gr
     return block_reduce<NT, false>(s, part);
 }
 
-// What a row of the policy loss has beside its logits.
 struct PolicyRow {
     float old, ref, adv, w;
 };
-__device__ __forceinline__ PolicyRow policy_row(const TokenRows& a, const PolicyArgs& p, int64_t i)
+__device__ __forceinline__ PolicyRow policy_row(const PolicyTerms& a, uint32_t i)
 {
-    return {p.old_logprobs[i], p.ref_logprobs ? p.ref_logprobs[i] : 0.0f, p.advantages[i], a.weights ? a.weights[i] : 1.0f};
+    return {a.old_logprobs[i], a.ref_logprobs ? a.ref_logprobs[i] : 0.0f, a.advantages[i], a.weights ? a.weights[i] : 1.0f};
 }
+__device__ __forceinline__ PolicyRow policy_row(const RowArgs&, uint32_t) { return {}; }
+__device__ __forceinline__ const float* weights_of(const PolicyTerms& a) { return a.weights; }
+__device__ __forceinline__ const float* weights_of(const RowArgs&) { return nullptr; }
 
 // The term of a row from its log-probability: the loss and d loss / d lp.
-__device__ __forceinline__ void policy_term(const PolicyArgs& p, PolicyRow v, float lp, float* each, float* down)
+__device__ __forceinline__ void policy_term(float clip_low, float clip_high, float kl_coef, bool kl, PolicyRow v, float lp, float* each, float* down)
 {
     const float ratio = expf(lp - v.old);
     const float free = ratio * v.adv;
-    const float clipped = fminf(fmaxf(ratio, p.clip_low), p.clip_high) * v.adv;
+    const float clipped = fminf(fmaxf(ratio, clip_low), clip_high) * v.adv;
     // NaN (an infinite ratio and no advantage) stays NaN
     float e = clipped < free ? -clipped : -free, s = clipped < free ? 0.0f : -free;
-    if (p.ref_logprobs) {
+    if (kl) {
         const float d = v.ref - lp, m = expm1f(d);
-        e += p.kl_coef * (m - d);
-        s -= p.kl_coef * m;
+        e += kl_coef * (m - d);
+        s -= kl_coef * m;
     }
     *each = v.w * e;
     *down = v.w * s;
 }
 
-// What is made of a row's sum.
-struct Outputs {
-    float* logprobs;           // [rows]
-    float2* stats;             // [rows] or NULL
-    double* exact;             // [rows] or NULL: lp in binary64 of rows that take part
-    float* down;               // [rows] or NULL: d loss / d lp of the policy loss, else 0
-    double* each;              // [rows] or NULL: the row's part of the policy loss
-    PolicyArgs policy;         // looked at if there is `each`
-};
-
-// The row takes no part (one thread).
-__device__ __forceinline__ void leave_out(const Outputs& o, int64_t i, float lp)
+// What is made of a row's sum (one thread): of a row that takes no part, and of one that does unless lp overflows.
+__device__ __forceinline__ void leave_out(const ScoreArgs& a, uint32_t i, float lp)
 {
-    o.logprobs[i] = lp;
-    if (o.stats) o.stats[i] = make_float2(0.0f, INFINITY);
-    if (o.down) o.down[i] = 0.0f;
-    if (o.each) o.each[i] = 0.0;
+    a.logprobs[i] = lp;
+    if (a.stats) a.stats[i] = make_float2(0.0f, INFINITY);
 }
-
-// (One thread.)
-__device__ __forceinline__ void finish(const Outputs& o, int64_t i, Scored q, bool careful, PolicyRow v)
+__device__ __forceinline__ void leave_out(const PairScoreArgs& a, uint32_t i, float lp)
+{
+    a.logprobs[i] = lp;
+    a.work[i] = {0.0, make_float2(0.0f, INFINITY), 0.0f, 0.0f};
+}
+__device__ __forceinline__ void leave_out(const PolicyScoreArgs& a, uint32_t i, float lp)
+{
+    a.logprobs[i] = lp;
+    a.work[i] = {0.0, make_float2(0.0f, INFINITY), 0.0f, 0.0f};
+}
+__device__ __forceinline__ void finish(const ScoreArgs& a, uint32_t i, Scored q, bool careful, PolicyRow)
+{
+    a.logprobs[i] = (float)q.lp;
+    if (a.stats) a.stats[i] = stats_of_row(q, careful);
+}
+__device__ __forceinline__ void finish(const PairScoreArgs& a, uint32_t i, Scored q, bool careful, PolicyRow)
+{
+    a.logprobs[i] = (float)q.lp;
+    a.work[i] = {q.lp, stats_of_row(q, careful), 0.0f, 0.0f};              // rows of no sequence keep a slope of zero
+}
+__device__ __forceinline__ void finish(const PolicyScoreArgs& a, uint32_t i, Scored q, bool careful, PolicyRow v)
 {
     const float lp = (float)q.lp;
     float e = 0.0f, d = 0.0f;
-    if (o.each && lp != -INFINITY) policy_term(o.policy, v, lp, &e, &d);
-    o.logprobs[i] = lp;
-    if (o.stats) o.stats[i] = stats_of_row(q, careful);
-    if (o.exact) o.exact[i] = q.lp;
-    if (o.down) o.down[i] = d;
-    if (o.each) o.each[i] = (double)e;
+    if (lp != -INFINITY) policy_term(a.clip_low, a.clip_high, a.kl_coef, a.ref_logprobs, v, lp, &e, &d);
+    a.logprobs[i] = lp;
+    a.work[i] = {(double)e, stats_of_row(q, careful), d, 0.0f};
 }
 
 // One workgroup per row.  The sum is taken relative to the row's own token, ref = z_t, so that no maximum has to be known, terms are added
 // as they arrive, and lp = -ln s; where that overflows (lp below -87) or a NaN is met, the row is read again, for the largest logit and
-// the sum relative to it.  Bound by the memory where there are many rows: 2,900 rows of 128,256 tokens in bf16 81 us, of which 0.53
-// of the 128-byte lines hold an allowed token (394 MB, 4.9 TB/s; torch's maximum over the rows of a matrix reads 4.9 to 5.2); by one
+// the sum relative to it.  Bound by the memory where there are many rows: 2,900 rows of 128,256 tokens in bf16 79 us, of which 0.53
+// of the 128-byte lines hold an allowed token (394 MB, 5.0 TB/s; torch's maximum over the rows of a matrix reads 4.9 to 5.2); by one
 // compute unit's stream of a long row where there are few (256 KB in 7.5 us, about 40 GB/s whatever is in flight); by the chain token,
 // bits, logits in short ones (2.8 us).
-template <int DTYPE, int NT, int U, bool BITS>
-__global__ void __launch_bounds__(NT, 8) token_stats_kernel(TokenRows a, Outputs o)
+template <typename A, int DTYPE, int NT, int U, bool BITS>
+__global__ void __launch_bounds__(NT, 8) token_stats_kernel(A a)
 {
-    using E = typename Elem<DTYPE>::type;
     __shared__ float s_part[NT / 64];
     __shared__ uint2 s_masks[16];
-    const int64_t i = block_index();
-    if (i >= a.rows) return;
-    const Row r = row_of(a, i);
-    const PolicyRow v = o.each ? policy_row(a, o.policy, i) : PolicyRow{};
+    const uint32_t i = blockIdx.x;
+    const Row r = row_of(a, weights_of(a), i);
+    const PolicyRow v = policy_row(a, i);
     const float c2 = a.inv_t * kLog2e;
     const int32_t n_groups = a.n_tokens / Elem<DTYPE>::kGroup;
     if (BITS && DTYPE == TDFA_BF16) {
         fill_masks(s_masks);
         __syncthreads();
     }
-    const E* row = static_cast<const E*>(a.logits) + i * a.row_stride;
+    const auto* row = row_at<DTYPE>(a.logits, i, a.stride16);
     if (!r.read) {
-        if (threadIdx.x == 0) leave_out(o, i, r.lp);
+        if (threadIdx.x == 0) leave_out(a, i, r.lp);
         return;
     }
     // the first bits are on their way together with the token's logit
     const RowBuffers buf = row_buffers<DTYPE>(row, r.bits, n_groups);
     uint32_t b[U];
     fetch_bits<DTYPE, NT, U, BITS>(buf, 0, b);
-    const float z = token_logit(r, row), last = last_element<DTYPE>(a, row, r.bits);
+    const float z = token_logit(r, row), last = last_element<DTYPE>(a.n_tokens, row, r.bits);
     if (z == -INFINITY) {
-        if (threadIdx.x == 0) leave_out(o, i, r.lp);
+        if (threadIdx.x == 0) leave_out(a, i, r.lp);
         return;
     }
     const float nb = -z * c2;
@@ -482,7 +544,7 @@ __global__ void __launch_bounds__(NT, 8) token_stats_kernel(TokenRows a, Outputs
     float s = block_reduce<NT, false>(sum[0] + sum[1], s_part);
     const bool careful = !usable(s);
     if (careful) s = careful_sum<DTYPE, NT, 2, BITS>(buf, n_groups, last, c2, &ref, s_masks, s_part);
-    if (threadIdx.x == 0) finish(o, i, careful ? score_careful(z, ref, a.inv_t, s) : score(z, c2, nb, s), careful, v);
+    if (threadIdx.x == 0) finish(a, i, careful ? score_careful(z, ref, a.inv_t, s) : score(z, c2, nb, s), careful, v);
 }
 
 // The largest logit and the sum relative to it of a part of a row; {kLowest, 0}: of none.
@@ -494,15 +556,13 @@ struct Part {
 // logit: lanes keep a running maximum and sum).  Bound by the memory: 300 rows of 256,000 tokens in fp32, half of whose lines are read,
 // 27 us (5.4 TB/s).
 template <int DTYPE, int NT, int U, bool BITS>
-__global__ void __launch_bounds__(NT) part_stats_kernel(TokenRows a, Part* out, int32_t parts, int32_t span)
+__global__ void __launch_bounds__(NT) part_stats_kernel(RowArgs a, const float* weights, Part* out, int32_t parts, int32_t span)
 {
-    using E = typename Elem<DTYPE>::type;
     __shared__ float s_part[NT / 64];
     __shared__ uint2 s_masks[16];
-    const int64_t w = block_index(), i = w / parts;
-    const int32_t part = (int32_t)(w - i * parts);
-    if (i >= a.rows) return;
-    const Row r = row_of(a, i);
+    const uint32_t i = blockIdx.x / (uint32_t)parts;
+    const int32_t part = (int32_t)(blockIdx.x - i * (uint32_t)parts);
+    const Row r = row_of(a, weights, i);
     if (!r.read) return;
     const float c2 = a.inv_t * kLog2e;
     const int32_t n_groups = a.n_tokens / Elem<DTYPE>::kGroup;
@@ -510,11 +570,11 @@ __global__ void __launch_bounds__(NT) part_stats_kernel(TokenRows a, Part* out, 
         fill_masks(s_masks);
         __syncthreads();
     }
-    const E* row = static_cast<const E*>(a.logits) + i * a.row_stride;
+    const auto* row = row_at<DTYPE>(a.logits, i, a.stride16);
     const int32_t end = min(n_groups, (part + 1) * span);
     const RowBuffers buf = row_buffers<DTYPE>(row, r.bits, end);
     // fmaxf with a number passes over a NaN
-    const float last = part == parts - 1 ? fmaxf(last_element<DTYPE>(a, row, r.bits), -INFINITY) : -INFINITY;
+    const float last = part == parts - 1 ? fmaxf(last_element<DTYPE>(a.n_tokens, row, r.bits), -INFINITY) : -INFINITY;
     float m = fmaxf(kLowest, last), s = __builtin_amdgcn_exp2f((last - m) * c2);
     for (int32_t g = part * span; g < end; g += NT * U) {
         uint4 x[U];
@@ -539,28 +599,27 @@ __global__ void __launch_bounds__(NT) part_stats_kernel(TokenRows a, Part* out, 
     }
     const float top = block_reduce<NT, true>(m, s_part);
     s = block_reduce<NT, false>(s * __builtin_amdgcn_exp2f((m - top) * c2), s_part);
-    if (threadIdx.x == 0) out[i * parts + part] = {top, s};
+    if (threadIdx.x == 0) out[blockIdx.x] = {top, s};
 }
 
 // A wavefront per row joins its parts, at most 64.  Bound by its chain of reads (4.7 us).
-template <int DTYPE>
-__global__ void __launch_bounds__(kThreads) join_parts_kernel(TokenRows a, Outputs o, const Part* in, int32_t parts)
+template <typename A, int DTYPE>
+__global__ void __launch_bounds__(kThreads) join_parts_kernel(A a, const Part* in, int32_t parts, uint32_t rows)
 {
-    using E = typename Elem<DTYPE>::type;
-    const int64_t i = block_index() * (kThreads / 64) + threadIdx.x / 64;
-    if (i >= a.rows) return;
+    const uint32_t i = blockIdx.x * (kThreads / 64) + threadIdx.x / 64;
+    if (i >= rows) return;
     const int lane = threadIdx.x & 63;
-    const Row r = row_of(a, i);
-    const PolicyRow v = o.each ? policy_row(a, o.policy, i) : PolicyRow{};
-    const float z = r.read ? token_logit(r, static_cast<const E*>(a.logits) + i * a.row_stride) : -INFINITY;
+    const Row r = row_of(a, weights_of(a), i);
+    const PolicyRow v = policy_row(a, i);
+    const float z = r.read ? token_logit(r, row_at<DTYPE>(a.logits, i, a.stride16)) : -INFINITY;
     if (z == -INFINITY) {
-        if (lane == 0) leave_out(o, i, r.lp);
+        if (lane == 0) leave_out(a, i, r.lp);
         return;
     }
     const float c2 = a.inv_t * kLog2e;
-    const Part mine = lane < parts ? in[i * parts + lane] : Part{kLowest, 0.0f};
+    const Part mine = lane < parts ? in[(int64_t)i * parts + lane] : Part{kLowest, 0.0f};
     const float top = wave_max(mine.m), s = wave_sum(mine.s * __builtin_amdgcn_exp2f((mine.m - top) * c2));
-    if (lane == 0) finish(o, i, score_careful(z, top, a.inv_t, s), true, v);
+    if (lane == 0) finish(a, i, score_careful(z, top, a.inv_t, s), true, v);
 }
 
 // What a row's gradient is made of: g_j = -d p_j, and d more at the token.
@@ -635,83 +694,80 @@ __device__ __forceinline__ float last_gradient(float z, Slope q, float c2, bool 
     return own ? g + q.d : g;
 }
 
+// Where the gradient of a row comes from: statistics and slopes that the caller gives; those that the launches before have left; or the pairs
+// of a preference loss of few rows, whose slopes each workgroup works out.  The losses are summed by the first workgroup of the last two.
+struct GivenGradArgs : RowArgs {
+    const float2* stats;
+    const float* down;
+    void* grad;
+    uint32_t grad_stride16;
+    int32_t parts;
+};
+struct WorkGradArgs : RowArgs {
+    const RowWork* work;
+    const double* each;        // the losses, `step` apart; with step 1 those of pairs, of which the mean is wanted
+    float* loss;
+    void* grad;
+    uint32_t grad_stride16, n;
+    int32_t parts, step;
+};
+struct PairArgsOnCard {        // of a preference loss
+    const float* ref_logprobs;
+    const int32_t* begin;
+    float* rewards;
+    int32_t n_pairs, rows;
+    float beta, smoothing;
+};
+struct FewPairsGradArgs {
+    const uint32_t* allow;
+    const void* logits;
+    const int32_t* states;
+    const int32_t* tokens;
+    const RowWork* work;
+    void* grad;
+    float* loss;
+    PairArgsOnCard pairs;
+    uint32_t stride16, grad_stride16;
+    int32_t n_tokens;
+    float inv_t;
+};
+static_assert(sizeof(FewPairsGradArgs) <= 112 && sizeof(WorkGradArgs) <= 112, "the arguments of a launch that costs the host little");
+
 // Sums of lp - ref over the rows of the two sequences of pair k, as far as `lane` of `width` lanes has them.  A sequence that reaches
 // outside the rows is cut there.
-__device__ __forceinline__ void add_pair(const PairArgs& p, int64_t rows, const double* exact, const float2* stats, int64_t k, int lane, int width, double (&sum)[2])
+__device__ __forceinline__ void add_pair(const PairArgsOnCard& p, const RowWork* work, int64_t k, int lane, int width, double (&sum)[2])
 {
-    const int64_t b0 = p.begin[2 * k], b1 = p.begin[2 * k + 1], b2 = p.begin[2 * k + 2];
+    const int32_t b0 = p.begin[2 * k], b1 = p.begin[2 * k + 1], b2 = p.begin[2 * k + 2];
 #pragma unroll
     for (int side = 0; side < 2; ++side) {
-        const int64_t from = max(side ? b1 : b0, (int64_t)0), to = min(side ? b2 : b1, rows);
+        const int64_t from = max(side ? b1 : b0, 0), to = min(side ? b2 : b1, p.rows);
         for (int64_t i = from + lane; i < to; i += width) {
-            const double lp = exact[i], ref = (double)p.ref_logprobs[i];
-            if (stats[i].y != INFINITY) sum[side] += lp - ref;
+            const double lp = work[i].value, ref = (double)p.ref_logprobs[i];
+            if (work[i].stats.y != INFINITY) sum[side] += lp - ref;
         }
     }
 }
 // softplus(x) = max(x, 0) + log1p(exp(-|x|)); binary32 from the difference of the rewards on.
-__device__ __forceinline__ float pair_loss(const PairArgs& p, float gap)
+__device__ __forceinline__ float pair_loss(const PairArgsOnCard& p, float gap)
 {
     const float tail = log1pf(expf(-fabsf(gap)));
     return (1.0f - p.smoothing) * (fmaxf(-gap, 0.0f) + tail) + p.smoothing * (fmaxf(gap, 0.0f) + tail);
 }
 // d loss / d lp of a row of the pair's first sequence.
-__device__ __forceinline__ float pair_slope(const PairArgs& p, float gap)
+__device__ __forceinline__ float pair_slope(const PairArgsOnCard& p, float gap)
 {
     return (p.smoothing / (1.0f + expf(-gap)) - (1.0f - p.smoothing) / (1.0f + expf(gap))) * (p.beta / (float)p.n_pairs);
 }
-
-// All pairs by one workgroup, 16 lanes to a pair: the rewards and the loss.
+// Both sums over the workgroup, in every thread.  Two barriers.
 template <int NT>
-__device__ __forceinline__ void sum_pairs(const PairArgs& p, int64_t rows, const double* exact, const float2* stats, float* loss, double (&part)[NT / 64])
+__device__ __forceinline__ void reduce_pair(double (&sum)[2], double (&part)[2][NT / 64])
 {
-    double total = 0.0;
-    const int lane = threadIdx.x & 15;
-    for (int64_t k0 = 0; k0 < p.n_pairs; k0 += NT / 16) {
-        const int64_t k = k0 + threadIdx.x / 16;
-        double sum[2] = {0.0, 0.0};
-        if (k < p.n_pairs) add_pair(p, rows, exact, stats, k, lane, 16, sum);
-#pragma unroll
-        for (int d = 8; d; d >>= 1) {
-            sum[0] += __shfl_xor(sum[0], d);
-            sum[1] += __shfl_xor(sum[1], d);
-        }
-        if (lane == 0 && k < p.n_pairs) {
-            const double chosen = (double)p.beta * sum[0], rejected = (double)p.beta * sum[1];
-            p.rewards[2 * k] = (float)chosen;
-            p.rewards[2 * k + 1] = (float)rejected;
-            total += (double)pair_loss(p, (float)(chosen - rejected));
-        }
-    }
-#pragma unroll
-    for (int d = 32; d; d >>= 1) total += __shfl_xor(total, d);
-    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = total;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int w = 1; w < NT / 64; ++w) total += part[w];
-        *loss = (float)(total / (double)p.n_pairs);
-    }
-}
-
-// d loss / d lp of row i, by the whole workgroup: its sequence is looked for and the pair's rewards are summed again.  Of few rows and
-// pairs this costs less than a launch that hands it on.
-template <int NT>
-__device__ __forceinline__ float slope_of_row(const PairArgs& p, int64_t rows, const double* exact, const float2* stats, int64_t i, int& found, double (&part)[2][NT / 64])
-{
-    if (threadIdx.x == 0) found = -1;
-    __syncthreads();
-    for (int k = threadIdx.x; k < 2 * p.n_pairs; k += NT)
-        if (p.begin[k] <= i && i < p.begin[k + 1]) found = k;
-    __syncthreads();
-    const int k = __builtin_amdgcn_readfirstlane(found);
-    if (k < 0) return 0.0f;
-    double sum[2] = {0.0, 0.0};
-    add_pair(p, rows, exact, stats, k / 2, threadIdx.x, NT, sum);
 #pragma unroll
     for (int d = 32; d; d >>= 1) {
         sum[0] += __shfl_xor(sum[0], d);
         sum[1] += __shfl_xor(sum[1], d);
     }
+    __syncthreads();
     if ((threadIdx.x & 63) == 0) {
         part[0][threadIdx.x >> 6] = sum[0];
         part[1][threadIdx.x >> 6] = sum[1];
@@ -724,80 +780,220 @@ __device__ __forceinline__ float slope_of_row(const PairArgs& p, int64_t rows, c
         sum[0] += part[0][w];
         sum[1] += part[1][w];
     }
-    const float slope = pair_slope(p, (float)((double)p.beta * sum[0] - (double)p.beta * sum[1]));
-    return k & 1 ? -slope : slope;
 }
-
-// loss = scale * the sum of each, by one workgroup, in an order that depends on nothing but n and NT.
-struct LossSum {
-    const double* each;
-    int64_t n;
-    double scale;
-    float* loss;               // or NULL: no sum is wanted
-};
+// A sum over the workgroup, in thread 0.  One barrier.
 template <int NT>
-__device__ __forceinline__ void sum_losses(const LossSum& q, double (&part)[NT / 64])
+__device__ __forceinline__ double reduce_sum(double sum, double (&part)[NT / 64])
 {
-    double sum = 0.0;
-    for (int64_t i = threadIdx.x; i < q.n; i += NT) sum += q.each[i];
 #pragma unroll
     for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
     __syncthreads();
-    if (threadIdx.x == 0) {
+    if (threadIdx.x == 0)
         for (int w = 1; w < NT / 64; ++w) sum += part[w];
-        *q.loss = (float)(sum * q.scale);
+    return sum;
+}
+
+// One workgroup per pair: the two rewards, the pair's loss, and d loss / d lp of every row of the pair.  Bound by its chain of reads
+// (32 pairs of 90 rows 4.7 us).
+__global__ void __launch_bounds__(kThreads) pair_kernel(PairArgsOnCard p, RowWork* work, double* each, int32_t blocks)
+{
+    __shared__ double s_part[2][kThreads / 64];
+    for (int64_t k = blockIdx.x; k < p.n_pairs; k += blocks) {
+        double sum[2] = {0.0, 0.0};
+        add_pair(p, work, k, threadIdx.x, kThreads, sum);
+        reduce_pair<kThreads>(sum, s_part);
+        const double chosen = (double)p.beta * sum[0], rejected = (double)p.beta * sum[1];
+        const float gap = (float)(chosen - rejected), slope = pair_slope(p, gap);
+        if (threadIdx.x == 0) {
+            p.rewards[2 * k] = (float)chosen;
+            p.rewards[2 * k + 1] = (float)rejected;
+            each[k] = (double)pair_loss(p, gap);
+        }
+        const int32_t b0 = p.begin[2 * k], b1 = p.begin[2 * k + 1], b2 = p.begin[2 * k + 2];
+        for (int64_t i = (int64_t)max(b0, 0) + threadIdx.x; i < min(b1, p.rows); i += kThreads) work[i].down = slope;
+        for (int64_t i = (int64_t)max(b1, 0) + threadIdx.x; i < min(b2, p.rows); i += kThreads) work[i].down = -slope;
     }
 }
-__global__ void __launch_bounds__(1024) loss_sum_kernel(LossSum q)
+
+// All pairs by one workgroup, 16 lanes to a pair: the rewards and the loss.
+template <int NT>
+__device__ __forceinline__ void sum_pairs(const PairArgsOnCard& p, const RowWork* work, float* loss, double (&part)[NT / 64])
+{
+    double total = 0.0;
+    const int lane = threadIdx.x & 15;
+    for (int64_t k0 = 0; k0 < p.n_pairs; k0 += NT / 16) {
+        const int64_t k = k0 + threadIdx.x / 16;
+        double sum[2] = {0.0, 0.0};
+        if (k < p.n_pairs) add_pair(p, work, k, lane, 16, sum);
+#pragma unroll
+        for (int d = 8; d; d >>= 1) {
+            sum[0] += __shfl_xor(sum[0], d);
+            sum[1] += __shfl_xor(sum[1], d);
+        }
+        if (lane == 0 && k < p.n_pairs) {
+            const double chosen = (double)p.beta * sum[0], rejected = (double)p.beta * sum[1];
+            p.rewards[2 * k] = (float)chosen;
+            p.rewards[2 * k + 1] = (float)rejected;
+            total += (double)pair_loss(p, (float)(chosen - rejected));
+        }
+    }
+    total = reduce_sum<NT>(total, part);
+    if (threadIdx.x == 0) *loss = (float)(total / (double)p.n_pairs);
+}
+
+// d loss / d lp of row i, by the whole workgroup: its sequence is looked for and the pair's rewards are summed again.  Of few rows and
+// pairs this costs less than a launch that hands it on.
+template <int NT>
+__device__ __forceinline__ float slope_of_row(const PairArgsOnCard& p, const RowWork* work, int32_t i, int& found, double (&part)[2][NT / 64])
+{
+    if (threadIdx.x == 0) found = -1;
+    __syncthreads();
+    for (int k = threadIdx.x; k < 2 * p.n_pairs; k += NT)
+        if (p.begin[k] <= i && i < p.begin[k + 1]) found = k;
+    __syncthreads();
+    const int k = __builtin_amdgcn_readfirstlane(found);
+    if (k < 0) return 0.0f;
+    double sum[2] = {0.0, 0.0};
+    add_pair(p, work, k / 2, threadIdx.x, NT, sum);
+    reduce_pair<NT>(sum, part);
+    const float slope = pair_slope(p, (float)((double)p.beta * sum[0] - (double)p.beta * sum[1]));
+    return k & 1 ? -slope : slope;
+}
+
+// loss = the sum of n losses, or their mean (step 1), by one workgroup, in an order that depends on nothing but n and NT.
+template <int NT>
+__device__ __forceinline__ void sum_losses(const double* each, int64_t n, int32_t step, float* loss, double (&part)[NT / 64])
+{
+    double sum = 0.0;
+    for (int64_t i = threadIdx.x; i < n; i += NT) sum += each[i * step];
+    sum = reduce_sum<NT>(sum, part);
+    if (threadIdx.x == 0) *loss = (float)(step == 1 ? (n ? sum / (double)n : 0.0) : sum);
+}
+__global__ void __launch_bounds__(1024) loss_sum_kernel(const double* each, uint32_t n, int32_t step, float* loss)
 {
     __shared__ double s_part[16];
-    sum_losses<1024>(q, s_part);
+    sum_losses<1024>(each, n, step, loss, s_part);
 }
+
+// The policy loss from the log-probabilities that a launch before has written: `span` rows to a workgroup, which leaves its sum in out, or
+// the loss if it is the only one.  Bound by its chain of reads (24 rows 1.5 us, 4,096 rows 4.4).
+struct PolicySumArgs {
+    const float* logprobs;
+    const float* old_logprobs;
+    const float* ref_logprobs;
+    const float* advantages;
+    const float* weights;
+    const int32_t* tokens;
+    float* loss;               // or NULL
+    double* out;
+    uint32_t rows, span;
+    float clip_low, clip_high, kl_coef;
+};
+__global__ void __launch_bounds__(1024) policy_sum_kernel(PolicySumArgs a)
+{
+    __shared__ double s_part[16];
+    const int64_t from = (int64_t)blockIdx.x * a.span, to = min(from + a.span, (int64_t)a.rows);
+    double sum = 0.0;
+    for (int64_t i = from + threadIdx.x; i < to; i += 1024) {
+        const PolicyRow v = {a.old_logprobs[i], a.ref_logprobs ? a.ref_logprobs[i] : 0.0f, a.advantages[i], a.weights ? a.weights[i] : 1.0f};
+        const float lp = a.logprobs[i];
+        float e, d;
+        policy_term(a.clip_low, a.clip_high, a.kl_coef, a.ref_logprobs, v, lp, &e, &d);
+        if (a.tokens[i] != TDFA_NO_TOKEN && v.w != 0.0f && lp != -INFINITY) sum += (double)e;          // of rows that take part
+    }
+    sum = reduce_sum<1024>(sum, s_part);
+    if (threadIdx.x == 0) {
+        if (a.loss) *a.loss = (float)sum;
+        else a.out[blockIdx.x] = sum;
+    }
+}
+
+// What a gradient workgroup knows of its row: the token, the allowed bits, the statistics, d loss / d lp (0: the row takes no part).  Only
+// what the caller gives is checked again.
+struct GradRow {
+    const uint32_t* bits;
+    int32_t token;
+    float2 stats;
+    float down;
+};
+template <int NT>
+__device__ __forceinline__ GradRow grad_row(const GivenGradArgs& a, uint32_t i)
+{
+    const float2 st = a.stats[i];
+    const float down = a.down[i];
+    const Row r = row_of(a, nullptr, i);
+    return {r.bits, r.token, st, r.read && st.y != INFINITY ? down : 0.0f};
+}
+template <int NT>
+__device__ __forceinline__ GradRow grad_row(const WorkGradArgs& a, uint32_t i)
+{
+    const float2 st = a.work[i].stats;
+    const float down = a.work[i].down;
+    const int32_t token = __builtin_amdgcn_readfirstlane(a.tokens[i]), q = a.allow ? __builtin_amdgcn_readfirstlane(a.states[i]) : 0;
+    if (st.y == INFINITY) return {nullptr, token, st, 0.0f};
+    return {a.allow ? bits_of(a.allow, q, a.n_tokens) : nullptr, token, st, down};
+}
+template <int NT>
+__device__ __forceinline__ GradRow grad_row(const FewPairsGradArgs& a, uint32_t i)
+{
+    __shared__ int s_found;
+    __shared__ double s_sums[2][NT / 64];
+    const float2 st = a.work[i].stats;
+    const int32_t token = __builtin_amdgcn_readfirstlane(a.tokens[i]), q = a.allow ? __builtin_amdgcn_readfirstlane(a.states[i]) : 0;
+    if (__builtin_amdgcn_readfirstlane(__float_as_int(st.y)) == 0x7F800000) return {nullptr, token, st, 0.0f};
+    const float down = slope_of_row<NT>(a.pairs, a.work, (int32_t)i, s_found, s_sums);
+    return {a.allow ? bits_of(a.allow, q, a.n_tokens) : nullptr, token, st, down};
+}
+// What the first workgroup does beside the rows; false: nothing, it takes a row like the others.
+template <int NT>
+__device__ __forceinline__ bool first_block(const GivenGradArgs&) { return false; }
+template <int NT>
+__device__ __forceinline__ bool first_block(const WorkGradArgs& a)
+{
+    __shared__ double s_part[NT / 64];
+    sum_losses<NT>(a.each, a.n, a.step, a.loss, s_part);
+    return true;
+}
+template <int NT>
+__device__ __forceinline__ bool first_block(const FewPairsGradArgs& a)
+{
+    __shared__ double s_part[NT / 64];
+    sum_pairs<NT>(a.pairs, a.work, a.loss, s_part);
+    return true;
+}
+template <typename A> constexpr uint32_t kFirst = 1;          // workgroups before those of the rows
+template <> constexpr uint32_t kFirst<GivenGradArgs> = 0;
+template <int SPAN, typename A>
+__device__ __forceinline__ int32_t parts_of(const A& a, int32_t) { return a.parts; }
+template <int SPAN>
+__device__ __forceinline__ int32_t parts_of(const FewPairsGradArgs&, int32_t n_groups) { return max(1, (n_groups + SPAN - 1) / SPAN); }
 
 // grad[i][j] = down[i] c ([j = t] - p_j) over A, 0 elsewhere; 0 throughout in a row that takes no part.  A workgroup
 // takes NT U groups of one row; the last of a row takes the elements behind the last whole group too.  Bound by the memory: 2,048 rows of
 // 128,256 tokens in bf16 105 us (525 MB written and 255 MB of lines read, in part from the 256 MB cache that the sums have left full:
-// 7.4 TB/s), 8 groups in flight per thread (4: 112, 2: 150).  One more workgroup, the first,
-// sums the losses that an earlier launch has left, if that is wanted.  PAIRS: d loss / d lp is worked out here (slope_of_row), and that first
-// workgroup does what the pairs' own launch would.
-template <int DTYPE, int NT, int U, bool BITS, bool PAIRS>
-__global__ void __launch_bounds__(NT)
-token_grad_kernel(TokenRows a, const float2* stats, const float* down, void* grad, int64_t grad_stride, int32_t parts, LossSum sum, PairArgs pairs, const double* exact)
+// 7.4 TB/s), 8 groups in flight per thread (4: 112, 2: 150).
+template <typename A, int DTYPE, int NT, int U, bool BITS>
+__global__ void __launch_bounds__(NT) token_grad_kernel(A a)
 {
-    using E = typename Elem<DTYPE>::type;
     constexpr int G = Elem<DTYPE>::kGroup;
     __shared__ uint2 s_masks[16];
     if (BITS && DTYPE == TDFA_BF16) {
         fill_masks(s_masks);
         __syncthreads();
     }
-    const float c2 = a.inv_t * kLog2e;
-    const int32_t n_groups = a.n_tokens / G;
-    int64_t w = block_index();
-    if (sum.loss && w-- == 0) {
-        __shared__ double s_part[NT / 64];
-        if constexpr (PAIRS) sum_pairs<NT>(pairs, a.rows, exact, stats, sum.loss, s_part);
-        else sum_losses<NT>(sum, s_part);
+    if (blockIdx.x < kFirst<A>) {
+        first_block<NT>(a);
         return;
     }
-    // (there are less than 2^32 parts of rows: a part is 16 KB or a row)
-    const int64_t i = (uint32_t)w / (uint32_t)parts;
-    const int32_t part = (int32_t)(w - i * parts);
-    if (i >= a.rows) return;
-    const Row r = row_of(a, i);
-    const float2 st = stats[i];
-    float slope;
-    if constexpr (PAIRS) {
-        __shared__ int s_found;
-        __shared__ double s_sums[2][NT / 64];
-        slope = slope_of_row<NT>(pairs, a.rows, exact, stats, i, s_found, s_sums);
-    } else {
-        slope = down[i];
-    }
-    const Slope q = shared_by_wave(slope_of<DTYPE>(r.read && st.y != INFINITY ? slope * a.inv_t : 0.0f, st.x, fabsf(st.y), c2, signbit(st.y)));
-    const E* row = static_cast<const E*>(a.logits) + i * a.row_stride;
-    E* out = static_cast<E*>(grad) + i * grad_stride;
+    const float c2 = a.inv_t * kLog2e;
+    const int32_t n_groups = a.n_tokens / G, parts = parts_of<NT * U>(a, n_groups);
+    const uint32_t w = blockIdx.x - kFirst<A>, i = w / (uint32_t)parts;
+    const int32_t part = (int32_t)(w - i * (uint32_t)parts);
+    const GradRow r = grad_row<NT>(a, i);
+    const Slope q = shared_by_wave(slope_of<DTYPE>(r.down * a.inv_t, r.stats.x, fabsf(r.stats.y), c2, signbit(r.stats.y)));
+    const auto* row = row_at<DTYPE>(a.logits, i, a.stride16);
+    auto* out = row_at<DTYPE>(a.grad, i, a.grad_stride16);
     const __amdgpu_buffer_rsrc_t to = buffer_of(out, (uint32_t)n_groups * 16u);
     const int32_t g0 = part * (NT * U), g = g0 + (int32_t)threadIdx.x;
     const int32_t behind = n_groups * G + (int32_t)threadIdx.x;
@@ -807,7 +1003,7 @@ token_grad_kernel(TokenRows a, const float2* stats, const float* down, void* gra
         if (part == parts - 1 && behind < a.n_tokens) store_rounded(out + behind, 0.0f);
         return;
     }
-    const float last = part == parts - 1 ? last_element<DTYPE>(a, row, r.bits) : -INFINITY;
+    const float last = part == parts - 1 ? last_element<DTYPE>(a.n_tokens, row, r.bits) : -INFINITY;
     uint4 x[U];
     uint32_t b[U];
     fetch<DTYPE, NT, U, BITS, true>(row_buffers<DTYPE>(row, r.bits, n_groups), g0, n_groups, x, b);
@@ -831,24 +1027,22 @@ constexpr int64_t kPartRows = 384;
 // instructions take two fifths of the time.  Two rows to a compute unit with half of each read twice: 316 us; workgroups that stay, and
 // fetch the next row into the registers that the gradient leaves: 119 us for the 1,024.
 template <int DTYPE, int NT, int R, bool BITS>
-__global__ void __launch_bounds__(NT, 4) policy_row_kernel(TokenRows a, PolicyArgs p, float* logprobs, double* each, void* grad, int64_t grad_stride)
+__global__ void __launch_bounds__(NT, 4) policy_row_kernel(PolicyRowArgs a)
 {
-    using E = typename Elem<DTYPE>::type;
     constexpr int G = Elem<DTYPE>::kGroup;
     __shared__ float s_part[NT / 64];
     __shared__ uint2 s_masks[16];
     __shared__ Slope s_slope;
-    const int64_t i = block_index();
-    if (i >= a.rows) return;
-    const Row r = row_of(a, i);
-    const PolicyRow v = policy_row(a, p, i);
+    const uint32_t i = blockIdx.x;
+    const Row r = row_of(a, a.weights, i);
+    const PolicyRow v = policy_row(a, i);
     const float c2 = a.inv_t * kLog2e;
     const int32_t n_groups = a.n_tokens / G;
     if (BITS && DTYPE == TDFA_BF16) {
         fill_masks(s_masks);
         __syncthreads();
     }
-    const E* row = static_cast<const E*>(a.logits) + i * a.row_stride;
+    const auto* row = row_at<DTYPE>(a.logits, i, a.stride16);
     const RowBuffers buf = row_buffers<DTYPE>(row, r.bits, n_groups);
     Slope q = {0.0f, 0.0f, 0.0f, 0.0f};
     float last = -INFINITY;
@@ -859,7 +1053,7 @@ __global__ void __launch_bounds__(NT, 4) policy_row_kernel(TokenRows a, PolicyAr
     if (r.read) {                                          // the bits are on their way together with the token's logit
         fetch_bits<DTYPE, NT, R, BITS>(buf, 0, b);
         z = token_logit(r, row);
-        last = last_element<DTYPE>(a, row, r.bits);
+        last = last_element<DTYPE>(a.n_tokens, row, r.bits);
     }
     if (z > -INFINITY) {
         fetch_groups<DTYPE, NT, R, BITS, true>(buf, 0, n_groups, x, b);
@@ -884,21 +1078,19 @@ __global__ void __launch_bounds__(NT, 4) policy_row_kernel(TokenRows a, PolicyAr
             const Scored sc = careful ? score_careful(z, ref, a.inv_t, s) : score(z, c2, nb, s);
             const float lp = (float)sc.lp;
             float e = 0.0f, d = 0.0f;
-            if (lp != -INFINITY) policy_term(p, v, lp, &e, &d);
+            if (lp != -INFINITY) policy_term(a.clip_low, a.clip_high, a.kl_coef, a.ref_logprobs, v, lp, &e, &d);
             if (threadIdx.x == 0) {
-                logprobs[i] = lp;
-                each[i] = (double)e;
+                a.logprobs[i] = lp;
                 s_slope = slope_of<DTYPE>(d * a.inv_t, sc.ref, sc.ls, c2, careful);
             }
         }
         __syncthreads();
         q = shared_by_wave(s_slope);
     } else if (threadIdx.x == 0) {
-        logprobs[i] = r.lp;
-        each[i] = 0.0;
+        a.logprobs[i] = r.lp;
     }
-    if (!grad) return;
-    E* out = static_cast<E*>(grad) + i * grad_stride;
+    if (!a.grad) return;
+    auto* out = row_at<DTYPE>(a.grad, i, a.grad_stride16);
     const __amdgpu_buffer_rsrc_t to = buffer_of(out, (uint32_t)n_groups * 16u);
     const int32_t behind = n_groups * G + (int32_t)threadIdx.x;
     if (q.d == 0.0f) {
@@ -913,49 +1105,6 @@ __global__ void __launch_bounds__(NT, 4) policy_row_kernel(TokenRows a, PolicyAr
     if (behind < a.n_tokens) store_rounded(out + behind, last_gradient(last, q, c2, behind == r.token));
 }
 
-// One workgroup per pair: the two rewards, the pair's loss, and d loss / d lp of every row of the pair.  Bound by its chain of reads
-// (32 pairs of 90 rows 4.7 us).
-__global__ void __launch_bounds__(kThreads)
-pair_kernel(PairArgs p, int64_t rows, const double* exact, const float2* stats, float* down, double* each)
-{
-    __shared__ double s_part[2][kThreads / 64];
-    for (int64_t k = blockIdx.x; k < p.n_pairs; k += gridDim.x) {
-        double sum[2] = {0.0, 0.0};
-        add_pair(p, rows, exact, stats, k, threadIdx.x, kThreads, sum);
-#pragma unroll
-        for (int d = 32; d; d >>= 1) {
-            sum[0] += __shfl_xor(sum[0], d);
-            sum[1] += __shfl_xor(sum[1], d);
-        }
-        __syncthreads();
-        if ((threadIdx.x & 63) == 0) {
-            s_part[0][threadIdx.x >> 6] = sum[0];
-            s_part[1][threadIdx.x >> 6] = sum[1];
-        }
-        __syncthreads();
-        sum[0] = s_part[0][0];
-        sum[1] = s_part[1][0];
-#pragma unroll
-        for (int w = 1; w < kThreads / 64; ++w) {
-            sum[0] += s_part[0][w];
-            sum[1] += s_part[1][w];
-        }
-        const double chosen = (double)p.beta * sum[0], rejected = (double)p.beta * sum[1];
-        const float gap = (float)(chosen - rejected);
-        if (threadIdx.x == 0) {
-            p.rewards[2 * k] = (float)chosen;
-            p.rewards[2 * k + 1] = (float)rejected;
-            each[k] = (double)pair_loss(p, gap);
-        }
-        if (down) {
-            const float slope = pair_slope(p, gap);
-            const int64_t b0 = p.begin[2 * k], b1 = p.begin[2 * k + 1], b2 = p.begin[2 * k + 2];
-            for (int64_t i = max(b0, (int64_t)0) + threadIdx.x; i < min(b1, rows); i += kThreads) down[i] = slope;
-            for (int64_t i = max(b1, (int64_t)0) + threadIdx.x; i < min(b2, rows); i += kThreads) down[i] = -slope;
-        }
-    }
-}
-
 // A launch that reports its own error (asking for the last one afterwards costs the host 0.4 us more).
 template <typename... Params, typename... Args>
 int launch(void (*kernel)(Params...), dim3 grid, unsigned threads, hipStream_t stream, Args... args)
@@ -968,32 +1117,91 @@ int launch(void (*kernel)(Params...), dim3 grid, unsigned threads, hipStream_t s
     }, params);
 }
 
-unsigned blocks_for(int64_t n) { return (unsigned)(n < 1 << 20 ? n : 1 << 20); }
-// At least n workgroups, whose threads stay below 2^32 in each dimension.
-dim3 grid_for(int64_t n) { return n <= 1 << 21 ? dim3((unsigned)n) : dim3(1u << 21, (unsigned)((n + (1 << 21) - 1) >> 21)); }
+// Workgroups of a launch, of 1,024 threads at most: a grid counts less than 2^32 threads, so that more rows go by several launches.
+constexpr int64_t kMaxBlocks = 1 << 21;
 
-template <int DTYPE, bool BITS>
-int stats_launch(const TokenRows& a, const Outputs& o, hipStream_t stream)
+RowArgs row_args(const TokenRows& a, int64_t from)
 {
-    const int32_t n_groups = a.n_tokens / Elem<DTYPE>::kGroup;
-    // Two rows or more to a compute unit, so that one is fetched while another is summed.
-    if (n_groups <= 64 * 4) return launch(token_stats_kernel<DTYPE, 64, 4, BITS>, grid_for(a.rows), 64, stream, a, o);
-    // Rows too few to fill the card are shared by more wavefronts each: 24 rows of 32,000 tokens in bf16 6.0 -> 5.1 us, 400 rows 8.2 -> 7.7;
-    // of 8,000 tokens 4.1 either way, 400 rows 4.5 -> 5.4.
-    if (a.rows <= 512 && n_groups > 256 * 8 && n_groups <= 512 * 16) return launch(token_stats_kernel<DTYPE, 1024, 4, BITS>, grid_for(a.rows), 1024, stream, a, o);
-    if (n_groups <= 256 * 16) return launch(token_stats_kernel<DTYPE, 256, 8, BITS>, grid_for(a.rows), 256, stream, a, o);
-    if (n_groups <= 512 * 16) return launch(token_stats_kernel<DTYPE, 512, 8, BITS>, grid_for(a.rows), 512, stream, a, o);
-    return launch(token_stats_kernel<DTYPE, 1024, 8, BITS>, grid_for(a.rows), 1024, stream, a, o);
+    const int64_t esz = a.dtype == TDFA_F32 ? 4 : 2;
+    return {a.allow, static_cast<const char*>(a.logits) + from * a.row_stride * esz, a.states ? a.states + from : nullptr, a.tokens + from,
+            (uint32_t)(a.rows > 1 ? a.row_stride * esz / 16 : 0), (int32_t)std::min<int64_t>(a.n_states, INT32_MAX), a.n_tokens, a.inv_t};
+}
+uint32_t grad_stride16(const TokenRows& a, int64_t grad_stride) { return (uint32_t)(a.rows > 1 ? grad_stride * (a.dtype == TDFA_F32 ? 4 : 2) / 16 : 0); }
+void* grad_from(const TokenRows& a, void* grad, int64_t grad_stride, int64_t from)
+{
+    return grad ? static_cast<char*>(grad) + from * grad_stride * (a.dtype == TDFA_F32 ? 4 : 2) : nullptr;
 }
 
-template <int DTYPE, bool BITS>
-int parts_launch(const TokenRows& a, const Outputs& o, Part* out, hipStream_t stream)
+// What a call scores into.
+struct Score {
+    float* logprobs;
+    float2* stats;             // for the caller, or NULL
+    RowWork* work;             // for a loss, or NULL
+    const PolicyArgs* policy;  // for the policy loss, or NULL
+};
+void fill(ScoreArgs& x, const TokenRows&, const Score& o, int64_t from)
+{
+    x.logprobs = o.logprobs + from;
+    x.stats = o.stats ? o.stats + from : nullptr;
+}
+void fill(PairScoreArgs& x, const TokenRows&, const Score& o, int64_t from)
+{
+    x.logprobs = o.logprobs + from;
+    x.work = o.work + from;
+}
+void fill_terms(PolicyTerms& x, const TokenRows& a, const PolicyArgs& p, float* logprobs, int64_t from)
+{
+    x.old_logprobs = p.old_logprobs + from;
+    x.ref_logprobs = p.ref_logprobs ? p.ref_logprobs + from : nullptr;
+    x.advantages = p.advantages + from;
+    x.weights = a.weights ? a.weights + from : nullptr;
+    x.logprobs = logprobs + from;
+    x.clip_low = p.clip_low;
+    x.clip_high = p.clip_high;
+    x.kl_coef = p.kl_coef;
+    x.grad_stride16 = 0;
+}
+void fill(PolicyScoreArgs& x, const TokenRows& a, const Score& o, int64_t from)
+{
+    fill_terms(x, a, *o.policy, o.logprobs, from);
+    x.work = o.work + from;
+}
+
+template <typename A, int DTYPE, bool BITS>
+int stats_launch(const TokenRows& a, const Score& o, hipStream_t stream)
+{
+    const int32_t n_groups = a.n_tokens / Elem<DTYPE>::kGroup;
+    for (int64_t from = 0; from < a.rows; from += kMaxBlocks) {
+        const dim3 grid((unsigned)std::min(a.rows - from, kMaxBlocks));
+        A x;
+        static_cast<RowArgs&>(x) = row_args(a, from);
+        fill(x, a, o, from);
+        int rc;
+        // Two rows or more to a compute unit, so that one is fetched while another is summed.  Rows too few to fill the card are shared by
+        // more wavefronts each: 24 rows of 32,000 tokens in bf16 6.0 -> 5.1 us, 400 rows 8.2 -> 7.7; of 8,000 tokens 4.1 either way, 400
+        // rows 4.5 -> 5.4.
+        if (n_groups <= 64 * 4) rc = launch(token_stats_kernel<A, DTYPE, 64, 4, BITS>, grid, 64, stream, x);
+        else if (a.rows <= 512 && n_groups > 256 * 8 && n_groups <= 512 * 16) rc = launch(token_stats_kernel<A, DTYPE, 1024, 4, BITS>, grid, 1024, stream, x);
+        else if (n_groups <= 256 * 16) rc = launch(token_stats_kernel<A, DTYPE, 256, 8, BITS>, grid, 256, stream, x);
+        else if (n_groups <= 512 * 16) rc = launch(token_stats_kernel<A, DTYPE, 512, 8, BITS>, grid, 512, stream, x);
+        else rc = launch(token_stats_kernel<A, DTYPE, 1024, 8, BITS>, grid, 1024, stream, x);
+        if (rc != TDFA_OK) return rc;
+    }
+    return TDFA_OK;
+}
+
+template <typename A, int DTYPE, bool BITS>
+int parts_launch(const TokenRows& a, const Score& o, Part* out, hipStream_t stream)
 {
     const int32_t n_groups = a.n_tokens / Elem<DTYPE>::kGroup, round = 256 * 8;
     const int32_t span = (n_groups + kMaxParts * round - 1) / (kMaxParts * round) * round, parts = (n_groups + span - 1) / span;
-    const int rc = launch(part_stats_kernel<DTYPE, 256, 8, BITS>, grid_for(a.rows * parts), 256, stream, a, out, parts, span);
+    A x;
+    static_cast<RowArgs&>(x) = row_args(a, 0);
+    fill(x, a, o, 0);
+    const int rc = launch(part_stats_kernel<DTYPE, 256, 8, BITS>, dim3((unsigned)(a.rows * parts)), 256, stream, static_cast<RowArgs&>(x), a.weights, out, parts, span);
     if (rc != TDFA_OK) return rc;
-    return launch(join_parts_kernel<DTYPE>, grid_for((a.rows + kThreads / 64 - 1) / (kThreads / 64)), kThreads, stream, a, o, out, parts);
+    return launch(join_parts_kernel<A, DTYPE>, dim3((unsigned)((a.rows + kThreads / 64 - 1) / (kThreads / 64))), kThreads, stream, x,
+                  static_cast<const Part*>(out), parts, (uint32_t)a.rows);
 }
 
 int64_t groups_of(const TokenRows& a) { return a.n_tokens / (a.dtype == TDFA_F32 ? Elem<TDFA_F32>::kGroup : Elem<TDFA_BF16>::kGroup); }
@@ -1003,85 +1211,85 @@ bool in_parts(const TokenRows& a) { return a.rows <= kPartRows && groups_of(a) >
 // parts: workspace for kMaxParts parts of each of the first kPartRows rows.  Few rows that are longer than a workgroup's registers are
 // shared out by parts, which a second launch joins: 1 row of 256,000 tokens in fp32 14.5 us by one workgroup, 6.8 so; 64 rows 34.5 and
 // 14.9, 300 rows 60.6 and 44.5; of 128,256 tokens 19.8 and 12.1, 28.7 and 24.9; 512 rows 38.1 and 37.9, in bf16 of 256,000 36.6 and 40.6.
-int stats_of(const TokenRows& a, const Outputs& o, Part* parts, hipStream_t stream)
+template <typename A>
+int stats_of(const TokenRows& a, const Score& o, Part* parts, hipStream_t stream)
 {
     if (in_parts(a)) {
-        if (a.dtype == TDFA_F32) return a.allow ? parts_launch<TDFA_F32, true>(a, o, parts, stream) : parts_launch<TDFA_F32, false>(a, o, parts, stream);
-        return a.allow ? parts_launch<TDFA_BF16, true>(a, o, parts, stream) : parts_launch<TDFA_BF16, false>(a, o, parts, stream);
+        if (a.dtype == TDFA_F32) return a.allow ? parts_launch<A, TDFA_F32, true>(a, o, parts, stream) : parts_launch<A, TDFA_F32, false>(a, o, parts, stream);
+        return a.allow ? parts_launch<A, TDFA_BF16, true>(a, o, parts, stream) : parts_launch<A, TDFA_BF16, false>(a, o, parts, stream);
     }
-    if (a.dtype == TDFA_F32) return a.allow ? stats_launch<TDFA_F32, true>(a, o, stream) : stats_launch<TDFA_F32, false>(a, o, stream);
-    return a.allow ? stats_launch<TDFA_BF16, true>(a, o, stream) : stats_launch<TDFA_BF16, false>(a, o, stream);
+    if (a.dtype == TDFA_F32) return a.allow ? stats_launch<A, TDFA_F32, true>(a, o, stream) : stats_launch<A, TDFA_F32, false>(a, o, stream);
+    return a.allow ? stats_launch<A, TDFA_BF16, true>(a, o, stream) : stats_launch<A, TDFA_BF16, false>(a, o, stream);
 }
 
-// What the gradient of a preference loss of few rows and pairs is made of; exact NULL: not that.
-struct FewPairs {
-    PairArgs pairs;
-    const double* exact;
-};
-
-template <int DTYPE, bool BITS, bool PAIRS>
-int grad_launch(const TokenRows& a, const float2* stats, const float* down, void* grad, int64_t grad_stride, const LossSum& sum, const FewPairs& few_pairs,
-                hipStream_t stream)
-{
-    const int32_t n_groups = a.n_tokens / Elem<DTYPE>::kGroup, more = sum.loss ? 1 : 0;
-    if constexpr (!PAIRS) {
-        if (n_groups <= 256)
-            return launch(token_grad_kernel<DTYPE, 64, 4, BITS, false>, grid_for(a.rows + more), 64, stream, a, stats, down, grad, grad_stride, 1, sum,
-                          few_pairs.pairs, few_pairs.exact);
-    }
-    // Few rows in parts of half the size: gradients of 128 rows of 32,000 tokens in bf16 7 -> 6 us; 2,048 of 128,256 107 -> 112.
-    const bool few = a.rows <= 128;
-    const int32_t span = few ? 256 * 4 : 256 * 8, parts = std::max(1, (n_groups + span - 1) / span);
-    return launch(few ? token_grad_kernel<DTYPE, 256, 4, BITS, PAIRS> : token_grad_kernel<DTYPE, 256, 8, BITS, PAIRS>, grid_for(a.rows * parts + more), 256,
-                  stream, a, stats, down, grad, grad_stride, parts, sum, few_pairs.pairs, few_pairs.exact);
-}
-
-}  // namespace
-
-bool token_logprobs_want_workspace(const TokenRows& a) { return in_parts(a); }
-
-int launch_token_logprobs(const TokenRows& a, float* logprobs, float* stats, void* workspace, hipStream_t stream)
-{
-    if (a.rows == 0) return TDFA_OK;
-    Outputs o = {};
-    o.logprobs = logprobs;
-    o.stats = reinterpret_cast<float2*>(stats);
-    return stats_of(a, o, static_cast<Part*>(workspace), stream);
-}
-
-template <bool PAIRS>
-static int grad_of(const TokenRows& a, const float2* stats, const float* down, void* grad, int64_t grad_stride, const LossSum& sum, const FewPairs& few,
-                   hipStream_t stream)
-{
-    if (a.dtype == TDFA_F32)
-        return a.allow ? grad_launch<TDFA_F32, true, PAIRS>(a, stats, down, grad, grad_stride, sum, few, stream)
-                       : grad_launch<TDFA_F32, false, PAIRS>(a, stats, down, grad, grad_stride, sum, few, stream);
-    return a.allow ? grad_launch<TDFA_BF16, true, PAIRS>(a, stats, down, grad, grad_stride, sum, few, stream)
-                   : grad_launch<TDFA_BF16, false, PAIRS>(a, stats, down, grad, grad_stride, sum, few, stream);
-}
-
-int launch_token_grad(const TokenRows& a, const float* stats, const float* down, void* grad, int64_t grad_stride, hipStream_t stream)
-{
-    if (a.rows == 0) return TDFA_OK;
-    return grad_of<false>(a, reinterpret_cast<const float2*>(stats), down, grad, grad_stride, LossSum{}, FewPairs{}, stream);
-}
-
-// Workspace: Part [kMaxParts] of each of the first kPartRows rows, double [rows] (lp, or the rows' losses), double [n_pairs] losses of the
-// pairs, float2 [rows] statistics, float [rows] d loss / d lp.
-static int64_t parts_bytes(int64_t rows) { return (rows < kPartRows ? rows : kPartRows) * kMaxParts * (int64_t)sizeof(Part); }
-int64_t loss_workspace(int64_t rows, int64_t n_pairs) { return parts_bytes(rows) + 8 * n_pairs + 20 * rows; }
-
-template <int DTYPE, bool BITS>
-static int policy_launch(const TokenRows& a, const PolicyArgs& p, float* logprobs, double* each, void* grad, int64_t grad_stride, hipStream_t stream)
+// set(x, from, parts) fills in what a launch for the rows from `from` on has beside the rows' arguments.
+template <typename A, int DTYPE, bool BITS, typename F>
+int grad_launch(const TokenRows& a, hipStream_t stream, F set)
 {
     const int32_t n_groups = a.n_tokens / Elem<DTYPE>::kGroup;
-    // The more wavefronts share a row, the sooner it is read: 1,500 rows of 32,000 tokens in bf16 34.4 us by 1,024 threads of 4 groups,
-    // 38.5 by 256 of 16; 24 rows 9.1 and 10.4 (of 20,000 tokens, 1,500 rows 27.6 and 26.3).
-    if (n_groups <= 64 * 8) return launch(policy_row_kernel<DTYPE, 64, 8, BITS>, grid_for(a.rows), 64, stream, a, p, logprobs, each, grad, grad_stride);
-    if (n_groups <= 256 * 8) return launch(policy_row_kernel<DTYPE, 256, 8, BITS>, grid_for(a.rows), 256, stream, a, p, logprobs, each, grad, grad_stride);
-    if (n_groups <= 1024 * 4) return launch(policy_row_kernel<DTYPE, 1024, 4, BITS>, grid_for(a.rows), 1024, stream, a, p, logprobs, each, grad, grad_stride);
-    if (n_groups <= 1024 * 8) return launch(policy_row_kernel<DTYPE, 1024, 8, BITS>, grid_for(a.rows), 1024, stream, a, p, logprobs, each, grad, grad_stride);
-    return launch(policy_row_kernel<DTYPE, 1024, 16, BITS>, grid_for(a.rows), 1024, stream, a, p, logprobs, each, grad, grad_stride);
+    // Few rows in parts of half the size: gradients of 128 rows of 32,000 tokens in bf16 7 -> 6 us; 2,048 of 128,256 107 -> 112.
+    constexpr bool kPairs = std::is_same_v<A, FewPairsGradArgs>;     // a row's slope is worked out by a whole workgroup
+    const bool few = a.rows <= 128, tiny = !kPairs && n_groups <= 64 * 4;
+    const int32_t span = tiny ? 64 * 4 : few ? 256 * 4 : 256 * 8, parts = std::max(1, (n_groups + span - 1) / span);
+    const int64_t most = (4 * kMaxBlocks - 1) / parts;     // workgroups of 256 threads
+    for (int64_t from = 0; from < a.rows; from += most) {
+        const dim3 grid((unsigned)(std::min(a.rows - from, most) * parts + kFirst<A>));
+        A x;
+        set(x, from, parts);
+        int rc;
+        if (tiny) rc = launch(token_grad_kernel<A, DTYPE, kPairs ? 256 : 64, 4, BITS>, grid, 64, stream, x);
+        else if (few) rc = launch(token_grad_kernel<A, DTYPE, 256, 4, BITS>, grid, 256, stream, x);
+        else rc = launch(token_grad_kernel<A, DTYPE, 256, 8, BITS>, grid, 256, stream, x);
+        if (rc != TDFA_OK) return rc;
+    }
+    return TDFA_OK;
+}
+template <typename A, typename F>
+int grad_of(const TokenRows& a, hipStream_t stream, F set)
+{
+    if (a.dtype == TDFA_F32) return a.allow ? grad_launch<A, TDFA_F32, true>(a, stream, set) : grad_launch<A, TDFA_F32, false>(a, stream, set);
+    return a.allow ? grad_launch<A, TDFA_BF16, true>(a, stream, set) : grad_launch<A, TDFA_BF16, false>(a, stream, set);
+}
+
+// The gradient from what the launches before have left, and the loss from n losses that lie `step` apart.
+int grad_of_work(const TokenRows& a, const RowWork* work, const double* each, int64_t n, int32_t step, float* loss, void* grad, int64_t grad_stride,
+                 hipStream_t stream)
+{
+    return grad_of<WorkGradArgs>(a, stream, [&](WorkGradArgs& x, int64_t from, int32_t parts) {
+        static_cast<RowArgs&>(x) = row_args(a, from);
+        x.work = work + from;
+        x.each = each;
+        x.loss = loss;
+        x.grad = grad_from(a, grad, grad_stride, from);
+        x.grad_stride16 = grad_stride16(a, grad_stride);
+        x.n = (uint32_t)n;
+        x.parts = parts;
+        x.step = step;
+    });
+}
+
+template <int DTYPE, bool BITS>
+int policy_launch(const TokenRows& a, const PolicyArgs& p, float* logprobs, void* grad, int64_t grad_stride, hipStream_t stream)
+{
+    const int32_t n_groups = a.n_tokens / Elem<DTYPE>::kGroup;
+    for (int64_t from = 0; from < a.rows; from += kMaxBlocks) {
+        const dim3 grid((unsigned)std::min(a.rows - from, kMaxBlocks));
+        PolicyRowArgs x;
+        static_cast<RowArgs&>(x) = row_args(a, from);
+        fill_terms(x, a, p, logprobs, from);
+        x.grad = grad_from(a, grad, grad_stride, from);
+        x.grad_stride16 = grad_stride16(a, grad_stride);
+        int rc;
+        // The more wavefronts share a row, the sooner it is read: 1,500 rows of 32,000 tokens in bf16 34.4 us by 1,024 threads of 4 groups,
+        // 38.5 by 256 of 16; 24 rows 9.1 and 10.4 (of 20,000 tokens, 1,500 rows 27.6 and 26.3).
+        if (n_groups <= 64 * 8) rc = launch(policy_row_kernel<DTYPE, 64, 8, BITS>, grid, 64, stream, x);
+        else if (n_groups <= 256 * 8) rc = launch(policy_row_kernel<DTYPE, 256, 8, BITS>, grid, 256, stream, x);
+        else if (n_groups <= 1024 * 4) rc = launch(policy_row_kernel<DTYPE, 1024, 4, BITS>, grid, 1024, stream, x);
+        else if (n_groups <= 1024 * 8) rc = launch(policy_row_kernel<DTYPE, 1024, 8, BITS>, grid, 1024, stream, x);
+        else rc = launch(policy_row_kernel<DTYPE, 1024, 16, BITS>, grid, 1024, stream, x);
+        if (rc != TDFA_OK) return rc;
+    }
+    return TDFA_OK;
 }
 
 // Whether a policy loss is scored and its gradient written by one launch, a workgroup per row that reads it once, or by two, which read
@@ -1094,58 +1302,89 @@ bool one_launch(const TokenRows& a)
     return n_groups <= kWholeGroups && (a.rows > 32 || n_groups <= 1024 * 4);
 }
 
+// Rows whose losses one workgroup sums: more are summed by one per kSumRows rows and then by one.
+constexpr int64_t kSumRows = 16384;
+
+// Workspace: Part [kMaxParts] of each of the first kPartRows rows, RowWork [rows], double [n_pairs] losses of the pairs.
+int64_t parts_bytes(int64_t rows) { return (rows < kPartRows ? rows : kPartRows) * kMaxParts * (int64_t)sizeof(Part); }
+
+}  // namespace
+
+int64_t loss_workspace(int64_t rows, int64_t n_pairs) { return parts_bytes(rows) + (int64_t)sizeof(RowWork) * rows + 8 * n_pairs; }
+
+bool token_logprobs_want_workspace(const TokenRows& a) { return in_parts(a); }
+
+int launch_token_logprobs(const TokenRows& a, float* logprobs, float* stats, void* workspace, hipStream_t stream)
+{
+    if (a.rows == 0) return TDFA_OK;
+    return stats_of<ScoreArgs>(a, Score{logprobs, reinterpret_cast<float2*>(stats), nullptr, nullptr}, static_cast<Part*>(workspace), stream);
+}
+
+int launch_token_grad(const TokenRows& a, const float* stats, const float* down, void* grad, int64_t grad_stride, hipStream_t stream)
+{
+    if (a.rows == 0) return TDFA_OK;
+    return grad_of<GivenGradArgs>(a, stream, [&](GivenGradArgs& x, int64_t from, int32_t parts) {
+        static_cast<RowArgs&>(x) = row_args(a, from);
+        x.stats = reinterpret_cast<const float2*>(stats) + from;
+        x.down = down + from;
+        x.grad = grad_from(a, grad, grad_stride, from);
+        x.grad_stride16 = grad_stride16(a, grad_stride);
+        x.parts = parts;
+    });
+}
+
 int launch_policy_loss(const TokenRows& a, const PolicyArgs& p, float* loss, float* logprobs, void* grad, int64_t grad_stride, void* workspace,
                        hipStream_t stream)
 {
-    Part* parts = static_cast<Part*>(workspace);
-    double* each = reinterpret_cast<double*>(static_cast<char*>(workspace) + parts_bytes(a.rows));
-    if (a.rows && one_launch(a)) {
-        const int rc = a.dtype == TDFA_F32 ? (a.allow ? policy_launch<TDFA_F32, true>(a, p, logprobs, each, grad, grad_stride, stream)
-                                                      : policy_launch<TDFA_F32, false>(a, p, logprobs, each, grad, grad_stride, stream))
-                                           : (a.allow ? policy_launch<TDFA_BF16, true>(a, p, logprobs, each, grad, grad_stride, stream)
-                                                      : policy_launch<TDFA_BF16, false>(a, p, logprobs, each, grad, grad_stride, stream));
+    if (a.rows && !(one_launch(a))) {
+        RowWork* work = reinterpret_cast<RowWork*>(static_cast<char*>(workspace) + parts_bytes(a.rows));
+        const int rc = stats_of<PolicyScoreArgs>(a, Score{logprobs, nullptr, work, &p}, static_cast<Part*>(workspace), stream);
         if (rc != TDFA_OK) return rc;
-    } else if (a.rows) {
-        Outputs o = {};
-        o.logprobs = logprobs;
-        o.each = each;
-        o.policy = p;
-        if (grad) {
-            o.stats = reinterpret_cast<float2*>(each + a.rows);
-            o.down = reinterpret_cast<float*>(o.stats + a.rows);
-        }
-        const int rc = stats_of(a, o, parts, stream);
-        if (rc != TDFA_OK || grad) return rc != TDFA_OK ? rc : grad_of<false>(a, o.stats, o.down, grad, grad_stride, LossSum{each, a.rows, 1.0, loss}, FewPairs{}, stream);
+        constexpr int32_t step = sizeof(RowWork) / sizeof(double);
+        if (grad) return grad_of_work(a, work, &work->value, a.rows, step, loss, grad, grad_stride, stream);
+        return launch(loss_sum_kernel, dim3(1), 1024, stream, static_cast<const double*>(&work->value), (uint32_t)a.rows, step, loss);
     }
-    return launch(loss_sum_kernel, dim3(1), 1024, stream, LossSum{each, a.rows, 1.0, loss});
+    if (a.rows) {
+        const int rc = a.dtype == TDFA_F32 ? (a.allow ? policy_launch<TDFA_F32, true>(a, p, logprobs, grad, grad_stride, stream)
+                                                      : policy_launch<TDFA_F32, false>(a, p, logprobs, grad, grad_stride, stream))
+                                           : (a.allow ? policy_launch<TDFA_BF16, true>(a, p, logprobs, grad, grad_stride, stream)
+                                                      : policy_launch<TDFA_BF16, false>(a, p, logprobs, grad, grad_stride, stream));
+        if (rc != TDFA_OK) return rc;
+    }
+    const bool alone = a.rows <= kSumRows;
+    double* sums = static_cast<double*>(workspace);
+    const unsigned blocks = alone ? 1u : (unsigned)((a.rows + kSumRows - 1) / kSumRows);
+    const PolicySumArgs x = {logprobs, p.old_logprobs, p.ref_logprobs, p.advantages, a.weights, a.tokens, alone ? loss : nullptr, sums,
+                             (uint32_t)a.rows, (uint32_t)kSumRows, p.clip_low, p.clip_high, p.kl_coef};
+    const int rc = launch(policy_sum_kernel, dim3(blocks), 1024, stream, x);
+    if (rc != TDFA_OK || alone) return rc;
+    return launch(loss_sum_kernel, dim3(1), 1024, stream, static_cast<const double*>(sums), (uint32_t)blocks, 0, loss);
 }
 
 int launch_preference_loss(const TokenRows& a, const PairArgs& p, float* loss, float* logprobs, void* grad, int64_t grad_stride, void* workspace,
                            hipStream_t stream)
 {
-    Part* parts = static_cast<Part*>(workspace);
-    double* exact = reinterpret_cast<double*>(static_cast<char*>(workspace) + parts_bytes(a.rows));
-    double* each = exact + a.rows;
-    Outputs o = {};
-    o.logprobs = logprobs;
-    o.exact = exact;
-    o.stats = reinterpret_cast<float2*>(each + p.n_pairs);
-    o.down = reinterpret_cast<float*>(o.stats + a.rows);                   // zero, for the rows of no sequence
+    RowWork* work = reinterpret_cast<RowWork*>(static_cast<char*>(workspace) + parts_bytes(a.rows));
+    double* each = reinterpret_cast<double*>(work + a.rows);
     if (a.rows) {
-        const int rc = stats_of(a, o, parts, stream);
+        const int rc = stats_of<PairScoreArgs>(a, Score{logprobs, nullptr, work, nullptr}, static_cast<Part*>(workspace), stream);
         if (rc != TDFA_OK) return rc;
     }
+    const PairArgsOnCard pairs = {p.ref_logprobs, p.begin, p.rewards, p.n_pairs, (int32_t)a.rows, p.beta, p.smoothing};
     // Few rows and pairs without the launch between the other two: 90 rows of 32,000 tokens in bf16 in 4 pairs 13.9 -> 12.2 us, 1,000 rows
-    // in 64 pairs 34.4 -> 32.5 (of 1,000 tokens 11.6 -> 13.0), and 3.3 us less of the host; 300 rows in 128 pairs 10.7 -> 16.8.
+    // in 64 pairs 34.4 -> 32.5 (of 1,000 tokens 11.6 -> 13.0), and 3 us less of the host; 300 rows in 128 pairs 10.7 -> 16.8.
     if (grad && a.rows && a.rows <= 1024 && p.n_pairs && p.n_pairs <= 64)
-        return grad_of<true>(a, o.stats, nullptr, grad, grad_stride, LossSum{nullptr, 0, 0.0, loss}, FewPairs{p, exact}, stream);
+        return grad_of<FewPairsGradArgs>(a, stream, [&](FewPairsGradArgs& x, int64_t, int32_t) {
+            const RowArgs r = row_args(a, 0);              // one launch: a row of 2^24 tokens has 4,096 parts at most, 2,048 where there are more than 128
+            x = {r.allow, r.logits, r.states, r.tokens, work, grad, loss, pairs, r.stride16, grad_stride16(a, grad_stride), r.n_tokens, r.inv_t};
+        });
     if (p.n_pairs) {
-        const int rc = launch(pair_kernel, dim3(blocks_for(p.n_pairs)), kThreads, stream, p, a.rows, exact, o.stats, o.down, each);
+        const int32_t blocks = (int32_t)std::min<int64_t>(p.n_pairs, kMaxBlocks);
+        const int rc = launch(pair_kernel, dim3((unsigned)blocks), kThreads, stream, pairs, work, each, blocks);
         if (rc != TDFA_OK) return rc;
     }
-    const LossSum sum = {each, p.n_pairs, p.n_pairs ? 1.0 / (double)p.n_pairs : 0.0, loss};
-    if (grad && a.rows) return grad_of<false>(a, o.stats, o.down, grad, grad_stride, sum, FewPairs{}, stream);
-    return launch(loss_sum_kernel, dim3(1), 1024, stream, sum);
+    if (grad && a.rows) return grad_of_work(a, work, each, p.n_pairs, 1, loss, grad, grad_stride, stream);
+    return launch(loss_sum_kernel, dim3(1), 1024, stream, static_cast<const double*>(each), (uint32_t)p.n_pairs, 1, loss);
 }
 
 }  // namespace tdfa

@@ -263,9 +263,7 @@ int launch_advance_tokens(const MaskArgs& table, int32_t batch, int32_t k, const
 // Rows of logits with a token each, under a constraint or none (loss.hip).
 struct TokenRows {
     const uint32_t* allow;              // allowed-bit rows of the table, or NULL: every token is allowed
-    const uint32_t* row_allowed;        // [n_states] tokens each state allows, or NULL if not known
     int64_t n_states;
-    int64_t row_words;
     const void* logits;
     int dtype;
     int64_t row_stride;
