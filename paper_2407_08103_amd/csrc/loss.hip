@@ -705,11 +705,11 @@ struct GivenGradArgs : RowArgs {
 };
 struct WorkGradArgs : RowArgs {
     const RowWork* work;
-    const double* each;        // the losses, `step` apart; with step 1 those of pairs, of which the mean is wanted
+    const double* each;        // the losses, `step` apart
     float* loss;
     void* grad;
     uint32_t grad_stride16, n;
-    int32_t parts, step;
+    int32_t parts, step, mean;
 };
 struct PairArgsOnCard {        // of a preference loss
     const float* ref_logprobs;
@@ -861,19 +861,19 @@ __device__ __forceinline__ float slope_of_row(const PairArgsOnCard& p, const Row
     return k & 1 ? -slope : slope;
 }
 
-// loss = the sum of n losses, or their mean (step 1), by one workgroup, in an order that depends on nothing but n and NT.
+// loss = the sum of n losses that lie `step` apart, or their mean, by one workgroup, in an order that depends on nothing but n and NT.
 template <int NT>
-__device__ __forceinline__ void sum_losses(const double* each, int64_t n, int32_t step, float* loss, double (&part)[NT / 64])
+__device__ __forceinline__ void sum_losses(const double* each, int64_t n, int32_t step, bool mean, float* loss, double (&part)[NT / 64])
 {
     double sum = 0.0;
     for (int64_t i = threadIdx.x; i < n; i += NT) sum += each[i * step];
     sum = reduce_sum<NT>(sum, part);
-    if (threadIdx.x == 0) *loss = (float)(step == 1 ? (n ? sum / (double)n : 0.0) : sum);
+    if (threadIdx.x == 0) *loss = (float)(mean && n ? sum / (double)n : sum);
 }
-__global__ void __launch_bounds__(1024) loss_sum_kernel(const double* each, uint32_t n, int32_t step, float* loss)
+__global__ void __launch_bounds__(1024) loss_sum_kernel(const double* each, uint32_t n, int32_t step, int32_t mean, float* loss)
 {
     __shared__ double s_part[16];
-    sum_losses<1024>(each, n, step, loss, s_part);
+    sum_losses<1024>(each, n, step, mean, loss, s_part);
 }
 
 // The policy loss from the log-probabilities that a launch before has written: `span` rows to a workgroup, which leaves its sum in out, or
@@ -952,7 +952,7 @@ template <int NT>
 __device__ __forceinline__ bool first_block(const WorkGradArgs& a)
 {
     __shared__ double s_part[NT / 64];
-    sum_losses<NT>(a.each, a.n, a.step, a.loss, s_part);
+    sum_losses<NT>(a.each, a.n, a.step, a.mean, a.loss, s_part);
     return true;
 }
 template <int NT>
@@ -1170,21 +1170,24 @@ void fill(PolicyScoreArgs& x, const TokenRows& a, const Score& o, int64_t from)
 template <typename A, int DTYPE, bool BITS>
 int stats_launch(const TokenRows& a, const Score& o, hipStream_t stream)
 {
+    constexpr bool kLong = std::is_same_v<A, PolicyScoreArgs>;             // of a policy loss only what one_launch leaves
     const int32_t n_groups = a.n_tokens / Elem<DTYPE>::kGroup;
     for (int64_t from = 0; from < a.rows; from += kMaxBlocks) {
         const dim3 grid((unsigned)std::min(a.rows - from, kMaxBlocks));
         A x;
         static_cast<RowArgs&>(x) = row_args(a, from);
         fill(x, a, o, from);
-        int rc;
+        int rc = TDFA_OK;
         // Two rows or more to a compute unit, so that one is fetched while another is summed.  Rows too few to fill the card are shared by
         // more wavefronts each: 24 rows of 32,000 tokens in bf16 6.0 -> 5.1 us, 400 rows 8.2 -> 7.7; of 8,000 tokens 4.1 either way, 400
         // rows 4.5 -> 5.4.
-        if (n_groups <= 64 * 4) rc = launch(token_stats_kernel<A, DTYPE, 64, 4, BITS>, grid, 64, stream, x);
-        else if (a.rows <= 512 && n_groups > 256 * 8 && n_groups <= 512 * 16) rc = launch(token_stats_kernel<A, DTYPE, 1024, 4, BITS>, grid, 1024, stream, x);
-        else if (n_groups <= 256 * 16) rc = launch(token_stats_kernel<A, DTYPE, 256, 8, BITS>, grid, 256, stream, x);
-        else if (n_groups <= 512 * 16) rc = launch(token_stats_kernel<A, DTYPE, 512, 8, BITS>, grid, 512, stream, x);
-        else rc = launch(token_stats_kernel<A, DTYPE, 1024, 8, BITS>, grid, 1024, stream, x);
+        if (a.rows <= 512 && n_groups > 256 * 8 && n_groups <= 512 * 16) rc = launch(token_stats_kernel<A, DTYPE, 1024, 4, BITS>, grid, 1024, stream, x);
+        else if (kLong || n_groups > 512 * 16) rc = launch(token_stats_kernel<A, DTYPE, 1024, 8, BITS>, grid, 1024, stream, x);
+        else if constexpr (!kLong) {
+            if (n_groups <= 64 * 4) rc = launch(token_stats_kernel<A, DTYPE, 64, 4, BITS>, grid, 64, stream, x);
+            else if (n_groups <= 256 * 16) rc = launch(token_stats_kernel<A, DTYPE, 256, 8, BITS>, grid, 256, stream, x);
+            else rc = launch(token_stats_kernel<A, DTYPE, 512, 8, BITS>, grid, 512, stream, x);
+        }
         if (rc != TDFA_OK) return rc;
     }
     return TDFA_OK;
@@ -1252,8 +1255,8 @@ int grad_of(const TokenRows& a, hipStream_t stream, F set)
 }
 
 // The gradient from what the launches before have left, and the loss from n losses that lie `step` apart.
-int grad_of_work(const TokenRows& a, const RowWork* work, const double* each, int64_t n, int32_t step, float* loss, void* grad, int64_t grad_stride,
-                 hipStream_t stream)
+int grad_of_work(const TokenRows& a, const RowWork* work, const double* each, int64_t n, int32_t step, bool mean, float* loss, void* grad,
+                 int64_t grad_stride, hipStream_t stream)
 {
     return grad_of<WorkGradArgs>(a, stream, [&](WorkGradArgs& x, int64_t from, int32_t parts) {
         static_cast<RowArgs&>(x) = row_args(a, from);
@@ -1265,6 +1268,7 @@ int grad_of_work(const TokenRows& a, const RowWork* work, const double* each, in
         x.n = (uint32_t)n;
         x.parts = parts;
         x.step = step;
+        x.mean = mean;
     });
 }
 
@@ -1341,8 +1345,8 @@ int launch_policy_loss(const TokenRows& a, const PolicyArgs& p, float* loss, flo
         const int rc = stats_of<PolicyScoreArgs>(a, Score{logprobs, nullptr, work, &p}, static_cast<Part*>(workspace), stream);
         if (rc != TDFA_OK) return rc;
         constexpr int32_t step = sizeof(RowWork) / sizeof(double);
-        if (grad) return grad_of_work(a, work, &work->value, a.rows, step, loss, grad, grad_stride, stream);
-        return launch(loss_sum_kernel, dim3(1), 1024, stream, static_cast<const double*>(&work->value), (uint32_t)a.rows, step, loss);
+        if (grad) return grad_of_work(a, work, &work->value, a.rows, step, false, loss, grad, grad_stride, stream);
+        return launch(loss_sum_kernel, dim3(1), 1024, stream, static_cast<const double*>(&work->value), (uint32_t)a.rows, step, 0, loss);
     }
     if (a.rows) {
         const int rc = a.dtype == TDFA_F32 ? (a.allow ? policy_launch<TDFA_F32, true>(a, p, logprobs, grad, grad_stride, stream)
@@ -1358,7 +1362,7 @@ int launch_policy_loss(const TokenRows& a, const PolicyArgs& p, float* loss, flo
                              (uint32_t)a.rows, (uint32_t)kSumRows, p.clip_low, p.clip_high, p.kl_coef};
     const int rc = launch(policy_sum_kernel, dim3(blocks), 1024, stream, x);
     if (rc != TDFA_OK || alone) return rc;
-    return launch(loss_sum_kernel, dim3(1), 1024, stream, static_cast<const double*>(sums), (uint32_t)blocks, 0, loss);
+    return launch(loss_sum_kernel, dim3(1), 1024, stream, static_cast<const double*>(sums), (uint32_t)blocks, 1, 0, loss);
 }
 
 int launch_preference_loss(const TokenRows& a, const PairArgs& p, float* loss, float* logprobs, void* grad, int64_t grad_stride, void* workspace,
@@ -1383,8 +1387,8 @@ int launch_preference_loss(const TokenRows& a, const PairArgs& p, float* loss, f
         const int rc = launch(pair_kernel, dim3((unsigned)blocks), kThreads, stream, pairs, work, each, blocks);
         if (rc != TDFA_OK) return rc;
     }
-    if (grad && a.rows) return grad_of_work(a, work, each, p.n_pairs, 1, loss, grad, grad_stride, stream);
-    return launch(loss_sum_kernel, dim3(1), 1024, stream, static_cast<const double*>(each), (uint32_t)p.n_pairs, 1, loss);
+    if (grad && a.rows) return grad_of_work(a, work, each, p.n_pairs, 1, true, loss, grad, grad_stride, stream);
+    return launch(loss_sum_kernel, dim3(1), 1024, stream, static_cast<const double*>(each), (uint32_t)p.n_pairs, 1, 1, loss);
 }
 
 }  // namespace tdfa

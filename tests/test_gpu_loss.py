@@ -566,3 +566,90 @@ def test_refusals(T):
             print("not refused:", k)
     torch.cuda.synchronize()
     _check_logprobs(T, c, 1.0)
+
+
+def _many_rows(T, rows, v=8):
+    """Rows of few tokens, in 64 bits on the GPU: (logits, tokens, lp, p)."""
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    x = torch.randn(rows, v, generator=g, device="cuda").bfloat16()
+    tokens = torch.randint(-1, v, (rows,), generator=g, device="cuda", dtype=torch.int32)
+    logp = torch.log_softmax(x.double(), dim=1)
+    live = tokens >= 0
+    lp = torch.where(live, logp.gather(1, tokens.clamp(min=0).long()[:, None])[:, 0], 0.0)
+    return x, tokens, live, lp, logp.exp()
+
+
+def _slopes_close(grad, p, tokens, live, down, tol_down):
+    """Against down ([j = t] - p_j), in bf16."""
+    want = -p
+    want[torch.arange(len(tokens), device="cuda")[live], tokens[live].long()] += 1.0
+    want *= torch.where(live, down, 0.0)[:, None]
+    tol = torch.where(live, down.abs(), 0.0)[:, None] * (2 * R.REL_SUM + 64 * R.U) + tol_down
+    tol = tol + 2.0 ** -8 * (want.abs() + tol) + 1e-37
+    assert bool(((grad.double() - want).abs() <= tol).all())
+
+
+@pytest.mark.parametrize("rows", [16385, (1 << 21) + 3])
+def test_more_rows_than_a_launch_has_workgroups(T, rows):
+    x, tokens, live, lp, p = _many_rows(T, rows)
+    tol = R.REL_SUM + 4 * R.U * lp.abs()
+    got, stats = torch.full((rows,), 9.0, device="cuda"), torch.full((rows, 2), 9.0, device="cuda")
+    T.token_logprobs(None, x, None, tokens, got, stats=stats)
+    assert bool(((got.double() - lp).abs() <= tol).all())
+    g = torch.Generator(device="cuda").manual_seed(1)
+    down = torch.randn(rows, generator=g, device="cuda")
+    grad = torch.full_like(x, 7.0)
+    T.token_logprobs_backward(None, x, None, tokens, stats, down, grad)
+    _slopes_close(grad, p, tokens, live, down.double(), 0.0)
+
+    old, adv = (lp + 0.05 * torch.randn(rows, generator=g, device="cuda")).float(), torch.randn(rows, generator=g, device="cuda")
+    loss, grad = torch.full((1,), 9.0, device="cuda"), torch.full_like(x, 7.0)
+    T.policy_loss(None, x, None, tokens, old, adv, loss, got, grad_logits=grad, clip=(1.0, math.inf))      # nothing is clipped
+    each = torch.where(live, -torch.exp(lp - old.double()) * adv.double(), 0.0)
+    size = float(each.abs().sum())
+    assert abs(float(loss) - float(each.sum())) <= size * (R.REL_SUM + 4 * R.U * float(lp.abs().max()) + 16 * R.U) + 1e-6 * abs(float(each.sum()))
+    assert bool(((got.double() - lp).abs() <= tol).all())
+    _slopes_close(grad, p, tokens, live, each, (each.abs() * (tol + 16 * R.U))[:, None])
+
+    cut = [0, rows // 3, rows - 9, rows - 1, rows]
+    begin, ref = torch.tensor(cut, dtype=torch.int32, device="cuda"), (lp + 0.01 * torch.randn(rows, generator=g, device="cuda")).float()
+    rewards, grad, beta = torch.full((4,), 9.0, device="cuda"), torch.full_like(x, 7.0), 4.0 / rows
+    T.preference_loss(None, x, None, tokens, ref, begin, loss, rewards, got, grad_logits=grad, beta=beta)
+    over = torch.where(live, lp - ref.double(), 0.0)
+    want = [beta * float(over[a:b].sum()) for a, b in zip(cut, cut[1:])]
+    # the sums' errors add up at worst
+    off = beta * rows * (R.REL_SUM + 4 * R.U * float(lp.abs().max())) + 8 * R.U
+    assert all(abs(float(a) - b) <= off for a, b in zip(rewards, want))
+    gap = [want[0] - want[1], want[2] - want[3]]
+    assert abs(float(loss) - sum(math.log1p(math.exp(-y)) for y in gap) / 2) <= 2 * off + 16 * R.U
+    down = torch.empty(rows, dtype=torch.float64, device="cuda")
+    for k, (a, b) in enumerate(zip(cut, cut[1:])):
+        down[a:b] = (beta if k % 2 else -beta) / 2 / (1.0 + math.exp(gap[k // 2]))
+    _slopes_close(grad, p, tokens, live, down, beta / 2 * (2 * off + 16 * R.U))
+
+
+def test_refusals_of_overlaps_and_strides(T):
+    x = torch.randn(4, 64, device="cuda").bfloat16()
+    tokens, f = torch.zeros(4, dtype=torch.int32, device="cuda"), [torch.ones(8, device="cuda") for _ in range(4)]
+    loss, rewards, begin = torch.zeros(1, device="cuda"), torch.zeros(2, device="cuda"), torch.tensor([0, 2, 4], dtype=torch.int32, device="cuda")
+    kept = [t.clone() for t in (x, tokens, *f)]
+    for old, adv, ref, weights, lp in [(0, 1, 2, 3, 0), (0, 1, 2, 3, 1), (0, 1, 2, 3, 2), (0, 1, 2, 3, 3)]:
+        with pytest.raises(T.TdfaError, match="overlaps"):
+            T.policy_loss(None, x, None, tokens, f[old][:4], f[adv][:4], loss, f[lp][3:7], ref_logprobs=f[ref][:4], weights=f[weights][:4], kl_coef=0.1)
+    with pytest.raises(T.TdfaError, match="overlaps"):
+        T.preference_loss(None, x, None, tokens, f[0][:4], begin, loss, rewards, f[0][:4])
+    with pytest.raises(T.TdfaError, match="overlaps"):
+        T.policy_loss(None, x, None, tokens, f[0][:4], f[1][:4], loss, tokens.view(torch.float32))
+    # next to one another is fine, and so is what is not read
+    T.policy_loss(None, x, None, tokens, f[0][:4], f[1][:4], loss, f[0][4:], ref_logprobs=f[0][4:])
+    f[0][4:] = 1.0
+    lib, far = T.lib(), (1 << 35)                          # elements of 2 bytes: 2^36 bytes
+    a = [x.data_ptr(), tokens.data_ptr(), f[0].data_ptr(), f[1].data_ptr()]
+    assert lib.tdfa_token_logprobs(None, a[0], 1, 2, 64, far, None, a[1], 1.0, a[2], None, None, 0, None) == -1
+    assert b"stride" in lib.tdfa_last_error()
+    assert lib.tdfa_token_logprobs_backward(None, a[0], 1, 2, 64, 64, None, a[1], 1.0, a[2], a[3], a[0], far, None) == -1
+    assert b"stride" in lib.tdfa_last_error()
+    assert lib.tdfa_token_logprobs(None, a[0], 1, 1, 64, far, None, a[1], 1.0, f[2].data_ptr(), None, None, 0, None) == 0       # one row has none
+    torch.cuda.synchronize()
+    f[2][:1] = 1.0
+    assert all(torch.equal(s, t) for s, t in zip(kept, (x, tokens, *f)))
