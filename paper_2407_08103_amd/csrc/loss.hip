@@ -500,10 +500,10 @@ __device__ __forceinline__ void finish(const PolicyScoreArgs& a, uint32_t i, Sco
 
 // One workgroup per row.  The sum is taken relative to the row's own token, ref = z_t, so that no maximum has to be known, terms are added
 // as they arrive, and lp = -ln s; where that overflows (lp below -87) or a NaN is met, the row is read again, for the largest logit and
-// the sum relative to it.  Bound by the memory where there are many rows: 2,900 rows of 128,256 tokens in bf16 79 us, of which 0.53
-// of the 128-byte lines hold an allowed token (394 MB, 5.0 TB/s; torch's maximum over the rows of a matrix reads 4.9 to 5.2); by one
+// the sum relative to it.  Bound by the memory where there are many rows: 2,900 rows of 128,256 tokens in bf16 77 us, of which 0.53
+// of the 128-byte lines hold an allowed token (394 MB, 5.1 TB/s; torch's maximum over the rows of a matrix reads 4.9 to 5.2); by one
 // compute unit's stream of a long row where there are few (256 KB in 7.5 us, about 40 GB/s whatever is in flight); by the chain token,
-// bits, logits in short ones (2.8 us).
+// bits, logits in short ones (2.5 us).
 template <typename A, int DTYPE, int NT, int U, bool BITS>
 __global__ void __launch_bounds__(NT, 8) token_stats_kernel(A a)
 {
@@ -795,7 +795,7 @@ __device__ __forceinline__ double reduce_sum(double sum, double (&part)[NT / 64]
 }
 
 // One workgroup per pair: the two rewards, the pair's loss, and d loss / d lp of every row of the pair.  Bound by its chain of reads
-// (32 pairs of 90 rows 4.7 us).
+// (32 pairs of 90 rows 4.8 us).
 __global__ void __launch_bounds__(kThreads) pair_kernel(PairArgsOnCard p, RowWork* work, double* each, int32_t blocks)
 {
     __shared__ double s_part[2][kThreads / 64];
@@ -877,7 +877,8 @@ __global__ void __launch_bounds__(1024) loss_sum_kernel(const double* each, uint
 }
 
 // The policy loss from the log-probabilities that a launch before has written: `span` rows to a workgroup, which leaves its sum in out, or
-// the loss if it is the only one.  Bound by its chain of reads (24 rows 1.5 us, 4,096 rows 4.4).
+// the loss if it is the only one.  Up to 1,024 rows 2.0 us, a chain of two reads; 4,096 rows 4.1, 8,192 rows 6.6, 16,384 rows 12.1, bound by the
+// exponentials of one compute unit (with the reads of four rows on their way together 3.3, 4.1, 6.3 and 10.5).
 struct PolicySumArgs {
     const float* logprobs;
     const float* old_logprobs;
@@ -971,7 +972,7 @@ __device__ __forceinline__ int32_t parts_of(const FewPairsGradArgs&, int32_t n_g
 
 // grad[i][j] = down[i] c ([j = t] - p_j) over A, 0 elsewhere; 0 throughout in a row that takes no part.  A workgroup
 // takes NT U groups of one row; the last of a row takes the elements behind the last whole group too.  Bound by the memory: 2,048 rows of
-// 128,256 tokens in bf16 105 us (525 MB written and 255 MB of lines read, in part from the 256 MB cache that the sums have left full:
+// 128,256 tokens in bf16 104 us (525 MB written and 255 MB of lines read, in part from the 256 MB cache that the sums have left full:
 // 7.4 TB/s), 8 groups in flight per thread (4: 112, 2: 150).
 template <typename A, int DTYPE, int NT, int U, bool BITS>
 __global__ void __launch_bounds__(NT) token_grad_kernel(A a)
@@ -1022,8 +1023,8 @@ constexpr int64_t kPartRows = 384;
 
 // One workgroup per row: the sum, the row's term, the gradient.  The row stays in registers between the sum and the gradient, R groups
 // to a thread: 1,024 threads hold 256 KB, half of a compute unit's registers, and the row is read once.  Bound by the memory: 1,024 rows
-// of 128,256 tokens in bf16 without a constraint 96 us for 263 MB read and as much written (5.5 TB/s; an elementwise product of such
-// matrices takes 87, a copy 100); 4,096 rows under one 289 us, 1.05 GB written and some 0.55 GB of lines read (5.5 TB/s).  Vector
+// of 128,256 tokens in bf16 without a constraint 91 us for 263 MB read and as much written (5.8 TB/s; an elementwise product of such
+// matrices takes 87, a copy 100); 4,096 rows under one 277 us, 1.05 GB written and some 0.55 GB of lines read (5.8 TB/s).  Vector
 // instructions take two fifths of the time.  Two rows to a compute unit with half of each read twice: 316 us; workgroups that stay, and
 // fetch the next row into the registers that the gradient leaves: 119 us for the 1,024.
 template <int DTYPE, int NT, int R, bool BITS>
@@ -1306,8 +1307,9 @@ bool one_launch(const TokenRows& a)
     return n_groups <= kWholeGroups && (a.rows > 32 || n_groups <= 1024 * 4);
 }
 
-// Rows whose losses one workgroup sums: more are summed by one per kSumRows rows and then by one.
-constexpr int64_t kSumRows = 16384;
+// Rows whose losses one workgroup sums, in 6.7 us; of more, each sums kSpanRows, in 4 us, and a further launch joins them in 2 to 5
+// (16,384 rows by one workgroup 12.1).
+constexpr int64_t kSumRows = 8192, kSpanRows = 2048;
 
 // Workspace: Part [kMaxParts] of each of the first kPartRows rows, RowWork [rows], double [n_pairs] losses of the pairs.
 int64_t parts_bytes(int64_t rows) { return (rows < kPartRows ? rows : kPartRows) * kMaxParts * (int64_t)sizeof(Part); }
@@ -1357,9 +1359,9 @@ int launch_policy_loss(const TokenRows& a, const PolicyArgs& p, float* loss, flo
     }
     const bool alone = a.rows <= kSumRows;
     double* sums = static_cast<double*>(workspace);
-    const unsigned blocks = alone ? 1u : (unsigned)((a.rows + kSumRows - 1) / kSumRows);
+    const unsigned blocks = alone ? 1u : (unsigned)((a.rows + kSpanRows - 1) / kSpanRows);
     const PolicySumArgs x = {logprobs, p.old_logprobs, p.ref_logprobs, p.advantages, a.weights, a.tokens, alone ? loss : nullptr, sums,
-                             (uint32_t)a.rows, (uint32_t)kSumRows, p.clip_low, p.clip_high, p.kl_coef};
+                             (uint32_t)a.rows, (uint32_t)(alone ? kSumRows : kSpanRows), p.clip_low, p.clip_high, p.kl_coef};
     const int rc = launch(policy_sum_kernel, dim3(blocks), 1024, stream, x);
     if (rc != TDFA_OK || alone) return rc;
     return launch(loss_sum_kernel, dim3(1), 1024, stream, static_cast<const double*>(sums), (uint32_t)blocks, 1, 0, loss);

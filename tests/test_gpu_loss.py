@@ -589,7 +589,7 @@ def _slopes_close(grad, p, tokens, live, down, tol_down):
     assert bool(((grad.double() - want).abs() <= tol).all())
 
 
-@pytest.mark.parametrize("rows", [16385, (1 << 21) + 3])
+@pytest.mark.parametrize("rows", [8193, 16385, (1 << 21) + 3])
 def test_more_rows_than_a_launch_has_workgroups(T, rows):
     x, tokens, live, lp, p = _many_rows(T, rows)
     tol = R.REL_SUM + 4 * R.U * lp.abs()
