@@ -1087,8 +1087,10 @@ __global__ void __launch_bounds__(NT, 4) policy_row_kernel(PolicyRowArgs a)
         }
         __syncthreads();
         q = shared_by_wave(s_slope);
-    } else if (threadIdx.x == 0) {
-        a.logprobs[i] = r.lp;
+    } else {
+        // A gradient may lie over the logits: no wavefront writes before all have read the token's logit (above, the sum's barriers see to it).
+        if (r.read) __syncthreads();
+        if (threadIdx.x == 0) a.logprobs[i] = r.lp;
     }
     if (!a.grad) return;
     auto* out = row_at<DTYPE>(a.grad, i, a.grad_stride16);
