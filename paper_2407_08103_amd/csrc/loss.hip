@@ -6,7 +6,9 @@
 // and s = sum over A of exp((z_j - m) c):
 //     lp = (z_t - m) c - ln s            p_j = exp((z_j - m) c) / s  in A, 0 elsewhere
 //     d lp / d z_j = c ([j = t] - p_j)
-// and every loss is a function of the rows' lp, so its gradient is that row times d loss / d lp.
+// and every loss is a function of the rows' lp, so its gradient is that row times d loss / d lp.  Where p_t is near 1, as
+// in a state that allows one token, s and p_t do not tell how near: the sums leave the token's own term out, o = the sum of
+// the others relative to it gives ln s = ln(1 + o), and 1 - p_t is worked out by itself.
 // All sums are held in binary32 (those over the rows of a sequence, and over all rows, in binary64),
 // and a gradient is rounded once, to the type of the logits.
 //
@@ -70,6 +72,22 @@ __device__ __forceinline__ uint4 pack(const float (&g)[Elem<DTYPE>::kGroup])
 }
 
 template <int DTYPE> constexpr uint32_t kNegInf = DTYPE == TDFA_F32 ? 0xFF800000u : 0xFF80FF80u;
+
+// Element j of a group.
+template <int DTYPE>
+__device__ __forceinline__ float element_of(uint4 x, int32_t j)
+{
+    if constexpr (DTYPE == TDFA_F32) {
+        return __uint_as_float(j == 0 ? x.x : j == 1 ? x.y : j == 2 ? x.z : x.w);
+    } else {
+        const uint32_t w = j < 2 ? x.x : j < 4 ? x.y : j < 6 ? x.z : x.w;
+        return __uint_as_float(j & 1 ? w & 0xFFFF0000u : w << 16);
+    }
+}
+__device__ __forceinline__ uint4 where(uint4 mask, uint32_t y, uint4 x)         // y under the mask, x elsewhere
+{
+    return make_uint4((y & mask.x) | (x.x & ~mask.x), (y & mask.y) | (x.y & ~mask.y), (y & mask.z) | (x.z & ~mask.z), (y & mask.w) | (x.w & ~mask.w));
+}
 
 // What the kernels are handed.  A launch whose arguments take at most 112 bytes, and whose kernel asks for nothing else (the size of its
 // grid, say), costs the host 2.6 us, a larger one 3.3; so strides are in units of 16 bytes, rows are numbered by the workgroups of a grid
@@ -263,6 +281,30 @@ __device__ __forceinline__ void fetch(const RowBuffers& row, int32_t g0, int32_t
     fetch_groups<DTYPE, NT, U, BITS, ONCE>(row, g0, n_groups, x, b);
 }
 
+// Where a row's token lies among the groups g0 + n + k NT that thread n takes: in the k-th of one thread, whose mask has its element's bits
+// (the others' is empty); k = -1: in none of them.
+struct Own {
+    int32_t k, j;              // element j of the group
+    bool mine;
+    uint4 mask;
+};
+template <int DTYPE, int NT, int U>
+__device__ __forceinline__ Own own_of(int32_t token, int32_t g0)
+{
+    constexpr int G = Elem<DTYPE>::kGroup;
+    const int32_t at = token / G - g0, j = token & (G - 1), word = DTYPE == TDFA_F32 ? j : j >> 1;
+    const bool mine = (int32_t)threadIdx.x == (at & (NT - 1));
+    const uint32_t m = !mine ? 0u : DTYPE == TDFA_F32 ? 0xFFFFFFFFu : j & 1 ? 0xFFFF0000u : 0xFFFFu;
+    return {(uint32_t)at < (uint32_t)(NT * U) ? at / NT : -1, j, mine, make_uint4(word == 0 ? m : 0, word == 1 ? m : 0, word == 2 ? m : 0, word == 3 ? m : 0)};
+}
+// Takes the token's own element out of the group, as if it were not allowed.
+template <int DTYPE, bool BITS>
+__device__ __forceinline__ void leave_own(const Own& own, uint4& x, uint32_t& b)
+{
+    if constexpr (BITS) b &= ~((own.mine ? 1u : 0u) << own.j);
+    else x = where(own.mask, kNegInf<DTYPE>, x);
+}
+
 // Puts -inf where a token of group g is not allowed or the row is at its end.  False: so it is in the whole wavefront.
 template <int DTYPE, bool BITS>
 __device__ __forceinline__ bool settle(uint4& x, uint32_t b, int32_t g, int32_t n_groups, const uint2 (&masks)[16])
@@ -310,14 +352,16 @@ __device__ __forceinline__ float max_group(uint4 x, float m)
     return m;
 }
 
-// Over fetched groups.  Bit k of `some`: the wavefront has an allowed token in its k-th groups.
+// Over fetched groups, but for the token's own element.  Bit k of `some`: the wavefront has another allowed token in its k-th groups.
 template <int DTYPE, int NT, int U, bool BITS>
-__device__ __forceinline__ void add_groups(uint4 (&x)[U], const uint32_t (&b)[U], int32_t g0, int32_t n_groups, const uint2 (&masks)[16], float c2, float nb,
-                                           float (&s)[2], uint32_t& some)
+__device__ __forceinline__ void add_groups(uint4 (&x)[U], uint32_t (&b)[U], int32_t g0, int32_t n_groups, const uint2 (&masks)[16], int32_t token, float c2,
+                                           float nb, float (&s)[2], uint32_t& some)
 {
+    const Own own = own_of<DTYPE, NT, U>(token, g0);
     some = 0;
 #pragma unroll
     for (int k = 0; k < U; ++k) {
+        if (k == own.k) leave_own<DTYPE, BITS>(own, x[k], b[k]);
         if (!settle<DTYPE, BITS>(x[k], b[k], g0 + (int32_t)threadIdx.x + k * NT, n_groups, masks)) continue;
         some |= 1u << k;
         add_group<DTYPE>(x[k], c2, nb, s);
@@ -325,12 +369,12 @@ __device__ __forceinline__ void add_groups(uint4 (&x)[U], const uint32_t (&b)[U]
     }
 }
 
-// The element behind the last whole group that belongs to this thread, -inf if there is none.
+// The element behind the last whole group that belongs to this thread, -inf if there is none or it is token `without`.
 template <int DTYPE>
-__device__ __forceinline__ float last_element(int32_t n_tokens, const typename Elem<DTYPE>::type* row, const uint32_t* bits)
+__device__ __forceinline__ float last_element(int32_t n_tokens, const typename Elem<DTYPE>::type* row, const uint32_t* bits, int32_t without)
 {
     const int32_t t = n_tokens / Elem<DTYPE>::kGroup * Elem<DTYPE>::kGroup + (int32_t)threadIdx.x;
-    return t < n_tokens && allowed(bits, t) ? to_f32(row[t]) : -INFINITY;
+    return t < n_tokens && t != without && allowed(bits, t) ? to_f32(row[t]) : -INFINITY;
 }
 
 // Over the 64 lanes of a wavefront, all of them active, by data-parallel primitives (no LDS); the result is uniform.
@@ -372,51 +416,55 @@ __device__ __forceinline__ float block_reduce(float v, float (&part)[NT / 64])
     return v;
 }
 
-// A sum of exponentials relative to `ref` that has neither overflowed nor met a NaN, and has the token's own term in it.
-__device__ __forceinline__ bool usable(float s) { return s >= 0.5f && s < 3.0e38f; }
+// Whether a row's own term and the sum of the others, both relative to about its own logit, are what they should be: not so where the
+// exponents overflowed or a NaN was met.
+__device__ __forceinline__ bool usable(float own, float others) { return own >= 0.25f && own <= 4.0f && others < 3.0e38f; }
 
-// ln s in binary64 from the logarithm of the significand in binary32: off by 2^-25 or so whatever s is, where the rounding of
-// a binary32 logarithm of 10 would be 2^-21.
-__device__ __forceinline__ double ln_of(float s)
+// ln(own + others) in binary64.  The sum is a significand between sqrt(1/2) and sqrt(2) and an exponent, so that the binary32 logarithm
+// is off by 2^-25 or so whatever the sum is (the rounding of a binary32 logarithm of 10 would be 2^-21) and keeps its bits where the sum
+// is near 1; what its rounding has lost, all of `others` where they are small beside an own term of 1, is added to first order.
+__device__ __forceinline__ double ln_total(float own, float others)
 {
-    int e;
-    const float m = frexpf(s, &e);
-    return (double)e * 0.69314718055994530942 + (double)logf(m);
+    const float s = own + others, t = s - own, lost = (own - (s - t)) + (others - t);
+    int e = __builtin_amdgcn_frexp_expf(s);
+    float m = __builtin_amdgcn_frexp_mantf(s);
+    if (m < 0.70710678f) {
+        m += m;
+        e -= 1;
+    }
+    return 0.69314718055994530942 * ((double)e + (double)__builtin_amdgcn_logf(m)) + (double)(lost * __builtin_amdgcn_rcpf(s));
 }
 
-// What a row's sum gives: p_j = exp((z_j - ref) c - ls), ls >= 0, and lp.
+// What a row's sum gives: p_j = exp((z_j - ref) c - ls), ls >= 0, 1 - p_t, and lp.
 struct Scored {
-    float ref, ls;
+    float ref, ls, rest;
     double lp;
 };
-// The statistics of a row as they are handed on: {ref, ls}, {ref, -ls} of a row that was summed with care and may hold NaN,
-// {0, +inf} of a row that takes no part.
+__device__ __forceinline__ float rest_of(float own, float others) { return others * __builtin_amdgcn_rcpf(own + others); }
+// The statistics of a row as they are handed on: {ref, ls}, {ref, -ls} of a row that was summed with care and may hold NaN or have a
+// reference other than its token's logit, {0, +inf} of a row that takes no part.
 __device__ __forceinline__ float2 stats_of_row(Scored q, bool careful)
 {
     return (float)q.lp == -INFINITY ? make_float2(0.0f, INFINITY) : make_float2(q.ref, careful ? -q.ls : q.ls);
 }
-// From a usable sum relative to the row's own token z.
-__device__ __forceinline__ Scored score(float z, float c2, float nb, float s)
+// The row's own term, 2^(z c2 + nb) with the rounding of nb in it as in all others.
+__device__ __forceinline__ float own_term(float z, float c2, float nb) { return __builtin_amdgcn_exp2f(fmaf(z, c2, nb)); }
+// From the row's own term and the sum of the others, both relative to `ref` (which is NaN where an allowed logit is +inf).
+__device__ __forceinline__ Scored score(float z, float ref, float own, float others, float inv_t)
 {
-    const double lp = fmin((double)fmaf(z, c2, nb) * 0.69314718055994530942 - ln_of(s), 0.0);
-    return {z, fabsf((float)lp), lp};
-}
-// From careful_sum (whose sum is NaN where an allowed logit is +inf).
-__device__ __forceinline__ Scored score_careful(float z, float ref, float inv_t, float s)
-{
-    const double ls = ln_of(s), lp = (double)(z - ref) * (double)inv_t - ls;
-    return {ref, fabsf((float)ls), lp > 0.0 ? 0.0 : lp};
+    const double ls = ln_total(own, others), lp = (double)(z - ref) * (double)inv_t - ls;
+    return {ref, fabsf((float)ls), rest_of(own, others), lp > 0.0 ? 0.0 : lp};
 }
 
-// Sum of the exponentials of a row relative to its largest logit, NaN passed over: what a row takes whose sum relative to its own
-// token is not usable.  Sets *ref to that logit.
+// Sum of the exponentials of a row relative to its largest logit, NaN passed over and the token's own left out: what a row takes whose
+// sum relative to its own token's logit z is not usable.  Sets *ref to the largest logit.
 template <int DTYPE, int NT, int U, bool BITS>
-__device__ __forceinline__ float careful_sum(const RowBuffers& row, int32_t n_groups, float last, float c2, float* ref, const uint2 (&masks)[16],
-                                             float (&part)[NT / 64])
+__device__ __forceinline__ float careful_sum(const RowBuffers& row, int32_t n_groups, int32_t token, float z, float last, float c2, float* ref,
+                                             const uint2 (&masks)[16], float (&part)[NT / 64])
 {
     uint4 x[U];
     uint32_t b[U];
-    float m = fmaxf(kLowest, last);
+    float m = fmaxf(fmaxf(kLowest, z), last);
     for (int32_t g = 0; g < n_groups; g += NT * U) {
         fetch<DTYPE, NT, U, BITS>(row, g, n_groups, x, b);
 #pragma unroll
@@ -427,9 +475,12 @@ __device__ __forceinline__ float careful_sum(const RowBuffers& row, int32_t n_gr
     float s = __builtin_amdgcn_exp2f((fmaxf(last, -INFINITY) - m) * c2);
     for (int32_t g = 0; g < n_groups; g += NT * U) {
         fetch<DTYPE, NT, U, BITS>(row, g, n_groups, x, b);
+        const Own own = own_of<DTYPE, NT, U>(token, g);
 #pragma unroll
-        for (int k = 0; k < U; ++k)
+        for (int k = 0; k < U; ++k) {
+            if (k == own.k) leave_own<DTYPE, BITS>(own, x[k], b[k]);
             if (settle<DTYPE, BITS>(x[k], b[k], g + (int32_t)threadIdx.x + k * NT, n_groups, masks)) add_group_careful<DTYPE>(x[k], c2, m, s);
+        }
     }
     *ref = m;
     return block_reduce<NT, false>(s, part);
@@ -499,7 +550,7 @@ __device__ __forceinline__ void finish(const PolicyScoreArgs& a, uint32_t i, Sco
 }
 
 // One workgroup per row.  The sum is taken relative to the row's own token, ref = z_t, so that no maximum has to be known, terms are added
-// as they arrive, and lp = -ln s; where that overflows (lp below -87) or a NaN is met, the row is read again, for the largest logit and
+// as they arrive, and lp = -ln(1 + the sum of the others); where that overflows (lp below -87) or a NaN is met, the row is read again, for the largest logit and
 // the sum relative to it.  Bound by the memory where there are many rows: 2,900 rows of 128,256 tokens in bf16 77 us, of which 0.53
 // of the 128-byte lines hold an allowed token (394 MB, 5.1 TB/s; torch's maximum over the rows of a matrix reads 4.9 to 5.2); by one
 // compute unit's stream of a long row where there are few (256 KB in 7.5 us, about 40 GB/s whatever is in flight); by the chain token,
@@ -527,7 +578,7 @@ __global__ void __launch_bounds__(NT, 8) token_stats_kernel(A a)
     const RowBuffers buf = row_buffers<DTYPE>(row, r.bits, n_groups);
     uint32_t b[U];
     fetch_bits<DTYPE, NT, U, BITS>(buf, 0, b);
-    const float z = token_logit(r, row), last = last_element<DTYPE>(a.n_tokens, row, r.bits);
+    const float z = token_logit(r, row), last = last_element<DTYPE>(a.n_tokens, row, r.bits, r.token);
     if (z == -INFINITY) {
         if (threadIdx.x == 0) leave_out(a, i, r.lp);
         return;
@@ -539,15 +590,21 @@ __global__ void __launch_bounds__(NT, 8) token_stats_kernel(A a)
         uint32_t some;
         if (g) fetch_bits<DTYPE, NT, U, BITS>(buf, g, b);
         fetch_groups<DTYPE, NT, U, BITS>(buf, g, n_groups, x, b);
-        add_groups<DTYPE, NT, U, BITS>(x, b, g, n_groups, s_masks, c2, nb, sum, some);
+        add_groups<DTYPE, NT, U, BITS>(x, b, g, n_groups, s_masks, r.token, c2, nb, sum, some);
     }
-    float s = block_reduce<NT, false>(sum[0] + sum[1], s_part);
-    const bool careful = !usable(s);
-    if (careful) s = careful_sum<DTYPE, NT, 2, BITS>(buf, n_groups, last, c2, &ref, s_masks, s_part);
-    if (threadIdx.x == 0) finish(a, i, careful ? score_careful(z, ref, a.inv_t, s) : score(z, c2, nb, s), careful, v);
+    float own = own_term(z, c2, nb), s = block_reduce<NT, false>(sum[0] + sum[1], s_part);
+    const bool careful = !usable(own, s);
+    if (careful) {
+        s = careful_sum<DTYPE, NT, 2, BITS>(buf, n_groups, r.token, z, last, c2, &ref, s_masks, s_part);
+        own = __builtin_amdgcn_exp2f((z - ref) * c2);
+    } else {
+        s *= __builtin_amdgcn_rcpf(own);
+        own = 1.0f;
+    }
+    if (threadIdx.x == 0) finish(a, i, score(z, ref, own, s, a.inv_t), careful, v);
 }
 
-// The largest logit and the sum relative to it of a part of a row; {kLowest, 0}: of none.
+// The largest logit and the sum relative to it of a part of a row without the token's own; {kLowest, 0}: of none.
 struct Part {
     float m, s;
 };
@@ -574,15 +631,17 @@ __global__ void __launch_bounds__(NT) part_stats_kernel(RowArgs a, const float* 
     const int32_t end = min(n_groups, (part + 1) * span);
     const RowBuffers buf = row_buffers<DTYPE>(row, r.bits, end);
     // fmaxf with a number passes over a NaN
-    const float last = part == parts - 1 ? fmaxf(last_element<DTYPE>(a.n_tokens, row, r.bits), -INFINITY) : -INFINITY;
+    const float last = part == parts - 1 ? fmaxf(last_element<DTYPE>(a.n_tokens, row, r.bits, r.token), -INFINITY) : -INFINITY;
     float m = fmaxf(kLowest, last), s = __builtin_amdgcn_exp2f((last - m) * c2);
     for (int32_t g = part * span; g < end; g += NT * U) {
         uint4 x[U];
         uint32_t b[U], some = 0;
         fetch<DTYPE, NT, U, BITS>(buf, g, end, x, b);
+        const Own own = own_of<DTYPE, NT, U>(r.token, g);
         float top = m;
 #pragma unroll
         for (int k = 0; k < U; ++k) {
+            if (k == own.k) leave_own<DTYPE, BITS>(own, x[k], b[k]);
             if (!settle<DTYPE, BITS>(x[k], b[k], g + (int32_t)threadIdx.x + k * NT, end, s_masks)) continue;
             some |= 1u << k;
             top = max_group<DTYPE>(x[k], top);
@@ -618,15 +677,21 @@ __global__ void __launch_bounds__(kThreads) join_parts_kernel(A a, const Part* i
     }
     const float c2 = a.inv_t * kLog2e;
     const Part mine = lane < parts ? in[(int64_t)i * parts + lane] : Part{kLowest, 0.0f};
-    const float top = wave_max(mine.m), s = wave_sum(mine.s * __builtin_amdgcn_exp2f((mine.m - top) * c2));
-    if (lane == 0) finish(a, i, score_careful(z, top, a.inv_t, s), true, v);
+    const float top = fmaxf(wave_max(mine.m), z), s = wave_sum(mine.s * __builtin_amdgcn_exp2f((mine.m - top) * c2));
+    if (lane == 0) finish(a, i, score(z, top, __builtin_amdgcn_exp2f((z - top) * c2), s, a.inv_t), true, v);
 }
 
-// What a row's gradient is made of: g_j = -d p_j, and d more at the token.
+// What a row's gradient is made of: g_j = -d p_j, but d (1 - p_t) at the token.
 struct Slope {
     float d, ref, k2;          // p_j = 2^((z_j - ref) c2 + k2)
     float fold;                // 16-bit gradients: |d| p_j = 2^(z_j c2 + fold), or NaN: not to be taken
 };
+// 1 - exp(lp), by its series (off by 2^-26 of itself) where it is small.
+__device__ __forceinline__ float rest_from(float lp)
+{
+    const float near = fmaf(lp, fmaf(lp, fmaf(lp, fmaf(lp, fmaf(lp, fmaf(lp, 1.0f / 5040.0f, 1.0f / 720.0f), 1.0f / 120.0f), 1.0f / 24.0f), 1.0f / 6.0f), 0.5f), 1.0f);
+    return lp > -0.35f ? -lp * near : 1.0f - __builtin_amdgcn_exp2f(lp * kLog2e);
+}
 // fold takes one rounding of a number of the size of ref c2 instead of a subtraction and a product per element.  Up to 2^10 it is
 // off by 2^-15 of p, which nothing that is rounded to 8 bits behind it shows; careful rows (a NaN among the logits) do without.
 template <int DTYPE>
@@ -640,9 +705,9 @@ __device__ __forceinline__ Slope slope_of(float d, float ref, float ls, float c2
 __device__ __forceinline__ float shared_by_wave(float x) { return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(x))); }
 __device__ __forceinline__ Slope shared_by_wave(Slope q) { return {shared_by_wave(q.d), shared_by_wave(q.ref), shared_by_wave(q.k2), shared_by_wave(q.fold)}; }
 
-// Gradient of one group; own: the token is in it.
+// Gradient of one group, the token's own element among the others.
 template <int DTYPE>
-__device__ __forceinline__ uint4 gradient_of(uint4 x, bool some, Slope q, float c2, bool folds, uint32_t sign, bool own, int32_t token)
+__device__ __forceinline__ uint4 gradient_of(uint4 x, bool some, Slope q, float c2, bool folds, uint32_t sign)
 {
     constexpr int G = Elem<DTYPE>::kGroup;
     if (!some) return make_uint4(0, 0, 0, 0);
@@ -651,10 +716,6 @@ __device__ __forceinline__ uint4 gradient_of(uint4 x, bool some, Slope q, float 
     if (folds) {
 #pragma unroll
         for (int j = 0; j < G; ++j) z[j] = __builtin_amdgcn_exp2f(fmaf(z[j], c2, q.fold));
-        if (own) {
-#pragma unroll
-            for (int j = 0; j < G; ++j) z[j] -= j == token % G ? fabsf(q.d) : 0.0f;
-        }
         const uint4 y = pack<DTYPE>(z);
         return make_uint4(y.x ^ sign, y.y ^ sign, y.z ^ sign, y.w ^ sign);
     }
@@ -662,10 +723,6 @@ __device__ __forceinline__ uint4 gradient_of(uint4 x, bool some, Slope q, float 
     for (int j = 0; j < G; ++j) {
         const float e = __builtin_amdgcn_exp2f(fmaf(z[j] - q.ref, c2, q.k2));
         z[j] = z[j] == z[j] ? -q.d * e : 0.0f;
-    }
-    if (own) {
-#pragma unroll
-        for (int j = 0; j < G; ++j) z[j] += j == token % G ? q.d : 0.0f;
     }
     return pack<DTYPE>(z);
 }
@@ -675,23 +732,23 @@ template <int DTYPE>
 struct Writer {
     Slope q;
     float c2;
-    int32_t token;
     bool folds;
     uint32_t sign;
-    __device__ __forceinline__ Writer(Slope q, float c2, int32_t token)
-        : q(q), c2(c2), token(token), folds(DTYPE == TDFA_BF16 && q.fold == q.fold), sign(q.d > 0.0f ? 0x80008000u : 0u) {}
-    // some: the wavefront has an allowed token in its groups
-    __device__ __forceinline__ void write(__amdgpu_buffer_rsrc_t out, int32_t g, uint4 x, bool some) const
+    __device__ __forceinline__ Writer(Slope q, float c2)
+        : q(q), c2(c2), folds(DTYPE == TDFA_BF16 && q.fold == q.fold), sign(q.d > 0.0f ? 0x80008000u : 0u) {}
+    // some: the wavefront has an allowed token in its groups; here: the token's own is in one of them, and its gradient is y.
+    __device__ __forceinline__ void write(__amdgpu_buffer_rsrc_t out, int32_t g, uint4 x, bool some, bool here, uint4 mask, float y) const
     {
-        set_group(out, g, gradient_of<DTYPE>(x, some, q, c2, folds, sign, g == token / Elem<DTYPE>::kGroup, token));
+        x = gradient_of<DTYPE>(x, some, q, c2, folds, sign);
+        if (here) x = where(mask, DTYPE == TDFA_F32 ? __float_as_uint(y) : rounded_pair(y, y), x);
+        set_group(out, g, x);
         next_group();
     }
 };
 // The same for an element behind the last whole group.
-__device__ __forceinline__ float last_gradient(float z, Slope q, float c2, bool own)
+__device__ __forceinline__ float last_gradient(float z, Slope q, float c2)
 {
-    const float g = z == z ? -q.d * __builtin_amdgcn_exp2f(fmaf(z - q.ref, c2, q.k2)) : 0.0f;
-    return own ? g + q.d : g;
+    return z == z ? -q.d * __builtin_amdgcn_exp2f(fmaf(z - q.ref, c2, q.k2)) : 0.0f;
 }
 
 // Where the gradient of a row comes from: statistics and slopes that the caller gives; those that the launches before have left; or the pairs
@@ -1004,17 +1061,28 @@ __global__ void __launch_bounds__(NT) token_grad_kernel(A a)
         if (part == parts - 1 && behind < a.n_tokens) store_rounded(out + behind, 0.0f);
         return;
     }
-    const float last = part == parts - 1 ? last_element<DTYPE>(a.n_tokens, row, r.bits) : -INFINITY;
+    const float last = part == parts - 1 ? last_element<DTYPE>(a.n_tokens, row, r.bits, -1) : -INFINITY;
     uint4 x[U];
     uint32_t b[U];
     fetch<DTYPE, NT, U, BITS, true>(row_buffers<DTYPE>(row, r.bits, n_groups), g0, n_groups, x, b);
-    const Writer<DTYPE> writer(q, c2, r.token);
+    const Writer<DTYPE> writer(q, c2);
+    const Own own = own_of<DTYPE, NT, U>(r.token, g0);
+    uint4 held = {};           // the groups with the token's own, which come last
+    bool held_some = false;
 #pragma unroll
     for (int k = 0; k < U; ++k) {
         const bool some = settle<DTYPE, BITS>(x[k], b[k], g + k * NT, n_groups, s_masks);
-        writer.write(to, g + k * NT, x[k], some);
+        if (k == own.k) {
+            held = x[k];
+            held_some = some;
+        } else {
+            writer.write(to, g + k * NT, x[k], some, false, own.mask, 0.0f);
+        }
     }
-    if (part == parts - 1 && behind < a.n_tokens) store_rounded(out + behind, last_gradient(last, q, c2, behind == r.token));
+    // lp from what the other elements are made of too: the statistics are the same whatever made them
+    const auto lp_of = [&](float z) { return fmaf(z - q.ref, a.inv_t, -fabsf(r.stats.y)); };
+    if (own.k >= 0) writer.write(to, g + own.k * NT, held, held_some, true, own.mask, q.d * rest_from(lp_of(element_of<DTYPE>(held, own.j))));
+    if (part == parts - 1 && behind < a.n_tokens) store_rounded(out + behind, behind == r.token ? q.d * rest_from(lp_of(last)) : last_gradient(last, q, c2));
 }
 
 constexpr int64_t kWholeGroups = 1024 * 16;
@@ -1034,6 +1102,7 @@ __global__ void __launch_bounds__(NT, 4) policy_row_kernel(PolicyRowArgs a)
     __shared__ float s_part[NT / 64];
     __shared__ uint2 s_masks[16];
     __shared__ Slope s_slope;
+    __shared__ float s_own;
     const uint32_t i = blockIdx.x;
     const Row r = row_of(a, a.weights, i);
     const PolicyRow v = policy_row(a, i);
@@ -1046,7 +1115,7 @@ __global__ void __launch_bounds__(NT, 4) policy_row_kernel(PolicyRowArgs a)
     const auto* row = row_at<DTYPE>(a.logits, i, a.stride16);
     const RowBuffers buf = row_buffers<DTYPE>(row, r.bits, n_groups);
     Slope q = {0.0f, 0.0f, 0.0f, 0.0f};
-    float last = -INFINITY;
+    float last = -INFINITY, own_slope = 0.0f;
     uint4 x[R];
     uint32_t some = 0;
     uint32_t b[R];
@@ -1054,17 +1123,17 @@ __global__ void __launch_bounds__(NT, 4) policy_row_kernel(PolicyRowArgs a)
     if (r.read) {                                          // the bits are on their way together with the token's logit
         fetch_bits<DTYPE, NT, R, BITS>(buf, 0, b);
         z = token_logit(r, row);
-        last = last_element<DTYPE>(a.n_tokens, row, r.bits);
+        last = last_element<DTYPE>(a.n_tokens, row, r.bits, r.token);
     }
     if (z > -INFINITY) {
         fetch_groups<DTYPE, NT, R, BITS, true>(buf, 0, n_groups, x, b);
         const float nb = -z * c2;
         float sum[2] = {__builtin_amdgcn_exp2f(fmaf(last, c2, nb)), 0.0f}, ref = z;
-        add_groups<DTYPE, NT, R, BITS>(x, b, 0, n_groups, s_masks, c2, nb, sum, some);
-        float s = block_reduce<NT, false>(sum[0] + sum[1], s_part);
-        const bool careful = !usable(s);
+        add_groups<DTYPE, NT, R, BITS>(x, b, 0, n_groups, s_masks, r.token, c2, nb, sum, some);
+        float own = own_term(z, c2, nb), s = block_reduce<NT, false>(sum[0] + sum[1], s_part);
+        const bool careful = !usable(own, s);
         if (careful) {
-            ref = fmaxf(kLowest, last);
+            ref = fmaxf(fmaxf(kLowest, z), last);
 #pragma unroll
             for (int k = 0; k < R; ++k)
                 if (some >> k & 1) ref = max_group<DTYPE>(x[k], ref);
@@ -1074,19 +1143,25 @@ __global__ void __launch_bounds__(NT, 4) policy_row_kernel(PolicyRowArgs a)
             for (int k = 0; k < R; ++k)
                 if (some >> k & 1) add_group_careful<DTYPE>(x[k], c2, ref, s);
             s = block_reduce<NT, false>(s, s_part);
+            own = __builtin_amdgcn_exp2f((z - ref) * c2);
+        } else {
+            s *= __builtin_amdgcn_rcpf(own);
+            own = 1.0f;
         }
         if (threadIdx.x < 64) {
-            const Scored sc = careful ? score_careful(z, ref, a.inv_t, s) : score(z, c2, nb, s);
+            const Scored sc = score(z, ref, own, s, a.inv_t);
             const float lp = (float)sc.lp;
             float e = 0.0f, d = 0.0f;
             if (lp != -INFINITY) policy_term(a.clip_low, a.clip_high, a.kl_coef, a.ref_logprobs, v, lp, &e, &d);
             if (threadIdx.x == 0) {
                 a.logprobs[i] = lp;
                 s_slope = slope_of<DTYPE>(d * a.inv_t, sc.ref, sc.ls, c2, careful);
+                s_own = d * a.inv_t * sc.rest;
             }
         }
         __syncthreads();
         q = shared_by_wave(s_slope);
+        own_slope = s_own;
     } else {
         // A gradient may lie over the logits: no wavefront writes before all have read the token's logit (above, the sum's barriers see to it).
         if (r.read) __syncthreads();
@@ -1102,10 +1177,11 @@ __global__ void __launch_bounds__(NT, 4) policy_row_kernel(PolicyRowArgs a)
         return;
     }
     some = __builtin_amdgcn_readfirstlane(some);
-    const Writer<DTYPE> writer(shared_by_wave(q), c2, r.token);
+    const Writer<DTYPE> writer(shared_by_wave(q), c2);
+    const Own own = own_of<DTYPE, NT, R>(r.token, 0);
 #pragma unroll
-    for (int k = 0; k < R; ++k) writer.write(to, (int32_t)threadIdx.x + k * NT, x[k], some >> k & 1);
-    if (behind < a.n_tokens) store_rounded(out + behind, last_gradient(last, q, c2, behind == r.token));
+    for (int k = 0; k < R; ++k) writer.write(to, (int32_t)threadIdx.x + k * NT, x[k], some >> k & 1, k == own.k, own.mask, own_slope);
+    if (behind < a.n_tokens) store_rounded(out + behind, behind == r.token ? own_slope : last_gradient(last, q, c2));
 }
 
 // A launch that reports its own error (asking for the last one afterwards costs the host 0.4 us more).

@@ -74,3 +74,88 @@ def test_gradient_in_place_of_rows_that_take_no_part(T, dtype, constrained, grou
     tol = 0.5 * np.where(live, R.tol_lp(lp64), 0.0).sum()
     check(x, lp, down, np.full(n, tol) + 2 * R.U * np.abs(down), "preference loss")
     _close(loss, np.array([want]), np.array([2 * tol + 2 * R.U * abs(want)]), "preference loss")
+
+
+def _all_gradients(T, c, temperature, down, old=None):
+    """[(what, lp, gradient, d loss / d lp)] of every call that writes a gradient, with a slope of `down` for every row."""
+    n, v, out = c.n, c.v, []
+    lp, stats, g = torch.full((n,), 9.0, device="cuda"), torch.full((n, 2), 9.0, device="cuda"), torch.full_like(c.x, 7.0)
+    T.token_logprobs(*c.args(), lp, temperature=temperature, stats=stats)
+    T.token_logprobs_backward(*c.args(), stats, torch.full((n,), down, device="cuda"), g[:, :v], temperature=temperature)
+    out.append(("backward", lp, g[:, :v], np.full(n, down)))
+    # the ratio is 1 where the old log-probability is lp, and nothing is clipped
+    lp2, g, loss = torch.full((n,), 9.0, device="cuda"), torch.full_like(c.x, 7.0), torch.zeros(1, device="cuda")
+    T.policy_loss(*c.args(), lp, torch.full((n,), -down, device="cuda"), loss, lp2, grad_logits=g[:, :v], temperature=temperature, clip=(1.0, math.inf))
+    out.append(("policy loss", lp2, g[:, :v], np.full(n, down)))
+    # rows against an empty sequence each, rewards of zero: every slope is -beta / (2 pairs)
+    begin = torch.from_numpy(np.repeat(np.arange(n + 1), 2)[1:].astype(np.int32)).cuda()
+    lp3, g, rewards = torch.full((n,), 9.0, device="cuda"), torch.full_like(c.x, 7.0), torch.zeros(2 * n, device="cuda")
+    T.preference_loss(*c.args(), lp, begin, loss, rewards, lp3, grad_logits=g[:, :v], temperature=temperature, beta=2.0 * n * abs(down))
+    out.append(("preference loss", lp3, g[:, :v], np.full(n, -abs(down))))
+    return out
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("constrained", [False, True])
+@pytest.mark.parametrize("n,v", [(6, 67), (6, 4099), (40, 9001), (6, 40001), (40, 70003), (6, 140003)])
+def test_own_element_of_a_likely_token(T, dtype, constrained, n, v):
+    """1 - p_t relative to itself, with p_t down to some 10^-6 below 1 and logits at which a folded exponent has few bits left; the token
+    in the first and the last group and behind it; a NaN among the logits of some rows."""
+    for logit, temperature in ((3.0, 1.0), (30.0, 1.0), (200.0, 1.0), (600.0, 1.0), (30.0, 0.1)):
+        c = Case(T, n, v, dtype, 42, constrained)
+        rng = np.random.default_rng([v, int(logit)])
+        x = c.x.float()
+        x[:, :v] = logit - temperature * (12.0 + math.log(v / 512) + 3.0 * torch.rand((n, v), device="cuda", generator=torch.Generator("cuda").manual_seed(v)))
+        allowed = [np.flatnonzero(c.on[i]) for i in range(n)]
+        for i in range(n):
+            if len(allowed[i]):
+                c.t[i] = allowed[i][[0, -1, len(allowed[i]) // 2][i % 3]] if len(allowed[i]) > 1 or i % 2 else allowed[i][0]
+                x[i, int(c.t[i])] = logit
+                other = int(rng.choice(allowed[i]))
+                if i % 4 == 3 and other != c.t[i]:
+                    x[i, other] = math.nan
+            else:
+                c.t[i] = -1
+        c.tokens = torch.from_numpy(c.t.astype(np.int32)).cuda()
+        c.x = x.to(c.x.dtype)
+        c.logits = c.x[:, :v]
+        c.z = c.logits.double().cpu().numpy()
+        _, live, logp = R.token_logprobs(c.z, c.on, c.t, temperature)
+        at = np.where(live, c.t, 0)
+        p = np.exp(np.where(np.isnan(logp), -np.inf, logp))
+        rows = np.arange(n)
+        others = p.copy()
+        others[rows, at] = 0.0
+        rest = others.sum(axis=1)
+        assert live.any() and rest[live].max() < 0.1
+        for what, lp, g, down in _all_gradients(T, c, temperature, 1 / 3):
+            scale = np.where(live, down / temperature, 0.0)
+            g = g.double().cpu().numpy()
+            # a sum of others is off by REL_SUM of itself at most; exponents of some |x| = 30 in binary32 add 3 u |x|, the inverse
+            # temperature, d and the two functions of it a few u; then the rounding to the gradient's type
+            rel = R.REL_SUM + 128 * R.U + (2.0 ** -8 if dtype == "bf16" else 2 * R.U)
+            want = scale * rest
+            off = np.abs(g[rows, at] - want)
+            assert (off[live] <= rel * np.abs(want[live])).all(), (what, logit, float((off / np.abs(want))[live].max()))
+            assert (off[live & (rest == 0)] == 0).all()
+            want = -scale[:, None] * others
+            g[rows[live], at[live]] = 0.0
+            # a folded exponent is off by some 2^-14 of p in 16 bits
+            assert (np.abs(g - want) <= (rel + 2.0 ** -13) * np.abs(want) + 1e-37).all(), (what, logit)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,v", [(5, 40), (70, 515), (70, 9000), (5, 40001), (5, 140003)])
+def test_forced_tokens_have_no_gradient(T, dtype, n, v):
+    """In a state that allows one token its log-probability and the whole gradient are zero, not a rounding of them."""
+    c = Case(T, n, v, dtype, 43)
+    only = int(torch.nonzero(c.delta[2] >= 0)[0, 0])
+    assert int((c.delta[2] >= 0).sum()) == 1
+    c.states[:] = 2
+    c.tokens[:] = only
+    for k, sigma in enumerate((1.0, 100.0)):
+        c.x[:, :v] = (c.x[:, :v].float() * sigma).to(c.x.dtype)
+        for temperature in (1.0, 0.7):
+            for what, lp, g, _ in _all_gradients(T, c, temperature, 1 / 3):
+                assert bool((lp == 0).all()), (what, lp)
+                assert bool((g == 0).all()), (what, k)
