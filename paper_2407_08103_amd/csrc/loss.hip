@@ -440,7 +440,12 @@ struct Scored {
     float ref, ls, rest;
     double lp;
 };
-__device__ __forceinline__ float rest_of(float own, float others) { return others * __builtin_amdgcn_rcpf(own + others); }
+// (A sum beyond 2^126 has no normal reciprocal; own's share of it is zero.)
+__device__ __forceinline__ float rest_of(float own, float others)
+{
+    const float r = __builtin_amdgcn_rcpf(own + others);
+    return others < own ? others * r : 1.0f - own * r;
+}
 // The statistics of a row as they are handed on: {ref, ls}, {ref, -ls} of a row that was summed with care and may hold NaN or have a
 // reference other than its token's logit, {0, +inf} of a row that takes no part.
 __device__ __forceinline__ float2 stats_of_row(Scored q, bool careful)
