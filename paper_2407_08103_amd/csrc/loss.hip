@@ -107,7 +107,7 @@ struct RowWork {
     double value;              // preference loss: lp; policy loss: the row's part of the loss
     float2 stats;
     float down;                // d loss / d lp
-    float unused;
+    float scale;               // exp(-ls)
 };
 // Log-probabilities and statistics for the caller, or for the preference loss.
 struct ScoreArgs : RowArgs {
@@ -369,6 +369,37 @@ __device__ __forceinline__ void add_groups(uint4 (&x)[U], uint32_t (&b)[U], int3
     }
 }
 
+// The same relative to the largest logit that the thread has met, m: a running maximum, and a sum that is scaled where it moves, four groups
+// at a time so that sums do not wait for all loads.  NaN is passed over.
+template <int DTYPE, int NT, int U, bool BITS>
+__device__ __forceinline__ void add_groups_running(uint4 (&x)[U], uint32_t (&b)[U], int32_t g0, int32_t n_groups, const uint2 (&masks)[16], int32_t token,
+                                                   float c2, float& m, float& s, uint32_t& some)
+{
+    static_assert(U % 4 == 0);
+    const Own own = own_of<DTYPE, NT, U>(token, g0);
+    some = 0;
+#pragma unroll
+    for (int k0 = 0; k0 < U; k0 += 4) {
+        float top = m;
+#pragma unroll
+        for (int k = k0; k < k0 + 4; ++k) {
+            if (k == own.k) leave_own<DTYPE, BITS>(own, x[k], b[k]);
+            if (!settle<DTYPE, BITS>(x[k], b[k], g0 + (int32_t)threadIdx.x + k * NT, n_groups, masks)) continue;
+            some |= 1u << k;
+            top = max_group<DTYPE>(x[k], top);
+            next_group();
+        }
+        s *= __builtin_amdgcn_exp2f((m - top) * c2);
+        m = top;
+#pragma unroll
+        for (int k = k0; k < k0 + 4; ++k) {
+            if (!(some >> k & 1)) continue;
+            add_group_careful<DTYPE>(x[k], c2, m, s);
+            next_group();
+        }
+    }
+}
+
 // The element behind the last whole group that belongs to this thread, -inf if there is none or it is token `without`.
 template <int DTYPE>
 __device__ __forceinline__ float last_element(int32_t n_tokens, const typename Elem<DTYPE>::type* row, const uint32_t* bits, int32_t without)
@@ -435,17 +466,11 @@ __device__ __forceinline__ double ln_total(float own, float others)
     return 0.69314718055994530942 * ((double)e + (double)__builtin_amdgcn_logf(m)) + (double)(lost * __builtin_amdgcn_rcpf(s));
 }
 
-// What a row's sum gives: p_j = exp((z_j - ref) c - ls), ls >= 0, 1 - p_t, and lp.
+// What a row's sum gives: p_j = exp((z_j - ref) c - ls), ls >= 0, exp(-ls), 1 - p_t, and lp.
 struct Scored {
-    float ref, ls, rest;
+    float ref, ls, scale, rest;
     double lp;
 };
-// (A sum beyond 2^126 has no normal reciprocal; own's share of it is zero.)
-__device__ __forceinline__ float rest_of(float own, float others)
-{
-    const float r = __builtin_amdgcn_rcpf(own + others);
-    return others < own ? others * r : 1.0f - own * r;
-}
 // The statistics of a row as they are handed on: {ref, ls}, {ref, -ls} of a row that was summed with care and may hold NaN or have a
 // reference other than its token's logit, {0, +inf} of a row that takes no part.
 __device__ __forceinline__ float2 stats_of_row(Scored q, bool careful)
@@ -457,8 +482,10 @@ __device__ __forceinline__ float own_term(float z, float c2, float nb) { return 
 // From the row's own term and the sum of the others, both relative to `ref` (which is NaN where an allowed logit is +inf).
 __device__ __forceinline__ Scored score(float z, float ref, float own, float others, float inv_t)
 {
-    const double ls = ln_total(own, others), lp = (double)(z - ref) * (double)inv_t - ls;
-    return {ref, fabsf((float)ls), rest_of(own, others), lp > 0.0 ? 0.0 : lp};
+    const double ls = ln_total(own, others), lp = ((double)z - (double)ref) * (double)inv_t - ls;
+    // a sum beyond 2^126 has no normal reciprocal; own's share of it is zero
+    const float scale = __builtin_amdgcn_rcpf(own + others);
+    return {ref, fabsf((float)ls), scale, others < own ? others * scale : 1.0f - own * scale, lp > 0.0 ? 0.0 : lp};
 }
 
 // Sum of the exponentials of a row relative to its largest logit, NaN passed over and the token's own left out: what a row takes whose
@@ -490,6 +517,20 @@ __device__ __forceinline__ float careful_sum(const RowBuffers& row, int32_t n_gr
     *ref = m;
     return block_reduce<NT, false>(s, part);
 }
+
+// The sum of a running one over the workgroup, relative to its largest maximum, which goes to *ref.
+template <int NT>
+__device__ __forceinline__ float sum_of_running(float m, float s, float c2, float* ref, float (&part)[NT / 64])
+{
+    *ref = block_reduce<NT, true>(m, part);
+    return block_reduce<NT, false>(s * __builtin_amdgcn_exp2f((m - *ref) * c2), part);
+}
+
+// What the sums of a row are taken relative to.  In 16 bits its own token's logit: no maximum is needed, and what the exponents lose where
+// that is far below the largest (2^-24 of the distance) the rounding of the gradients hides.  In fp32 it would show: gradients of a
+// token 10 below the largest were off by 6e-7 of themselves and 80 below by 4e-6, and are by 1e-7 whatever the token, so there a
+// running maximum is kept.
+template <int DTYPE> constexpr bool kRelativeToMax = DTYPE == TDFA_F32;
 
 struct PolicyRow {
     float old, ref, adv, w;
@@ -543,7 +584,7 @@ __device__ __forceinline__ void finish(const ScoreArgs& a, uint32_t i, Scored q,
 __device__ __forceinline__ void finish(const PairScoreArgs& a, uint32_t i, Scored q, bool careful, PolicyRow)
 {
     a.logprobs[i] = (float)q.lp;
-    a.work[i] = {q.lp, stats_of_row(q, careful), 0.0f, 0.0f};              // rows of no sequence keep a slope of zero
+    a.work[i] = {q.lp, stats_of_row(q, careful), 0.0f, q.scale};              // rows of no sequence keep a slope of zero
 }
 __device__ __forceinline__ void finish(const PolicyScoreArgs& a, uint32_t i, Scored q, bool careful, PolicyRow v)
 {
@@ -551,18 +592,19 @@ __device__ __forceinline__ void finish(const PolicyScoreArgs& a, uint32_t i, Sco
     float e = 0.0f, d = 0.0f;
     if (lp != -INFINITY) policy_term(a.clip_low, a.clip_high, a.kl_coef, a.ref_logprobs, v, lp, &e, &d);
     a.logprobs[i] = lp;
-    a.work[i] = {(double)e, stats_of_row(q, careful), d, 0.0f};
+    a.work[i] = {(double)e, stats_of_row(q, careful), d, q.scale};
 }
 
-// One workgroup per row.  The sum is taken relative to the row's own token, ref = z_t, so that no maximum has to be known, terms are added
-// as they arrive, and lp = -ln(1 + the sum of the others); where that overflows (lp below -87) or a NaN is met, the row is read again, for the largest logit and
-// the sum relative to it.  Bound by the memory where there are many rows: 2,900 rows of 128,256 tokens in bf16 77 us, of which 0.53
+// One workgroup per row.  In 16 bits the sum is taken relative to the row's own token, ref = z_t, so that no maximum has to be known, terms
+// are added as they arrive, and lp = -ln(1 + the sum of the others); where that overflows (lp below -87) or a NaN is met, the row is read
+// again, for the largest logit and the sum relative to it.  In fp32 lanes keep a running maximum.  Bound by the memory where there are many rows: 2,900 rows of 128,256 tokens in bf16 77 us, of which 0.53
 // of the 128-byte lines hold an allowed token (394 MB, 5.1 TB/s; torch's maximum over the rows of a matrix reads 4.9 to 5.2); by one
 // compute unit's stream of a long row where there are few (256 KB in 7.5 us, about 40 GB/s whatever is in flight); by the chain token,
 // bits, logits in short ones (2.5 us).
 template <typename A, int DTYPE, int NT, int U, bool BITS>
 __global__ void __launch_bounds__(NT, 8) token_stats_kernel(A a)
 {
+    constexpr bool kMax = kRelativeToMax<DTYPE>;
     __shared__ float s_part[NT / 64];
     __shared__ uint2 s_masks[16];
     const uint32_t i = blockIdx.x;
@@ -589,22 +631,31 @@ __global__ void __launch_bounds__(NT, 8) token_stats_kernel(A a)
         return;
     }
     const float nb = -z * c2;
-    float sum[2] = {__builtin_amdgcn_exp2f(fmaf(last, c2, nb)), 0.0f}, ref = z;
+    float m = fmaxf(fmaxf(kLowest, z), last), sum[2] = {__builtin_amdgcn_exp2f(kMax ? (fmaxf(last, -INFINITY) - m) * c2 : fmaf(last, c2, nb)), 0.0f};
     for (int32_t g = 0; g < n_groups; g += NT * U) {
         uint4 x[U];
         uint32_t some;
         if (g) fetch_bits<DTYPE, NT, U, BITS>(buf, g, b);
         fetch_groups<DTYPE, NT, U, BITS>(buf, g, n_groups, x, b);
-        add_groups<DTYPE, NT, U, BITS>(x, b, g, n_groups, s_masks, r.token, c2, nb, sum, some);
+        if constexpr (kMax) add_groups_running<DTYPE, NT, U, BITS>(x, b, g, n_groups, s_masks, r.token, c2, m, sum[0], some);
+        else add_groups<DTYPE, NT, U, BITS>(x, b, g, n_groups, s_masks, r.token, c2, nb, sum, some);
     }
-    float own = own_term(z, c2, nb), s = block_reduce<NT, false>(sum[0] + sum[1], s_part);
-    const bool careful = !usable(own, s);
+    float own, s, ref;
+    bool careful = true;
+    if constexpr (kMax) {
+        s = sum_of_running<NT>(m, sum[0], c2, &ref, s_part);
+    } else {
+        s = block_reduce<NT, false>(sum[0] + sum[1], s_part);
+        own = own_term(z, c2, nb);
+        careful = !usable(own, s);
+        if (careful) s = careful_sum<DTYPE, NT, 2, BITS>(buf, n_groups, r.token, z, last, c2, &ref, s_masks, s_part);
+    }
     if (careful) {
-        s = careful_sum<DTYPE, NT, 2, BITS>(buf, n_groups, r.token, z, last, c2, &ref, s_masks, s_part);
         own = __builtin_amdgcn_exp2f((z - ref) * c2);
     } else {
         s *= __builtin_amdgcn_rcpf(own);
         own = 1.0f;
+        ref = z;
     }
     if (threadIdx.x == 0) finish(a, i, score(z, ref, own, s, a.inv_t), careful, v);
 }
@@ -640,29 +691,12 @@ __global__ void __launch_bounds__(NT) part_stats_kernel(RowArgs a, const float* 
     float m = fmaxf(kLowest, last), s = __builtin_amdgcn_exp2f((last - m) * c2);
     for (int32_t g = part * span; g < end; g += NT * U) {
         uint4 x[U];
-        uint32_t b[U], some = 0;
+        uint32_t b[U], some;
         fetch<DTYPE, NT, U, BITS>(buf, g, end, x, b);
-        const Own own = own_of<DTYPE, NT, U>(r.token, g);
-        float top = m;
-#pragma unroll
-        for (int k = 0; k < U; ++k) {
-            if (k == own.k) leave_own<DTYPE, BITS>(own, x[k], b[k]);
-            if (!settle<DTYPE, BITS>(x[k], b[k], g + (int32_t)threadIdx.x + k * NT, end, s_masks)) continue;
-            some |= 1u << k;
-            top = max_group<DTYPE>(x[k], top);
-            next_group();
-        }
-        s *= __builtin_amdgcn_exp2f((m - top) * c2);
-        m = top;
-#pragma unroll
-        for (int k = 0; k < U; ++k) {
-            if (!(some >> k & 1)) continue;
-            add_group_careful<DTYPE>(x[k], c2, m, s);
-            next_group();
-        }
+        add_groups_running<DTYPE, NT, U, BITS>(x, b, g, end, s_masks, r.token, c2, m, s, some);
     }
-    const float top = block_reduce<NT, true>(m, s_part);
-    s = block_reduce<NT, false>(s * __builtin_amdgcn_exp2f((m - top) * c2), s_part);
+    float top;
+    s = sum_of_running<NT>(m, s, c2, &top, s_part);
     if (threadIdx.x == 0) out[blockIdx.x] = {top, s};
 }
 
@@ -688,8 +722,9 @@ __global__ void __launch_bounds__(kThreads) join_parts_kernel(A a, const Part* i
 
 // What a row's gradient is made of: g_j = -d p_j, but d (1 - p_t) at the token.
 struct Slope {
-    float d, ref, k2;          // p_j = 2^((z_j - ref) c2 + k2)
-    float fold;                // 16-bit gradients: |d| p_j = 2^(z_j c2 + fold), or NaN: not to be taken
+    float d, ref;
+    float k;                   // 16 bits: p_j = 2^((z_j - ref) c2 + k), fp32: -d p_j = k 2^((z_j - ref) c2), which keeps exponents of likely tokens small
+    float fold;                // 16 bits: |d| p_j = 2^(z_j c2 + fold), or NaN: not to be taken
 };
 // 1 - exp(lp), by its series (off by 2^-26 of itself) where it is small.
 __device__ __forceinline__ float rest_from(float lp)
@@ -700,16 +735,27 @@ __device__ __forceinline__ float rest_from(float lp)
 // fold takes one rounding of a number of the size of ref c2 instead of a subtraction and a product per element.  Up to 2^10 it is
 // off by 2^-15 of p, which nothing that is rounded to 8 bits behind it shows; careful rows (a NaN among the logits) do without.
 template <int DTYPE>
-__device__ __forceinline__ Slope slope_of(float d, float ref, float ls, float c2, bool careful)
+__device__ __forceinline__ Slope slope_of(float d, float ref, float ls, float scale, float c2, bool careful)
 {
-    const float k2 = -ls * kLog2e, nb = -ref * c2;
-    const bool folds = DTYPE == TDFA_BF16 && !careful && fabsf(nb) < 1024.0f;
-    return {d, ref, k2, folds ? nb + (k2 + __builtin_amdgcn_logf(fabsf(d))) : __uint_as_float(0x7FC00000u)};
+    if constexpr (DTYPE == TDFA_F32) {
+        return {d, ref, -d * scale, 0.0f};
+    } else {
+        const float k = -ls * kLog2e, nb = -ref * c2;
+        const bool folds = !careful && fabsf(nb) < 1024.0f;
+        return {d, ref, k, folds ? nb + (k + __builtin_amdgcn_logf(fabsf(d))) : __uint_as_float(0x7FC00000u)};
+    }
 }
 
 __device__ __forceinline__ float shared_by_wave(float x) { return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(x))); }
-__device__ __forceinline__ Slope shared_by_wave(Slope q) { return {shared_by_wave(q.d), shared_by_wave(q.ref), shared_by_wave(q.k2), shared_by_wave(q.fold)}; }
+__device__ __forceinline__ Slope shared_by_wave(Slope q) { return {shared_by_wave(q.d), shared_by_wave(q.ref), shared_by_wave(q.k), shared_by_wave(q.fold)}; }
 
+// Gradient of one element other than the token's own.
+template <int DTYPE>
+__device__ __forceinline__ float gradient_of(float z, Slope q, float c2)
+{
+    const float g = DTYPE == TDFA_F32 ? q.k * __builtin_amdgcn_exp2f((z - q.ref) * c2) : -q.d * __builtin_amdgcn_exp2f(fmaf(z - q.ref, c2, q.k));
+    return z == z ? g : 0.0f;
+}
 // Gradient of one group, the token's own element among the others.
 template <int DTYPE>
 __device__ __forceinline__ uint4 gradient_of(uint4 x, bool some, Slope q, float c2, bool folds, uint32_t sign)
@@ -725,10 +771,7 @@ __device__ __forceinline__ uint4 gradient_of(uint4 x, bool some, Slope q, float 
         return make_uint4(y.x ^ sign, y.y ^ sign, y.z ^ sign, y.w ^ sign);
     }
 #pragma unroll
-    for (int j = 0; j < G; ++j) {
-        const float e = __builtin_amdgcn_exp2f(fmaf(z[j] - q.ref, c2, q.k2));
-        z[j] = z[j] == z[j] ? -q.d * e : 0.0f;
-    }
+    for (int j = 0; j < G; ++j) z[j] = gradient_of<DTYPE>(z[j], q, c2);
     return pack<DTYPE>(z);
 }
 
@@ -750,12 +793,6 @@ struct Writer {
         next_group();
     }
 };
-// The same for an element behind the last whole group.
-__device__ __forceinline__ float last_gradient(float z, Slope q, float c2)
-{
-    return z == z ? -q.d * __builtin_amdgcn_exp2f(fmaf(z - q.ref, c2, q.k2)) : 0.0f;
-}
-
 // Where the gradient of a row comes from: statistics and slopes that the caller gives; those that the launches before have left; or the pairs
 // of a preference loss of few rows, whose slopes each workgroup works out.  The losses are summed by the first workgroup of the last two.
 struct GivenGradArgs : RowArgs {
@@ -979,6 +1016,7 @@ struct GradRow {
     int32_t token;
     float2 stats;
     float down;
+    float scale;               // exp(-ls), of fp32 rows
 };
 template <int NT>
 __device__ __forceinline__ GradRow grad_row(const GivenGradArgs& a, uint32_t i)
@@ -986,16 +1024,16 @@ __device__ __forceinline__ GradRow grad_row(const GivenGradArgs& a, uint32_t i)
     const float2 st = a.stats[i];
     const float down = a.down[i];
     const Row r = row_of(a, nullptr, i);
-    return {r.bits, r.token, st, r.read && st.y != INFINITY ? down : 0.0f};
+    return {r.bits, r.token, st, r.read && st.y != INFINITY ? down : 0.0f, expf(-fabsf(st.y))};
 }
 template <int NT>
 __device__ __forceinline__ GradRow grad_row(const WorkGradArgs& a, uint32_t i)
 {
     const float2 st = a.work[i].stats;
-    const float down = a.work[i].down;
+    const float down = a.work[i].down, scale = a.work[i].scale;
     const int32_t token = __builtin_amdgcn_readfirstlane(a.tokens[i]), q = a.allow ? __builtin_amdgcn_readfirstlane(a.states[i]) : 0;
-    if (st.y == INFINITY) return {nullptr, token, st, 0.0f};
-    return {a.allow ? bits_of(a.allow, q, a.n_tokens) : nullptr, token, st, down};
+    if (st.y == INFINITY) return {nullptr, token, st, 0.0f, 0.0f};
+    return {a.allow ? bits_of(a.allow, q, a.n_tokens) : nullptr, token, st, down, scale};
 }
 template <int NT>
 __device__ __forceinline__ GradRow grad_row(const FewPairsGradArgs& a, uint32_t i)
@@ -1004,9 +1042,9 @@ __device__ __forceinline__ GradRow grad_row(const FewPairsGradArgs& a, uint32_t 
     __shared__ double s_sums[2][NT / 64];
     const float2 st = a.work[i].stats;
     const int32_t token = __builtin_amdgcn_readfirstlane(a.tokens[i]), q = a.allow ? __builtin_amdgcn_readfirstlane(a.states[i]) : 0;
-    if (__builtin_amdgcn_readfirstlane(__float_as_int(st.y)) == 0x7F800000) return {nullptr, token, st, 0.0f};
-    const float down = slope_of_row<NT>(a.pairs, a.work, (int32_t)i, s_found, s_sums);
-    return {a.allow ? bits_of(a.allow, q, a.n_tokens) : nullptr, token, st, down};
+    if (__builtin_amdgcn_readfirstlane(__float_as_int(st.y)) == 0x7F800000) return {nullptr, token, st, 0.0f, 0.0f};
+    const float scale = a.work[i].scale, down = slope_of_row<NT>(a.pairs, a.work, (int32_t)i, s_found, s_sums);
+    return {a.allow ? bits_of(a.allow, q, a.n_tokens) : nullptr, token, st, down, scale};
 }
 // What the first workgroup does beside the rows; false: nothing, it takes a row like the others.
 template <int NT>
@@ -1054,7 +1092,7 @@ __global__ void __launch_bounds__(NT) token_grad_kernel(A a)
     const uint32_t w = blockIdx.x - kFirst<A>, i = w / (uint32_t)parts;
     const int32_t part = (int32_t)(w - i * (uint32_t)parts);
     const GradRow r = grad_row<NT>(a, i);
-    const Slope q = shared_by_wave(slope_of<DTYPE>(r.down * a.inv_t, r.stats.x, fabsf(r.stats.y), c2, signbit(r.stats.y)));
+    const Slope q = shared_by_wave(slope_of<DTYPE>(r.down * a.inv_t, r.stats.x, fabsf(r.stats.y), r.scale, c2, signbit(r.stats.y)));
     const auto* row = row_at<DTYPE>(a.logits, i, a.stride16);
     auto* out = row_at<DTYPE>(a.grad, i, a.grad_stride16);
     const __amdgpu_buffer_rsrc_t to = buffer_of(out, (uint32_t)n_groups * 16u);
@@ -1087,7 +1125,7 @@ __global__ void __launch_bounds__(NT) token_grad_kernel(A a)
     // lp from what the other elements are made of too: the statistics are the same whatever made them
     const auto lp_of = [&](float z) { return fmaf(z - q.ref, a.inv_t, -fabsf(r.stats.y)); };
     if (own.k >= 0) writer.write(to, g + own.k * NT, held, held_some, true, own.mask, q.d * rest_from(lp_of(element_of<DTYPE>(held, own.j))));
-    if (part == parts - 1 && behind < a.n_tokens) store_rounded(out + behind, behind == r.token ? q.d * rest_from(lp_of(last)) : last_gradient(last, q, c2));
+    if (part == parts - 1 && behind < a.n_tokens) store_rounded(out + behind, behind == r.token ? q.d * rest_from(lp_of(last)) : gradient_of<DTYPE>(last, q, c2));
 }
 
 constexpr int64_t kWholeGroups = 1024 * 16;
@@ -1132,27 +1170,36 @@ __global__ void __launch_bounds__(NT, 4) policy_row_kernel(PolicyRowArgs a)
     }
     if (z > -INFINITY) {
         fetch_groups<DTYPE, NT, R, BITS, true>(buf, 0, n_groups, x, b);
-        const float nb = -z * c2;
-        float sum[2] = {__builtin_amdgcn_exp2f(fmaf(last, c2, nb)), 0.0f}, ref = z;
-        add_groups<DTYPE, NT, R, BITS>(x, b, 0, n_groups, s_masks, r.token, c2, nb, sum, some);
-        float own = own_term(z, c2, nb), s = block_reduce<NT, false>(sum[0] + sum[1], s_part);
-        const bool careful = !usable(own, s);
-        if (careful) {
-            ref = fmaxf(fmaxf(kLowest, z), last);
-#pragma unroll
-            for (int k = 0; k < R; ++k)
-                if (some >> k & 1) ref = max_group<DTYPE>(x[k], ref);
-            ref = block_reduce<NT, true>(ref, s_part);
-            s = __builtin_amdgcn_exp2f((fmaxf(last, -INFINITY) - ref) * c2);
-#pragma unroll
-            for (int k = 0; k < R; ++k)
-                if (some >> k & 1) add_group_careful<DTYPE>(x[k], c2, ref, s);
-            s = block_reduce<NT, false>(s, s_part);
-            own = __builtin_amdgcn_exp2f((z - ref) * c2);
+        float s, ref = z, own = 1.0f;
+        bool careful = true;
+        if constexpr (kRelativeToMax<DTYPE>) {
+            float m = fmaxf(fmaxf(kLowest, z), last);
+            s = __builtin_amdgcn_exp2f((fmaxf(last, -INFINITY) - m) * c2);
+            add_groups_running<DTYPE, NT, R, BITS>(x, b, 0, n_groups, s_masks, r.token, c2, m, s, some);
+            s = sum_of_running<NT>(m, s, c2, &ref, s_part);
         } else {
+            const float nb = -z * c2;
+            float sum[2] = {__builtin_amdgcn_exp2f(fmaf(last, c2, nb)), 0.0f};
+            add_groups<DTYPE, NT, R, BITS>(x, b, 0, n_groups, s_masks, r.token, c2, nb, sum, some);
+            s = block_reduce<NT, false>(sum[0] + sum[1], s_part);
+            own = own_term(z, c2, nb);
+            careful = !usable(own, s);
             s *= __builtin_amdgcn_rcpf(own);
             own = 1.0f;
+            if (careful) {
+                ref = fmaxf(fmaxf(kLowest, z), last);
+#pragma unroll
+                for (int k = 0; k < R; ++k)
+                    if (some >> k & 1) ref = max_group<DTYPE>(x[k], ref);
+                ref = block_reduce<NT, true>(ref, s_part);
+                s = __builtin_amdgcn_exp2f((fmaxf(last, -INFINITY) - ref) * c2);
+#pragma unroll
+                for (int k = 0; k < R; ++k)
+                    if (some >> k & 1) add_group_careful<DTYPE>(x[k], c2, ref, s);
+                s = block_reduce<NT, false>(s, s_part);
+            }
         }
+        if (careful) own = __builtin_amdgcn_exp2f((z - ref) * c2);
         if (threadIdx.x < 64) {
             const Scored sc = score(z, ref, own, s, a.inv_t);
             const float lp = (float)sc.lp;
@@ -1160,7 +1207,7 @@ __global__ void __launch_bounds__(NT, 4) policy_row_kernel(PolicyRowArgs a)
             if (lp != -INFINITY) policy_term(a.clip_low, a.clip_high, a.kl_coef, a.ref_logprobs, v, lp, &e, &d);
             if (threadIdx.x == 0) {
                 a.logprobs[i] = lp;
-                s_slope = slope_of<DTYPE>(d * a.inv_t, sc.ref, sc.ls, c2, careful);
+                s_slope = slope_of<DTYPE>(d * a.inv_t, sc.ref, sc.ls, sc.scale, c2, careful);
                 s_own = d * a.inv_t * sc.rest;
             }
         }
@@ -1186,7 +1233,7 @@ __global__ void __launch_bounds__(NT, 4) policy_row_kernel(PolicyRowArgs a)
     const Own own = own_of<DTYPE, NT, R>(r.token, 0);
 #pragma unroll
     for (int k = 0; k < R; ++k) writer.write(to, (int32_t)threadIdx.x + k * NT, x[k], some >> k & 1, k == own.k, own.mask, own_slope);
-    if (behind < a.n_tokens) store_rounded(out + behind, behind == r.token ? own_slope : last_gradient(last, q, c2));
+    if (behind < a.n_tokens) store_rounded(out + behind, behind == r.token ? own_slope : gradient_of<DTYPE>(last, q, c2));
 }
 
 // A launch that reports its own error (asking for the last one afterwards costs the host 0.4 us more).

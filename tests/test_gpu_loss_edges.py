@@ -159,3 +159,40 @@ def test_forced_tokens_have_no_gradient(T, dtype, n, v):
             for what, lp, g, _ in _all_gradients(T, c, temperature, 1 / 3):
                 assert bool((lp == 0).all()), (what, lp)
                 assert bool((g == 0).all()), (what, k)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,v", [(200, 515), (200, 5000), (20, 32003), (200, 32003), (100, 70003), (400, 70003)])
+def test_unlikely_tokens(T, dtype, n, v):
+    """Tokens up to 80 below the largest logit: neither log-probabilities nor the gradients of the likely tokens lose bits by it."""
+    for far in (0, 10, 25, 80):
+        c = Case(T, n, v, dtype, 44, constrained=False)
+        c.t = np.arange(n) * 7 % v
+        c.tokens = torch.from_numpy(c.t.astype(np.int32)).cuda()
+        at = c.tokens.long()[:, None]
+        x = c.logits.float()
+        c.logits.scatter_(1, at, (x.amax(1, keepdim=True) - far).to(c.x.dtype))
+        logp = torch.log_softmax(c.logits.double(), dim=1)
+        lp64 = logp.gather(1, at)[:, 0]
+        top = c.logits.double().amax(1)
+        ls = torch.logsumexp(c.logits.double(), 1) - top
+        likely = logp.scatter(1, at, -math.inf).topk(20, dim=1).indices
+        below = float((top[:, None] - c.logits.double().gather(1, likely)).max())
+        drawn = None
+        for what, lp, g, down in _all_gradients(T, c, 1.0, 0.5 / n):
+            down = torch.from_numpy(down).cuda()
+            if what == "preference loss":        # beta is 1, and the reference the first call's lp as it was rounded to binary32
+                down = -1.0 / n / (1.0 + torch.exp(lp64 - drawn.double()))
+            drawn = lp if drawn is None else drawn
+            # lp is rounded once to binary32; the logarithm, and sums whose roundings have no common sign, add some u.  In 16 bits the
+            # exponents are relative to the token and off by u of their size, up to |lp|, as well
+            bound = R.U * (lp64.abs() * (1 if dtype == "f32" else 3) + 8)
+            off = (lp.double() - lp64).abs()
+            assert bool((off <= bound).all()), (what, far, float((off / bound).max()))
+            if dtype == "f32":
+                # ln s is rounded to binary32, the exponents are off by 2 u of their size, the functions and products by a few u; the
+                # slope of a preference loss follows the 8 u of lp with at most half of them and has an exponential of its own
+                bound = R.U * (float(ls.max()) + 2 * below + 8 + (8 if what == "preference loss" else 0))
+                off = (g.double().gather(1, likely) / (-down[:, None] * logp.exp().gather(1, likely)) - 1).abs()
+                assert bool((off <= bound).all()), (what, far, float((off / bound).max()))
+                assert float(off.square().mean().sqrt()) <= bound / 2, (what, far, float(off.square().mean().sqrt()) / R.U)
