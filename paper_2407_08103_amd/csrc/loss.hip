@@ -846,11 +846,12 @@ __device__ __forceinline__ void add_pair(const PairArgsOnCard& p, const RowWork*
         }
     }
 }
-// softplus(x) = max(x, 0) + log1p(exp(-|x|)); binary32 from the difference of the rewards on.
+// softplus(x) = max(x, 0) + log1p(exp(-|x|)); binary32 from the difference of the rewards on.  A gap may be infinite (a reference that gives
+// a token probability zero), which a side of weight zero has nothing of.
 __device__ __forceinline__ float pair_loss(const PairArgsOnCard& p, float gap)
 {
-    const float tail = log1pf(expf(-fabsf(gap)));
-    return (1.0f - p.smoothing) * (fmaxf(-gap, 0.0f) + tail) + p.smoothing * (fmaxf(gap, 0.0f) + tail);
+    const float weight = gap > 0.0f ? p.smoothing : 1.0f - p.smoothing;
+    return log1pf(expf(-fabsf(gap))) + (weight == 0.0f ? 0.0f : weight * fabsf(gap));
 }
 // d loss / d lp of a row of the pair's first sequence.
 __device__ __forceinline__ float pair_slope(const PairArgsOnCard& p, float gap)

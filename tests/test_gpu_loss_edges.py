@@ -196,3 +196,42 @@ def test_unlikely_tokens(T, dtype, n, v):
                 off = (g.double().gather(1, likely) / (-down[:, None] * logp.exp().gather(1, likely)) - 1).abs()
                 assert bool((off <= bound).all()), (what, far, float((off / bound).max()))
                 assert float(off.square().mean().sqrt()) <= bound / 2, (what, far, float(off.square().mean().sqrt()) / R.U)
+
+
+@pytest.mark.parametrize("pairs", [4, 70])
+@pytest.mark.parametrize("grad", [False, True])
+@pytest.mark.parametrize("smoothing", [0.0, 0.1, 1.0])
+def test_infinite_gaps(T, pairs, grad, smoothing):
+    """A reference that gives a token probability zero has -inf there: the pair's gap is infinite, its loss the limit (0 on the side of
+    weight zero), its slopes finite, and the other pairs' are what they are by themselves; rewards of inf - inf stay NaN."""
+    n, v = 2 * pairs, 64
+    c = Case(T, n, v, "f32", 45, constrained=False)
+    c.t = np.arange(n) % v
+    c.tokens = torch.from_numpy(c.t.astype(np.int32)).cuda()
+    lp64, live, logp = R.token_logprobs(c.z, c.on, c.t, 1.0)
+    begin = torch.arange(n + 1, dtype=torch.int32, device="cuda")
+    for at, both in (([0], False), ([3], False), ([0, 3], False), ([4, 5], True)):
+        ref = lp64 + c.rng.normal(0, 0.3, size=n)
+        ref = ref.astype(np.float32)
+        ref[at] = -math.inf
+        loss, rewards, lp = torch.full((1,), 9.0, device="cuda"), torch.full((n,), 9.0, device="cuda"), torch.full((n,), 9.0, device="cuda")
+        g = torch.full_like(c.x, 7.0)
+        T.preference_loss(None, c.logits, None, c.tokens, c.f32(ref), begin, loss, rewards, lp, grad_logits=g[:, :v] if grad else None, beta=0.5,
+                          smoothing=smoothing)
+        reward = 0.5 * (lp64 - ref.astype(np.float64))
+        assert np.array_equal(np.isinf(rewards.cpu().numpy()), np.isinf(reward))
+        with np.errstate(invalid="ignore"):
+            gap = reward[0::2] - reward[1::2]
+        if both:
+            assert math.isnan(float(loss))
+            continue
+        each = sum((w * np.logaddexp(0.0, s * gap) for w, s in ((1.0 - smoothing, -1.0), (smoothing, 1.0)) if w), np.zeros(pairs))
+        want = float(each.mean())
+        tol = 0.0 if math.isinf(want) else float(R.tol_lp(lp64).max()) + 4 * R.U * abs(want)
+        _close(loss, np.array([want]), np.array([tol]), "loss")
+        if grad:
+            with np.errstate(over="ignore"):
+                slope = (smoothing / (1.0 + np.exp(-gap)) - (1.0 - smoothing) / (1.0 + np.exp(gap))) * 0.5 / pairs
+            down = np.stack([slope, -slope], 1).reshape(-1)
+            want = R.gradient(logp, c.t, live, down, 1.0)
+            _close(g[:, :v], want, R.tol_gradient(want, logp, c.t, live, down, np.abs(down) * 8 * R.U + 0.5 / pairs * R.tol_lp(lp64), 1.0, False), "gradient")
