@@ -469,7 +469,8 @@ TDFA_API int tdfa_token_logprobs(const tdfa_table *table, const void *logits_dev
  *   grad_logprobs_dev : device, float [rows].
  *   grad_dev          : device, [rows][grad_stride] of the type of the logits, rows 16-byte aligned, the first
  *                       n_tokens of every row are written.  May be logits_dev (with grad_stride = row_stride); the
- *                       two must not overlap otherwise. */
+ *                       two must not overlap otherwise, and rows of one may lie between those of the other only where
+ *                       both strides are the same. */
 TDFA_API int tdfa_token_logprobs_backward(const tdfa_table *table, const void *logits_dev, int dtype, int32_t rows,
                         int32_t n_tokens, int64_t row_stride, const int32_t *states_dev, const int32_t *tokens_dev,
                         float temperature, const float *stats_dev, const float *grad_logprobs_dev,

@@ -1787,12 +1787,17 @@ int tdfa_sample_noise(int32_t batch, int32_t n_tokens, uint64_t seed, uint64_t o
 
 namespace {
 
-// Whether the bytes of two sets of rows may meet.
+// Whether two sets of rows have a byte in common; with different strides, whether the ranges that they lie in do.
 bool rows_meet(const void* x, int64_t x_stride, const void* y, int64_t y_stride, int64_t rows, int64_t n_tokens, int64_t esz)
 {
     const uintptr_t x0 = reinterpret_cast<uintptr_t>(x), y0 = reinterpret_cast<uintptr_t>(y);
-    const uintptr_t xb = (uintptr_t)(((rows - 1) * x_stride + n_tokens) * esz), yb = (uintptr_t)(((rows - 1) * y_stride + n_tokens) * esz);
-    return x0 < y0 + yb && y0 < x0 + xb;
+    if (x_stride != y_stride) {
+        const uintptr_t xb = (uintptr_t)(((rows - 1) * x_stride + n_tokens) * esz), yb = (uintptr_t)(((rows - 1) * y_stride + n_tokens) * esz);
+        return x0 < y0 + yb && y0 < x0 + xb;
+    }
+    // the rows of one lie between two of the other: y's row j + k at (k + q) strides and r bytes from x's row j
+    const int64_t stride = x_stride * esz, width = n_tokens * esz, d = (int64_t)(y0 - x0), r = (d % stride + stride) % stride, q = (d - r) / stride;
+    return (std::abs(q) < rows && r < width) || (std::abs(q + 1) < rows && stride - r < width);
 }
 
 constexpr int32_t kMaxTokens = 1 << 24;                  // of a vocabulary; the kernels reach a row by 32-bit offsets

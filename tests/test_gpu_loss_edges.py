@@ -235,3 +235,40 @@ def test_infinite_gaps(T, pairs, grad, smoothing):
             down = np.stack([slope, -slope], 1).reshape(-1)
             want = R.gradient(logp, c.t, live, down, 1.0)
             _close(g[:, :v], want, R.tol_gradient(want, logp, c.t, live, down, np.abs(down) * 8 * R.U + 0.5 / pairs * R.tol_lp(lp64), 1.0, False), "gradient")
+
+
+def test_gradient_rows_between_the_logits_rows(T):
+    """One buffer for both, row by row beside one another or one behind the other, is no overlap; rows that share an element are."""
+    c = Case(T, 6, 200, "bf16", 46)
+    lp, stats, d = torch.zeros(6, device="cuda"), torch.zeros((6, 2), device="cuda"), torch.ones(6, device="cuda")
+    want = torch.zeros_like(c.x)
+    T.token_logprobs(*c.args(), lp, stats=stats)
+    T.token_logprobs_backward(*c.args(), stats, d, want[:, :200])
+    buf = torch.empty((14, 464), dtype=torch.bfloat16, device="cuda")
+
+    def run(x, g):
+        buf.fill_(5.0)
+        x.copy_(c.logits)
+        T.token_logprobs_backward(c.table, x, c.states, c.tokens, stats, d, g)
+        assert torch.equal(g, want[:, :200]) and torch.equal(x, c.logits)
+        kept = buf.clone()
+        for part in (x, g):
+            torch.as_strided(kept, part.shape, part.stride(), part.storage_offset()).fill_(5.0)
+        assert bool((kept == 5.0).all())
+
+    for first, second in ((0, 200), (200, 0), (8, 256), (264, 0)):
+        run(buf[:6, first:first + 200], buf[:6, second:second + 200])
+        run(buf[:6, first:first + 200], buf[8:14, second:second + 200])
+        run(buf[4:10, first:first + 200], buf[:6, second:second + 200])
+    run(buf[:6, :200], buf[6:12, :200])                              # behind the last row
+    run(buf[:6, 264:], buf[7:13, :200])
+    x = buf[:6, :200]
+    for g in (buf[:6, 192:392], buf[1:7, :200], buf[5:11, 8:208]):
+        for a, b in ((x, g), (g, x)):
+            with pytest.raises(T.TdfaError, match="overlaps"):
+                T.token_logprobs_backward(c.table, a, c.states, c.tokens, stats, d, b)
+    flat = buf.view(-1)
+    far, near = torch.as_strided(flat, (6, 200), (464, 1)), torch.as_strided(flat, (6, 200), (464, 1), 272)       # 272 + 200 > 464
+    for a, b in ((far, near), (near, far), (far, torch.as_strided(flat, (6, 200), (472, 1), 208))):               # (another stride between the rows)
+        with pytest.raises(T.TdfaError, match="overlaps"):
+            T.token_logprobs_backward(c.table, a, c.states, c.tokens, stats, d, b)
