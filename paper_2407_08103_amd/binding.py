@@ -439,7 +439,7 @@ def _workspace(workspace, rows, n_pairs, logits, stream):
             workspace = torch.empty(n, dtype=torch.uint8, device=logits.device)
         else:
             if not isinstance(stream, torch.cuda.Stream):
-                stream = torch.cuda.ExternalStream(int(stream), device=logits.device)
+                stream = torch.cuda.ExternalStream(_stream(stream), device=logits.device)
             with torch.cuda.stream(stream):
                 workspace = torch.empty(n, dtype=torch.uint8, device=logits.device)
     return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace

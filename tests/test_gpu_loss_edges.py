@@ -1,5 +1,6 @@
 """Log-probabilities and losses where a row's own token, a gap or an address goes to its limit."""
 import math
+import types
 
 import numpy as np
 import pytest
@@ -272,3 +273,37 @@ def test_gradient_rows_between_the_logits_rows(T):
     for a, b in ((far, near), (near, far), (far, torch.as_strided(flat, (6, 200), (472, 1), 208))):               # (another stride between the rows)
         with pytest.raises(T.TdfaError, match="overlaps"):
             T.token_logprobs_backward(c.table, a, c.states, c.tokens, stats, d, b)
+
+
+def _stream_forms(stream):
+    return {"stream": stream, "handle": stream.cuda_stream, "object with a handle": types.SimpleNamespace(cuda_stream=stream.cuda_stream)}
+
+
+@pytest.mark.parametrize("form", ["stream", "handle", "object with a handle", "default handle"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_calls_on_another_stream(T, form, dtype):
+    """All calls on a stream of the caller's, with workspaces from torch on that stream: scoring of rows that want one, both losses, and the
+    gradient from statistics; the same bits as on the current stream."""
+    c = Case(T, 20, 70003 if dtype == "f32" else 140003, dtype, 47)
+    n, v = c.n, c.v
+    begin, ones = torch.tensor([0, 5, 9, 14, 20], dtype=torch.int32, device="cuda"), torch.ones(n, device="cuda")
+    side = torch.cuda.current_stream() if form == "default handle" else torch.cuda.Stream()
+    given = side.cuda_stream if form == "default handle" else _stream_forms(side)[form]
+
+    def run(stream):
+        out = [torch.full((n,), 9.0, device="cuda"), torch.full((n, 2), 9.0, device="cuda"), torch.full_like(c.x, 7.0), torch.full((1,), 9.0, device="cuda"),
+               torch.full((n,), 9.0, device="cuda"), torch.full_like(c.x, 7.0), torch.full((1,), 9.0, device="cuda"), torch.full((4,), 9.0, device="cuda"),
+               torch.full((n,), 9.0, device="cuda"), torch.full_like(c.x, 7.0)]
+        lp, stats, g, loss, lp2, g2, loss2, rewards, lp3, g3 = out
+        side.wait_stream(torch.cuda.current_stream())
+        T.token_logprobs(*c.args(), lp, stats=stats, stream=stream)
+        T.token_logprobs_backward(*c.args(), stats, ones, g[:, :v], stream=stream)
+        T.policy_loss(*c.args(), ones, ones, loss, lp2, grad_logits=g2[:, :v], ref_logprobs=ones, kl_coef=0.0, stream=stream)
+        T.preference_loss(*c.args(), ones, begin, loss2, rewards, lp3, grad_logits=g3[:, :v], stream=stream)
+        torch.cuda.current_stream().wait_stream(side)
+        return out
+
+    want, got = run(None), run(given)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+    assert bool(torch.isfinite(got[3]).all()) and not bool((got[0] == 9.0).any())
