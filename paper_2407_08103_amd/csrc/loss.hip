@@ -732,8 +732,9 @@ __device__ __forceinline__ float rest_from(float lp)
     const float near = fmaf(lp, fmaf(lp, fmaf(lp, fmaf(lp, fmaf(lp, fmaf(lp, 1.0f / 5040.0f, 1.0f / 720.0f), 1.0f / 120.0f), 1.0f / 24.0f), 1.0f / 6.0f), 0.5f), 1.0f);
     return lp > -0.35f ? -lp * near : 1.0f - __builtin_amdgcn_exp2f(lp * kLog2e);
 }
-// fold takes one rounding of a number of the size of ref c2 instead of a subtraction and a product per element.  Up to 2^10 it is
-// off by 2^-15 of p, which nothing that is rounded to 8 bits behind it shows; careful rows (a NaN among the logits) do without.
+// fold takes two roundings instead of a subtraction and a product per element: of ref c2, up to 2^10 here, and of its sum with k and
+// log2 |d|, which may pass that (k and a small slope add up to -126 each).  They are 2^-15 and 2^-14 of the exponent at most, 2^-13.8 of p,
+// next to a rounding of the result by up to 2^-8.  Careful rows (a NaN among the logits) do without.
 template <int DTYPE>
 __device__ __forceinline__ Slope slope_of(float d, float ref, float ls, float scale, float c2, bool careful)
 {

@@ -307,3 +307,32 @@ def test_calls_on_another_stream(T, form, dtype):
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(want, got))
     assert bool(torch.isfinite(got[3]).all()) and not bool((got[0] == 9.0).any())
+
+
+@pytest.mark.parametrize("n,v", [(6, 515), (40, 9001), (40, 70003)])
+def test_folded_exponents_at_their_largest(T, n, v):
+    """16-bit gradients of logits between 512 and 1,023 in units of the exponent, with slopes down to 10^-30."""
+    for sign, far in ((1.0, 0.0), (-1.0, 0.0), (1.0, 60.0), (-1.0, 60.0)):
+        c = Case(T, n, v, "bf16", 48, constrained=False)
+        g = torch.Generator("cuda").manual_seed(v)
+        level = torch.linspace(380.0, 690.0 if sign > 0 else 690.0 - far, n, device="cuda")[:, None]
+        x = sign * level + 8.0 * torch.rand((n, v), device="cuda", generator=g)
+        c.t = np.arange(n) * 11 % v
+        at = torch.from_numpy(c.t).cuda()[:, None]
+        x.scatter_(1, at, x.amax(1, keepdim=True) - far)
+        c.x[:, :v] = x.to(c.x.dtype)
+        c.tokens = at[:, 0].int()
+        z2 = (c.logits.float().gather(1, at).abs() * 1.4427).cpu().numpy()
+        assert (z2 < 1024).all() and z2.max() > 870 and z2.min() > 450
+        p = torch.softmax(c.logits.double(), dim=1)
+        for down in (1.0, -1e-10, 1e-30):
+            lp, stats, got = torch.zeros(n, device="cuda"), torch.zeros((n, 2), device="cuda"), torch.zeros_like(c.x)
+            T.token_logprobs(*c.args(), lp, stats=stats)
+            T.token_logprobs_backward(*c.args(), stats, torch.full((n,), down, device="cuda"), got[:, :v])
+            want = (-down * p).scatter(1, at, 0.0)
+            want.scatter_(1, at, -want.sum(1, keepdim=True))
+            # exponents off by 2^-15 + 2^-14 + 2^-17 (the difference itself), sums by REL_SUM and what their own exponents lose, 3 u 2^7;
+            # a result below the normal numbers is off by half of the smallest
+            rel = 2.0 ** -8 + 1.02 * math.log(2) * (2.0 ** -15 + 2.0 ** -14 + 2.0 ** -17) + 2 * R.REL_SUM + 384 * R.U
+            off = (got[:, :v].double() - want).abs()
+            assert bool((off <= rel * want.abs() + 1.2e-38).all()), (sign, far, down, float((off / want.abs().clamp(min=1e-37)).max()))
