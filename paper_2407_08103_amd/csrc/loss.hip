@@ -324,6 +324,13 @@ __device__ __forceinline__ bool settle(uint4& x, uint32_t b, int32_t g, int32_t 
     return true;
 }
 
+// -ref c2 as it is rounded by itself: the compiler, which does not see that it is a product, makes no product and sum one around it.
+__device__ __forceinline__ float offset_of(float ref, float c2)
+{
+    float nb = -(ref * c2);
+    asm("" : "+v"(nb));
+    return nb;
+}
 // Sum of 2^(z c2 + nb), nb = -ref c2 rounded: the rounding moves all terms, the token's own among them, by the same factor.
 template <int DTYPE>
 __device__ __forceinline__ void add_group(uint4 x, float c2, float nb, float (&s)[2])
@@ -369,11 +376,19 @@ __device__ __forceinline__ void add_groups(uint4 (&x)[U], uint32_t (&b)[U], int3
     }
 }
 
+// 2 to the power of (from - to) c2: what a sum relative to `from` is scaled by.  The roundings of from c2 and to c2 are in the terms (not
+// if SAFE), so it is the difference of these.
+template <bool SAFE>
+__device__ __forceinline__ float rescale(float from, float to, float c2)
+{
+    return __builtin_amdgcn_exp2f(SAFE ? (from - to) * c2 : offset_of(to, c2) - offset_of(from, c2));
+}
 // The same relative to the largest logit that the thread has met, m: a running maximum, and a sum that is scaled where it moves, four groups
-// at a time so that sums do not wait for all loads.  NaN is passed over.
-template <int DTYPE, int NT, int U, bool BITS>
+// at a time so that sums do not wait for all loads.  Exponents are z c2 - m c2 with m c2 rounded (SAFE: differences taken first and NaN
+// passed over, which takes half as many instructions again).
+template <int DTYPE, int NT, int U, bool BITS, bool SAFE>
 __device__ __forceinline__ void add_groups_running(uint4 (&x)[U], uint32_t (&b)[U], int32_t g0, int32_t n_groups, const uint2 (&masks)[16], int32_t token,
-                                                   float c2, float& m, float& s, uint32_t& some)
+                                                   float c2, float& m, float (&s)[2], uint32_t& some)
 {
     static_assert(U % 4 == 0);
     const Own own = own_of<DTYPE, NT, U>(token, g0);
@@ -389,12 +404,15 @@ __device__ __forceinline__ void add_groups_running(uint4 (&x)[U], uint32_t (&b)[
             top = max_group<DTYPE>(x[k], top);
             next_group();
         }
-        s *= __builtin_amdgcn_exp2f((m - top) * c2);
+        const float nb = offset_of(top, c2), scale = rescale<SAFE>(m, top, c2);
+        s[0] *= scale;
+        s[1] *= scale;
         m = top;
 #pragma unroll
         for (int k = k0; k < k0 + 4; ++k) {
             if (!(some >> k & 1)) continue;
-            add_group_careful<DTYPE>(x[k], c2, m, s);
+            if constexpr (SAFE) add_group_careful<DTYPE>(x[k], c2, m, s[0]);
+            else add_group<DTYPE>(x[k], c2, nb, s);
             next_group();
         }
     }
@@ -518,12 +536,37 @@ __device__ __forceinline__ float careful_sum(const RowBuffers& row, int32_t n_gr
     return block_reduce<NT, false>(s, part);
 }
 
-// The sum of a running one over the workgroup, relative to its largest maximum, which goes to *ref.
-template <int NT>
-__device__ __forceinline__ float sum_of_running(float m, float s, float c2, float* ref, float (&part)[NT / 64])
+// The sum of running ones over the workgroup, relative to its largest maximum, which goes to *ref, in every thread.  One barrier: the
+// wavefronts leave a maximum and a sum each, and the lanes of every wavefront join those.
+template <int NT, bool SAFE>
+__device__ __forceinline__ float sum_of_running(float m, float s, float c2, float* ref, float (&part)[2][NT / 64])
 {
-    *ref = block_reduce<NT, true>(m, part);
-    return block_reduce<NT, false>(s * __builtin_amdgcn_exp2f((m - *ref) * c2), part);
+    float top = wave_max(m);
+    s = wave_sum(s * rescale<SAFE>(m, top, c2));
+    if constexpr (NT > 64) {
+        constexpr int W = NT / 64;
+        static_assert(W == 4 || W == 8 || W == 16);
+        if ((threadIdx.x & 63) == 0) {
+            part[0][threadIdx.x >> 6] = top;
+            part[1][threadIdx.x >> 6] = s;
+        }
+        __syncthreads();
+        const float mine = part[0][threadIdx.x & (W - 1)];
+        s = part[1][threadIdx.x & (W - 1)];
+        top = fmaxf(mine, lane_swap<0xB1>(mine));
+        top = fmaxf(top, lane_swap<0x4E>(top));
+        if constexpr (W >= 8) top = fmaxf(top, lane_swap<0x141>(top));
+        if constexpr (W >= 16) top = fmaxf(top, lane_swap<0x140>(top));
+        s *= rescale<SAFE>(mine, top, c2);
+        s += lane_swap<0xB1>(s);
+        s += lane_swap<0x4E>(s);
+        if constexpr (W >= 8) s += lane_swap<0x141>(s);
+        if constexpr (W >= 16) s += lane_swap<0x140>(s);
+        top = lane_value(top, 0);
+        s = lane_value(s, 0);
+    }
+    *ref = top;
+    return SAFE ? s : s * __builtin_amdgcn_exp2f(-fmaf(top, c2, offset_of(top, c2)));      // the rounding of top c2 is in all terms
 }
 
 // What the sums of a row are taken relative to.  In 16 bits its own token's logit: no maximum is needed, and what the exponents lose where
@@ -605,7 +648,7 @@ template <typename A, int DTYPE, int NT, int U, bool BITS>
 __global__ void __launch_bounds__(NT, 8) token_stats_kernel(A a)
 {
     constexpr bool kMax = kRelativeToMax<DTYPE>;
-    __shared__ float s_part[NT / 64];
+    __shared__ float s_part[NT / 64], s_running[2][NT / 64];
     __shared__ uint2 s_masks[16];
     const uint32_t i = blockIdx.x;
     const Row r = row_of(a, weights_of(a), i);
@@ -630,34 +673,29 @@ __global__ void __launch_bounds__(NT, 8) token_stats_kernel(A a)
         if (threadIdx.x == 0) leave_out(a, i, r.lp);
         return;
     }
-    const float nb = -z * c2;
-    float m = fmaxf(fmaxf(kLowest, z), last), sum[2] = {__builtin_amdgcn_exp2f(kMax ? (fmaxf(last, -INFINITY) - m) * c2 : fmaf(last, c2, nb)), 0.0f};
+    float m = kMax ? fmaxf(z, last) : z;
+    const float nb = offset_of(m, c2);
+    float sum[2] = {__builtin_amdgcn_exp2f(fmaf(last, c2, nb)), 0.0f};
     for (int32_t g = 0; g < n_groups; g += NT * U) {
         uint4 x[U];
         uint32_t some;
         if (g) fetch_bits<DTYPE, NT, U, BITS>(buf, g, b);
         fetch_groups<DTYPE, NT, U, BITS>(buf, g, n_groups, x, b);
-        if constexpr (kMax) add_groups_running<DTYPE, NT, U, BITS>(x, b, g, n_groups, s_masks, r.token, c2, m, sum[0], some);
+        if constexpr (kMax) add_groups_running<DTYPE, NT, U, BITS, false>(x, b, g, n_groups, s_masks, r.token, c2, m, sum, some);
         else add_groups<DTYPE, NT, U, BITS>(x, b, g, n_groups, s_masks, r.token, c2, nb, sum, some);
     }
-    float own, s, ref;
-    bool careful = true;
+    float own = 1.0f, s, ref = z;
     if constexpr (kMax) {
-        s = sum_of_running<NT>(m, sum[0], c2, &ref, s_part);
+        s = sum_of_running<NT, false>(m, sum[0] + sum[1], c2, &ref, s_running);
     } else {
         s = block_reduce<NT, false>(sum[0] + sum[1], s_part);
         own = own_term(z, c2, nb);
-        careful = !usable(own, s);
-        if (careful) s = careful_sum<DTYPE, NT, 2, BITS>(buf, n_groups, r.token, z, last, c2, &ref, s_masks, s_part);
-    }
-    if (careful) {
-        own = __builtin_amdgcn_exp2f((z - ref) * c2);
-    } else {
         s *= __builtin_amdgcn_rcpf(own);
-        own = 1.0f;
-        ref = z;
     }
-    if (threadIdx.x == 0) finish(a, i, score(z, ref, own, s, a.inv_t), careful, v);
+    const bool careful = !usable(own, s);
+    if (careful) s = careful_sum<DTYPE, NT, 2, BITS>(buf, n_groups, r.token, z, last, c2, &ref, s_masks, s_part);
+    own = kMax || careful ? __builtin_amdgcn_exp2f((z - ref) * c2) : 1.0f;
+    if (threadIdx.x == 0) finish(a, i, score(z, ref, own, s, a.inv_t), kMax || careful, v);
 }
 
 // The largest logit and the sum relative to it of a part of a row without the token's own; {kLowest, 0}: of none.
@@ -671,7 +709,7 @@ struct Part {
 template <int DTYPE, int NT, int U, bool BITS>
 __global__ void __launch_bounds__(NT) part_stats_kernel(RowArgs a, const float* weights, Part* out, int32_t parts, int32_t span)
 {
-    __shared__ float s_part[NT / 64];
+    __shared__ float s_running[2][NT / 64];
     __shared__ uint2 s_masks[16];
     const uint32_t i = blockIdx.x / (uint32_t)parts;
     const int32_t part = (int32_t)(blockIdx.x - i * (uint32_t)parts);
@@ -688,16 +726,16 @@ __global__ void __launch_bounds__(NT) part_stats_kernel(RowArgs a, const float* 
     const RowBuffers buf = row_buffers<DTYPE>(row, r.bits, end);
     // fmaxf with a number passes over a NaN
     const float last = part == parts - 1 ? fmaxf(last_element<DTYPE>(a.n_tokens, row, r.bits, r.token), -INFINITY) : -INFINITY;
-    float m = fmaxf(kLowest, last), s = __builtin_amdgcn_exp2f((last - m) * c2);
+    float m = fmaxf(kLowest, last), s[2] = {__builtin_amdgcn_exp2f((last - m) * c2), 0.0f};
     for (int32_t g = part * span; g < end; g += NT * U) {
         uint4 x[U];
         uint32_t b[U], some;
         fetch<DTYPE, NT, U, BITS>(buf, g, end, x, b);
-        add_groups_running<DTYPE, NT, U, BITS>(x, b, g, end, s_masks, r.token, c2, m, s, some);
+        add_groups_running<DTYPE, NT, U, BITS, true>(x, b, g, end, s_masks, r.token, c2, m, s, some);
     }
     float top;
-    s = sum_of_running<NT>(m, s, c2, &top, s_part);
-    if (threadIdx.x == 0) out[blockIdx.x] = {top, s};
+    const float sum = sum_of_running<NT, true>(m, s[0], c2, &top, s_running);
+    if (threadIdx.x == 0) out[blockIdx.x] = {top, sum};
 }
 
 // A wavefront per row joins its parts, at most 64.  Bound by its chain of reads (4.7 us).
@@ -1144,7 +1182,7 @@ template <int DTYPE, int NT, int R, bool BITS>
 __global__ void __launch_bounds__(NT, 4) policy_row_kernel(PolicyRowArgs a)
 {
     constexpr int G = Elem<DTYPE>::kGroup;
-    __shared__ float s_part[NT / 64];
+    __shared__ float s_part[NT / 64], s_running[2][NT / 64];
     __shared__ uint2 s_masks[16];
     __shared__ Slope s_slope;
     __shared__ float s_own;
@@ -1172,36 +1210,33 @@ __global__ void __launch_bounds__(NT, 4) policy_row_kernel(PolicyRowArgs a)
     }
     if (z > -INFINITY) {
         fetch_groups<DTYPE, NT, R, BITS, true>(buf, 0, n_groups, x, b);
-        float s, ref = z, own = 1.0f;
-        bool careful = true;
-        if constexpr (kRelativeToMax<DTYPE>) {
-            float m = fmaxf(fmaxf(kLowest, z), last);
-            s = __builtin_amdgcn_exp2f((fmaxf(last, -INFINITY) - m) * c2);
-            add_groups_running<DTYPE, NT, R, BITS>(x, b, 0, n_groups, s_masks, r.token, c2, m, s, some);
-            s = sum_of_running<NT>(m, s, c2, &ref, s_part);
+        constexpr bool kMax = kRelativeToMax<DTYPE>;
+        float m = kMax ? fmaxf(z, last) : z;
+        const float nb = offset_of(m, c2);
+        float sum[2] = {__builtin_amdgcn_exp2f(fmaf(last, c2, nb)), 0.0f}, own = 1.0f, s, ref = z;
+        if constexpr (kMax) {
+            add_groups_running<DTYPE, NT, R, BITS, false>(x, b, 0, n_groups, s_masks, r.token, c2, m, sum, some);
+            s = sum_of_running<NT, false>(m, sum[0] + sum[1], c2, &ref, s_running);
         } else {
-            const float nb = -z * c2;
-            float sum[2] = {__builtin_amdgcn_exp2f(fmaf(last, c2, nb)), 0.0f};
             add_groups<DTYPE, NT, R, BITS>(x, b, 0, n_groups, s_masks, r.token, c2, nb, sum, some);
             s = block_reduce<NT, false>(sum[0] + sum[1], s_part);
             own = own_term(z, c2, nb);
-            careful = !usable(own, s);
             s *= __builtin_amdgcn_rcpf(own);
-            own = 1.0f;
-            if (careful) {
-                ref = fmaxf(fmaxf(kLowest, z), last);
-#pragma unroll
-                for (int k = 0; k < R; ++k)
-                    if (some >> k & 1) ref = max_group<DTYPE>(x[k], ref);
-                ref = block_reduce<NT, true>(ref, s_part);
-                s = __builtin_amdgcn_exp2f((fmaxf(last, -INFINITY) - ref) * c2);
-#pragma unroll
-                for (int k = 0; k < R; ++k)
-                    if (some >> k & 1) add_group_careful<DTYPE>(x[k], c2, ref, s);
-                s = block_reduce<NT, false>(s, s_part);
-            }
         }
-        if (careful) own = __builtin_amdgcn_exp2f((z - ref) * c2);
+        const bool careful = !usable(own, s);
+        if (careful) {
+            ref = fmaxf(fmaxf(kLowest, z), last);
+#pragma unroll
+            for (int k = 0; k < R; ++k)
+                if (some >> k & 1) ref = max_group<DTYPE>(x[k], ref);
+            ref = block_reduce<NT, true>(ref, s_part);
+            s = __builtin_amdgcn_exp2f((fmaxf(last, -INFINITY) - ref) * c2);
+#pragma unroll
+            for (int k = 0; k < R; ++k)
+                if (some >> k & 1) add_group_careful<DTYPE>(x[k], c2, ref, s);
+            s = block_reduce<NT, false>(s, s_part);
+        }
+        own = kMax || careful ? __builtin_amdgcn_exp2f((z - ref) * c2) : 1.0f;
         if (threadIdx.x < 64) {
             const Scored sc = score(z, ref, own, s, a.inv_t);
             const float lp = (float)sc.lp;
@@ -1209,7 +1244,7 @@ __global__ void __launch_bounds__(NT, 4) policy_row_kernel(PolicyRowArgs a)
             if (lp != -INFINITY) policy_term(a.clip_low, a.clip_high, a.kl_coef, a.ref_logprobs, v, lp, &e, &d);
             if (threadIdx.x == 0) {
                 a.logprobs[i] = lp;
-                s_slope = slope_of<DTYPE>(d * a.inv_t, sc.ref, sc.ls, sc.scale, c2, careful);
+                s_slope = slope_of<DTYPE>(d * a.inv_t, sc.ref, sc.ls, sc.scale, c2, kMax || careful);
                 s_own = d * a.inv_t * sc.rest;
             }
         }
