@@ -1407,10 +1407,10 @@ int grad_launch(const TokenRows& a, hipStream_t stream, F set)
         const dim3 grid((unsigned)(std::min(a.rows - from, most) * parts + kFirst<A>));
         A x;
         set(x, from, parts);
-        int rc;
-        if (tiny) rc = launch(token_grad_kernel<A, DTYPE, kPairs ? 256 : 64, 4, BITS>, grid, 64, stream, x);
-        else if (few) rc = launch(token_grad_kernel<A, DTYPE, 256, 4, BITS>, grid, 256, stream, x);
-        else rc = launch(token_grad_kernel<A, DTYPE, 256, 8, BITS>, grid, 256, stream, x);
+        int rc = TDFA_OK;
+        if (few && !tiny) rc = launch(token_grad_kernel<A, DTYPE, 256, 4, BITS>, grid, 256, stream, x);
+        else if (!tiny) rc = launch(token_grad_kernel<A, DTYPE, 256, 8, BITS>, grid, 256, stream, x);
+        else if constexpr (!kPairs) rc = launch(token_grad_kernel<A, DTYPE, 64, 4, BITS>, grid, 64, stream, x);
         if (rc != TDFA_OK) return rc;
     }
     return TDFA_OK;
