@@ -1544,9 +1544,11 @@ int launch_preference_loss(const TokenRows& a, const PairArgs& p, float* loss, f
         if (rc != TDFA_OK) return rc;
     }
     const PairArgsOnCard pairs = {p.ref_logprobs, p.begin, p.rewards, p.n_pairs, (int32_t)a.rows, p.beta, p.smoothing};
-    // Few rows and pairs without the launch between the other two: 90 rows of 32,000 tokens in bf16 in 4 pairs 13.9 -> 12.2 us, 1,000 rows
-    // in 64 pairs 34.4 -> 32.5 (of 1,000 tokens 11.6 -> 13.0), and 3 us less of the host; 300 rows in 128 pairs 10.7 -> 16.8.
-    if (grad && a.rows && a.rows <= 1024 && p.n_pairs && p.n_pairs <= 64)
+    // Few rows and pairs without the launch between the other two, unless pairs are long, whose sums every workgroup of a gradient takes
+    // again: 90 rows of 32,000 tokens in bf16 in 4 pairs 13.3 -> 11.7 us, 1,000 rows in 64 pairs 32.6 -> 30.4, in 4 pairs 32.9 -> 32.8, in
+    // 2 pairs 33.8 -> 36.5 and in one 33.6 -> 39.2 (of 128,256 tokens 92.8 -> 91.1 in 4, 93.4 -> 92.3 in one, in fp32 163 -> 169; 300 rows of
+    // few tokens in 128 pairs 10.7 -> 16.8), and 3 us less of the host.
+    if (grad && a.rows && a.rows <= 1024 && a.rows <= 256 * (int64_t)p.n_pairs && p.n_pairs <= 64)
         return grad_of<FewPairsGradArgs>(a, stream, [&](FewPairsGradArgs& x, int64_t, int32_t) {
             const RowArgs r = row_args(a, 0);              // one launch: a row of 2^24 tokens has 4,096 parts at most, 2,048 where there are more than 128
             x = {r.allow, r.logits, r.states, r.tokens, work, grad, loss, pairs, r.stride16, grad_stride16(a, grad_stride), r.n_tokens, r.inv_t};

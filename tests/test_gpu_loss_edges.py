@@ -7,7 +7,7 @@ import pytest
 import torch
 
 import loss_ref as R
-from test_gpu_loss import Case, _close
+from test_gpu_loss import Case, _close, _run_preference
 
 pytestmark = pytest.mark.gpu
 
@@ -336,3 +336,12 @@ def test_folded_exponents_at_their_largest(T, n, v):
             rel = 2.0 ** -8 + 1.02 * math.log(2) * (2.0 ** -15 + 2.0 ** -14 + 2.0 ** -17) + 2 * R.REL_SUM + 384 * R.U
             off = (got[:, :v].double() - want).abs()
             assert bool((off <= rel * want.abs() + 1.2e-38).all()), (sign, far, down, float((off / want.abs().clamp(min=1e-37)).max()))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,pairs", [(256, 1), (257, 1), (512, 2), (513, 2), (1000, 1), (1024, 64), (1025, 64), (1000, 65)])
+def test_preference_pairs_of_any_length(T, dtype, n, pairs):
+    """Around the numbers of rows and pairs at which the launch between scores and gradients is left out; one pair holds most rows."""
+    cut = sorted({0, n, *range(n - 2 * pairs + 1, n)})
+    cut = [0] * (2 * pairs + 1 - len(cut)) + cut
+    _run_preference(T, Case(T, n, 515, dtype, 49), 1.0, 0.2, 0.1, cut)
