@@ -1377,11 +1377,18 @@ int parts_launch(const TokenRows& a, const Score& o, Part* out, hipStream_t stre
 
 int64_t groups_of(const TokenRows& a) { return a.n_tokens / (a.dtype == TDFA_F32 ? Elem<TDFA_F32>::kGroup : Elem<TDFA_BF16>::kGroup); }
 
-bool in_parts(const TokenRows& a) { return a.rows <= kPartRows && groups_of(a) > kWholeGroups; }
+// Rows that are longer than a workgroup's registers, too few of them to fill the card, are shared out by parts, which a second launch joins:
+// one row of 128,256 tokens in fp32 8.0 us by one workgroup, 5.6 so, 64 rows 12.9 and 10.0.  Up to 256 rows have a compute unit each, and the
+// join costs more than the parts bring unless rows are very long (200 rows 14.1 and 15.8; of 256,000 tokens 28.0 and 24.8; in bf16 18.5 and
+// 20.8, of 512,000 35.1 and 32.5); of 257 rows some compute units have two (300 rows 23.8 and 19.7; in bf16 of 256,000 29.9 and 27.1,
+// of 140,000 18.6 and 19.3), and from some 400 on there is no difference (512 rows 31.0 and 30.9).
+bool in_parts(const TokenRows& a)
+{
+    const int64_t n_groups = groups_of(a);
+    return n_groups > kWholeGroups && (a.rows <= 64 || (a.rows > 256 && a.rows <= kPartRows) || (a.rows <= 256 && n_groups > 3 * kWholeGroups));
+}
 
-// parts: workspace for kMaxParts parts of each of the first kPartRows rows.  Few rows that are longer than a workgroup's registers are
-// shared out by parts, which a second launch joins: 1 row of 256,000 tokens in fp32 14.5 us by one workgroup, 6.8 so; 64 rows 34.5 and
-// 14.9, 300 rows 60.6 and 44.5; of 128,256 tokens 19.8 and 12.1, 28.7 and 24.9; 512 rows 38.1 and 37.9, in bf16 of 256,000 36.6 and 40.6.
+// parts: workspace for kMaxParts parts of each of the first kPartRows rows.
 template <typename A>
 int stats_of(const TokenRows& a, const Score& o, Part* parts, hipStream_t stream)
 {

@@ -7,7 +7,7 @@ import pytest
 import torch
 
 import loss_ref as R
-from test_gpu_loss import Case, _close, _run_preference
+from test_gpu_loss import TYPES, Case, _close, _run_preference
 
 pytestmark = pytest.mark.gpu
 
@@ -345,3 +345,33 @@ def test_preference_pairs_of_any_length(T, dtype, n, pairs):
     cut = sorted({0, n, *range(n - 2 * pairs + 1, n)})
     cut = [0] * (2 * pairs + 1 - len(cut)) + cut
     _run_preference(T, Case(T, n, 515, dtype, 49), 1.0, 0.2, 0.1, cut)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,groups", [(64, 16400), (65, 16400), (256, 16400), (257, 16400), (100, 49152), (100, 49153)])
+def test_long_rows_around_their_parts(T, dtype, n, groups):
+    """Around the numbers of long rows that are shared out by parts, by scoring with its gradient and by the losses."""
+    v = groups * (4 if dtype == "f32" else 8) + 1
+    g = torch.Generator("cuda").manual_seed(n)
+    x = (2.0 * torch.randn(n, -(-v // 8) * 8, device="cuda", generator=g)).to(TYPES[dtype])
+    tokens = torch.randint(0, v, (n,), device="cuda", generator=g, dtype=torch.int32)
+    at = tokens.long()[:, None]
+    lp64 = torch.cat([torch.log_softmax(x[i:i + 32, :v].double(), dim=1).gather(1, at[i:i + 32]) for i in range(0, n, 32)])[:, 0]
+    lp, stats, lp2, lp3 = torch.zeros(n, device="cuda"), torch.zeros((n, 2), device="cuda"), torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda")
+    T.token_logprobs(None, x[:, :v], None, tokens, lp, stats=stats)
+    bound = R.U * (3 * lp64.abs() + 8)
+    assert bool(((lp.double() - lp64).abs() <= bound).all())
+    down, loss, grads = torch.full((n,), 0.5, device="cuda"), torch.zeros(1, device="cuda"), [torch.zeros_like(x) for _ in range(2)]
+    T.token_logprobs_backward(None, x[:, :v], None, tokens, stats, down, grads[0][:, :v])
+    T.policy_loss(None, x[:, :v], None, tokens, lp, -down, loss, lp2, grad_logits=grads[1][:, :v], clip=(1.0, math.inf))
+    T.preference_loss(None, x[:, :v], None, tokens, lp, torch.tensor([0, n, n], dtype=torch.int32, device="cuda"), loss, torch.zeros(2, device="cuda"), lp3)
+    for other in (lp2, lp3):
+        assert bool(((other.double() - lp64).abs() <= bound).all())
+    for i in range(0, n, 32):
+        p = torch.softmax(x[i:i + 32, :v].double(), dim=1)
+        want = (-0.5 * p).scatter(1, at[i:i + 32], 0.0)
+        want.scatter_(1, at[i:i + 32], -want.sum(1, keepdim=True))
+        for got in grads:
+            # exponents of some 20, off by 3 u of their size, a folded one by 2^-13.8 of p in 16 bits, and the rounding to the type
+            rel = 2 * R.REL_SUM + 64 * R.U + (2.0 ** -8 + 2.0 ** -13.7 if dtype == "bf16" else 2 * R.U)
+            assert bool(((got[i:i + 32, :v].double() - want).abs() <= rel * want.abs() + 1.2e-38).all())
