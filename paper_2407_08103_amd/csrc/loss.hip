@@ -1473,12 +1473,13 @@ int policy_launch(const TokenRows& a, const PolicyArgs& p, float* logprobs, void
 
 // Whether a policy loss is scored and its gradient written by one launch, a workgroup per row that reads it once, or by two, which read
 // it twice but share the second out by parts of rows.  Two are faster where few long rows leave compute units idle (24 rows of
-// 128,256 tokens in bf16 14.9 us against 18.4, of 64,000 11.0 against 12.1; 96 rows 21.8 against 20.1) and where a row does not fit
-// a workgroup's registers (300 rows of 256,000 in fp32 117 us, 167 with half of every row read twice by one launch).
+// 128,256 tokens in bf16 14.8 us against 17.3, of 64,000 10.1 against 11.5; 40 rows 17.0 and 17.4, 11.5 and 11.8; 64 rows 19.1 and 18.0, 12.6
+// and 12.0; 24, 40 and 64 rows of 60,000 in fp32 12.7, 14.2 and 16.5 against 13.9, 14.2 and 14.6) and where a row does not fit a
+// workgroup's registers (300 rows of 256,000 in fp32 117 us, 167 with half of every row read twice by one launch).
 bool one_launch(const TokenRows& a)
 {
     const int64_t n_groups = groups_of(a);
-    return n_groups <= kWholeGroups && (a.rows > 32 || n_groups <= 1024 * 4);
+    return n_groups <= kWholeGroups && (a.rows > 40 || n_groups <= 1024 * 4);
 }
 
 // Rows whose losses one workgroup sums, in 6.7 us; of more, each sums kSpanRows, in 4 us, and a further launch joins them in 2 to 5
