@@ -421,7 +421,10 @@ TDFA_API int tdfa_sample_noise(int32_t batch, int32_t n_tokens, uint64_t seed, u
 /* A language model that decodes under a constraint is the policy that tdfa_sample_step draws from:
  * in state q the softmax of logits / temperature over the tokens that q allows (Algorithm 2 with a
  * sampler).  The calls below score and train that policy on rows of logits, one row per token: the
- * log-probability of the row's token, its gradient, and two losses made of them.
+ * log-probability of the row's token, its gradient, and two losses made of them.  It is the policy
+ * without a cut: a draw with top_k > 0 takes its tokens from the softmax over what the cut leaves, and
+ * these calls score them as if there were none (the same holds for tdfa_pda_sample_step, whose allowed
+ * sets can be given as rows of a wrapped table).
  *
  * Arguments they share:
  *   table       : the constraint, dense or packed, or NULL: every token is allowed.
@@ -505,7 +508,8 @@ TDFA_API int tdfa_policy_loss(const tdfa_table *table, const void *logits_dev, i
  *     reward_k = beta * the sum of lp - ref over the rows of sequence k that take part     (binary64)
  *     g_p      = reward_{2p} - reward_{2p + 1}
  *     loss     = the mean over the pairs of (1 - smoothing) softplus(-g) + smoothing softplus(g)
- * where softplus(x) = ln(1 + exp(x)); with smoothing = 0 that is -ln of the logistic function of g.  A sequence may have
+ * where softplus(x) = ln(1 + exp(x)); with smoothing = 0 that is -ln of the logistic function of g.  A ref of -inf makes its
+ * sequence's reward and the gap infinite, and the loss and its slope what they tend to there.  A sequence may have
  * no rows; rows that belong to no sequence have a gradient of zero.
  *   ref_logprobs_dev : device, float [rows]: lp under the reference model (read for the rows that take part).
  *   begin_dev        : device, int32 [2 * n_pairs + 1], not decreasing, in 0 .. rows (what lies outside is cut off there).

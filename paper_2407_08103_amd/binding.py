@@ -447,8 +447,8 @@ def _workspace(workspace, rows, n_pairs, logits, stream):
 
 def token_logprobs(table: Table | None, logits: torch.Tensor, states: torch.Tensor | None, tokens: torch.Tensor, logprobs: torch.Tensor,
                    temperature: float = 1.0, stats: torch.Tensor | None = None, workspace: torch.Tensor | None = None, stream=None) -> None:
-    """tdfa_token_logprobs.  logits: [rows, >= n_tokens] float32 or bfloat16 on the GPU; table None: no
-    constraint, and every column is a token.  states, tokens: int32 [rows]; logprobs: float32 [rows], and
+    """tdfa_token_logprobs: of the policy that sample_step draws from with top_k=0.  logits: [rows, >= n_tokens]
+    float32 or bfloat16 on the GPU; table None: no constraint, and every column is a token.  states, tokens: int32 [rows]; logprobs: float32 [rows], and
     stats: float32 [rows, 2] if the gradient is wanted later, are written.  workspace: at least
     loss_workspace_bytes(rows) bytes, allocated by torch if not given."""
     a = _rows_args(table, logits, states, tokens, temperature)
