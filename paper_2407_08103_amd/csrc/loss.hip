@@ -497,7 +497,7 @@ __device__ __forceinline__ float2 stats_of_row(Scored q, bool careful)
 }
 // The row's own term, 2^(z c2 + nb) with the rounding of nb in it as in all others.
 __device__ __forceinline__ float own_term(float z, float c2, float nb) { return __builtin_amdgcn_exp2f(fmaf(z, c2, nb)); }
-// From the row's own term and the sum of the others, both relative to `ref` (which is NaN where an allowed logit is +inf).
+// From the row's own term and the sum of the others, both relative to `ref` (the sum is NaN where an allowed logit is +inf).
 __device__ __forceinline__ Scored score(float z, float ref, float own, float others, float inv_t)
 {
     const double ls = ln_total(own, others), lp = ((double)z - (double)ref) * (double)inv_t - ls;
@@ -640,10 +640,11 @@ __device__ __forceinline__ void finish(const PolicyScoreArgs& a, uint32_t i, Sco
 
 // One workgroup per row.  In 16 bits the sum is taken relative to the row's own token, ref = z_t, so that no maximum has to be known, terms
 // are added as they arrive, and lp = -ln(1 + the sum of the others); where that overflows (lp below -87) or a NaN is met, the row is read
-// again, for the largest logit and the sum relative to it.  In fp32 lanes keep a running maximum.  Bound by the memory where there are many rows: 2,900 rows of 128,256 tokens in bf16 77 us, of which 0.53
-// of the 128-byte lines hold an allowed token (394 MB, 5.1 TB/s; torch's maximum over the rows of a matrix reads 4.9 to 5.2); by one
-// compute unit's stream of a long row where there are few (256 KB in 7.5 us, about 40 GB/s whatever is in flight); by the chain token,
-// bits, logits in short ones (2.5 us).
+// again, for the largest logit and the sum relative to it.  In fp32 lanes keep a running maximum.  Bound by the memory where there are
+// many rows: 2,900 rows of 128,256 tokens in bf16, on changing inputs, 83 us, of which 0.53 of the 128-byte lines hold an allowed token
+// (394 MB, 4.7 TB/s; torch's maximum over the rows of a matrix reads 4.9 to 5.2), 2,047 of 32,003 in fp32 27 us (126 MB, 4.6 TB/s); by one
+// compute unit's stream of a long row where there are few (256 KB in 7.4 us, about 40 GB/s whatever is in flight); by the chain token, bits,
+// logits in short ones (2.6 us).
 template <typename A, int DTYPE, int NT, int U, bool BITS>
 __global__ void __launch_bounds__(NT, 8) token_stats_kernel(A a)
 {
@@ -704,8 +705,8 @@ struct Part {
 };
 
 // One workgroup per part of `span` groups of a row: few long rows are shared out, and every part finds a reference of its own (its largest
-// logit: lanes keep a running maximum and sum).  Bound by the memory: 300 rows of 256,000 tokens in fp32, half of whose lines are read,
-// 27 us (5.4 TB/s).
+// logit: lanes keep a running maximum and sum, which begin at no logit of the row, so with differences taken first).  Bound by the memory: 300 rows of 256,000 tokens in fp32, half of whose lines are read
+// (0.15 GB), on changing inputs 28 us (5.3 TB/s).
 template <int DTYPE, int NT, int U, bool BITS>
 __global__ void __launch_bounds__(NT) part_stats_kernel(RowArgs a, const float* weights, Part* out, int32_t parts, int32_t span)
 {
@@ -738,7 +739,7 @@ __global__ void __launch_bounds__(NT) part_stats_kernel(RowArgs a, const float* 
     if (threadIdx.x == 0) out[blockIdx.x] = {top, sum};
 }
 
-// A wavefront per row joins its parts, at most 64.  Bound by its chain of reads (4.7 us).
+// A wavefront per row joins its parts, at most 64.  Bound by its chain of reads (4.8 us).
 template <typename A, int DTYPE>
 __global__ void __launch_bounds__(kThreads) join_parts_kernel(A a, const Part* in, int32_t parts, uint32_t rows)
 {
@@ -1173,9 +1174,9 @@ constexpr int kMaxParts = 64;
 constexpr int64_t kPartRows = 384;
 
 // One workgroup per row: the sum, the row's term, the gradient.  The row stays in registers between the sum and the gradient, R groups
-// to a thread: 1,024 threads hold 256 KB, half of a compute unit's registers, and the row is read once.  Bound by the memory: 1,024 rows
-// of 128,256 tokens in bf16 without a constraint 91 us for 263 MB read and as much written (5.8 TB/s; an elementwise product of such
-// matrices takes 87, a copy 100); 4,096 rows under one 277 us, 1.05 GB written and some 0.55 GB of lines read (5.8 TB/s).  Vector
+// to a thread: 1,024 threads hold 256 KB, half of a compute unit's registers, and the row is read once.  Bound by the memory, on changing
+// inputs: 1,024 rows of 128,256 tokens in bf16 without a constraint 95 us for 263 MB read and as much written (5.5 TB/s; an elementwise
+// product of such matrices takes 87, a copy 100); 4,096 rows under one 280 us, 1.05 GB written and 0.51 GB of lines read (5.6 TB/s).  Vector
 // instructions take two fifths of the time.  Two rows to a compute unit with half of each read twice: 316 us; workgroups that stay, and
 // fetch the next row into the registers that the gradient leaves: 119 us for the 1,024.
 template <int DTYPE, int NT, int R, bool BITS>
