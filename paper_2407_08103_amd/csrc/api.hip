@@ -1934,7 +1934,7 @@ int tdfa_policy_loss(const tdfa_table* table, const void* logits_dev, int dtype,
     if (rows > 0 && kl_coef != 0.0f && !ref_logprobs_dev) return fail(TDFA_E_INVALID_ARG, "a KL term wants ref_logprobs");
     if (grad_dev) rc = check_grad(a, grad_dev, grad_stride);
     if (rc == TDFA_OK) rc = check_workspace(workspace_dev, workspace_bytes, rows, 0);
-    if (rc == TDFA_OK) rc = check_logprobs(logprobs_dev, rows, {a.states, tokens_dev, old_logprobs_dev, kl_coef != 0.0f ? ref_logprobs_dev : nullptr, advantages_dev, weights_dev});
+    if (rc == TDFA_OK) rc = check_logprobs(logprobs_dev, rows, {table ? states_dev : nullptr, tokens_dev, old_logprobs_dev, kl_coef != 0.0f ? ref_logprobs_dev : nullptr, advantages_dev, weights_dev});
     if (rc != TDFA_OK) return rc;
     a.weights = weights_dev;
     const tdfa::PolicyArgs p = {old_logprobs_dev, kl_coef != 0.0f ? ref_logprobs_dev : nullptr, advantages_dev, 1.0f - clip_low, 1.0f + clip_high, kl_coef};
@@ -1959,7 +1959,7 @@ int tdfa_preference_loss(const tdfa_table* table, const void* logits_dev, int dt
     if (rows > 0 && (!ref_logprobs_dev || !logprobs_dev)) return fail(TDFA_E_INVALID_ARG, "ref_logprobs or logprobs is NULL");
     if (grad_dev) rc = check_grad(a, grad_dev, grad_stride);
     if (rc == TDFA_OK) rc = check_workspace(workspace_dev, workspace_bytes, rows, n_pairs);
-    if (rc == TDFA_OK) rc = check_logprobs(logprobs_dev, rows, {a.states, tokens_dev, ref_logprobs_dev});
+    if (rc == TDFA_OK) rc = check_logprobs(logprobs_dev, rows, {table ? states_dev : nullptr, tokens_dev, ref_logprobs_dev});
     if (rc != TDFA_OK) return rc;
     const tdfa::PairArgs p = {ref_logprobs_dev, begin_dev, n_pairs, beta, smoothing, rewards_dev};
     return launch_preference_loss(a, p, loss_dev, logprobs_dev, n_tokens > 0 ? grad_dev : nullptr, grad_stride, workspace_dev,

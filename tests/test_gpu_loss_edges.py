@@ -375,3 +375,37 @@ def test_long_rows_around_their_parts(T, dtype, n, groups):
             # exponents of some 20, off by 3 u of their size, a folded one by 2^-13.8 of p in 16 bits, and the rounding to the type
             rel = 2 * R.REL_SUM + 64 * R.U + (2.0 ** -8 + 2.0 ** -13.7 if dtype == "bf16" else 2 * R.U)
             assert bool(((got[i:i + 32, :v].double() - want).abs() <= rel * want.abs() + 1.2e-38).all())
+
+
+def test_states_without_a_table_are_not_read(T):
+    """So that log-probabilities may be written over them."""
+    x, tokens = torch.randn(4, 64, device="cuda"), torch.zeros(4, dtype=torch.int32, device="cuda")
+    f, loss, rewards = torch.ones(4, device="cuda"), torch.zeros(1, device="cuda"), torch.zeros(2, device="cuda")
+    want, states = torch.zeros(4, device="cuda"), torch.full((4,), 9, dtype=torch.int32, device="cuda")
+    T.token_logprobs(None, x, None, tokens, want)
+    T.policy_loss(None, x, states, tokens, f, f, loss, states.view(torch.float32))
+    assert torch.equal(states.view(torch.float32), want)
+    states.fill_(9)
+    T.preference_loss(None, x, states, tokens, f, torch.tensor([0, 2, 4], dtype=torch.int32, device="cuda"), loss, rewards, states.view(torch.float32))
+    assert torch.equal(states.view(torch.float32), want)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rows_without_tokens(T, dtype):
+    """A vocabulary of no tokens: no row takes part, and nothing is written behind it."""
+    x = torch.full((5, 64), 3.0, dtype=TYPES[dtype], device="cuda")
+    tokens = torch.tensor([-1, 0, 3, -1, -7], dtype=torch.int32, device="cuda")
+    f, loss, rewards = torch.ones(5, device="cuda"), torch.full((1,), 9.0, device="cuda"), torch.full((2,), 9.0, device="cuda")
+    want = [0.0, -math.inf, -math.inf, 0.0, -math.inf]
+    lp, stats = torch.full((5,), 9.0, device="cuda"), torch.full((5, 2), 9.0, device="cuda")
+    T.token_logprobs(None, x[:, :0], None, tokens, lp, stats=stats)
+    assert lp.tolist() == want and stats.tolist() == [[0.0, math.inf]] * 5
+    T.token_logprobs_backward(None, x[:, :0], None, tokens, stats, f, x[:, :0])
+    for grad in (None, x[:, :0]):
+        lp.fill_(9.0)
+        T.policy_loss(None, x[:, :0], None, tokens, f, f, loss, lp, grad_logits=grad)
+        assert lp.tolist() == want and float(loss) == 0.0
+        lp.fill_(9.0)
+        T.preference_loss(None, x[:, :0], None, tokens, f, torch.tensor([0, 2, 5], dtype=torch.int32, device="cuda"), loss, rewards, lp, grad_logits=grad)
+        assert lp.tolist() == want and rewards.tolist() == [0.0, 0.0] and abs(float(loss) - math.log(2.0)) < 1e-6
+    assert bool((x == 3.0).all())
