@@ -16,79 +16,16 @@
 // binary32 (a logit of the type's lowest value may be further below m than that) and the row's
 // weight is not zero.  Of the others one without a token or of weight 0 reports 0 and is not read, any
 // other -inf.
-#include "tdfa_internal.h"
+#include "rows_device.h"
 
 #include <algorithm>
 #include <cmath>
-#include <tuple>
 #include <type_traits>
 
 namespace tdfa {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr float kLog2e = 1.44269504088896341f;
-constexpr float kLowest = -3.402823466e38f;
-
-// Logits are read and gradients written in groups of 16 bytes.
-template <int DTYPE> struct Elem { using type = float; static constexpr int kGroup = 4; };
-template <> struct Elem<TDFA_BF16> { using type = uint16_t; static constexpr int kGroup = 8; };
-
-__device__ __forceinline__ float to_f32(float x) { return x; }
-__device__ __forceinline__ float to_f32(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
-__device__ __forceinline__ void store_rounded(float* p, float x) { *p = x; }
-__device__ __forceinline__ void store_rounded(uint16_t* p, float x)
-{
-    const __bf16 r = (__bf16)x;                              // nearest even
-    *p = __builtin_bit_cast(uint16_t, r);
-}
-__device__ __forceinline__ uint32_t rounded_pair(float lo, float hi)
-{
-    typedef __bf16 pair __attribute__((ext_vector_type(2)));
-    const pair r = {(__bf16)lo, (__bf16)hi};
-    return __builtin_bit_cast(uint32_t, r);
-}
-
-template <int DTYPE>
-__device__ __forceinline__ void unpack(uint4 x, float (&z)[Elem<DTYPE>::kGroup])
-{
-    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        if constexpr (DTYPE == TDFA_F32) {
-            z[k] = __uint_as_float(w[k]);
-        } else {
-            z[2 * k] = __uint_as_float(w[k] << 16);
-            z[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
-        }
-    }
-}
-
-template <int DTYPE>
-__device__ __forceinline__ uint4 pack(const float (&g)[Elem<DTYPE>::kGroup])
-{
-    if constexpr (DTYPE == TDFA_F32) return make_uint4(__float_as_uint(g[0]), __float_as_uint(g[1]), __float_as_uint(g[2]), __float_as_uint(g[3]));
-    else return make_uint4(rounded_pair(g[0], g[1]), rounded_pair(g[2], g[3]), rounded_pair(g[4], g[5]), rounded_pair(g[6], g[7]));
-}
-
-template <int DTYPE> constexpr uint32_t kNegInf = DTYPE == TDFA_F32 ? 0xFF800000u : 0xFF80FF80u;
-
-// Element j of a group.
-template <int DTYPE>
-__device__ __forceinline__ float element_of(uint4 x, int32_t j)
-{
-    if constexpr (DTYPE == TDFA_F32) {
-        return __uint_as_float(j == 0 ? x.x : j == 1 ? x.y : j == 2 ? x.z : x.w);
-    } else {
-        const uint32_t w = j < 2 ? x.x : j < 4 ? x.y : j < 6 ? x.z : x.w;
-        return __uint_as_float(j & 1 ? w & 0xFFFF0000u : w << 16);
-    }
-}
-__device__ __forceinline__ uint4 where(uint4 mask, uint32_t y, uint4 x)         // y under the mask, x elsewhere
-{
-    return make_uint4((y & mask.x) | (x.x & ~mask.x), (y & mask.y) | (x.y & ~mask.y), (y & mask.z) | (x.z & ~mask.z), (y & mask.w) | (x.w & ~mask.w));
-}
-
 // What the kernels are handed.  A launch whose arguments take at most 112 bytes, and whose kernel asks for nothing else (the size of its
 // grid, say), costs the host 2.6 us, a larger one 3.3; so strides are in units of 16 bytes, rows are numbered by the workgroups of a grid
 // that has no others, and what a call keeps of a row lies together.  A workgroup does one thing and ends: a loop over rows would
@@ -136,21 +73,6 @@ struct PolicyRowArgs : PolicyTerms {
 };
 static_assert(sizeof(PolicyScoreArgs) <= 112 && sizeof(PolicyRowArgs) <= 112, "see above");
 
-template <int DTYPE>
-__device__ __forceinline__ const typename Elem<DTYPE>::type* row_at(const void* rows, uint32_t i, uint32_t stride16)
-{
-    return reinterpret_cast<const typename Elem<DTYPE>::type*>(static_cast<const char*>(rows) + (uint64_t)i * stride16 * 16u);
-}
-template <int DTYPE>
-__device__ __forceinline__ typename Elem<DTYPE>::type* row_at(void* rows, uint32_t i, uint32_t stride16)
-{
-    return reinterpret_cast<typename Elem<DTYPE>::type*>(static_cast<char*>(rows) + (uint64_t)i * stride16 * 16u);
-}
-__device__ __forceinline__ const uint32_t* bits_of(const uint32_t* allow, int32_t q, int32_t n_tokens)
-{
-    return allow + (int64_t)q * ((((int64_t)n_tokens + 31) / 32 + 3) / 4 * 4);
-}
-
 // What is known about a row before its logits are read.
 struct Row {
     const uint32_t* bits;      // its state's allowed bits, or NULL: every token is allowed
@@ -178,11 +100,6 @@ __device__ __forceinline__ Row row_of(const RowArgs& a, const float* weights, ui
     return r;
 }
 
-__device__ __forceinline__ bool allowed(const uint32_t* bits, int32_t t)
-{
-    return !bits || (bits[t >> 5] >> (t & 31) & 1);
-}
-
 // The logit of a row's token, -inf if it is not allowed or NaN: the row takes part if it is above -inf (unless lp overflows).
 template <typename E>
 __device__ __forceinline__ float token_logit(const Row& r, const E* row)
@@ -193,92 +110,6 @@ __device__ __forceinline__ float token_logit(const Row& r, const E* row)
     word = __builtin_amdgcn_readfirstlane(word);
     z = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(z)));
     return (word >> (r.token & 31) & 1) && z == z ? z : -INFINITY;
-}
-
-// Masks of four 16-bit elements by their four allowed bits: an entry of 8 bytes per bit pattern.  16 entries lie in 32
-// different banks, so that lanes never wait for one another.
-__device__ __forceinline__ void fill_masks(uint2 (&masks)[16])
-{
-    const uint32_t n = threadIdx.x;
-    if (n < 16) masks[n] = make_uint2((n & 1 ? 0xFFFFu : 0u) | (n & 2 ? 0xFFFF0000u : 0u), (n & 4 ? 0xFFFFu : 0u) | (n & 8 ? 0xFFFF0000u : 0u));
-}
-
-// -inf in place of the elements that are not allowed.
-template <int DTYPE>
-__device__ __forceinline__ uint4 keep_allowed(uint4 x, uint32_t bits, const uint2 (&masks)[16])
-{
-    constexpr uint32_t none = kNegInf<DTYPE>;
-    if constexpr (DTYPE == TDFA_F32) {
-        return make_uint4(bits & 1 ? x.x : none, bits & 2 ? x.y : none, bits & 4 ? x.z : none, bits & 8 ? x.w : none);
-    } else {
-        const uint2 a = masks[bits & 15], b = masks[bits >> 4];
-        return make_uint4((x.x & a.x) | (none & ~a.x), (x.y & a.y) | (none & ~a.y), (x.z & b.x) | (none & ~b.x), (x.w & b.y) | (none & ~b.y));
-    }
-}
-
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-
-// The whole groups of a row, and their allowed bits, as buffers: a read behind the end gives 0 and a write there is dropped, both
-// without reaching the memory, so that no access needs a branch and the compiler knows how many are in flight.  (A row is at most
-// 2^26 bytes long.)
-struct RowBuffers {
-    __amdgpu_buffer_rsrc_t x, bits;
-};
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const void* base, uint32_t bytes)
-{
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, (int)bytes, 0x00027000);
-}
-template <int DTYPE>
-__device__ __forceinline__ RowBuffers row_buffers(const void* row, const uint32_t* bits, int32_t n_groups)
-{
-    return {buffer_of(row, (uint32_t)n_groups * 16u), buffer_of(bits, DTYPE == TDFA_F32 ? (uint32_t)(n_groups + 1) / 2u : (uint32_t)n_groups)};
-}
-constexpr uint32_t kNowhere = 0x80000000u;
-constexpr int kPastCaches = 2;             // the nt bit of an access
-// ONCE: what is read is not read again, and leaves the caches to what is.
-template <bool ONCE>
-__device__ __forceinline__ uint4 group_at(__amdgpu_buffer_rsrc_t rows, uint32_t offset)
-{
-    const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(rows, (int)offset, 0, ONCE ? kPastCaches : 0);
-    return make_uint4(x.x, x.y, x.z, x.w);
-}
-// Gradients are written past the caches: 1,024 rows of 128,256 tokens in bf16 113 us, 95 so.
-__device__ __forceinline__ void set_group(__amdgpu_buffer_rsrc_t rows, int32_t g, uint4 x)
-{
-    const u32x4 y = {x.x, x.y, x.z, x.w};
-    __builtin_amdgcn_raw_buffer_store_b128(y, rows, g * 16, 0, kPastCaches);
-}
-// What is made of one group is finished before the next is begun: the registers of eight elements at a time, not of all.
-__device__ __forceinline__ void next_group() { __builtin_amdgcn_sched_barrier(0); }
-
-// The allowed bits of groups g0 + threadIdx.x + k NT of a row, k < U, and the groups; those without an allowed token are not fetched.
-template <int DTYPE, int NT, int U, bool BITS>
-__device__ __forceinline__ void fetch_bits(const RowBuffers& row, int32_t g0, uint32_t (&b)[U])
-{
-    const int32_t g = g0 + (int32_t)threadIdx.x;
-#pragma unroll
-    for (int k = 0; k < U; ++k) {
-        const int32_t at = g + k * NT;
-        if constexpr (BITS) b[k] = __builtin_amdgcn_raw_buffer_load_b8(row.bits, DTYPE == TDFA_F32 ? at >> 1 : at, 0, 0);
-        else b[k] = 0;
-    }
-}
-template <int DTYPE, int NT, int U, bool BITS, bool ONCE = false>
-__device__ __forceinline__ void fetch_groups(const RowBuffers& row, int32_t g0, int32_t n_groups, uint4 (&x)[U], uint32_t (&b)[U])
-{
-    const int32_t g = g0 + (int32_t)threadIdx.x;
-#pragma unroll
-    for (int k = 0; k < U; ++k) {
-        const int32_t at = g + k * NT;
-        if constexpr (BITS && DTYPE == TDFA_F32) b[k] = at < n_groups ? b[k] >> ((at & 1) * 4) & 15u : 0u;
-        x[k] = group_at<ONCE>(row.x, BITS && b[k] == 0 ? kNowhere : (uint32_t)at * 16u);
-    }
-}
-template <int DTYPE, int NT, int U, bool BITS, bool ONCE = false>
-__device__ __forceinline__ void fetch(const RowBuffers& row, int32_t g0, int32_t n_groups, uint4 (&x)[U], uint32_t (&b)[U])
-{
-    fetch_bits<DTYPE, NT, U, BITS>(row, g0, b);
-    fetch_groups<DTYPE, NT, U, BITS, ONCE>(row, g0, n_groups, x, b);
 }
 
 // Where a row's token lies among the groups g0 + n + k NT that thread n takes: in the k-th of one thread, whose mask has its element's bits
@@ -305,32 +136,6 @@ __device__ __forceinline__ void leave_own(const Own& own, uint4& x, uint32_t& b)
     else x = where(own.mask, kNegInf<DTYPE>, x);
 }
 
-// Puts -inf where a token of group g is not allowed or the row is at its end.  False: so it is in the whole wavefront.
-template <int DTYPE, bool BITS>
-__device__ __forceinline__ bool settle(uint4& x, uint32_t b, int32_t g, int32_t n_groups, const uint2 (&masks)[16])
-{
-    if constexpr (BITS) {
-        if (!__ballot(b != 0)) return false;
-        x = keep_allowed<DTYPE>(x, b, masks);
-        asm volatile("" : "+v"(x.x), "+v"(x.y), "+v"(x.z), "+v"(x.w));      // masked once, not again in every element
-    } else {
-        const int32_t g0 = __builtin_amdgcn_readfirstlane(g);             // (lanes are in the order of their groups)
-        if (g0 >= n_groups) return false;
-        if (g0 + 63 >= n_groups && g >= n_groups) {
-            constexpr uint32_t none = kNegInf<DTYPE>;
-            x = make_uint4(none, none, none, none);
-        }
-    }
-    return true;
-}
-
-// -ref c2 as it is rounded by itself: the compiler, which does not see that it is a product, makes no product and sum one around it.
-__device__ __forceinline__ float offset_of(float ref, float c2)
-{
-    float nb = -(ref * c2);
-    asm("" : "+v"(nb));
-    return nb;
-}
 // Sum of 2^(z c2 + nb), nb = -ref c2 rounded: the rounding moves all terms, the token's own among them, by the same factor.
 template <int DTYPE>
 __device__ __forceinline__ void add_group(uint4 x, float c2, float nb, float (&s)[2])
@@ -349,16 +154,6 @@ __device__ __forceinline__ void add_group_careful(uint4 x, float c2, float ref, 
 #pragma unroll
     for (int j = 0; j < Elem<DTYPE>::kGroup; ++j) s += __builtin_amdgcn_exp2f((fmaxf(z[j], -INFINITY) - ref) * c2);
 }
-template <int DTYPE>
-__device__ __forceinline__ float max_group(uint4 x, float m)
-{
-    float z[Elem<DTYPE>::kGroup];
-    unpack<DTYPE>(x, z);
-#pragma unroll
-    for (int j = 0; j < Elem<DTYPE>::kGroup; ++j) m = fmaxf(m, z[j]);
-    return m;
-}
-
 // Over fetched groups, but for the token's own element.  Bit k of `some`: the wavefront has another allowed token in its k-th groups.
 template <int DTYPE, int NT, int U, bool BITS>
 __device__ __forceinline__ void add_groups(uint4 (&x)[U], uint32_t (&b)[U], int32_t g0, int32_t n_groups, const uint2 (&masks)[16], int32_t token, float c2,
@@ -376,13 +171,6 @@ __device__ __forceinline__ void add_groups(uint4 (&x)[U], uint32_t (&b)[U], int3
     }
 }
 
-// 2 to the power of (from - to) c2: what a sum relative to `from` is scaled by.  The roundings of from c2 and to c2 are in the terms (not
-// if SAFE), so it is the difference of these.
-template <bool SAFE>
-__device__ __forceinline__ float rescale(float from, float to, float c2)
-{
-    return __builtin_amdgcn_exp2f(SAFE ? (from - to) * c2 : offset_of(to, c2) - offset_of(from, c2));
-}
 // The same relative to the largest logit that the thread has met, m: a running maximum, and a sum that is scaled where it moves, four groups
 // at a time so that sums do not wait for all loads.  Exponents are z c2 - m c2 with m c2 rounded (SAFE: differences taken first and NaN
 // passed over, which takes half as many instructions again).
@@ -416,53 +204,6 @@ __device__ __forceinline__ void add_groups_running(uint4 (&x)[U], uint32_t (&b)[
             next_group();
         }
     }
-}
-
-// The element behind the last whole group that belongs to this thread, -inf if there is none or it is token `without`.
-template <int DTYPE>
-__device__ __forceinline__ float last_element(int32_t n_tokens, const typename Elem<DTYPE>::type* row, const uint32_t* bits, int32_t without)
-{
-    const int32_t t = n_tokens / Elem<DTYPE>::kGroup * Elem<DTYPE>::kGroup + (int32_t)threadIdx.x;
-    return t < n_tokens && t != without && allowed(bits, t) ? to_f32(row[t]) : -INFINITY;
-}
-
-// Over the 64 lanes of a wavefront, all of them active, by data-parallel primitives (no LDS); the result is uniform.
-template <int CTRL>
-__device__ __forceinline__ float lane_swap(float v)
-{
-    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, true));
-}
-__device__ __forceinline__ float lane_value(float v, int lane) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane)); }
-__device__ __forceinline__ float wave_sum(float v)
-{
-    v += lane_swap<0xB1>(v);           // quad_perm [1,0,3,2]
-    v += lane_swap<0x4E>(v);           // quad_perm [2,3,0,1]
-    v += lane_swap<0x141>(v);          // row_half_mirror
-    v += lane_swap<0x140>(v);          // row_mirror
-    return (lane_value(v, 0) + lane_value(v, 16)) + (lane_value(v, 32) + lane_value(v, 48));
-}
-__device__ __forceinline__ float wave_max(float v)
-{
-    v = fmaxf(v, lane_swap<0xB1>(v));
-    v = fmaxf(v, lane_swap<0x4E>(v));
-    v = fmaxf(v, lane_swap<0x141>(v));
-    v = fmaxf(v, lane_swap<0x140>(v));
-    return fmaxf(fmaxf(lane_value(v, 0), lane_value(v, 16)), fmaxf(lane_value(v, 32), lane_value(v, 48)));
-}
-// Sum (MAX: maximum) over the workgroup, in every thread and in one order.  Two barriers.
-template <int NT, bool MAX>
-__device__ __forceinline__ float block_reduce(float v, float (&part)[NT / 64])
-{
-    v = MAX ? wave_max(v) : wave_sum(v);
-    if constexpr (NT > 64) {
-        __syncthreads();
-        if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
-        __syncthreads();
-        v = part[0];
-#pragma unroll
-        for (int w = 1; w < NT / 64; ++w) v = MAX ? fmaxf(v, part[w]) : v + part[w];
-    }
-    return v;
 }
 
 // Whether a row's own term and the sum of the others, both relative to about its own logit, are what they should be: not so where the
@@ -534,39 +275,6 @@ __device__ __forceinline__ float careful_sum(const RowBuffers& row, int32_t n_gr
     }
     *ref = m;
     return block_reduce<NT, false>(s, part);
-}
-
-// The sum of running ones over the workgroup, relative to its largest maximum, which goes to *ref, in every thread.  One barrier: the
-// wavefronts leave a maximum and a sum each, and the lanes of every wavefront join those.
-template <int NT, bool SAFE>
-__device__ __forceinline__ float sum_of_running(float m, float s, float c2, float* ref, float (&part)[2][NT / 64])
-{
-    float top = wave_max(m);
-    s = wave_sum(s * rescale<SAFE>(m, top, c2));
-    if constexpr (NT > 64) {
-        constexpr int W = NT / 64;
-        static_assert(W == 4 || W == 8 || W == 16);
-        if ((threadIdx.x & 63) == 0) {
-            part[0][threadIdx.x >> 6] = top;
-            part[1][threadIdx.x >> 6] = s;
-        }
-        __syncthreads();
-        const float mine = part[0][threadIdx.x & (W - 1)];
-        s = part[1][threadIdx.x & (W - 1)];
-        top = fmaxf(mine, lane_swap<0xB1>(mine));
-        top = fmaxf(top, lane_swap<0x4E>(top));
-        if constexpr (W >= 8) top = fmaxf(top, lane_swap<0x141>(top));
-        if constexpr (W >= 16) top = fmaxf(top, lane_swap<0x140>(top));
-        s *= rescale<SAFE>(mine, top, c2);
-        s += lane_swap<0xB1>(s);
-        s += lane_swap<0x4E>(s);
-        if constexpr (W >= 8) s += lane_swap<0x141>(s);
-        if constexpr (W >= 16) s += lane_swap<0x140>(s);
-        top = lane_value(top, 0);
-        s = lane_value(s, 0);
-    }
-    *ref = top;
-    return SAFE ? s : s * __builtin_amdgcn_exp2f(-fmaf(top, c2, offset_of(top, c2)));      // the rounding of top c2 is in all terms
 }
 
 // What the sums of a row are taken relative to.  In 16 bits its own token's logit: no maximum is needed, and what the exponents lose where
@@ -786,7 +494,6 @@ __device__ __forceinline__ Slope slope_of(float d, float ref, float ls, float sc
     }
 }
 
-__device__ __forceinline__ float shared_by_wave(float x) { return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(x))); }
 __device__ __forceinline__ Slope shared_by_wave(Slope q) { return {shared_by_wave(q.d), shared_by_wave(q.ref), shared_by_wave(q.k), shared_by_wave(q.fold)}; }
 
 // Gradient of one element other than the token's own.
@@ -1273,21 +980,6 @@ __global__ void __launch_bounds__(NT, 4) policy_row_kernel(PolicyRowArgs a)
     for (int k = 0; k < R; ++k) writer.write(to, (int32_t)threadIdx.x + k * NT, x[k], some >> k & 1, k == own.k, own.mask, own_slope);
     if (behind < a.n_tokens) store_rounded(out + behind, behind == r.token ? own_slope : gradient_of<DTYPE>(last, q, c2));
 }
-
-// A launch that reports its own error (asking for the last one afterwards costs the host 0.4 us more).
-template <typename... Params, typename... Args>
-int launch(void (*kernel)(Params...), dim3 grid, unsigned threads, hipStream_t stream, Args... args)
-{
-    std::tuple<Params...> params(args...);
-    return std::apply([&](Params&... p) -> int {
-        void* at[] = {&p...};
-        TDFA_HIP(hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, dim3(threads), at, 0, stream));
-        return TDFA_OK;
-    }, params);
-}
-
-// Workgroups of a launch, of 1,024 threads at most: a grid counts less than 2^32 threads, so that more rows go by several launches.
-constexpr int64_t kMaxBlocks = 1 << 21;
 
 RowArgs row_args(const TokenRows& a, int64_t from)
 {
