@@ -416,6 +416,67 @@ TDFA_API int tdfa_sample_step_at(const tdfa_table *table, const void *logits_dev
 TDFA_API int tdfa_sample_noise(int32_t batch, int32_t n_tokens, uint64_t seed, uint64_t offset,
                       float *noise_dev, void *stream);
 
+/* ---- draws from given random numbers, and the most likely tokens -------------------------------- */
+
+/* Two more ways to choose tokens of rows of logits, under a constraint or without one.  Arguments they share:
+ *   table       : the constraint, dense or packed, or NULL: every token is allowed.
+ *   logits_dev, dtype, row_stride : as tdfa_mask_step ([rows][row_stride], rows 16-byte aligned, the first n_tokens of
+ *                 each row are used, nothing behind them is read; rows less than 2^36 bytes apart).
+ *   n_tokens    : 0 .. 2^24; that of the table if there is one.
+ *   states_dev  : device, int32 [rows]; may be NULL without a table.
+ *   workspace_dev, workspace_bytes : device memory for the call's own use, 16-byte aligned, of at least
+ *                 tdfa_select_workspace_bytes(rows, n_tokens) bytes; NULL where that is 0.  It need not be cleared, and must not be used by
+ *                 anything else until the call's work is done.
+ * Row i has logits l, allowed set A (of states[i]), the largest logit m in A, and weights w_t = exp((l_t - m) / T) in A.
+ * NaN counts as -inf and -0 as +0, and a logit outside A has no effect whatever it is.  Tokens are in the order of their
+ * logits, the largest first, and of their ids among equal logits.  Where m is +inf the tokens that have it weigh 1 and
+ * all others nothing.  Weights and their sums are held in 64 bits.
+ * What a call writes must not overlap anything else that it reads or writes, but for new_states in place of states.
+ * The calls enqueue on `stream` and return, allocate nothing and may be captured into a graph.  Results depend on the arguments
+ * only, not on the order in which anything runs.  Errors: INVALID_ARG, DEVICE. */
+
+/* Workspace in bytes; -1 if rows or n_tokens is negative. */
+TDFA_API int64_t tdfa_select_workspace_bytes(int32_t rows, int32_t n_tokens);
+
+/* The decode step with the token drawn with a number that the caller gives, cut by top-k, top-p and min-p:
+ *     K = { t in A : l_t is at least the top_k-th largest logit in A }         (counted with multiplicity)
+ *     P = { t in K : the tokens of K with a logit above l_t weigh less than top_p of what K weighs }, and those of logit m
+ *     N = { t in P : w_t >= min_p }
+ *     tokens[i] = the first t of N, in the order of the tokens, up to which (t included) the weights of N add up to more than
+ *                 u times their sum;   new_states[i] = delta_T[q][tokens[i]];   logprobs[i] = ln(w_t / the sum of N).
+ * So u = 0 gives the most likely token, and tokens with equal logits are cut together or not at all.  A number within 2^-40 or so of the border
+ * between two tokens may give either, always the same one for the same arguments.
+ * If A is empty: tokens[i] = TDFA_NO_TOKEN, new_states[i] = q, logprobs[i] = 0.  If q is no row of the table: TDFA_NO_TOKEN,
+ * TDFA_DEAD and 0.  If m is -inf: the lowest id in A, with a log-probability of -inf.
+ *   uniforms_dev   : device, float [rows], 0 .. 1 (less counts as 0, as NaN does, and more as 1; at 1 the last token of N is drawn, or
+ *                    one from which on those of N weigh less than 2^-40 of it).
+ *   temperature    : T >= 0, finite.  0: the first token in the order, with a log-probability of 0.
+ *   top_k          : >= 0; 0: no cut.   top_p : 0 .. 1; 1: no cut.   min_p : 0 .. 1; 0: no cut.
+ *   params_dev     : device, float [rows][4], 16-byte aligned, or NULL.  The temperature, top_k (a whole number), top_p and min_p of every row,
+ *                    in place of those above, which are not read then.  A temperature that is not above 0 counts as 0, a top_k outside 1 .. 2^31 as
+ *                    0, top_p and min_p are clamped to 0 .. 1, and NaN is no cut.
+ *   tokens_dev     : device, int32 [rows], written.
+ *   new_states_dev : device, int32 [rows], written; may equal states_dev; NULL without a table.
+ *   logprobs_dev   : device, float [rows], written, or NULL. */
+TDFA_API int tdfa_draw_step(const tdfa_table *table, const void *logits_dev, int dtype, int32_t rows, int32_t n_tokens,
+                   int64_t row_stride, const int32_t *states_dev, const float *uniforms_dev,
+                   float temperature, int32_t top_k, float top_p, float min_p, const float *params_dev,
+                   int32_t *tokens_dev, int32_t *new_states_dev, float *logprobs_dev,
+                   void *workspace_dev, int64_t workspace_bytes, void *stream);
+
+#define TDFA_TOP_MAX 256   /* most tokens a row that tdfa_top_logprobs lists, and most that tdfa_distill_loss takes */
+
+/* The k first tokens of A with a logit above -inf, in the order of the tokens, and their log-probabilities
+ *     lp = (l_t - m) / T - ln(the sum over A of w)
+ * which are those that tdfa_token_logprobs gives (NaN where m is +inf).  Places that are left over get TDFA_NO_TOKEN and -inf.
+ *   k            : 1 .. TDFA_TOP_MAX.
+ *   temperature  : > 0, finite.
+ *   ids_dev      : device, int32 [rows][k], written.
+ *   logprobs_dev : device, float [rows][k], written. */
+TDFA_API int tdfa_top_logprobs(const tdfa_table *table, const void *logits_dev, int dtype, int32_t rows, int32_t n_tokens,
+                   int64_t row_stride, const int32_t *states_dev, float temperature, int32_t k,
+                   int32_t *ids_dev, float *logprobs_dev, void *workspace_dev, int64_t workspace_bytes, void *stream);
+
 /* ---- scoring and training the constrained policy ---------------------------------------------- */
 
 /* A language model that decodes under a constraint is the policy that tdfa_sample_step draws from:

@@ -19,6 +19,7 @@ NO_TOKEN = -1
 F32, BF16 = 0, 1
 PATH_AUTO, PATH_WALK, PATH_PAIRS, PATH_STAGED = 0, 1, 2, 3
 OK = 0
+TOP_MAX = 256
 
 _lib = None
 _LOGITS = {torch.float32: F32, torch.bfloat16: BF16}        # element types of logits
@@ -105,6 +106,11 @@ def lib():
         L.tdfa_policy_loss.argtypes = (rows + [C.c_void_p] * 4 + [C.c_float] * 3 + [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64] + work)
         L.tdfa_preference_loss.argtypes = (rows + [C.c_void_p, C.c_void_p, C.c_int32, C.c_float, C.c_float] +
                                            [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64] + work)
+        chosen = [C.c_void_p, C.c_void_p, C.c_int, C.c_int32, C.c_int32, C.c_int64, C.c_void_p]
+        L.tdfa_select_workspace_bytes.restype = C.c_int64
+        L.tdfa_select_workspace_bytes.argtypes = [C.c_int32, C.c_int32]
+        L.tdfa_draw_step.argtypes = chosen + [C.c_void_p, C.c_float, C.c_int32, C.c_float, C.c_float] + [C.c_void_p] * 4 + work
+        L.tdfa_top_logprobs.argtypes = chosen + [C.c_float, C.c_int32, C.c_void_p, C.c_void_p] + work
         _lib = L
     return _lib
 
@@ -508,6 +514,82 @@ def preference_loss(table: Table | None, logits: torch.Tensor, states: torch.Ten
     ws, n, _held = _workspace(workspace, rows, pairs, logits, stream)
     _check(lib().tdfa_preference_loss(*a, *vectors, pairs, float(beta), float(smoothing), *out, *_grad_args(logits, grad_logits),
                                       ws, n, _stream(stream)))
+
+
+def _chosen_args(table, logits, states):
+    """The leading arguments that the calls which choose tokens of rows share."""
+    dtype = _LOGITS.get(logits.dtype)
+    if dtype is None:
+        raise TypeError("logits must be float32 or bfloat16")
+    if logits.dim() != 2 or not logits.is_cuda:
+        raise ValueError("logits must be [rows, n] on the GPU")
+    (rows, n), (stride, inner), device = logits.shape, logits.stride(), logits.get_device()
+    if device != torch.cuda.current_device():
+        raise ValueError("logits must be on the current device")
+    if inner != 1 and n > 1:
+        raise ValueError("logits must have unit inner stride")
+    if rows <= 1:
+        stride = max(stride, n)
+    handle = None
+    if table is not None:
+        if n < table.n_tokens:
+            raise ValueError("logits have fewer columns than the table has tokens")
+        handle, n = table._h, table.n_tokens
+    return handle, logits.data_ptr(), dtype, rows, n, stride, _vector(states, "states", torch.int32, rows, device, table is None)
+
+
+def select_workspace_bytes(rows: int, n_tokens: int) -> int:
+    """tdfa_select_workspace_bytes."""
+    return int(lib().tdfa_select_workspace_bytes(rows, n_tokens))
+
+
+def _workspace_of(need: int, workspace, logits, stream):
+    """Address and size of the caller's workspace, or of one of `need` bytes from torch's allocator, which hands it out again only
+    behind the work of the stream that it was allocated on; and the tensor, to be held until the call is made."""
+    if workspace is not None:
+        if not workspace.is_contiguous() or workspace.device != logits.device:
+            raise ValueError("workspace must be contiguous on the logits' device")
+    elif need == 0:
+        return None, 0, None
+    elif stream is None:
+        workspace = torch.empty(need, dtype=torch.uint8, device=logits.device)
+    else:
+        if not isinstance(stream, torch.cuda.Stream):
+            stream = torch.cuda.ExternalStream(_stream(stream), device=logits.device)
+        with torch.cuda.stream(stream):
+            workspace = torch.empty(need, dtype=torch.uint8, device=logits.device)
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
+
+
+def draw_step(table: Table | None, logits: torch.Tensor, states: torch.Tensor | None, uniforms: torch.Tensor, tokens: torch.Tensor,
+              new_states: torch.Tensor | None, temperature: float = 1.0, top_k: int = 0, top_p: float = 1.0, min_p: float = 0.0,
+              params: torch.Tensor | None = None, logprobs: torch.Tensor | None = None, workspace: torch.Tensor | None = None, stream=None) -> None:
+    """tdfa_draw_step: the decode step with the token drawn with a number in 0 .. 1 that the caller gives, after cuts by
+    top-k, top-p and min-p.  logits: [rows, >= n_tokens] float32 or bfloat16 on the GPU; table None: no constraint, every column is a token,
+    and states and new_states may be None.  states, tokens, new_states: int32 [rows], uniforms: float32 [rows];
+    params: float32 [rows, 4], the temperature, top_k, top_p and min_p of every row, in place of the four arguments;
+    tokens, new_states (which may be states) and logprobs (float32 [rows], if given: of the token in what it was drawn from) are written."""
+    a = _chosen_args(table, logits, states)
+    rows, dev = a[3], logits.get_device()
+    vectors = (_vector(params, "params", torch.float32, 4 * rows, dev, True), _vector(tokens, "tokens", torch.int32, rows, dev),
+               _vector(new_states, "new_states", torch.int32, rows, dev, table is None), _vector(logprobs, "logprobs", torch.float32, rows, dev, True))
+    ws, n, _held = _workspace_of(lib().tdfa_select_workspace_bytes(rows, a[4]), workspace, logits, stream)
+    _check(lib().tdfa_draw_step(*a, _vector(uniforms, "uniforms", torch.float32, rows, dev), float(temperature), int(top_k), float(top_p),
+                                float(min_p), *vectors, ws, n, _stream(stream)))
+
+
+def top_logprobs(table: Table | None, logits: torch.Tensor, states: torch.Tensor | None, ids: torch.Tensor, logprobs: torch.Tensor,
+                 temperature: float = 1.0, workspace: torch.Tensor | None = None, stream=None) -> None:
+    """tdfa_top_logprobs: the most likely tokens of every row and their log-probabilities.  table, logits, states as draw_step;
+    ids: int32 [rows, k] and logprobs: float32 [rows, k] are written, k 1 .. TOP_MAX."""
+    a = _chosen_args(table, logits, states)
+    rows, dev = a[3], logits.get_device()
+    if ids.dim() != 2 or ids.shape != logprobs.shape or ids.shape[0] < rows:
+        raise ValueError("ids and logprobs must be [rows, k]")
+    k = ids.shape[1]
+    ws, n, _held = _workspace_of(lib().tdfa_select_workspace_bytes(rows, a[4]), workspace, logits, stream)
+    _check(lib().tdfa_top_logprobs(*a, float(temperature), k, _vector(ids, "ids", torch.int32, rows * k, dev),
+                                   _vector(logprobs, "logprobs", torch.float32, rows * k, dev), ws, n, _stream(stream)))
 
 
 def advance_tokens(table: Table, states: torch.Tensor, tokens: torch.Tensor, history: torch.Tensor,

@@ -1885,6 +1885,143 @@ int64_t tdfa_loss_workspace_bytes(int32_t rows, int32_t n_pairs)
     return rows < 0 || n_pairs < 0 ? -1 : tdfa::loss_workspace(rows, n_pairs);
 }
 
+namespace {
+
+// Argument checks and kernel arguments shared by the calls that choose tokens of rows.
+int prepare_logits(const tdfa_table* table, const void* logits_dev, int dtype, int32_t rows, int32_t n_tokens, int64_t row_stride,
+                   const int32_t* states_dev, float temperature, const void* workspace_dev, int64_t workspace_bytes, tdfa::LogitRows* a)
+{
+    if (dtype != TDFA_F32 && dtype != TDFA_BF16) return fail(TDFA_E_INVALID_ARG, "unknown dtype %d", dtype);
+    if (rows < 0 || n_tokens < 0) return fail(TDFA_E_INVALID_ARG, "rows %d or n_tokens %d is negative", rows, n_tokens);
+    if (n_tokens > kMaxTokens) return fail(TDFA_E_INVALID_ARG, "n_tokens %d exceeds %d", n_tokens, kMaxTokens);
+    if (table && table->n_tokens != n_tokens) return fail(TDFA_E_INVALID_ARG, "n_tokens %d differs from the table's %d", n_tokens, table->n_tokens);
+    if (row_stride < n_tokens) return fail(TDFA_E_INVALID_ARG, "row_stride %lld < n_tokens %d", (long long)row_stride, n_tokens);
+    const int64_t esz = dtype == TDFA_F32 ? 4 : 2;
+    if (rows > 1 && row_stride > kMaxRowBytes / esz) return fail(TDFA_E_INVALID_ARG, "row_stride %lld is too large", (long long)row_stride);
+    if (rows > 0) {
+        if ((!logits_dev && n_tokens > 0) || (table && !states_dev)) return fail(TDFA_E_INVALID_ARG, "logits or states is NULL");
+        if ((reinterpret_cast<uintptr_t>(logits_dev) & 15) || (rows > 1 && ((row_stride * esz) & 15)))
+            return fail(TDFA_E_INVALID_ARG, "logits rows must be 16-byte aligned");
+        const int64_t need = tdfa::select_workspace(rows, n_tokens);
+        if (need > 0) {
+            if (!workspace_dev || workspace_bytes < need)
+                return fail(TDFA_E_INVALID_ARG, "workspace of %lld bytes, %lld are wanted", workspace_dev ? (long long)workspace_bytes : 0LL, (long long)need);
+            if (reinterpret_cast<uintptr_t>(workspace_dev) & 15) return fail(TDFA_E_INVALID_ARG, "workspace must be 16-byte aligned");
+        }
+    }
+    *a = tdfa::LogitRows();
+    if (table) {
+        a->allow = table->allow;
+        a->n_states = table->n_rows;
+    }
+    a->logits = logits_dev;
+    a->dtype = dtype;
+    a->row_stride = row_stride;
+    a->rows = rows;
+    a->n_tokens = n_tokens;
+    a->states = table ? states_dev : nullptr;
+    a->temperature = temperature;
+    return TDFA_OK;
+}
+
+// What a call reads or writes.
+struct Span {
+    const void* at;
+    int64_t bytes;
+    const char* name;
+};
+bool meet(const Span& x, const Span& y)
+{
+    const uintptr_t p = reinterpret_cast<uintptr_t>(x.at), q = reinterpret_cast<uintptr_t>(y.at);
+    return p && q && x.bytes > 0 && y.bytes > 0 && p < q + (uintptr_t)y.bytes && q < p + (uintptr_t)x.bytes;
+}
+// No output may overlap another one or an input.
+int check_apart(std::initializer_list<Span> outputs, std::initializer_list<Span> inputs)
+{
+    for (const Span* x = outputs.begin(); x != outputs.end(); ++x) {
+        for (const Span* y = outputs.begin(); y != x; ++y)
+            if (meet(*x, *y)) return fail(TDFA_E_INVALID_ARG, "%s overlaps %s", x->name, y->name);
+        for (const Span& y : inputs)
+            if (meet(*x, y)) return fail(TDFA_E_INVALID_ARG, "%s overlaps %s", x->name, y.name);
+    }
+    return TDFA_OK;
+}
+Span span_of(const tdfa::LogitRows& a)
+{
+    return {a.logits, ((a.rows - 1) * a.row_stride + a.n_tokens) * (a.dtype == TDFA_F32 ? 4 : 2), "the logits"};
+}
+
+}  // namespace
+
+int64_t tdfa_select_workspace_bytes(int32_t rows, int32_t n_tokens)
+{
+    return rows < 0 || n_tokens < 0 ? -1 : tdfa::select_workspace(rows, n_tokens);
+}
+
+int tdfa_draw_step(const tdfa_table* table, const void* logits_dev, int dtype, int32_t rows, int32_t n_tokens, int64_t row_stride,
+                   const int32_t* states_dev, const float* uniforms_dev, float temperature, int32_t top_k, float top_p, float min_p,
+                   const float* params_dev, int32_t* tokens_dev, int32_t* new_states_dev, float* logprobs_dev, void* workspace_dev,
+                   int64_t workspace_bytes, void* stream)
+{
+    clear_error();
+    if (!params_dev) {
+        if (!(temperature >= 0.0f) || temperature > 3.402823466e38f)
+            return fail(TDFA_E_INVALID_ARG, "temperature %g is negative or not finite", (double)temperature);
+        if (top_k < 0) return fail(TDFA_E_INVALID_ARG, "top_k %d is negative", top_k);
+        if (!(top_p >= 0.0f && top_p <= 1.0f) || !(min_p >= 0.0f && min_p <= 1.0f))
+            return fail(TDFA_E_INVALID_ARG, "top_p %g or min_p %g is outside 0 .. 1", (double)top_p, (double)min_p);
+    }
+    tdfa::LogitRows a;
+    int rc = prepare_logits(table, logits_dev, dtype, rows, n_tokens, row_stride, states_dev, temperature, workspace_dev, workspace_bytes, &a);
+    if (rc != TDFA_OK || rows == 0) return rc;
+    if (!uniforms_dev || !tokens_dev || (table && !new_states_dev)) return fail(TDFA_E_INVALID_ARG, "uniforms, tokens or new_states is NULL");
+    if (misaligned(params_dev, 16)) return fail(TDFA_E_INVALID_ARG, "params must be 16-byte aligned");
+    const int64_t each = (int64_t)rows * 4;
+    const Span states = {a.states, each, "states"}, next = {table ? new_states_dev : nullptr, each, "new_states"};
+    const Span logits = span_of(a), uniforms = {uniforms_dev, each, "uniforms"}, params = {params_dev, 4 * each, "params"};
+    rc = check_apart({{tokens_dev, each, "tokens"}, {logprobs_dev, each, "logprobs"}, next, {workspace_dev, workspace_bytes, "the workspace"}},
+                     {logits, uniforms, params});
+    if (rc == TDFA_OK)
+        rc = check_apart({{tokens_dev, each, "tokens"}, {logprobs_dev, each, "logprobs"}, {workspace_dev, workspace_bytes, "the workspace"}}, {states});
+    if (rc != TDFA_OK) return rc;
+    if (table && new_states_dev != states_dev && meet(next, states)) return fail(TDFA_E_INVALID_ARG, "new_states overlaps states without being the same");
+    tdfa::DrawRows d = {};
+    if (table) {
+        d.delta = table->delta;
+        d.targets = table->targets;
+        d.row_begin = table->row_begin;
+        d.dir = table->dir;
+        d.new_states = new_states_dev;
+    }
+    d.uniforms = uniforms_dev;
+    d.params = params_dev;
+    d.top_k = top_k;
+    d.top_p = top_p;
+    d.min_p = min_p;
+    d.tokens = tokens_dev;
+    d.logprobs = logprobs_dev;
+    return launch_draw_step(a, d, workspace_dev, static_cast<hipStream_t>(stream));
+}
+
+int tdfa_top_logprobs(const tdfa_table* table, const void* logits_dev, int dtype, int32_t rows, int32_t n_tokens, int64_t row_stride,
+                      const int32_t* states_dev, float temperature, int32_t k, int32_t* ids_dev, float* logprobs_dev, void* workspace_dev,
+                      int64_t workspace_bytes, void* stream)
+{
+    clear_error();
+    if (!(temperature > 0.0f) || temperature > 3.402823466e38f)
+        return fail(TDFA_E_INVALID_ARG, "temperature %g is not positive and finite", (double)temperature);
+    if (k < 1 || k > TDFA_TOP_MAX) return fail(TDFA_E_INVALID_ARG, "k %d is outside 1 .. %d", k, TDFA_TOP_MAX);
+    tdfa::LogitRows a;
+    int rc = prepare_logits(table, logits_dev, dtype, rows, n_tokens, row_stride, states_dev, temperature, workspace_dev, workspace_bytes, &a);
+    if (rc != TDFA_OK || rows == 0) return rc;
+    if (!ids_dev || !logprobs_dev) return fail(TDFA_E_INVALID_ARG, "ids or logprobs is NULL");
+    const int64_t each = (int64_t)rows * 4;
+    rc = check_apart({{ids_dev, each * k, "ids"}, {logprobs_dev, each * k, "logprobs"}, {workspace_dev, workspace_bytes, "the workspace"}},
+                     {span_of(a), {a.states, each, "states"}});
+    if (rc != TDFA_OK) return rc;
+    return launch_top_logprobs(a, k, ids_dev, logprobs_dev, workspace_dev, static_cast<hipStream_t>(stream));
+}
+
 int tdfa_token_logprobs(const tdfa_table* table, const void* logits_dev, int dtype, int32_t rows, int32_t n_tokens, int64_t row_stride,
                         const int32_t* states_dev, const int32_t* tokens_dev, float temperature, float* logprobs_dev, float* stats_dev,
                         void* workspace_dev, int64_t workspace_bytes, void* stream)

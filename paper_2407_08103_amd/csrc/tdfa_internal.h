@@ -299,6 +299,36 @@ int launch_policy_loss(const TokenRows& a, const PolicyArgs& p, float* loss, flo
 int launch_preference_loss(const TokenRows& a, const PairArgs& p, float* loss, float* logprobs, void* grad, int64_t grad_stride, void* workspace,
                            hipStream_t stream);
 
+// Rows of logits under a constraint or none, of which tokens are chosen (draw.hip).
+struct LogitRows {
+    const uint32_t* allow;              // allowed-bit rows of the table, or NULL: every token is allowed
+    int64_t n_states;
+    const void* logits;
+    int dtype;
+    int64_t row_stride;
+    int64_t rows;
+    int32_t n_tokens;
+    const int32_t* states;
+    float temperature;
+};
+struct DrawRows {
+    const int32_t* delta;               // the edges of the table, dense or packed as in MaskArgs, or all NULL: no table
+    const int32_t* targets;
+    const int64_t* row_begin;
+    const uint32_t* dir;
+    const float* uniforms;              // [rows]
+    const float* params;                // [rows][4]: temperature, top_k, top_p, min_p; or NULL: those below, and the temperature
+    int32_t top_k;
+    float top_p, min_p;
+    int32_t* tokens;
+    int32_t* new_states;                // or NULL: no table
+    float* logprobs;                    // or NULL
+};
+// Bytes of workspace that the launchers below want (16-byte aligned).
+int64_t select_workspace(int64_t rows, int64_t n_tokens);
+int launch_draw_step(const LogitRows& a, const DrawRows& d, void* workspace, hipStream_t stream);
+int launch_top_logprobs(const LogitRows& a, int32_t k, int32_t* ids, float* logprobs, void* workspace, hipStream_t stream);
+
 // Between reads and writes of LDS by different lanes of one wavefront: a wavefront's LDS instructions are carried out in order, so
 // that only the compiler is to be kept from moving one past another.
 __device__ __forceinline__ void wave_lds_sync()
