@@ -586,6 +586,35 @@ TDFA_API int tdfa_preference_loss(const tdfa_table *table, const void *logits_de
                         float *loss_dev, float *rewards_dev, float *logprobs_dev, void *grad_dev, int64_t grad_stride,
                         void *workspace_dev, int64_t workspace_bytes, void *stream);
 
+/* Distillation from a teacher's most likely tokens, and its gradient.  A row has k slots with a token and the teacher's value for
+ * it, a log-probability as tdfa_top_logprobs gives it or a logit, at the temperature of the loss.  A slot is live if its token is in A,
+ * its value is finite, and z of the token is above -inf and so is its lp in binary32.  With p_j = softmax of the student's z c over A as above,
+ *     tail = 0 : q = softmax of the values over the live slots; r = 0.
+ *     tail = 1 : q = exp(min(value, 0)); r = max(0, 1 - the sum of q), the probability that the teacher leaves to the tail, which is all
+ *                tokens of A that no live slot names; r = 0 if there are none with a z above -inf.
+ *     l        = the sum over the live slots of q (ln q - ln p) + r (ln r - ln p_tail)      (p_tail: the sum of p over the tail)
+ *     d l / d z_j = c (p_j M - the q of the slots that name j) for named tokens, c (p_j M - r p_j / p_tail) in the tail, 0 outside A,
+ *                   with M = the sum of q + r
+ *     loss     = the sum over the rows of w l.
+ * So the values need not have seen the constraint: with tail = 0 slots whose tokens it does not allow drop out, and the rest are
+ * made a distribution again.  A token may have several slots.  A row without a live slot, in a state that is no row of the table, or of weight 0
+ * (whose logits are not read) takes no part: l = 0 and a gradient of zero.  An allowed logit of +inf makes the row's loss and gradient NaN.
+ *   k              : 1 .. TDFA_TOP_MAX.
+ *   ids_dev        : device, int32 [rows][k]; what is no token (TDFA_NO_TOKEN, say) is an empty slot.
+ *   values_dev     : device, float [rows][k].
+ *   weights_dev    : device, float [rows], or NULL: all 1.
+ *   tail           : 0 or 1.
+ *   loss_dev       : device, float [1], written (0 if there are no rows).
+ *   losses_dev     : device, float [rows], written: l.
+ *   grad_dev       : as above, d loss / d logits, or NULL: not wanted.
+ *   workspace_dev  : at least tdfa_distill_workspace_bytes(rows) bytes, 16-byte aligned, as above. */
+TDFA_API int64_t tdfa_distill_workspace_bytes(int32_t rows);      /* -1 if rows is negative */
+TDFA_API int tdfa_distill_loss(const tdfa_table *table, const void *logits_dev, int dtype, int32_t rows,
+                        int32_t n_tokens, int64_t row_stride, const int32_t *states_dev, float temperature,
+                        int32_t k, const int32_t *ids_dev, const float *values_dev, const float *weights_dev, int tail,
+                        float *loss_dev, float *losses_dev, void *grad_dev, int64_t grad_stride,
+                        void *workspace_dev, int64_t workspace_bytes, void *stream);
+
 /* ---- terminal labels (Section 2.5.1, wildcard matching) -------------------------------------- */
 
 /* Applies terminal edges to a compiled table.  A terminal edge (state, label, target) stands for

@@ -111,6 +111,10 @@ def lib():
         L.tdfa_select_workspace_bytes.argtypes = [C.c_int32, C.c_int32]
         L.tdfa_draw_step.argtypes = chosen + [C.c_void_p, C.c_float, C.c_int32, C.c_float, C.c_float] + [C.c_void_p] * 4 + work
         L.tdfa_top_logprobs.argtypes = chosen + [C.c_float, C.c_int32, C.c_void_p, C.c_void_p] + work
+        L.tdfa_distill_workspace_bytes.restype = C.c_int64
+        L.tdfa_distill_workspace_bytes.argtypes = [C.c_int32]
+        L.tdfa_distill_loss.argtypes = (chosen + [C.c_float, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int] +
+                                        [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64] + work)
         _lib = L
     return _lib
 
@@ -590,6 +594,30 @@ def top_logprobs(table: Table | None, logits: torch.Tensor, states: torch.Tensor
     ws, n, _held = _workspace_of(lib().tdfa_select_workspace_bytes(rows, a[4]), workspace, logits, stream)
     _check(lib().tdfa_top_logprobs(*a, float(temperature), k, _vector(ids, "ids", torch.int32, rows * k, dev),
                                    _vector(logprobs, "logprobs", torch.float32, rows * k, dev), ws, n, _stream(stream)))
+
+
+def distill_workspace_bytes(rows: int) -> int:
+    """tdfa_distill_workspace_bytes."""
+    return int(lib().tdfa_distill_workspace_bytes(rows))
+
+
+def distill_loss(table: Table | None, logits: torch.Tensor, states: torch.Tensor | None, teacher_ids: torch.Tensor, teacher_logprobs: torch.Tensor,
+                 loss: torch.Tensor, losses: torch.Tensor, grad_logits: torch.Tensor | None = None, weights: torch.Tensor | None = None,
+                 temperature: float = 1.0, tail: bool = False, workspace: torch.Tensor | None = None, stream=None) -> None:
+    """tdfa_distill_loss: the divergence of the student from a teacher's most likely tokens.  table, logits, states as draw_step; teacher_ids: int32
+    [rows, k] and teacher_logprobs: float32 [rows, k], as top_logprobs writes them (k 1 .. TOP_MAX, NO_TOKEN: an empty slot); weights: float32 [rows].  tail: what the
+    teacher's probabilities leave of 1 is that of all other tokens; else they are made a distribution.
+    loss: float32 [1], losses: float32 [rows] and grad_logits (if given: of the type and shape of logits, may be logits) are written."""
+    a = _chosen_args(table, logits, states)
+    rows, dev, f32 = a[3], logits.get_device(), torch.float32
+    if teacher_ids.dim() != 2 or teacher_ids.shape != teacher_logprobs.shape or teacher_ids.shape[0] < rows:
+        raise ValueError("teacher_ids and teacher_logprobs must be [rows, k]")
+    k = teacher_ids.shape[1]
+    vectors = (_vector(teacher_ids, "teacher_ids", torch.int32, rows * k, dev), _vector(teacher_logprobs, "teacher_logprobs", f32, rows * k, dev),
+               _vector(weights, "weights", f32, rows, dev, True))
+    out = _vector(loss, "loss", f32, 1, dev), _vector(losses, "losses", f32, rows, dev)
+    ws, n, _held = _workspace_of(lib().tdfa_distill_workspace_bytes(rows), workspace, logits, stream)
+    _check(lib().tdfa_distill_loss(*a, float(temperature), k, *vectors, int(bool(tail)), *out, *_grad_args(logits, grad_logits), ws, n, _stream(stream)))
 
 
 def advance_tokens(table: Table, states: torch.Tensor, tokens: torch.Tensor, history: torch.Tensor,

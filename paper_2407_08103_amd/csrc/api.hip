@@ -1887,9 +1887,14 @@ int64_t tdfa_loss_workspace_bytes(int32_t rows, int32_t n_pairs)
 
 namespace {
 
-// Argument checks and kernel arguments shared by the calls that choose tokens of rows.
+struct Workspace {
+    const void* at;
+    int64_t bytes, need;
+};
+
+// Argument checks and kernel arguments shared by the calls that choose tokens of rows, and distillation.
 int prepare_logits(const tdfa_table* table, const void* logits_dev, int dtype, int32_t rows, int32_t n_tokens, int64_t row_stride,
-                   const int32_t* states_dev, float temperature, const void* workspace_dev, int64_t workspace_bytes, tdfa::LogitRows* a)
+                   const int32_t* states_dev, float temperature, Workspace workspace, tdfa::LogitRows* a)
 {
     if (dtype != TDFA_F32 && dtype != TDFA_BF16) return fail(TDFA_E_INVALID_ARG, "unknown dtype %d", dtype);
     if (rows < 0 || n_tokens < 0) return fail(TDFA_E_INVALID_ARG, "rows %d or n_tokens %d is negative", rows, n_tokens);
@@ -1902,11 +1907,10 @@ int prepare_logits(const tdfa_table* table, const void* logits_dev, int dtype, i
         if ((!logits_dev && n_tokens > 0) || (table && !states_dev)) return fail(TDFA_E_INVALID_ARG, "logits or states is NULL");
         if ((reinterpret_cast<uintptr_t>(logits_dev) & 15) || (rows > 1 && ((row_stride * esz) & 15)))
             return fail(TDFA_E_INVALID_ARG, "logits rows must be 16-byte aligned");
-        const int64_t need = tdfa::select_workspace(rows, n_tokens);
-        if (need > 0) {
-            if (!workspace_dev || workspace_bytes < need)
-                return fail(TDFA_E_INVALID_ARG, "workspace of %lld bytes, %lld are wanted", workspace_dev ? (long long)workspace_bytes : 0LL, (long long)need);
-            if (reinterpret_cast<uintptr_t>(workspace_dev) & 15) return fail(TDFA_E_INVALID_ARG, "workspace must be 16-byte aligned");
+        if (workspace.need > 0) {
+            if (!workspace.at || workspace.bytes < workspace.need)
+                return fail(TDFA_E_INVALID_ARG, "workspace of %lld bytes, %lld are wanted", workspace.at ? (long long)workspace.bytes : 0LL, (long long)workspace.need);
+            if (reinterpret_cast<uintptr_t>(workspace.at) & 15) return fail(TDFA_E_INVALID_ARG, "workspace must be 16-byte aligned");
         }
     }
     *a = tdfa::LogitRows();
@@ -1972,7 +1976,8 @@ int tdfa_draw_step(const tdfa_table* table, const void* logits_dev, int dtype, i
             return fail(TDFA_E_INVALID_ARG, "top_p %g or min_p %g is outside 0 .. 1", (double)top_p, (double)min_p);
     }
     tdfa::LogitRows a;
-    int rc = prepare_logits(table, logits_dev, dtype, rows, n_tokens, row_stride, states_dev, temperature, workspace_dev, workspace_bytes, &a);
+    int rc = prepare_logits(table, logits_dev, dtype, rows, n_tokens, row_stride, states_dev, temperature,
+                            {workspace_dev, workspace_bytes, rows > 0 && n_tokens >= 0 ? tdfa::select_workspace(rows, n_tokens) : 0}, &a);
     if (rc != TDFA_OK || rows == 0) return rc;
     if (!uniforms_dev || !tokens_dev || (table && !new_states_dev)) return fail(TDFA_E_INVALID_ARG, "uniforms, tokens or new_states is NULL");
     if (misaligned(params_dev, 16)) return fail(TDFA_E_INVALID_ARG, "params must be 16-byte aligned");
@@ -2012,7 +2017,8 @@ int tdfa_top_logprobs(const tdfa_table* table, const void* logits_dev, int dtype
         return fail(TDFA_E_INVALID_ARG, "temperature %g is not positive and finite", (double)temperature);
     if (k < 1 || k > TDFA_TOP_MAX) return fail(TDFA_E_INVALID_ARG, "k %d is outside 1 .. %d", k, TDFA_TOP_MAX);
     tdfa::LogitRows a;
-    int rc = prepare_logits(table, logits_dev, dtype, rows, n_tokens, row_stride, states_dev, temperature, workspace_dev, workspace_bytes, &a);
+    int rc = prepare_logits(table, logits_dev, dtype, rows, n_tokens, row_stride, states_dev, temperature,
+                            {workspace_dev, workspace_bytes, rows > 0 && n_tokens >= 0 ? tdfa::select_workspace(rows, n_tokens) : 0}, &a);
     if (rc != TDFA_OK || rows == 0) return rc;
     if (!ids_dev || !logprobs_dev) return fail(TDFA_E_INVALID_ARG, "ids or logprobs is NULL");
     const int64_t each = (int64_t)rows * 4;
@@ -2101,6 +2107,50 @@ int tdfa_preference_loss(const tdfa_table* table, const void* logits_dev, int dt
     const tdfa::PairArgs p = {ref_logprobs_dev, begin_dev, n_pairs, beta, smoothing, rewards_dev};
     return launch_preference_loss(a, p, loss_dev, logprobs_dev, n_tokens > 0 ? grad_dev : nullptr, grad_stride, workspace_dev,
                                   static_cast<hipStream_t>(stream));
+}
+
+int64_t tdfa_distill_workspace_bytes(int32_t rows) { return rows < 0 ? -1 : tdfa::distill_workspace(rows); }
+
+int tdfa_distill_loss(const tdfa_table* table, const void* logits_dev, int dtype, int32_t rows, int32_t n_tokens, int64_t row_stride,
+                      const int32_t* states_dev, float temperature, int32_t k, const int32_t* ids_dev, const float* values_dev,
+                      const float* weights_dev, int tail, float* loss_dev, float* losses_dev, void* grad_dev, int64_t grad_stride,
+                      void* workspace_dev, int64_t workspace_bytes, void* stream)
+{
+    clear_error();
+    const volatile float one = 1.0f;
+    if (!(temperature > 0.0f) || !(one / temperature > 0.0f) || one / temperature > 2.3e38f)
+        return fail(TDFA_E_INVALID_ARG, "log2(e) / temperature is not finite for temperature %g", (double)temperature);
+    if (k < 1 || k > TDFA_TOP_MAX) return fail(TDFA_E_INVALID_ARG, "k %d is outside 1 .. %d", k, TDFA_TOP_MAX);
+    if (tail != 0 && tail != 1) return fail(TDFA_E_INVALID_ARG, "tail %d is neither 0 nor 1", tail);
+    tdfa::LogitRows a;
+    int rc = prepare_logits(table, logits_dev, dtype, rows, n_tokens, row_stride, states_dev, temperature,
+                            {workspace_dev, workspace_bytes, rows > 0 ? tdfa::distill_workspace(rows) : 0}, &a);
+    if (rc != TDFA_OK) return rc;
+    if (!loss_dev) return fail(TDFA_E_INVALID_ARG, "loss is NULL");
+    const int64_t each = (int64_t)rows * 4;
+    if (rows > 0) {
+        if (!ids_dev || !values_dev || !losses_dev) return fail(TDFA_E_INVALID_ARG, "ids, values or losses is NULL");
+        tdfa::TokenRows t = tdfa::TokenRows();
+        t.logits = logits_dev;
+        t.dtype = dtype;
+        t.row_stride = row_stride;
+        t.rows = rows;
+        t.n_tokens = n_tokens;
+        if (grad_dev) rc = check_grad(t, grad_dev, grad_stride);
+        if (rc != TDFA_OK) return rc;
+        const Span states = {a.states, each, "states"}, ids = {ids_dev, each * k, "ids"}, values = {values_dev, each * k, "values"},
+                   weights = {weights_dev, each, "weights"}, loss = {loss_dev, 4, "loss"}, losses = {losses_dev, each, "losses"},
+                   work = {workspace_dev, workspace_bytes, "the workspace"};
+        rc = check_apart({loss, losses, work}, {span_of(a), states, ids, values, weights});
+        if (rc == TDFA_OK && grad_dev && n_tokens > 0) {
+            const Span grad = {grad_dev, ((rows - 1) * grad_stride + n_tokens) * (dtype == TDFA_F32 ? 4 : 2), "the gradient"};
+            for (const Span& x : {states, ids, values, weights, loss, losses, work})
+                if (meet(grad, x)) return fail(TDFA_E_INVALID_ARG, "the gradient overlaps %s", x.name);
+        }
+        if (rc != TDFA_OK) return rc;
+    }
+    const tdfa::DistillRows d = {ids_dev, values_dev, weights_dev, losses_dev, k, tail};
+    return launch_distill_loss(a, d, loss_dev, n_tokens > 0 ? grad_dev : nullptr, grad_stride, workspace_dev, static_cast<hipStream_t>(stream));
 }
 
 int tdfa_table_apply_terminals(tdfa_table* table, int32_t n_edges, const int32_t* edge_state_host,

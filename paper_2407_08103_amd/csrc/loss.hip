@@ -628,19 +628,6 @@ __device__ __forceinline__ void reduce_pair(double (&sum)[2], double (&part)[2][
         sum[1] += part[1][w];
     }
 }
-// A sum over the workgroup, in thread 0.  One barrier.
-template <int NT>
-__device__ __forceinline__ double reduce_sum(double sum, double (&part)[NT / 64])
-{
-#pragma unroll
-    for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
-    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
-    __syncthreads();
-    if (threadIdx.x == 0)
-        for (int w = 1; w < NT / 64; ++w) sum += part[w];
-    return sum;
-}
-
 // One workgroup per pair: the two rewards, the pair's loss, and d loss / d lp of every row of the pair.  Bound by its chain of reads
 // (32 pairs of 90 rows 4.8 us).
 __global__ void __launch_bounds__(kThreads) pair_kernel(PairArgsOnCard p, RowWork* work, double* each, int32_t blocks)
@@ -706,21 +693,6 @@ __device__ __forceinline__ float slope_of_row(const PairArgsOnCard& p, const Row
     reduce_pair<NT>(sum, part);
     const float slope = pair_slope(p, (float)((double)p.beta * sum[0] - (double)p.beta * sum[1]));
     return k & 1 ? -slope : slope;
-}
-
-// loss = the sum of n losses that lie `step` apart, or their mean, by one workgroup, in an order that depends on nothing but n and NT.
-template <int NT>
-__device__ __forceinline__ void sum_losses(const double* each, int64_t n, int32_t step, bool mean, float* loss, double (&part)[NT / 64])
-{
-    double sum = 0.0;
-    for (int64_t i = threadIdx.x; i < n; i += NT) sum += each[i * step];
-    sum = reduce_sum<NT>(sum, part);
-    if (threadIdx.x == 0) *loss = (float)(mean && n ? sum / (double)n : sum);
-}
-__global__ void __launch_bounds__(1024) loss_sum_kernel(const double* each, uint32_t n, int32_t step, int32_t mean, float* loss)
-{
-    __shared__ double s_part[16];
-    sum_losses<1024>(each, n, step, mean, loss, s_part);
 }
 
 // The policy loss from the log-probabilities that a launch before has written: `span` rows to a workgroup, which leaves its sum in out, or

@@ -304,6 +304,34 @@ __device__ __forceinline__ float sum_of_running(float m, float s, float c2, floa
 
 __device__ __forceinline__ float shared_by_wave(float x) { return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(x))); }
 
+// A sum over the workgroup, in thread 0.  One barrier.
+template <int NT>
+__device__ __forceinline__ double reduce_sum(double sum, double (&part)[NT / 64])
+{
+#pragma unroll
+    for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0)
+        for (int w = 1; w < NT / 64; ++w) sum += part[w];
+    return sum;
+}
+
+// loss = the sum of n losses that lie `step` apart, or their mean, by one workgroup, in an order that depends on nothing but n and NT.
+template <int NT>
+__device__ __forceinline__ void sum_losses(const double* each, int64_t n, int32_t step, bool mean, float* loss, double (&part)[NT / 64])
+{
+    double sum = 0.0;
+    for (int64_t i = threadIdx.x; i < n; i += NT) sum += each[i * step];
+    sum = reduce_sum<NT>(sum, part);
+    if (threadIdx.x == 0) *loss = (float)(mean && n ? sum / (double)n : sum);
+}
+[[maybe_unused]] __global__ void __launch_bounds__(1024) loss_sum_kernel(const double* each, uint32_t n, int32_t step, int32_t mean, float* loss)
+{
+    __shared__ double s_part[16];
+    sum_losses<1024>(each, n, step, mean, loss, s_part);
+}
+
 // A launch that reports its own error (asking for the last one afterwards costs the host 0.4 us more).
 template <typename... Params, typename... Args>
 int launch(void (*kernel)(Params...), dim3 grid, unsigned threads, hipStream_t stream, Args... args)

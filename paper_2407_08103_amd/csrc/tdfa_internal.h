@@ -329,6 +329,18 @@ int64_t select_workspace(int64_t rows, int64_t n_tokens);
 int launch_draw_step(const LogitRows& a, const DrawRows& d, void* workspace, hipStream_t stream);
 int launch_top_logprobs(const LogitRows& a, int32_t k, int32_t* ids, float* logprobs, void* workspace, hipStream_t stream);
 
+// Rows of a student's logits with a teacher's most likely tokens (distill.hip).
+struct DistillRows {
+    const int32_t* ids;                 // [rows][k]
+    const float* values;                // [rows][k]
+    const float* weights;               // [rows] or NULL
+    float* losses;                      // [rows]
+    int32_t k;
+    int32_t tail;
+};
+int64_t distill_workspace(int64_t rows);
+int launch_distill_loss(const LogitRows& a, const DistillRows& d, float* loss, void* grad, int64_t grad_stride, void* workspace, hipStream_t stream);
+
 // Between reads and writes of LDS by different lanes of one wavefront: a wavefront's LDS instructions are carried out in order, so
 // that only the compiler is to be kept from moving one past another.
 __device__ __forceinline__ void wave_lds_sync()

@@ -53,3 +53,23 @@ def test_workspace(lib):
     assert lib.tdfa_select_workspace_bytes(0, 0) == 0
     assert lib.tdfa_select_workspace_bytes(-1, 5) == -1 and lib.tdfa_select_workspace_bytes(5, -1) == -1
     assert lib.tdfa_select_workspace_bytes(4096, 1 << 24) >= 0
+
+
+def distill(lib, logits=A, dtype=0, rows=ROWS, n=N, stride=N, temperature=1.0, k=5, ids=B, values=D, weights=None, tail=0, loss=E, losses=E + 64, grad=None, grad_stride=N,
+            ws=0x800000, ws_bytes=4096):
+    return lib.tdfa_distill_loss(None, logits, dtype, rows, n, stride, None, temperature, k, ids, values, weights, tail, loss, losses, grad, grad_stride, ws, ws_bytes, None)
+
+
+@pytest.mark.parametrize("bad,says", COMMON + [(dict(temperature=0.0), b"temperature"), (dict(temperature=1e-45), b"temperature"), (dict(k=0), b"k 0"), (dict(k=257), b"k 257"),
+                                               (dict(tail=2), b"tail"), (dict(tail=-1), b"tail"), (dict(ids=None), b"NULL"), (dict(values=None), b"NULL"),
+                                               (dict(loss=None), b"NULL"), (dict(losses=None), b"NULL"), (dict(ws=None), b"workspace"), (dict(ws_bytes=31), b"workspace"),
+                                               (dict(ws=0x800008), b"aligned"), (dict(losses=D + 16), b"overlaps"), (dict(loss=B), b"overlaps"), (dict(losses=E), b"overlaps"),
+                                               (dict(grad=0x90008), b"aligned"), (dict(grad=0x90000, grad_stride=N - 4), b"grad_stride"),
+                                               (dict(grad=A + 16), b"overlaps"), (dict(grad=B), b"overlaps"), (dict(grad=0x800000 - 4 * N), b"overlaps")])
+def test_distill(lib, bad, says):
+    assert distill(lib, **bad) == -1 and says in lib.tdfa_last_error(), lib.tdfa_last_error()
+
+
+def test_distill_workspace(lib):
+    assert lib.tdfa_distill_workspace_bytes(0) == 0 and lib.tdfa_distill_workspace_bytes(-1) == -1
+    assert lib.tdfa_distill_workspace_bytes(2 ** 31 - 1) >= 8 * (2 ** 31 - 1)
