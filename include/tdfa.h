@@ -607,8 +607,8 @@ TDFA_API int tdfa_preference_loss(const tdfa_table *table, const void *logits_de
  *   loss_dev       : device, float [1], written (0 if there are no rows).
  *   losses_dev     : device, float [rows], written: l.
  *   grad_dev       : as above, d loss / d logits, or NULL: not wanted.
- *   workspace_dev  : at least tdfa_distill_workspace_bytes(rows) bytes, 16-byte aligned, as above. */
-TDFA_API int64_t tdfa_distill_workspace_bytes(int32_t rows);      /* -1 if rows is negative */
+ *   workspace_dev  : at least tdfa_distill_workspace_bytes(rows, n_tokens, k) bytes, 16-byte aligned, as above. */
+TDFA_API int64_t tdfa_distill_workspace_bytes(int32_t rows, int32_t n_tokens, int32_t k);      /* -1 if one is negative */
 TDFA_API int tdfa_distill_loss(const tdfa_table *table, const void *logits_dev, int dtype, int32_t rows,
                         int32_t n_tokens, int64_t row_stride, const int32_t *states_dev, float temperature,
                         int32_t k, const int32_t *ids_dev, const float *values_dev, const float *weights_dev, int tail,

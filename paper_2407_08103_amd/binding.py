@@ -112,7 +112,7 @@ def lib():
         L.tdfa_draw_step.argtypes = chosen + [C.c_void_p, C.c_float, C.c_int32, C.c_float, C.c_float] + [C.c_void_p] * 4 + work
         L.tdfa_top_logprobs.argtypes = chosen + [C.c_float, C.c_int32, C.c_void_p, C.c_void_p] + work
         L.tdfa_distill_workspace_bytes.restype = C.c_int64
-        L.tdfa_distill_workspace_bytes.argtypes = [C.c_int32]
+        L.tdfa_distill_workspace_bytes.argtypes = [C.c_int32, C.c_int32, C.c_int32]
         L.tdfa_distill_loss.argtypes = (chosen + [C.c_float, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int] +
                                         [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64] + work)
         _lib = L
@@ -596,9 +596,9 @@ def top_logprobs(table: Table | None, logits: torch.Tensor, states: torch.Tensor
                                    _vector(logprobs, "logprobs", torch.float32, rows * k, dev), ws, n, _stream(stream)))
 
 
-def distill_workspace_bytes(rows: int) -> int:
+def distill_workspace_bytes(rows: int, n_tokens: int, k: int) -> int:
     """tdfa_distill_workspace_bytes."""
-    return int(lib().tdfa_distill_workspace_bytes(rows))
+    return int(lib().tdfa_distill_workspace_bytes(rows, n_tokens, k))
 
 
 def distill_loss(table: Table | None, logits: torch.Tensor, states: torch.Tensor | None, teacher_ids: torch.Tensor, teacher_logprobs: torch.Tensor,
@@ -616,7 +616,7 @@ def distill_loss(table: Table | None, logits: torch.Tensor, states: torch.Tensor
     vectors = (_vector(teacher_ids, "teacher_ids", torch.int32, rows * k, dev), _vector(teacher_logprobs, "teacher_logprobs", f32, rows * k, dev),
                _vector(weights, "weights", f32, rows, dev, True))
     out = _vector(loss, "loss", f32, 1, dev), _vector(losses, "losses", f32, rows, dev)
-    ws, n, _held = _workspace_of(lib().tdfa_distill_workspace_bytes(rows), workspace, logits, stream)
+    ws, n, _held = _workspace_of(lib().tdfa_distill_workspace_bytes(rows, a[4], k), workspace, logits, stream)
     _check(lib().tdfa_distill_loss(*a, float(temperature), k, *vectors, int(bool(tail)), *out, *_grad_args(logits, grad_logits), ws, n, _stream(stream)))
 
 

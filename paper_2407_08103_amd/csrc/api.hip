@@ -2109,7 +2109,10 @@ int tdfa_preference_loss(const tdfa_table* table, const void* logits_dev, int dt
                                   static_cast<hipStream_t>(stream));
 }
 
-int64_t tdfa_distill_workspace_bytes(int32_t rows) { return rows < 0 ? -1 : tdfa::distill_workspace(rows); }
+int64_t tdfa_distill_workspace_bytes(int32_t rows, int32_t n_tokens, int32_t k)
+{
+    return rows < 0 || n_tokens < 0 || k < 0 ? -1 : tdfa::distill_workspace(rows, n_tokens, k);
+}
 
 int tdfa_distill_loss(const tdfa_table* table, const void* logits_dev, int dtype, int32_t rows, int32_t n_tokens, int64_t row_stride,
                       const int32_t* states_dev, float temperature, int32_t k, const int32_t* ids_dev, const float* values_dev,
@@ -2124,7 +2127,7 @@ int tdfa_distill_loss(const tdfa_table* table, const void* logits_dev, int dtype
     if (tail != 0 && tail != 1) return fail(TDFA_E_INVALID_ARG, "tail %d is neither 0 nor 1", tail);
     tdfa::LogitRows a;
     int rc = prepare_logits(table, logits_dev, dtype, rows, n_tokens, row_stride, states_dev, temperature,
-                            {workspace_dev, workspace_bytes, rows > 0 ? tdfa::distill_workspace(rows) : 0}, &a);
+                            {workspace_dev, workspace_bytes, rows > 0 && n_tokens >= 0 ? tdfa::distill_workspace(rows, n_tokens, k) : 0}, &a);
     if (rc != TDFA_OK) return rc;
     if (!loss_dev) return fail(TDFA_E_INVALID_ARG, "loss is NULL");
     const int64_t each = (int64_t)rows * 4;

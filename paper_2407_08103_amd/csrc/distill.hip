@@ -19,7 +19,7 @@ namespace {
 
 constexpr int kSlots = TDFA_TOP_MAX;
 constexpr int kHash = 1024;            // places for the named tokens of a row
-constexpr int kMarks = 16384;          // bytes, one for a group of the row: the tokens of it that are named
+constexpr int kMarks = 16384;          // most groups that a workgroup takes: a byte for each says which of its tokens are named
 
 struct DistillArgs {
     const uint32_t* allow;     // or NULL: every token is allowed
@@ -52,42 +52,60 @@ struct Exponent {
     __device__ __forceinline__ float of(float x) const { return __builtin_amdgcn_exp2f(fmaf(x, hi, x * lo)); }
 };
 
-template <int NT>
-struct Shared {
+constexpr uint32_t kNone = 0xFFFFFFFFu;
+
+// The named tokens of a workgroup's part of a row.
+struct Names {
     uint32_t marks[kMarks / 4];
-    uint32_t key[kHash];       // named tokens, kNone: free
+    uint32_t key[kHash];       // tokens, kNone: free
     float value[kHash];        // gradient of the token
+};
+// What a workgroup shares that works out a row's numbers.
+template <int NT>
+struct Shared : Names {
     float running[2][NT / 64];
     double part[NT / 64];
     double teacher[kSlots];    // of rows that name a token twice
     uint32_t named[kSlots];
-    float factor;              // of the tail's gradients
+    float factor;
     int again, active;
     uint2 masks[16];
 };
-constexpr uint32_t kNone = 0xFFFFFFFFu;
 
 __device__ __forceinline__ uint32_t place_of(uint32_t id) { return id * 2654435761u >> 22; }
 static_assert(kHash == 1 << 10);
 // The place of token id, kNone if it is not named.
-template <int NT>
-__device__ __forceinline__ uint32_t find(const Shared<NT>& s, uint32_t id)
+__device__ __forceinline__ uint32_t find(const Names& s, uint32_t id)
 {
     for (uint32_t h = place_of(id);; h = (h + 1) & (kHash - 1)) {
         if (s.key[h] == id) return h;
         if (s.key[h] == kNone) return kNone;
     }
 }
-// The named tokens of group g, as bits.  Groups kMarks apart share a byte, so of a longer row its bits are looked up.
-template <int DTYPE, int NT>
-__device__ __forceinline__ uint32_t named_in(const Shared<NT>& s, int32_t g, int32_t n_groups)
+// Its place, made if it is new (*first).  kHash is four times the slots of a row: there is room.
+__device__ __forceinline__ uint32_t enter(Names& s, uint32_t id, bool* first)
+{
+    for (uint32_t h = place_of(id);; h = (h + 1) & (kHash - 1)) {
+        const uint32_t was = atomicCAS(&s.key[h], kNone, id);
+        *first = was == kNone;
+        if (*first || was == id) return h;
+    }
+}
+// The marks are for `count` groups from g0 on; a token behind the row's whole groups has none.
+template <int DTYPE>
+__device__ __forceinline__ void mark(Names& s, int32_t id, int32_t g0, int32_t count)
 {
     constexpr int G = Elem<DTYPE>::kGroup;
-    uint32_t b = reinterpret_cast<const uint8_t*>(s.marks)[g & (kMarks - 1)];
-    if (n_groups > kMarks && b)
-        for (int j = 0; j < G; ++j)
-            if ((b >> j & 1) && find(s, (uint32_t)(g * G + j)) == kNone) b &= ~(1u << j);
-    return b;
+    const uint32_t g = (uint32_t)(id / G - g0);
+    if (g < (uint32_t)count) atomicOr(&s.marks[g >> 2], 1u << ((g & 3) * 8 + id % G));
+}
+__device__ __forceinline__ uint32_t named_in(const Names& s, int32_t g) { return reinterpret_cast<const uint8_t*>(s.marks)[g]; }
+
+template <int NT>
+__device__ __forceinline__ void clear_names(Names& s, int32_t count)
+{
+    for (int j = threadIdx.x; j < kHash; j += NT) s.key[j] = kNone;
+    for (int j = threadIdx.x; j < (count + 3) / 4; j += NT) s.marks[j] = 0;
 }
 
 // Sum over the workgroup in binary64, in every thread and in one order.  Two barriers.
@@ -105,33 +123,56 @@ __device__ __forceinline__ double block_total(double v, double (&part)[NT / 64])
     return v;
 }
 
-// -inf in place of what is not in the tail.
-template <int DTYPE, bool BITS, int NT>
-__device__ __forceinline__ void keep_tail(const Shared<NT>& s, uint4& x, uint32_t b, int32_t g, int32_t n_groups)
+// A group as it is loaded: its elements are taken out of it where they are used, not kept from one use to the next.
+__device__ __forceinline__ void held(uint4& x) { asm volatile("" : "+v"(x.x), "+v"(x.y), "+v"(x.z), "+v"(x.w)); }
+
+// -inf in place of what is not in the tail; `named` bits of a group of which b are allowed and that lies in the row.  False: there is
+// nothing of the tail in the groups of the wavefront.
+template <int DTYPE, bool BITS>
+__device__ __forceinline__ bool keep_tail(uint4& x, uint32_t b, bool inside, uint32_t named, const uint2 (&masks)[16])
 {
     constexpr uint32_t all = (1u << Elem<DTYPE>::kGroup) - 1u;
-    uint32_t on = BITS ? b : g < n_groups ? all : 0u;
-    if (on) on &= ~named_in<DTYPE>(s, g, n_groups);
-    if (__ballot(on != all)) x = keep_allowed<DTYPE>(x, on, s.masks);
+    const uint32_t on = (BITS ? b : inside ? all : 0u) & ~named;
+    if (!__ballot(on != 0)) return false;
+    if (__ballot(on != all)) x = keep_allowed<DTYPE>(x, on, masks);
+    held(x);
+    return true;
 }
 
-// Adds U groups to a sum relative to a running maximum.  SAFE: NaN is passed over.
-template <int DTYPE, int U, bool SAFE>
-__device__ __forceinline__ void add_running(const uint4 (&x)[U], const Exponent& c, float& m, float& sum)
+// Adds groups k0 .. k0 + B - 1, as far as the bits of `some` say, to a sum relative to a running maximum.  SAFE: NaN is passed over.
+template <int DTYPE, int U, int B, bool SAFE>
+__device__ __forceinline__ void add_running(uint4 (&x)[U], int k0, uint32_t some, const Exponent& c, float& m, float& sum)
 {
     float top = m;
 #pragma unroll
-    for (int k = 0; k < U; ++k) top = max_group<DTYPE>(x[k], top);
+    for (int k = k0; k < k0 + B; ++k) {
+        if (!(some >> k & 1)) continue;
+        top = max_group<DTYPE>(x[k], top);
+        next_group();
+    }
     sum *= c.of(m - top);
     m = top;
 #pragma unroll
-    for (int k = 0; k < U; ++k) {
+    for (int k = k0; k < k0 + B; ++k) {
+        if (!(some >> k & 1)) continue;
         float z[Elem<DTYPE>::kGroup];
+        held(x[k]);
         unpack<DTYPE>(x[k], z);
 #pragma unroll
         for (int j = 0; j < Elem<DTYPE>::kGroup; ++j) sum += c.of((SAFE ? fmaxf(z[j], -INFINITY) : z[j]) - m);
         next_group();
     }
+}
+// The same relative to a logit that is known before, by one rounded product and sum for an exponent: nb = -ref hi, rounded.
+template <int DTYPE, int U>
+__device__ __forceinline__ void add_relative(uint4 (&x)[U], int k, float hi, float nb, float (&sum)[2])
+{
+    float z[Elem<DTYPE>::kGroup];
+    held(x[k]);
+    unpack<DTYPE>(x[k], z);
+#pragma unroll
+    for (int j = 0; j < Elem<DTYPE>::kGroup; ++j) sum[j & 1] += __builtin_amdgcn_exp2f(fmaf(z[j], hi, nb));
+    next_group();
 }
 
 // Running sums of all threads joined, relative to the largest maximum, in every thread.  Two barriers.
@@ -155,174 +196,435 @@ __device__ __forceinline__ float join_running(float& m, float sum, const Exponen
     return sum;
 }
 
-// Gradients of one group whose elements outside the tail are -inf.
-template <int DTYPE, int NT>
-__device__ __forceinline__ uint4 gradient_group(const Shared<NT>& s, uint4 x, int32_t g, int32_t n_groups, const Exponent& c, float factor, float m, bool careful)
+// What a row's gradients are made of: those of the tail are factor exp((z - ref) c).
+struct Slope {
+    float factor, ref;
+    bool careful;              // there is a NaN among the tail's logits, or something beyond the reach of binary32
+};
+// 16 bits: |factor| in the exponent, which saves a product and a difference for each element and is off by 2^-14 or so of itself, beside a
+// rounding by up to 2^-8.
+struct Fold {
+    float at;                  // NaN: not to be taken
+    uint32_t sign;
+};
+__device__ __forceinline__ Fold fold_of(const Slope& q, const Exponent& c)
+{
+    const float nb = -(q.ref * c.hi);
+    const bool folds = !q.careful && fabsf(nb) < 1024.0f && q.factor != 0.0f;
+    return {shared_by_wave(folds ? nb + __builtin_amdgcn_logf(fabsf(q.factor)) : __uint_as_float(0x7FC00000u)), q.factor < 0.0f ? 0x80008000u : 0u};
+}
+template <int DTYPE>
+__device__ __forceinline__ float gradient_of(float z, const Slope& q, const Exponent& c)
+{
+    return q.factor * c.of((q.careful ? fmaxf(z, -INFINITY) : z) - q.ref);
+}
+// y in place of element j of a group.
+template <int DTYPE>
+__device__ __forceinline__ uint4 with_element(uint4 x, int32_t j, float y)
+{
+    const uint32_t v = DTYPE == TDFA_F32 ? __float_as_uint(y) : rounded_pair(y, y), m = DTYPE == TDFA_F32 ? 0xFFFFFFFFu : j & 1 ? 0xFFFF0000u : 0xFFFFu;
+    const int32_t word = DTYPE == TDFA_F32 ? j : j >> 1;
+    return where(make_uint4(word == 0 ? m : 0, word == 1 ? m : 0, word == 2 ? m : 0, word == 3 ? m : 0), v, x);
+}
+// Gradients of a group whose elements outside the tail are -inf.  some: there is any of the tail in the wavefront's groups.
+template <int DTYPE>
+__device__ __forceinline__ uint4 gradient_group(const Names& s, uint4 x, bool some, uint32_t named, int32_t g, const Slope& q, const Fold& f, const Exponent& c)
 {
     constexpr int G = Elem<DTYPE>::kGroup;
     float z[G];
-    unpack<DTYPE>(x, z);
+    if (!some) {
+        x = make_uint4(0, 0, 0, 0);
+    } else if (DTYPE == TDFA_BF16 && f.at == f.at) {
+        held(x);
+        unpack<DTYPE>(x, z);
 #pragma unroll
-    for (int j = 0; j < G; ++j) {
-        const float d = (careful ? fmaxf(z[j], -INFINITY) : z[j]) - m;
-        z[j] = factor * (DTYPE == TDFA_F32 ? c.of(d) : __builtin_amdgcn_exp2f(d * c.hi));
+        for (int j = 0; j < G; ++j) z[j] = __builtin_amdgcn_exp2f(fmaf(z[j], c.hi, f.at));
+        x = pack<DTYPE>(z);
+        x = make_uint4(x.x ^ f.sign, x.y ^ f.sign, x.z ^ f.sign, x.w ^ f.sign);
+    } else {
+        held(x);
+        unpack<DTYPE>(x, z);
+#pragma unroll
+        for (int j = 0; j < G; ++j) z[j] = gradient_of<DTYPE>(z[j], q, c);
+        x = pack<DTYPE>(z);
     }
-    const uint32_t b = g < n_groups ? named_in<DTYPE>(s, g, n_groups) : 0u;
-    if (b)
-#pragma unroll
-        for (int j = 0; j < G; ++j)
-            if (b >> j & 1) z[j] = s.value[find(s, (uint32_t)(g * G + j))];
-    return pack<DTYPE>(z);
+    for (; named; named &= named - 1) {
+        const int32_t j = __builtin_ctz(named);
+        x = with_element<DTYPE>(x, j, s.value[find(s, (uint32_t)(g * G + j))]);
+    }
+    return x;
 }
 
-// One workgroup per row.  R > 0: a row of at most NT R groups stays in registers between the sum and the gradient.  R = 0: a row of any
-// length, read twice.
-template <int DTYPE, int NT, int R, bool BITS>
-__global__ void __launch_bounds__(NT, 4) distill_row_kernel(DistillArgs a)
+// The slot of a thread: its token, the teacher's value, the student's logit.
+struct Slot {
+    int32_t id;
+    float value, z;
+    bool live, owner;          // owner: of the token's place
+    uint32_t place;
+};
+struct Head {
+    Slot slot;
+    float weight;
+    const uint32_t* bits;
+    bool read;                 // the row's logits have to be read
+};
+template <int DTYPE, bool BITS>
+__device__ __forceinline__ Head head_of(const DistillArgs& a, uint32_t i)
 {
-    constexpr int G = Elem<DTYPE>::kGroup, U = R ? R : 8, B = 4;             // groups to a thread at a time, and in a step of the sum
-    __shared__ Shared<NT> s;
-    const uint32_t i = blockIdx.x;
-    const int tid = (int)threadIdx.x;
-    const int32_t n_groups = a.n_tokens / G;
-    const auto* row = row_at<DTYPE>(a.logits, i, a.stride16);
-    // the slot of this thread
-    int32_t id = -1;
-    float value = 0.0f;
-    if (tid < a.k) {
-        id = a.ids[(uint64_t)i * a.k + tid];
-        value = a.values[(uint64_t)i * a.k + tid];
+    Head h = {{-1, 0.0f, -INFINITY, false, false, kNone}, 1.0f, a.allow, true};
+    if ((int)threadIdx.x < a.k) {
+        h.slot.id = a.ids[(uint64_t)i * a.k + threadIdx.x];
+        h.slot.value = a.values[(uint64_t)i * a.k + threadIdx.x];
     }
-    const float w = a.weights ? a.weights[i] : 1.0f;
-    const int32_t q = BITS ? __builtin_amdgcn_readfirstlane(a.states[i]) : 0;
-    const bool read = w != 0.0f && (!BITS || (q >= 0 && q < a.n_states));
-    const uint32_t* bits = BITS && read ? bits_of(a.allow, q, a.n_tokens) : a.allow;
-    const Exponent c(a.temperature);
-    const double inv_t = 1.0 / (double)a.temperature;
-    bool live = read && id >= 0 && id < a.n_tokens && fabsf(value) < INFINITY;
-    float z = -INFINITY;
-    if (live) {
-        live = !BITS || allowed(bits, id);
-        z = to_f32(row[id]);
-        live = live && z > -INFINITY;
+    if (a.weights) h.weight = shared_by_wave(a.weights[i]);
+    h.read = h.weight != 0.0f;
+    if constexpr (BITS) {
+        const int32_t q = __builtin_amdgcn_readfirstlane(a.states[i]);
+        h.read = h.read && q >= 0 && q < a.n_states;
+        if (h.read) h.bits = bits_of(a.allow, q, a.n_tokens);
     }
-    const RowBuffers buf = row_buffers<DTYPE>(row, bits, n_groups);
-    uint4 x[U];
-    uint32_t b[U];
-    if (R && read) fetch<DTYPE, NT, U, BITS, true>(buf, 0, n_groups, x, b);
-    for (int j = tid; j < kHash; j += NT) s.key[j] = kNone;
-    for (int j = tid; j < min(kMarks, n_groups + 3) / 4; j += NT) s.marks[j] = 0;
-    if (tid < kSlots) s.named[tid] = kNone;
+    Slot& t = h.slot;
+    t.live = h.read && t.id >= 0 && t.id < a.n_tokens && fabsf(t.value) < INFINITY;
+    if (t.live) {
+        t.live = !BITS || allowed(h.bits, t.id);
+        t.z = to_f32(row_at<DTYPE>(a.logits, i, a.stride16)[t.id]);
+        t.live = t.live && t.z > -INFINITY;
+    }
+    return h;
+}
+// Enters the slots; the marks are for the row's first `count` groups.  False: no slot is live.  Two barriers.
+template <int DTYPE, int NT>
+__device__ __forceinline__ bool enter_slots(Shared<NT>& s, Slot& t, int32_t count)
+{
+    clear_names<NT>(s, count);
+    if (threadIdx.x < kSlots) s.named[threadIdx.x] = t.live ? (uint32_t)t.id : kNone;
     fill_masks(s.masks);
-    if (tid == 0) s.again = s.active = 0;
+    if (threadIdx.x == 0) s.again = s.active = 0;
     __syncthreads();
-    // Every named token has a place; the slot that takes it first owns it.
-    uint32_t place = kNone;
-    bool owner = false;
-    if (live) {
+    if (t.live) {
         s.active = 1;
-        s.named[tid] = (uint32_t)id;
-        for (place = place_of((uint32_t)id);; place = (place + 1) & (kHash - 1)) {
-            const uint32_t was = atomicCAS(&s.key[place], kNone, (uint32_t)id);
-            owner = was == kNone;
-            if (owner || was == (uint32_t)id) break;
-        }
-        if (!owner) s.again = 1;
-        if (id / G < n_groups) atomicOr(&s.marks[(id / G & (kMarks - 1)) >> 2], 1u << ((id / G & 3) * 8 + id % G));
+        t.place = enter(s, (uint32_t)t.id, &t.owner);
+        if (!t.owner) s.again = 1;
+        mark<DTYPE>(s, t.id, 0, count);
     }
     __syncthreads();
-    const int32_t behind = n_groups * G + tid;
-    auto* out = row_at<DTYPE>(a.grad, i, a.grad_stride16);
-    const __amdgpu_buffer_rsrc_t to = buffer_of(out, (uint32_t)n_groups * 16u);
-    if (!s.active) {
-        if (tid == 0) {
-            a.losses[i] = 0.0f;
-            a.work[i] = 0.0;
-        }
-        if (!a.grad) return;
-        for (int32_t g = tid; g < n_groups; g += NT) set_group(to, g, make_uint4(0, 0, 0, 0));
-        if (behind < a.n_tokens) store_rounded(out + behind, 0.0f);
-        return;
-    }
-    // The tail: its largest logit m, and its sum relative to that.
-    const uint32_t place_behind = behind < a.n_tokens ? find(s, (uint32_t)behind) : kNone;
-    const float last = last_element<DTYPE>(a.n_tokens, row, bits, place_behind != kNone ? behind : -1);
-    float m, sum;
-    const auto add_row = [&](auto safe) {
-        constexpr bool SAFE = decltype(safe)::value;
-        m = fmaxf(last, kLowest);
-        sum = c.of((SAFE ? fmaxf(last, -INFINITY) : last) - m);
-        for (int32_t g0 = 0; g0 < (R ? 1 : n_groups); g0 += NT * U) {
-            if (!R) fetch<DTYPE, NT, U, BITS>(buf, g0, n_groups, x, b);
-#pragma unroll
-            for (int k = 0; k < U; k += B) {
-                uint4 y[B];
-#pragma unroll
-                for (int j = 0; j < B; ++j) {
-                    if (!R || !SAFE) keep_tail<DTYPE, BITS>(s, x[k + j], b[k + j], g0 + tid + (k + j) * NT, n_groups);
-                    y[j] = x[k + j];
-                }
-                add_running<DTYPE, B, SAFE>(y, c, m, sum);
-            }
-        }
-        sum = join_running<NT>(m, sum, c, s.running);
-    };
-    add_row(std::false_type());
-    const bool careful = !(sum < INFINITY);
-    if (careful) add_row(std::true_type());
-    const bool tail = sum != 0.0f;                         // (NaN where an allowed logit is +inf, as everything below)
-    // The row's numbers, in binary64: the whole sum relative to the largest logit, the teacher's probabilities, the loss.
-    const float most = block_reduce<NT, true>(fmaxf(live ? z : -INFINITY, tail ? m : -INFINITY), s.running[0]);
-    const double down = ((double)m - (double)most) * inv_t, mine = live ? exp(((double)z - (double)most) * inv_t) : 0.0;
-    const double total = (tail ? exp(down) * (double)sum : 0.0) + block_total<NT>(owner ? mine : 0.0, s.part);
-    const double ln_total = log(total), lp = ((double)z - (double)most) * inv_t - ln_total;
-    const bool counts = live && (float)lp != -INFINITY;
+    return s.active;
+}
+
+// The numbers of a row from its slots and the tail's sum relative to ref, in binary64: the loss, and what the gradients are made
+// of: s.factor, and the value of every owner's place, behind a barrier.
+template <int NT>
+__device__ __forceinline__ void row_numbers(const DistillArgs& a, uint32_t i, const Slot& t, float weight, float ref, double sum, Shared<NT>& s)
+{
+    const double inv_t = 1.0 / (double)a.temperature;
+    const bool tail = sum != 0.0;                          // (NaN where an allowed logit is +inf, as everything below)
+    const float most = fmaxf(block_reduce<NT, true>(t.live ? t.z : -INFINITY, s.running[0]), tail ? ref : -INFINITY);
+    const double down = ((double)ref - (double)most) * inv_t, mine = t.live ? exp(((double)t.z - (double)most) * inv_t) : 0.0;
+    const double total = (tail ? exp(down) * sum : 0.0) + block_total<NT>(t.owner ? mine : 0.0, s.part);
+    const double ln_total = log(total), lp = ((double)t.z - (double)most) * inv_t - ln_total;
+    const bool counts = t.live && (float)lp != -INFINITY;
     double teacher, mass, rest = 0.0;
     if (a.tail) {
-        teacher = counts ? exp(fmin((double)value, 0.0)) : 0.0;
+        teacher = counts ? exp(fmin((double)t.value, 0.0)) : 0.0;
         mass = block_total<NT>(teacher, s.part);
         if (tail) rest = fmax(1.0 - mass, 0.0);
         mass += rest;
     } else {
-        const float best = block_reduce<NT, true>(counts ? value : -INFINITY, s.running[0]);
-        teacher = counts ? exp((double)value - (double)best) : 0.0;
+        const float best = block_reduce<NT, true>(counts ? t.value : -INFINITY, s.running[0]);
+        teacher = counts ? exp((double)t.value - (double)best) : 0.0;
         mass = block_total<NT>(teacher, s.part);
         teacher = mass > 0.0 ? teacher / mass : 0.0;
         mass = mass > 0.0 ? 1.0 : 0.0;
     }
     double loss = block_total<NT>(teacher > 0.0 ? teacher * (log(teacher) - lp) : 0.0, s.part);
-    if (rest > 0.0) loss += rest * (log(rest) - (down + log((double)sum) - ln_total));
-    const double scale = (double)w * inv_t;
-    if (tid == 0) {
+    if (rest > 0.0) loss += rest * (log(rest) - (down + log(sum) - ln_total));
+    const double scale = (double)weight * inv_t;
+    if (threadIdx.x == 0) {
         a.losses[i] = (float)loss;
-        a.work[i] = (double)w * loss;
-        s.factor = tail ? (float)(scale * (mass * exp(down) / total - rest / (double)sum)) : 0.0f;
+        a.work[i] = (double)weight * loss;
+        s.factor = tail ? (float)(scale * (mass * exp(down) / total - rest / sum)) : 0.0f;
     }
-    if (!a.grad) return;
     if (s.again) {                                         // the slots of one token added up, in their order
-        if (tid < kSlots) s.teacher[tid] = teacher;
+        if (threadIdx.x < kSlots) s.teacher[threadIdx.x] = teacher;
         __syncthreads();
-        if (owner) {
+        if (t.owner) {
             teacher = 0.0;
             for (int j = 0; j < a.k; ++j)
-                if (s.named[j] == (uint32_t)id) teacher += s.teacher[j];
+                if (s.named[j] == (uint32_t)t.id) teacher += s.teacher[j];
         }
     }
-    if (owner) s.value[place] = (float)(scale * (mine / total * mass - teacher));
+    if (t.owner) s.value[t.place] = (float)(scale * (mine / total * mass - teacher));
     __syncthreads();
-    const float factor = shared_by_wave(s.factor);
-    for (int32_t g0 = 0; g0 < (R ? 1 : n_groups); g0 += NT * U) {
-        if (!R) fetch<DTYPE, NT, U, BITS>(buf, g0, n_groups, x, b);
-#pragma unroll
-        for (int k = 0; k < U; ++k) {
-            const int32_t g = g0 + tid + k * NT;
-            if (!R) keep_tail<DTYPE, BITS>(s, x[k], b[k], g, n_groups);
-            set_group(to, g, gradient_group<DTYPE>(s, x[k], g, n_groups, c, factor, m, careful));
-            next_group();
-        }
+}
+__device__ __forceinline__ void no_loss(const DistillArgs& a, uint32_t i)
+{
+    if (threadIdx.x == 0) {
+        a.losses[i] = 0.0f;
+        a.work[i] = 0.0;
     }
-    if (behind < a.n_tokens)
-        store_rounded(out + behind, place_behind != kNone ? s.value[place_behind] : factor * c.of((careful ? fmaxf(last, -INFINITY) : last) - m));
+}
+
+// One workgroup per row, of at most NT R groups, which stay in registers between the sum and the gradient.  16 bits: the sum is relative to the
+// largest logit that is named, so that terms are added as they arrive; where that does not do, and in fp32, whose gradients would show what
+// exponents lose far from the largest logit, relative to a running maximum.
+template <int DTYPE, int NT, int R, bool BITS>
+__global__ void __launch_bounds__(NT, 4) distill_row_kernel(DistillArgs a)
+{
+    constexpr int G = Elem<DTYPE>::kGroup, B = 4;          // B groups to a step of the running maximum
+    static_assert(NT * R <= kMarks);
+    __shared__ Shared<NT> s;
+    const uint32_t i = blockIdx.x;
+    const int tid = (int)threadIdx.x;
+    const int32_t n_groups = a.n_tokens / G;
+    const auto* row = row_at<DTYPE>(a.logits, i, a.stride16);
+    auto* out = row_at<DTYPE>(a.grad, i, a.grad_stride16);
+    const __amdgpu_buffer_rsrc_t to = buffer_of(out, (uint32_t)n_groups * 16u);
+    const int32_t behind = n_groups * G + tid;
+    Head h = head_of<DTYPE, BITS>(a, i);
+    uint4 x[R];
+    uint32_t b[R];
+    if (h.read) fetch<DTYPE, NT, R, BITS, true>(row_buffers<DTYPE>(row, h.bits, n_groups), 0, n_groups, x, b);
+    if (!h.read || !enter_slots<DTYPE, NT>(s, h.slot, n_groups)) {
+        no_loss(a, i);
+        if (!a.grad) return;
+        for (int32_t g = tid; g < n_groups; g += NT) set_group(to, g, make_uint4(0, 0, 0, 0));
+        if (behind < a.n_tokens) store_rounded(out + behind, 0.0f);
+        return;
+    }
+    const Exponent c(a.temperature);
+    const uint32_t place_behind = behind < a.n_tokens ? find(s, (uint32_t)behind) : kNone;
+    const float last = last_element<DTYPE>(a.n_tokens, row, h.bits, place_behind != kNone ? behind : -1);
+    // The tail's sum, and the groups that have something of it (bits of `some`, for the wavefront) or a named token (bits of `names`).
+    uint32_t some = 0, names = 0;
+    float ref = -INFINITY, sum = NAN;
+    double whole;
+    const auto settle_group = [&](int k) {
+        const int32_t g = tid + k * NT;
+        const uint32_t named = g < n_groups ? named_in(s, g) : 0u;
+        names |= (named ? 1u : 0u) << k;
+        const bool any = keep_tail<DTYPE, BITS>(x[k], b[k], g < n_groups, named, s.masks);
+        some |= (any ? 1u : 0u) << k;
+        return any;
+    };
+    if constexpr (DTYPE == TDFA_BF16) {
+        ref = block_reduce<NT, true>(h.slot.live ? h.slot.z : -INFINITY, s.running[0]);
+        const float nb = offset_of(ref, c.hi);
+        float sums[2] = {__builtin_amdgcn_exp2f(fmaf(last, c.hi, nb)), 0.0f};
+#pragma unroll
+        for (int k = 0; k < R; ++k)
+            if (settle_group(k)) add_relative<DTYPE>(x, k, c.hi, nb, sums);
+        sum = block_reduce<NT, false>(sums[0] + sums[1], s.running[1]);
+        // the rounding of ref hi is in all terms
+        whole = (double)sum * (double)__builtin_amdgcn_exp2f(-fmaf(ref, c.hi, nb));
+    }
+    bool careful = false;
+    if (DTYPE == TDFA_F32 || !(sum > 1.0e-30f && sum < 1.0e30f)) {
+        const auto add_row = [&](auto safe) {
+            constexpr bool SAFE = decltype(safe)::value;
+            ref = fmaxf(last, kLowest);
+            sum = c.of((SAFE ? fmaxf(last, -INFINITY) : last) - ref);
+#pragma unroll
+            for (int k = 0; k < R; k += B) {
+                if (DTYPE == TDFA_F32 && !SAFE)
+#pragma unroll
+                    for (int j = 0; j < B; ++j) settle_group(k + j);
+                add_running<DTYPE, R, B, SAFE>(x, k, some, c, ref, sum);
+            }
+            sum = join_running<NT>(ref, sum, c, s.running);
+        };
+        if (DTYPE == TDFA_F32) add_row(std::false_type());
+        careful = DTYPE == TDFA_BF16 || !(sum < INFINITY);
+        if (careful) add_row(std::true_type());
+        whole = (double)sum;
+    }
+    row_numbers<NT>(a, i, h.slot, h.weight, ref, whole, s);
+    if (!a.grad) return;
+    some = __builtin_amdgcn_readfirstlane(some);
+    const Slope q = {shared_by_wave(s.factor), shared_by_wave(ref), careful};
+    const Fold f = fold_of(q, c);
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+        const int32_t g = tid + k * NT;
+        set_group(to, g, gradient_group<DTYPE>(s, x[k], some >> k & 1, names >> k & 1 ? named_in(s, g) : 0u, g, q, f, c));
+        next_group();
+    }
+    if (behind < a.n_tokens) store_rounded(out + behind, place_behind != kNone ? s.value[place_behind] : gradient_of<DTYPE>(last, q, c));
+}
+
+// ---- rows that do not stay in registers: sums by parts, the numbers of the rows, gradients by parts ----------
+
+struct PartArgs : DistillArgs {
+    float2* parts;             // [rows][n_parts]: the largest logit of the tail in the part, and the sum relative to it, below 0 if it was taken with care
+    int32_t n_parts, span;     // groups to a part
+};
+struct NumbersArgs : DistillArgs {
+    const float2* parts;
+    uint2* named;              // [rows][k]: token and gradient of every slot (kNone: none)
+    float4* slopes;            // [rows]: factor, ref, careful, whether the row takes part
+    int32_t n_parts;
+};
+struct PartGradArgs {
+    const uint32_t* allow;
+    const void* logits;
+    const int32_t* states;
+    void* grad;
+    const uint2* named;
+    const float4* slopes;
+    uint32_t stride16, grad_stride16;
+    int32_t n_tokens, k, n_parts;
+    float temperature;
+};
+static_assert(sizeof(PartGradArgs) <= 112);
+
+// The sum of a part of a row's tail, and its last part's elements behind the whole groups.
+template <int DTYPE, int NT, int U, bool BITS>
+__global__ void __launch_bounds__(NT) distill_part_kernel(PartArgs a)
+{
+    constexpr int G = Elem<DTYPE>::kGroup, B = 4;
+    __shared__ uint32_t s_marks[kMarks / 4];
+    __shared__ uint2 s_masks[16];
+    __shared__ float s_running[2][NT / 64];
+    __shared__ uint32_t s_behind;
+    const uint32_t i = blockIdx.x / (uint32_t)a.n_parts;
+    const int32_t part = (int32_t)(blockIdx.x - i * (uint32_t)a.n_parts), n_groups = a.n_tokens / G, g0 = part * a.span, count = min(a.span, n_groups - g0);
+    const int tid = (int)threadIdx.x;
+    const auto* row = row_at<DTYPE>(a.logits, i, a.stride16);
+    const bool ends = part == a.n_parts - 1;
+    if (a.weights && a.weights[i] == 0.0f) return;
+    const uint32_t* bits = a.allow;
+    if constexpr (BITS) {
+        const int32_t q = __builtin_amdgcn_readfirstlane(a.states[i]);
+        if (q < 0 || q >= a.n_states) return;
+        bits = bits_of(a.allow, q, a.n_tokens);
+    }
+    for (int j = tid; j < (count + 3) / 4; j += NT) s_marks[j] = 0;
+    fill_masks(s_masks);
+    if (tid == 0) s_behind = 0;
+    __syncthreads();
+    for (int j = tid; j < a.k; j += NT) {
+        const int32_t id = a.ids[(uint64_t)i * a.k + j];
+        // (of a token that is not allowed, or -inf, a mark changes nothing)
+        if (id < 0 || id >= a.n_tokens || !(fabsf(a.values[(uint64_t)i * a.k + j]) < INFINITY)) continue;
+        const int32_t g = id / G - g0;
+        if (g >= 0 && g < count) atomicOr(&s_marks[g >> 2], 1u << ((g & 3) * 8 + id % G));
+        else if (id >= n_groups * G) atomicOr(&s_behind, 1u << (id % G));
+    }
+    __syncthreads();
+    const Exponent c(a.temperature);
+    const RowBuffers buf = row_buffers<DTYPE>(row, bits, n_groups);
+    const float last = ends && !(s_behind >> (tid & 31) & 1) ? last_element<DTYPE>(a.n_tokens, row, bits, -1) : -INFINITY;
+    float m, sum;
+    const auto add_part = [&](auto safe) {
+        constexpr bool SAFE = decltype(safe)::value;
+        m = fmaxf(last, kLowest);
+        sum = c.of((SAFE ? fmaxf(last, -INFINITY) : last) - m);
+        uint4 x[U];
+        uint32_t b[U];
+        for (int32_t at = 0; at < count; at += NT * U) {
+            fetch<DTYPE, NT, U, BITS>(buf, g0 + at, g0 + count, x, b);
+            uint32_t some = 0;
+#pragma unroll
+            for (int k = 0; k < U; k += B) {
+#pragma unroll
+                for (int j = k; j < k + B; ++j) {
+                    const int32_t g = at + tid + j * NT;
+                    const bool inside = g < count;
+                    some |= (keep_tail<DTYPE, BITS>(x[j], inside ? b[j] : 0u, inside, inside ? reinterpret_cast<const uint8_t*>(s_marks)[g] : 0u, s_masks) ? 1u : 0u) << j;
+                }
+                add_running<DTYPE, U, B, SAFE>(x, k, some, c, m, sum);
+            }
+        }
+        sum = join_running<NT>(m, sum, c, s_running);
+    };
+    add_part(std::false_type());
+    const bool careful = !(sum < INFINITY);
+    if (careful) add_part(std::true_type());
+    if (tid == 0) a.parts[blockIdx.x] = make_float2(m, careful ? -sum : sum);
+}
+
+// One workgroup per row: its numbers from its slots and the sums of its parts.
+template <int DTYPE, bool BITS>
+__global__ void __launch_bounds__(256) distill_numbers_kernel(NumbersArgs a)
+{
+    __shared__ Shared<256> s;
+    const uint32_t i = blockIdx.x;
+    Head h = head_of<DTYPE, BITS>(a, i);
+    const bool active = enter_slots<DTYPE, 256>(s, h.slot, 0);
+    float ref = kLowest;
+    bool careful = false;
+    double sum = 0.0;
+    if (active) {
+        const double inv_t = 1.0 / (double)a.temperature;
+        for (int32_t p = 0; p < a.n_parts; ++p)
+            if (a.parts[(uint64_t)i * a.n_parts + p].y != 0.0f) ref = fmaxf(ref, a.parts[(uint64_t)i * a.n_parts + p].x);
+        for (int32_t p = 0; p < a.n_parts; ++p) {
+            const float2 v = a.parts[(uint64_t)i * a.n_parts + p];
+            careful = careful || !(v.y >= 0.0f);
+            if (v.y != 0.0f) sum += fabs((double)v.y) * (v.x == ref ? 1.0 : exp(((double)v.x - (double)ref) * inv_t));
+        }
+        row_numbers<256>(a, i, h.slot, h.weight, ref, sum, s);
+    } else {
+        no_loss(a, i);
+    }
+    if ((int)threadIdx.x < a.k)
+        a.named[(uint64_t)i * a.k + threadIdx.x] =
+            make_uint2(h.slot.live ? (uint32_t)h.slot.id : kNone, h.slot.live ? __float_as_uint(s.value[h.slot.place]) : 0u);
+    if (threadIdx.x == 0) a.slopes[i] = make_float4(active ? s.factor : 0.0f, ref, careful ? 1.0f : 0.0f, active ? 1.0f : 0.0f);
+}
+
+// Gradients of NT U groups of a row, the last part with the elements behind the whole groups.
+template <int DTYPE, int NT, int U, bool BITS>
+__global__ void __launch_bounds__(NT) distill_grad_kernel(PartGradArgs a)
+{
+    constexpr int G = Elem<DTYPE>::kGroup;
+    __shared__ Names s;
+    __shared__ uint2 s_masks[16];
+    const uint32_t i = blockIdx.x / (uint32_t)a.n_parts;
+    const int32_t part = (int32_t)(blockIdx.x - i * (uint32_t)a.n_parts), n_groups = a.n_tokens / G, g0 = part * NT * U, count = min(NT * U, n_groups - g0);
+    const int tid = (int)threadIdx.x;
+    const auto* row = row_at<DTYPE>(a.logits, i, a.stride16);
+    auto* out = row_at<DTYPE>(a.grad, i, a.grad_stride16);
+    const __amdgpu_buffer_rsrc_t to = buffer_of(out, (uint32_t)n_groups * 16u);
+    const int32_t behind = part == a.n_parts - 1 ? n_groups * G + tid : a.n_tokens;
+    const float4 v = a.slopes[i];
+    if (shared_by_wave(v.w) == 0.0f) {
+#pragma unroll
+        for (int k = 0; k < U; ++k) set_group(to, g0 + tid + k * NT, make_uint4(0, 0, 0, 0));
+        if (behind < a.n_tokens) store_rounded(out + behind, 0.0f);
+        return;
+    }
+    const uint32_t* bits = BITS ? bits_of(a.allow, __builtin_amdgcn_readfirstlane(a.states[i]), a.n_tokens) : nullptr;
+    uint2 mine = make_uint2(kNone, 0u);
+    if (tid < a.k) mine = a.named[(uint64_t)i * a.k + tid];
+    uint4 x[U];
+    uint32_t b[U];
+    fetch<DTYPE, NT, U, BITS, true>(row_buffers<DTYPE>(row, bits, n_groups), g0, n_groups, x, b);
+    clear_names<NT>(s, count);
+    fill_masks(s_masks);
+    __syncthreads();
+    static_assert(NT >= kSlots);
+    if (mine.x != kNone && (int32_t)mine.x >= g0 * G && ((int32_t)mine.x < (g0 + count) * G || part == a.n_parts - 1)) {
+        bool first;
+        s.value[enter(s, mine.x, &first)] = __uint_as_float(mine.y);       // (slots of one token have the same)
+        mark<DTYPE>(s, (int32_t)mine.x, g0, count);
+    }
+    __syncthreads();
+    const Exponent c(a.temperature);
+    const Slope q = {shared_by_wave(v.x), shared_by_wave(v.y), __builtin_amdgcn_readfirstlane(v.z != 0.0f) != 0};
+    const Fold f = fold_of(q, c);
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+        const int32_t at = tid + k * NT, g = g0 + at;
+        const uint32_t named = at < count ? named_in(s, at) : 0u;
+        const bool some = keep_tail<DTYPE, BITS>(x[k], b[k], at < count, named, s_masks);
+        set_group(to, g, gradient_group<DTYPE>(s, x[k], some, named, g, q, f, c));
+        next_group();
+    }
+    if (behind < a.n_tokens) {
+        const uint32_t place = find(s, (uint32_t)behind);
+        const float last = last_element<DTYPE>(a.n_tokens, row, bits, -1);
+        store_rounded(out + behind, place != kNone ? s.value[place] : gradient_of<DTYPE>(last, q, c));
+    }
 }
 
 template <int DTYPE, bool BITS>
@@ -332,19 +634,73 @@ int rows_of(const DistillArgs& x, unsigned rows, hipStream_t stream)
     if (n_groups <= 256 * 4) return launch(distill_row_kernel<DTYPE, 256, 4, BITS>, dim3(rows), 256, stream, x);
     if (n_groups <= 256 * 16) return launch(distill_row_kernel<DTYPE, 256, 16, BITS>, dim3(rows), 256, stream, x);
     if (n_groups <= 512 * 16) return launch(distill_row_kernel<DTYPE, 512, 16, BITS>, dim3(rows), 512, stream, x);
-    if (n_groups <= 1024 * 16) return launch(distill_row_kernel<DTYPE, 1024, 16, BITS>, dim3(rows), 1024, stream, x);
-    return launch(distill_row_kernel<DTYPE, 1024, 0, BITS>, dim3(rows), 1024, stream, x);
+    return launch(distill_row_kernel<DTYPE, 1024, 16, BITS>, dim3(rows), 1024, stream, x);
+}
+
+constexpr int kPartThreads = 256, kPartGroups = 8;        // groups in flight per thread of the launches over parts
+constexpr int32_t kPiece = kPartThreads * kPartGroups;
+
+int32_t groups_of(int dtype, int64_t n_tokens) { return (int32_t)(n_tokens / (dtype == TDFA_F32 ? 4 : 8)); }
+bool by_parts(int64_t rows, int32_t n_groups) { return n_groups > kMarks || (rows <= 40 && n_groups > 4096); }
+// Groups to a part of the sums: about 1,024 workgroups, of whole pieces, none of more than kMarks groups.
+int32_t span_of(int64_t rows, int32_t n_groups)
+{
+    const int64_t pieces = (n_groups + kPiece - 1) / kPiece, parts = std::max<int64_t>(1, std::min<int64_t>(pieces, 1024 / std::max<int64_t>(rows, 1)));
+    return (int32_t)std::min<int64_t>(kMarks, (pieces + parts - 1) / parts * kPiece);
+}
+int64_t aligned(int64_t bytes) { return (bytes + 15) / 16 * 16; }
+
+template <int DTYPE, bool BITS>
+int parts_of(const DistillArgs& x, int64_t rows, int32_t span, float2* parts, uint2* named, float4* slopes, hipStream_t stream)
+{
+    const int32_t n_groups = x.n_tokens / Elem<DTYPE>::kGroup, n_parts = (n_groups + span - 1) / span;
+    PartArgs p;
+    static_cast<DistillArgs&>(p) = x;
+    p.parts = parts;
+    p.n_parts = n_parts;
+    p.span = span;
+    int rc = launch(distill_part_kernel<DTYPE, kPartThreads, kPartGroups, BITS>, dim3((unsigned)(rows * n_parts)), kPartThreads, stream, p);
+    if (rc != TDFA_OK) return rc;
+    NumbersArgs n;
+    static_cast<DistillArgs&>(n) = x;
+    n.parts = parts;
+    n.named = named;
+    n.slopes = slopes;
+    n.n_parts = n_parts;
+    rc = launch(distill_numbers_kernel<DTYPE, BITS>, dim3((unsigned)rows), 256, stream, n);
+    if (rc != TDFA_OK || !x.grad) return rc;
+    const int32_t grad_parts = (n_groups + kPiece - 1) / kPiece;
+    const PartGradArgs g = {x.allow, x.logits, x.states, x.grad, named, slopes, x.stride16, x.grad_stride16, x.n_tokens, x.k, grad_parts, x.temperature};
+    return launch(distill_grad_kernel<DTYPE, kPartThreads, kPartGroups, BITS>, dim3((unsigned)(rows * grad_parts)), kPartThreads, stream, g);
 }
 
 }  // namespace
 
-int64_t distill_workspace(int64_t rows) { return 8 * rows; }
+// The rows' losses; where rows are taken by parts (of 16-bit logits, which have fewer groups, always if of fp32 ones) the slots' and parts' numbers as well.
+int64_t distill_workspace(int64_t rows, int64_t n_tokens, int64_t k)
+{
+    int64_t bytes = aligned(8 * rows);
+    const int32_t most = groups_of(TDFA_F32, n_tokens);
+    if (!by_parts(rows, most)) return bytes;
+    int64_t parts = 0;
+    for (int dtype : {TDFA_F32, TDFA_BF16}) {
+        const int32_t n = groups_of(dtype, n_tokens), span = span_of(rows, n);
+        parts = std::max<int64_t>(parts, (n + span - 1) / span);
+    }
+    return bytes + 16 * rows + aligned(8 * rows * k) + aligned(8 * rows * parts);
+}
 
 int launch_distill_loss(const LogitRows& a, const DistillRows& d, float* loss, void* grad, int64_t grad_stride, void* workspace, hipStream_t stream)
 {
     const int64_t esz = a.dtype == TDFA_F32 ? 4 : 2;
+    const int32_t n_groups = groups_of(a.dtype, a.n_tokens), span = span_of(a.rows, n_groups);
+    const bool parted = by_parts(a.rows, n_groups);
     double* work = static_cast<double*>(workspace);
-    for (int64_t from = 0; from < a.rows; from += kMaxBlocks) {
+    float4* slopes = reinterpret_cast<float4*>(static_cast<char*>(workspace) + aligned(8 * a.rows));
+    uint2* named = reinterpret_cast<uint2*>(slopes + a.rows);
+    float2* parts = reinterpret_cast<float2*>(reinterpret_cast<char*>(named) + aligned(8 * a.rows * d.k));
+    const int64_t n_parts = parted ? std::max((n_groups + span - 1) / span, (n_groups + kPiece - 1) / kPiece) : 1, step = std::max<int64_t>(1, kMaxBlocks / n_parts);
+    for (int64_t from = 0; from < a.rows; from += step) {
         DistillArgs x;
         x.allow = a.allow;
         x.logits = static_cast<const char*>(a.logits) + from * a.row_stride * esz;
@@ -362,9 +718,16 @@ int launch_distill_loss(const LogitRows& a, const DistillRows& d, float* loss, v
         x.k = d.k;
         x.tail = d.tail;
         x.temperature = a.temperature;
-        const unsigned rows = (unsigned)std::min<int64_t>(kMaxBlocks, a.rows - from);
-        const int rc = a.dtype == TDFA_F32 ? (a.allow ? rows_of<TDFA_F32, true>(x, rows, stream) : rows_of<TDFA_F32, false>(x, rows, stream))
-                                           : (a.allow ? rows_of<TDFA_BF16, true>(x, rows, stream) : rows_of<TDFA_BF16, false>(x, rows, stream));
+        const int64_t rows = std::min<int64_t>(step, a.rows - from);
+        const auto go = [&](auto dtype, auto bits) {
+            constexpr int DTYPE = decltype(dtype)::value;
+            constexpr bool BITS = decltype(bits)::value;
+            return parted ? parts_of<DTYPE, BITS>(x, rows, span, parts, named, slopes, stream) : rows_of<DTYPE, BITS>(x, (unsigned)rows, stream);
+        };
+        using F32 = std::integral_constant<int, TDFA_F32>;
+        using BF16 = std::integral_constant<int, TDFA_BF16>;
+        const int rc = a.dtype == TDFA_F32 ? (a.allow ? go(F32(), std::true_type()) : go(F32(), std::false_type()))
+                                           : (a.allow ? go(BF16(), std::true_type()) : go(BF16(), std::false_type()));
         if (rc != TDFA_OK) return rc;
     }
     return launch(loss_sum_kernel, dim3(1), 1024, stream, static_cast<const double*>(work), (uint32_t)a.rows, 1, 0, loss);

@@ -338,7 +338,7 @@ struct DistillRows {
     int32_t k;
     int32_t tail;
 };
-int64_t distill_workspace(int64_t rows);
+int64_t distill_workspace(int64_t rows, int64_t n_tokens, int64_t k);
 int launch_distill_loss(const LogitRows& a, const DistillRows& d, float* loss, void* grad, int64_t grad_stride, void* workspace, hipStream_t stream);
 
 // Between reads and writes of LDS by different lanes of one wavefront: a wavefront's LDS instructions are carried out in order, so

@@ -71,5 +71,6 @@ def test_distill(lib, bad, says):
 
 
 def test_distill_workspace(lib):
-    assert lib.tdfa_distill_workspace_bytes(0) == 0 and lib.tdfa_distill_workspace_bytes(-1) == -1
-    assert lib.tdfa_distill_workspace_bytes(2 ** 31 - 1) >= 8 * (2 ** 31 - 1)
+    size = lib.tdfa_distill_workspace_bytes
+    assert size(0, 0, 1) == 0 and size(-1, 0, 1) == -1 and size(1, -1, 1) == -1 and size(1, 1, -1) == -1
+    assert size(2 ** 31 - 1, 1 << 24, 256) >= (2 ** 31 - 1) * (8 + 16 + 8 * 256)

@@ -245,7 +245,7 @@ def test_captured(T):
     lists = [slots(x, 30, np.random.default_rng(i)) for i, x in enumerate(r)]
     x, ids, values = r[0].x.clone(), torch.from_numpy(lists[0][0]).cuda(), torch.from_numpy(lists[0][1]).cuda()
     loss, losses, grad = torch.empty(1, device="cuda"), torch.empty(9, device="cuda"), torch.zeros_like(x)
-    ws = torch.empty(T.distill_workspace_bytes(9), dtype=torch.uint8, device="cuda")
+    ws = torch.empty(T.distill_workspace_bytes(9, 6007, 30), dtype=torch.uint8, device="cuda")
 
     def call():
         T.distill_loss(r[0].table, x[:, :6007], r[0].states, ids, values, loss, losses, grad_logits=grad[:, :6007], tail=True, workspace=ws)
