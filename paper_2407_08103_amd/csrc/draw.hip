@@ -30,7 +30,7 @@ __device__ __forceinline__ uint32_t key_of(float z)
 __device__ __forceinline__ float logit_of(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key & 0x7FFFFFFFu : ~key); }
 constexpr uint32_t kKeyNegInf = 0x007FFFFFu, kKeyPosInf = 0xFF800000u;
 
-constexpr int kList = 2048;            // tokens that are put in order in LDS
+constexpr int kList = 256;             // tokens that are put in order in LDS
 
 struct SelectArgs {
     const uint32_t* allow;     // or NULL: every token is allowed
@@ -123,16 +123,70 @@ __device__ __forceinline__ void for_each(const RowOf<DTYPE>& r, F&& f)
     if (t < r.n_tokens && (!BITS || allowed(r.bits, t))) f(t, to_f32(r.row[t]));
 }
 
+// The same row as the threads of a workgroup hold it: R > 0 groups each, in registers, or R = 0: read again by every look at it.
+template <int DTYPE, int NT, int R, bool BITS>
+struct Held {
+    static constexpr int G = Elem<DTYPE>::kGroup, U = R ? R : 8;
+    static constexpr uint32_t kAll = (1u << G) - 1u;
+    RowBuffers buf;
+    int32_t n_groups;
+    uint4 x[U];
+    uint32_t b[U];
+    float last;                // the element behind the whole groups that belongs to this thread
+    bool has_last;             // and whether it is allowed
+
+    __device__ __forceinline__ void load(const RowOf<DTYPE>& r)
+    {
+        n_groups = r.n_tokens / G;
+        buf = row_buffers<DTYPE>(r.row, r.bits, n_groups);
+        if constexpr (R > 0) {
+            fetch_bits<DTYPE, NT, U, BITS>(buf, 0, b);
+            fetch_groups<DTYPE, NT, U, BITS>(buf, 0, n_groups, x, b);
+        }
+        const int32_t t = n_groups * G + (int32_t)threadIdx.x;
+        has_last = t < r.n_tokens && (!BITS || allowed(r.bits, t));
+        last = has_last ? to_f32(r.row[t]) : -INFINITY;
+    }
+    __device__ __forceinline__ uint32_t on_of(int k, int32_t g) const { return BITS ? b[k] : g < n_groups ? kAll : 0u; }
+    // f(group, its elements, which of them are allowed) for the groups of this thread; those of a wavefront lie side by side, and one
+    // without an allowed token is passed over.
+    template <typename F>
+    __device__ __forceinline__ void each(F&& f)
+    {
+        for (int32_t g0 = 0; g0 < (R ? 1 : n_groups); g0 += NT * U) {
+            if constexpr (R == 0) fetch<DTYPE, NT, U, BITS>(buf, g0, n_groups, x, b);
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+                const int32_t g = g0 + (int32_t)threadIdx.x + k * NT;
+                const uint32_t on = on_of(k, g);
+                if (!__ballot(on != 0)) continue;
+                f(g, x[k], on);
+                next_group();
+            }
+        }
+    }
+};
+
 // What the workgroup of a row shares.
+constexpr uint32_t kBins = 11273;       // see bin_of
 template <int NT>
 struct Shared {
+    union {
+        u64 bin[256];          // of one digit
+        alignas(16) uint32_t count[kBins];
+        uint32_t chunk[kBins];
+    };
     u64 list[kList];           // keys above, complements of ids below
+    u64 sorted[kList];
     double cum[kList];
-    u64 bin[256];
+    uint32_t rank[kList];
     double part[NT / 64];
     uint32_t word[NT / 64];
     uint32_t n;
     u64 found[2];
+    double mass[3];
+    u64 least;
+    uint32_t at[4];
 };
 
 template <int NT>
@@ -176,52 +230,51 @@ __device__ __forceinline__ uint32_t count_allowed(const uint32_t* bits, int32_t 
 
 // ---- a few tokens: put in order ----------------------------------------------------------------
 
-// Puts list[0 .. n) in order, the largest first; list[n .. the next power of two) is overwritten.
+// list[0 .. n) in order, the largest first, in sorted[]: every entry counts those above it.  n <= kList; three barriers.
 template <int NT>
-__device__ __forceinline__ void sort_list(u64 (&list)[kList], uint32_t n)
+__device__ __forceinline__ void sort_list(Shared<NT>& s, uint32_t n)
 {
     uint32_t size = 64;
     while (size < n) size <<= 1;
-    for (uint32_t i = n + threadIdx.x; i < size; i += NT) list[i] = 0;
+    const uint32_t i = threadIdx.x & (size - 1), first = threadIdx.x / size, step = NT / size;
+    static_assert(NT >= kList);
+    if (threadIdx.x < kList) s.rank[threadIdx.x] = 0;
     __syncthreads();
-    for (uint32_t k = 2; k <= size; k <<= 1)
-        for (uint32_t j = k >> 1; j; j >>= 1) {
-            for (uint32_t i = threadIdx.x; i < size / 2; i += NT) {
-                const uint32_t lo = (i / j) * 2 * j + (i & (j - 1)), hi = lo + j;
-                const u64 x = list[lo], y = list[hi];
-                if ((x < y) == ((lo & k) == 0)) {
-                    list[lo] = y;
-                    list[hi] = x;
-                }
-            }
-            __syncthreads();
-        }
+    u64 mine = 0;
+    if (i < n) {
+        mine = s.list[i];
+        uint32_t above = 0;
+        for (uint32_t j = first; j < n; j += step) above += s.list[j] > mine ? 1u : 0u;
+        if (above) atomicAdd(&s.rank[i], above);
+    }
+    __syncthreads();
+    if (first == 0 && i < n) s.sorted[s.rank[i]] = mine;
+    __syncthreads();
 }
 
-// cum[i] = weights of list[0 .. i] added up, n of them.
+// cum[i] = weights of sorted[0 .. i] added up, n of them.  By one wavefront.
 template <int NT>
 __device__ __forceinline__ void sum_list(Shared<NT>& s, uint32_t n, float m, double inv_t)
 {
-    const uint32_t per = (n + NT - 1) / NT, from = threadIdx.x * per;
-    double mine = 0.0;
-    for (uint32_t i = from; i < min(from + per, n); ++i) {
-        mine += weight_of(logit_of((uint32_t)(s.list[i] >> 32)), m, inv_t);
-        s.cum[i] = mine;
+    constexpr uint32_t per = kList / 64;
+    const uint32_t lane = threadIdx.x & 63, from = lane * per;
+    double w[per], mine = 0.0;
+#pragma unroll
+    for (uint32_t j = 0; j < per; ++j) {
+        if (from + j < n) mine += weight_of(logit_of((uint32_t)(s.sorted[from + j] >> 32)), m, inv_t);
+        w[j] = mine;
     }
     double upto = mine;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
         const double other = __shfl_up(upto, d);
-        if ((int)(threadIdx.x & 63) >= d) upto += other;
+        if ((int)lane >= d) upto += other;
     }
-    if ((threadIdx.x & 63) == 63) s.part[threadIdx.x >> 6] = upto;
-    __syncthreads();
-    double before = 0.0;
-    for (uint32_t w = 0; w < threadIdx.x >> 6; ++w) before += s.part[w];
-    const double below = __shfl_up(upto, 1);
-    if (threadIdx.x & 63) before += below;
-    for (uint32_t i = from; i < min(from + per, n); ++i) s.cum[i] += before;
-    __syncthreads();
+    const double below = __shfl_up(upto, 1), before = lane ? below : 0.0;
+#pragma unroll
+    for (uint32_t j = 0; j < per; ++j)
+        if (from + j < n) s.cum[from + j] = before + w[j];
+    wave_lds_sync();
 }
 
 // The first i in 0 .. n for which holds(i), which holds from there on; n if it holds for none.  By one wavefront, 64 places at a time.
@@ -248,8 +301,8 @@ struct Drawn {
 template <int NT>
 __device__ __forceinline__ Drawn draw_of_list(const Shared<NT>& s, uint32_t n, float m, const Setting& q)
 {
-    const auto key = [&](uint32_t i) { return (uint32_t)(s.list[i] >> 32); };
-    const auto id = [&](uint32_t i) { return (int32_t)~(uint32_t)s.list[i]; };
+    const auto key = [&](uint32_t i) { return (uint32_t)(s.sorted[i] >> 32); };
+    const auto id = [&](uint32_t i) { return (int32_t)~(uint32_t)s.sorted[i]; };
     const auto end_of = [&](uint32_t i) {                  // behind the tokens of the same logit
         const uint32_t k = key(i);
         return first_where(n, [&](uint32_t j) { return key(j) < k; });
@@ -396,19 +449,367 @@ __device__ Drawn draw_by_digits(Shared<NT>& s, const RowOf<DTYPE>& r, const Sett
     return {(int32_t)id, lp};
 }
 
-// The allowed tokens of a row, in order, with their running sums; a row of at most kList of them.
-template <int DTYPE, int NT, bool BITS>
-__device__ __forceinline__ uint32_t list_row(Shared<NT>& s, const RowOf<DTYPE>& r, double inv_t, float* m)
+// Takes hold of a row.  How many tokens are allowed; one or two barriers.
+template <int DTYPE, int NT, int R, bool BITS>
+__device__ __forceinline__ uint32_t load_row(Shared<NT>& s, Held<DTYPE, NT, R, BITS>& row, const RowOf<DTYPE>& r)
 {
+    row.load(r);
+    if (!BITS) return (uint32_t)r.n_tokens;
+    if (R == 0) return count_allowed<NT>(r.bits, r.n_tokens, s.word);
+    uint32_t n = row.has_last ? 1u : 0u;
+#pragma unroll
+    for (int k = 0; k < (R ? R : 1); ++k) n += (uint32_t)__popc(row.b[k]);
+    return block_sum<NT>(n, s.word);
+}
+
+// The tokens of a row for which wanted(token, logit) holds, at most kList, in order.  How many there are; five barriers.
+template <int DTYPE, int NT, int R, bool BITS, typename F>
+__device__ __forceinline__ uint32_t list_of(Shared<NT>& s, Held<DTYPE, NT, R, BITS>& row, F&& wanted)
+{
+    constexpr int G = Elem<DTYPE>::kGroup;
     if (threadIdx.x == 0) s.n = 0;
     __syncthreads();
-    for_each<DTYPE, NT, BITS>(r, [&](int32_t t, float z) { s.list[atomicAdd(&s.n, 1u)] = (u64)key_of(z) << 32 | ~(uint32_t)t; });
+    const auto add = [&](int32_t t, float z) {
+        const uint32_t i = atomicAdd(&s.n, 1u);
+        if (i < (uint32_t)kList) s.list[i] = (u64)key_of(z) << 32 | ~(uint32_t)t;
+    };
+    row.each([&](int32_t g, uint4 x, uint32_t on) {
+        float z[G];
+        unpack<DTYPE>(x, z);
+#pragma unroll
+        for (int j = 0; j < G; ++j)
+            if ((on >> j & 1) && wanted(g * G + j, z[j])) add(g * G + j, z[j]);
+    });
+    const int32_t behind = row.n_groups * G + (int32_t)threadIdx.x;
+    if (row.has_last && wanted(behind, row.last)) add(behind, row.last);
     __syncthreads();
-    const uint32_t n = s.n;
-    sort_list<NT>(s.list, n);
-    *m = logit_of((uint32_t)(s.list[0] >> 32));
-    if (*m != -INFINITY) sum_list<NT>(s, n, *m, inv_t);
+    const uint32_t n = min(s.n, (uint32_t)kList);
+    sort_list<NT>(s, n);
     return n;
+}
+
+// ---- 16-bit logits: how many tokens have each logit ----------------------------------------------
+
+// Logits of 16 bits take few values: with the number of tokens that have each, a row's weights need an exponential for a value, not for a
+// token, and their sums do not depend on the order in which the tokens were counted.  Values of a magnitude from 2^-36 to 2^8 have a bin each, 128
+// to a power of two, in the order of the values:
+//     3: those up to -2^8, 4 .. 5635: negative ones, 5636: around zero, and NaN, 5637 .. 5639: just below 2^-36, 5640 .. 11271: positive ones,
+//     11272: those from 2^8 on.
+// Bins are read four at a time, hence the three before the positive ones and the place where it all begins.  (Of 10^5 logits spread like a few
+// units around zero some lie below 2^-20: with bins from there on, one row of twenty was left to the digits.)
+constexpr uint32_t kLowDown = 0x2D7Fu, kLowUp = kLowDown - 3, kHigh = 0x4380u, kHalf = kHigh - kLowDown - 1;     // in units of a bf16's last place
+constexpr uint32_t kLowBin = 3, kZeroBin = kLowBin + kHalf + 1, kHighBin = kZeroBin + kHalf + 4;
+static_assert(kHighBin + 1 == kBins && kHalf % 8 == 0 && kZeroBin % 4 == 0);
+__device__ __forceinline__ uint32_t bin_of(float z)
+{
+    const float hi = __uint_as_float(kHigh << 16);
+    const uint32_t up = __float_as_uint(__builtin_amdgcn_fmed3f(z, __uint_as_float(kLowUp << 16), hi));
+    const uint32_t down = __float_as_uint(__builtin_amdgcn_fmed3f(-z, __uint_as_float(kLowDown << 16), hi));
+    return (up + ((kZeroBin - kLowUp + kLowDown) << 16) - down) >> 16;
+}
+// The value of a bin that has one (the zero bin: 0).
+__device__ __forceinline__ float value_of(uint32_t bin)
+{
+    return bin == kZeroBin ? 0.0f : __uint_as_float(bin > kZeroBin ? (kLowUp + bin - kZeroBin) << 16 : (kLowDown + kZeroBin - bin) << 16 | 0x80000000u);
+}
+
+// A thread's share of the bins that have a value: stretches of eight that lie together, the largest values first; the zero bin belongs to the
+// stretch of the smallest positive values.
+constexpr uint32_t kStretches = 2 * kHalf / 8;
+template <int NT> constexpr uint32_t kShare = (kStretches + NT - 1) / NT;
+__device__ __forceinline__ uint32_t top_of(uint32_t stretch) { return kHighBin - 1 - 8 * stretch - (stretch >= kHalf / 8 ? 4 : 0); }
+__device__ __forceinline__ bool has_zero(uint32_t stretch) { return stretch == kHalf / 8 - 1; }
+template <int NT>
+__device__ __forceinline__ uint32_t counts_of(const Shared<NT>& s, uint32_t stretch, uint32_t (&n)[8])       // the largest value's first; whether there are any
+{
+    const uint4 hi = *reinterpret_cast<const uint4*>(&s.count[top_of(stretch) - 3]), lo = *reinterpret_cast<const uint4*>(&s.count[top_of(stretch) - 7]);
+    n[0] = hi.w; n[1] = hi.z; n[2] = hi.y; n[3] = hi.x; n[4] = lo.w; n[5] = lo.z; n[6] = lo.y; n[7] = lo.x;
+    return (hi.x | hi.y | hi.z | hi.w) | (lo.x | lo.y | lo.z | lo.w);
+}
+// f(bin, tokens, weight) in the order of the values, for bins with tokens.
+template <int NT, typename F>
+__device__ __forceinline__ void each_bin(const Shared<NT>& s, float m, double inv_t, F&& f)
+{
+    for (uint32_t p = 0; p < kShare<NT>; ++p) {
+        const uint32_t o = threadIdx.x * kShare<NT> + p;
+        if (o >= kStretches) return;
+        const uint32_t top = top_of(o);
+        uint32_t n[8];
+        if (counts_of<NT>(s, o, n)) {
+            // the values lie equally far from one another: a weight is a power of one factor, unless that is beyond all reach
+            const double first = (double)value_of(top) - (double)m, step = ((double)value_of(top - 1) - (double)value_of(top)) * inv_t;
+            const bool by_steps = step > -16.0;
+            const double factor = by_steps ? exp(step) : 0.0;
+            double w = by_steps ? exp(first * inv_t) : 0.0;
+#pragma unroll
+            for (uint32_t j = 0; j < 8; ++j) {
+                if (n[j]) f(top - j, n[j], by_steps && value_of(top - j) != m ? w : weight_of(value_of(top - j), m, inv_t));        // (of the largest: 1)
+                w *= factor;
+            }
+        }
+        if (has_zero(o) && s.count[kZeroBin]) f(kZeroBin, s.count[kZeroBin], weight_of(0.0f, m, inv_t));
+    }
+}
+
+constexpr int32_t kCountedGroups = 64 * (int32_t)kBins;      // of longer rows find_nth has no room for the parts
+
+// What the counts tell all threads of a workgroup, and this one of the bins before its own.
+struct Counted {
+    float m;                   // the largest logit
+    uint32_t n_before, n_upto;
+    double before, upto;       // weights up to this thread's bins, and with them
+};
+
+// Counts the tokens of a row by their logits, and weighs them.  False: there are logits that the bins do not tell apart and that matter.
+template <int NT, int R, bool BITS>
+__device__ __forceinline__ bool count_row(Shared<NT>& s, Held<TDFA_BF16, NT, R, BITS>& row, double inv_t, Counted& c)
+{
+    if (row.n_groups > kCountedGroups) return false;
+    for (uint32_t j = threadIdx.x; j < kBins; j += NT) s.count[j] = 0;
+    __syncthreads();
+    row.each([&](int32_t, uint4 x, uint32_t on) {
+        float z[8];
+        unpack<TDFA_BF16>(x, z);
+        // (a token that is not allowed adds nothing, wherever; a group without any is not in the registers)
+        if (on)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) atomicAdd(&s.count[bin_of(z[j])], on >> j & 1u);
+    });
+    if (row.has_last) atomicAdd(&s.count[bin_of(row.last)], 1u);
+    __syncthreads();
+    if (s.count[kHighBin] | s.count[kZeroBin + 1] | s.count[kZeroBin + 2] | s.count[kZeroBin + 3]) return false;
+    if (s.count[kZeroBin]) {                               // NaN counts as -inf, and other numbers than zero have no bin
+        if (threadIdx.x < 2) s.at[threadIdx.x] = 0;
+        __syncthreads();
+        uint32_t odd = 0, nans = 0;
+        const auto look = [&](float z) {
+            nans += z != z ? 1u : 0u;
+            odd += z != 0.0f && bin_of(z) == kZeroBin && z == z ? 1u : 0u;
+        };
+        row.each([&](int32_t, uint4 x, uint32_t on) {
+            float z[8];
+            unpack<TDFA_BF16>(x, z);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (on >> j & 1) look(z[j]);
+        });
+        if (row.has_last) look(row.last);
+        if (nans) atomicAdd(&s.at[0], nans);
+        if (odd) atomicAdd(&s.at[1], odd);
+        __syncthreads();
+        if (s.at[1]) return false;
+        if (threadIdx.x == 0) s.count[kZeroBin] -= s.at[0];
+        __syncthreads();
+    }
+    // the largest logit
+    uint32_t top = 0;
+#pragma unroll
+    for (uint32_t p = 0; p < kShare<NT>; ++p) {
+        const uint32_t o = threadIdx.x * kShare<NT> + p;
+        uint32_t n[8];
+        if (top || o >= kStretches) continue;
+        if (counts_of<NT>(s, o, n))
+#pragma unroll
+            for (int j = 7; j >= 0; --j)
+                if (n[j]) top = top_of(o) - (uint32_t)j;
+        if (!top && has_zero(o) && s.count[kZeroBin]) top = kZeroBin;
+    }
+    top = block_max<NT>(top, s.word);
+    if (!top) return false;
+    c.m = value_of(top);
+    // what is not above -2^8 has to weigh next to nothing: less than 2^24 exp(-64) of the whole
+    if (s.count[kLowBin] && !((-256.0 - (double)c.m) * inv_t < -64.0) && inv_t != 0.0) return false;
+    uint32_t n = 0;
+    double w = 0.0;
+    if (inv_t != 0.0)
+        each_bin<NT>(s, c.m, inv_t, [&](uint32_t, uint32_t tokens, double weight) {
+            n += tokens;
+            w += (double)tokens * weight;
+        });
+    // sums before and up to every thread: what one ends with is to the last bit what the next begins with
+    uint32_t n_sum = n;
+    double sum = w;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const uint32_t n_other = __shfl_up(n_sum, d);
+        const double other = __shfl_up(sum, d);
+        if ((int)(threadIdx.x & 63) >= d) {
+            n_sum += n_other;
+            sum += other;
+        }
+    }
+    __syncthreads();
+    if ((threadIdx.x & 63) == 63) {
+        s.word[threadIdx.x >> 6] = n_sum;
+        s.part[threadIdx.x >> 6] = sum;
+    }
+    __syncthreads();
+    uint32_t n_base = 0;
+    double base = 0.0;
+    for (uint32_t v = 0; v < threadIdx.x >> 6; ++v) {
+        n_base += s.word[v];
+        base += s.part[v];
+    }
+    const uint32_t n_below = __shfl_up(n_sum, 1);
+    const double below = __shfl_up(sum, 1);
+    c.n_before = threadIdx.x & 63 ? n_base + n_below : n_base;
+    c.before = threadIdx.x & 63 ? base + below : base;
+    c.n_upto = n_base + n_sum;
+    c.upto = base + sum;
+    return true;
+}
+// Weights of the whole row.
+template <int NT>
+__device__ __forceinline__ double whole_weight(const Shared<NT>& s)
+{
+    double sum = 0.0;
+    for (int v = 0; v < NT / 64; ++v) sum += s.part[v];
+    return sum;
+}
+
+// The nth (from 0) of the allowed tokens with logit v, by id.  By the whole workgroup; the result is wavefront 0's.
+template <int DTYPE, int NT, int R, bool BITS>
+__device__ __forceinline__ int32_t find_nth(Shared<NT>& s, Held<DTYPE, NT, R, BITS>& row, float v, uint32_t nth)
+{
+    constexpr int G = Elem<DTYPE>::kGroup;
+    const auto matches = [&](uint4 x, uint32_t on) {
+        float z[G];
+        unpack<DTYPE>(x, z);
+        uint32_t found = 0;
+#pragma unroll
+        for (int j = 0; j < G; ++j) found |= (z[j] == v ? 1u : 0u) << j;
+        return found & on;
+    };
+    // how many there are in every 64 groups, which a wavefront holds
+    const uint32_t lane = threadIdx.x & 63, chunks = (uint32_t)(row.n_groups + 63) / 64;
+    for (uint32_t j = threadIdx.x; j < chunks; j += NT) s.chunk[j] = 0;
+    __syncthreads();
+    row.each([&](int32_t g, uint4 x, uint32_t on) {
+        const uint32_t found = matches(x, on);
+        const u64 any = __ballot(found != 0);
+        if (!any) return;
+        uint32_t n = (uint32_t)__popc(found);
+        if (__ballot(n > 1)) {
+#pragma unroll
+            for (int d = 32; d; d >>= 1) n += __shfl_xor(n, d);
+        } else {
+            n = (uint32_t)__popcll(any);
+        }
+        if (lane == 0) s.chunk[g >> 6] = n;
+    });
+    __syncthreads();
+    if (threadIdx.x >= 64) return 0;
+    const uint32_t per = (chunks + 63) / 64;
+    uint32_t mine = 0;
+    for (uint32_t j = lane * per; j < min(lane * per + per, chunks); ++j) mine += s.chunk[j];
+    uint32_t upto = mine;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const uint32_t other = __shfl_up(upto, d);
+        if ((int)lane >= d) upto += other;
+    }
+    const u64 here = __ballot(upto > nth);
+    if (!here) {                                           // behind the whole groups: the tokens of the first lanes
+        const uint32_t left = nth - __shfl(upto, 63);
+        const u64 behind = __ballot(row.has_last && row.last == v), mask = __ballot(row.has_last && row.last == v && (uint32_t)__popcll(behind & ((1ull << lane) - 1)) == left);
+        return row.n_groups * G + (mask ? __builtin_ctzll(mask) : 0);
+    }
+    const int src = __builtin_ctzll(here);
+    uint32_t chunk = lane * per, left = nth - (upto - mine);
+    if ((int)lane == src)
+        for (; left >= s.chunk[chunk]; ++chunk) left -= s.chunk[chunk];
+    chunk = __shfl(chunk, src);
+    left = __shfl(left, src);
+    const int32_t g = (int32_t)(chunk * 64 + lane);
+    uint32_t on = (1u << G) - 1u;
+    if constexpr (BITS) {
+        on = __builtin_amdgcn_raw_buffer_load_b8(row.buf.bits, DTYPE == TDFA_F32 ? g >> 1 : g, 0, 0);
+        if (DTYPE == TDFA_F32) on = on >> ((g & 1) * 4) & 15u;
+    }
+    if (g >= row.n_groups) on = 0;
+    uint32_t found = matches(group_at<false>(row.buf.x, (uint32_t)g * 16u), on), n = (uint32_t)__popc(found);
+    upto = n;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const uint32_t other = __shfl_up(upto, d);
+        if ((int)lane >= d) upto += other;
+    }
+    const u64 at = __ballot(upto > left);
+    const int owner = at ? __builtin_ctzll(at) : 0;
+    left -= upto - n;                                      // (of the owner's lane)
+    if ((int)lane == owner)
+        for (; left; --left) found &= found - 1;
+    return __shfl(g * G + (found ? __builtin_ctz(found) : 0), owner);
+}
+
+// The draw from a row whose tokens have been counted.  By the whole workgroup; the result is wavefront 0's.
+template <int NT, int R, bool BITS>
+__device__ __forceinline__ Drawn draw_of_counts(Shared<NT>& s, Held<TDFA_BF16, NT, R, BITS>& row, const Counted& c, const Setting& q)
+{
+    if (q.inv_t == 0.0) return {find_nth<TDFA_BF16>(s, row, c.m, 0), 0.0f};
+    const double whole = whole_weight<NT>(s);
+    if (threadIdx.x == 0) s.mass[0] = s.mass[1] = whole;
+    if (threadIdx.x == 1) s.least = 0;
+    __syncthreads();
+    // Every cut leaves a beginning of the order: what it leaves of the weights, as far as it goes.
+    if (q.top_k) {
+        if (c.n_before < q.top_k && q.top_k <= c.n_upto) {
+            uint32_t n = c.n_before;
+            double sum = c.before;
+            each_bin<NT>(s, c.m, q.inv_t, [&](uint32_t, uint32_t tokens, double w) {
+                if (n < q.top_k) sum += (double)tokens * w;
+                n += tokens;
+            });
+            s.mass[0] = fmin(sum, c.upto);                 // (which is the next thread's beginning, however it has been rounded)
+        }
+        __syncthreads();
+    }
+    double kept = s.mass[0];
+    if (q.top_p < 1.0) {
+        const double enough = fmax(q.top_p * kept, 1e-300);
+        if (c.before < enough && enough <= c.upto) {
+            double sum = c.before;
+            each_bin<NT>(s, c.m, q.inv_t, [&](uint32_t, uint32_t tokens, double w) {
+                if (sum < enough) sum += (double)tokens * w;
+            });
+            s.mass[1] = fmin(sum, c.upto);
+        }
+    }
+    if (q.min_p > 0.0) {
+        double sum = c.before, least = 0.0;
+        each_bin<NT>(s, c.m, q.inv_t, [&](uint32_t, uint32_t tokens, double w) {
+            sum += (double)tokens * w;
+            if (w >= q.min_p) least = sum;
+        });
+        if (least > 0.0) atomicMax(&s.least, (u64)__double_as_longlong(fmin(least, c.upto)));
+    }
+    __syncthreads();
+    kept = fmin(kept, s.mass[1]);
+    if (q.min_p > 0.0) kept = fmin(kept, __longlong_as_double((long long)s.least));
+    // the bin up to which the weights come to more than the target, which stays below what is kept
+    const double target = fmin(q.u * kept, __longlong_as_double(__double_as_longlong(kept) - 1));
+    if (c.before <= target && target < c.upto) {
+        double sum = c.before, before = sum, w_at = 1.0;
+        uint32_t at = 0, tokens_at = 1;
+        each_bin<NT>(s, c.m, q.inv_t, [&](uint32_t bin, uint32_t tokens, double w) {
+            if (sum > target && at) return;
+            if (w > 0.0 || !at) {
+                at = bin;
+                tokens_at = tokens;
+                before = sum;
+                w_at = w;
+            }
+            sum += (double)tokens * w;
+        });
+        s.at[0] = at;
+        s.at[1] = (uint32_t)fmin(fmax((target - before) / w_at, 0.0), (double)(tokens_at - 1));
+        s.mass[2] = w_at / kept;
+    }
+    __syncthreads();
+    const float v = value_of(s.at[0]);
+    const uint32_t nth = s.at[1];
+    const double share = s.mass[2];
+    return {find_nth<TDFA_BF16>(s, row, v, nth), (float)log(share)};
 }
 
 __device__ __forceinline__ int32_t target_of(const DrawArgs& a, int32_t q, int32_t token)
@@ -437,22 +838,33 @@ __device__ __forceinline__ StateOf state_of(const SelectArgs& a, uint32_t i)
 }
 
 // One workgroup per sequence.
-template <int DTYPE, int NT, bool BITS>
-__global__ void __launch_bounds__(NT) draw_step_kernel(DrawArgs a)
+template <int DTYPE, int NT, int R, bool BITS>
+__global__ void __launch_bounds__(NT, 4) draw_step_kernel(DrawArgs a)
 {
     __shared__ Shared<NT> s;
     const uint32_t i = blockIdx.x;
     const StateOf st = state_of(a, i);
     const Setting q = setting_of(a, i);
     const RowOf<DTYPE> r = {row_at<DTYPE>(a.logits, i, a.stride16), st.bits, a.n_tokens};
-    const uint32_t n = !st.valid ? 0u : BITS ? count_allowed<NT>(st.bits, a.n_tokens, s.word) : (uint32_t)a.n_tokens;
+    Held<DTYPE, NT, R, BITS> row;
+    uint32_t n = 0;
+    if (st.valid) n = load_row<DTYPE, NT, R, BITS>(s, row, r);
     Drawn d = {TDFA_NO_TOKEN, 0.0f};
     if (n > (uint32_t)kList) {
-        d = draw_by_digits<DTYPE, NT, BITS>(s, r, q);
+        bool done = false;
+        if constexpr (DTYPE == TDFA_BF16) {
+            Counted c;
+            done = count_row<NT, R, BITS>(s, row, q.inv_t, c);
+            if (done) d = draw_of_counts<NT, R, BITS>(s, row, c, q);
+        }
+        if (!done) d = draw_by_digits<DTYPE, NT, BITS>(s, r, q);
     } else if (n) {
-        float m;
-        list_row<DTYPE, NT, BITS>(s, r, q.inv_t, &m);
-        if (threadIdx.x < 64) d = draw_of_list<NT>(s, n, m, q);
+        list_of<DTYPE, NT, R, BITS>(s, row, [](int32_t, float) { return true; });
+        if (threadIdx.x < 64) {
+            const float m = logit_of((uint32_t)(s.sorted[0] >> 32));
+            if (m != -INFINITY) sum_list<NT>(s, n, m, q.inv_t);
+            d = draw_of_list<NT>(s, n, m, q);
+        }
     }
     if (threadIdx.x == 0) {
         a.tokens[i] = d.token;
@@ -461,52 +873,104 @@ __global__ void __launch_bounds__(NT) draw_step_kernel(DrawArgs a)
     }
 }
 
-// One workgroup per row: the k first tokens in order, and their log-probabilities.
+// The first k tokens of a row of any kind, in order, in sorted[], and what the row weighs.  How many there are, 0 if all are -inf.
 template <int DTYPE, int NT, bool BITS>
-__global__ void __launch_bounds__(NT) top_logprobs_kernel(TopArgs a)
+__device__ uint32_t top_by_digits(Shared<NT>& s, const RowOf<DTYPE>& r, uint32_t k, double inv_t, float* m, double* total)
+{
+    uint32_t top = 0;
+    for_each<DTYPE, NT, BITS>(r, [&](int32_t, float z) { top = max(top, key_of(z)); });
+    *m = logit_of(block_max<NT>(top, s.word));
+    if (*m == -INFINITY) return 0;
+    // the k-th largest key, and how many larger ones there are; of the tokens that have it those of the lowest ids
+    u64 larger, unused;
+    const uint32_t key = key_at<NT>(s, k, &larger, [&](auto&& f) { for_each<DTYPE, NT, BITS>(r, [&](int32_t, float z) { f(key_of(z), (u64)1); }); });
+    const uint32_t last = ~key_at<NT>(s, k - larger, &unused, [&](auto&& f) {
+        for_each<DTYPE, NT, BITS>(r, [&](int32_t t, float z) { f(~(uint32_t)t, (u64)(key_of(z) == key)); });
+    });
+    const Whole w = whole_of(*m, inv_t, r.n_tokens);
+    u64 sum = 0;
+    if (threadIdx.x == 0) s.n = 0;
+    __syncthreads();
+    for_each<DTYPE, NT, BITS>(r, [&](int32_t t, float z) {
+        sum += w.of(z);
+        if (key_of(z) > key || (key_of(z) == key && (uint32_t)t <= last)) s.list[atomicAdd(&s.n, 1u)] = (u64)key_of(z) << 32 | ~(uint32_t)t;
+    });
+    *total = (double)block_sum<NT>(sum, s) / w.scale;
+    const uint32_t n = s.n;
+    sort_list<NT>(s, n);
+    return n;
+}
+
+// The same from counts; 0: they do not tell.
+template <int NT, int R, bool BITS>
+__device__ __forceinline__ uint32_t top_of_counts(Shared<NT>& s, Held<TDFA_BF16, NT, R, BITS>& row, uint32_t k, double inv_t, float* m, double* total)
+{
+    Counted c;
+    if (!count_row<NT, R, BITS>(s, row, inv_t, c)) return 0;
+    *m = c.m;
+    *total = whole_weight<NT>(s);
+    if (threadIdx.x == 0) s.at[0] = 0;
+    __syncthreads();
+    if (c.n_before < k && k <= c.n_upto) {
+        uint32_t n = c.n_before;
+        each_bin<NT>(s, c.m, inv_t, [&](uint32_t bin, uint32_t tokens, double) {
+            if (n < k) {
+                s.at[0] = bin;
+                s.at[1] = n;
+                s.at[2] = tokens;
+            }
+            n += tokens;
+        });
+    }
+    __syncthreads();
+    if (!s.at[0]) return 0;                                // fewer than k above -2^8
+    const float v = value_of(s.at[0]);
+    const uint32_t larger = s.at[1], equal = s.at[2];
+    int32_t last = INT32_MAX;
+    if (larger + equal > (uint32_t)kList) {                // more than are wanted have that logit: those of the lowest ids
+        const int32_t t = find_nth<TDFA_BF16>(s, row, v, k - larger - 1);
+        __syncthreads();
+        if (threadIdx.x == 0) s.at[3] = (uint32_t)t;
+        __syncthreads();
+        last = (int32_t)s.at[3];
+    }
+    return list_of<TDFA_BF16, NT, R, BITS>(s, row, [&](int32_t t, float z) { return z > v || (z == v && t <= last); });
+}
+
+// One workgroup per row: the k first tokens in order, and their log-probabilities.
+template <int DTYPE, int NT, int R, bool BITS>
+__global__ void __launch_bounds__(NT, 4) top_logprobs_kernel(TopArgs a)
 {
     __shared__ Shared<NT> s;
     const uint32_t i = blockIdx.x, k = (uint32_t)a.k;
     const StateOf st = state_of(a, i);
     const RowOf<DTYPE> r = {row_at<DTYPE>(a.logits, i, a.stride16), st.bits, a.n_tokens};
     const double inv_t = 1.0 / (double)a.temperature;
-    uint32_t n = !st.valid ? 0u : BITS ? count_allowed<NT>(st.bits, a.n_tokens, s.word) : (uint32_t)a.n_tokens;
+    Held<DTYPE, NT, R, BITS> row;
+    uint32_t n = 0;
+    if (st.valid) n = load_row<DTYPE, NT, R, BITS>(s, row, r);
     float m = -INFINITY;
     double total = 0.0;
     if (n > (uint32_t)kList) {
-        uint32_t top = 0;
-        for_each<DTYPE, NT, BITS>(r, [&](int32_t, float z) { top = max(top, key_of(z)); });
-        m = logit_of(block_max<NT>(top, s.word));
-        if (m != -INFINITY) {
-            // the k-th largest key, and how many larger ones there are; of the tokens that have it those of the lowest ids
-            u64 larger, unused;
-            const uint32_t key = key_at<NT>(s, k, &larger, [&](auto&& f) { for_each<DTYPE, NT, BITS>(r, [&](int32_t, float z) { f(key_of(z), (u64)1); }); });
-            const uint32_t last = ~key_at<NT>(s, k - larger, &unused, [&](auto&& f) {
-                for_each<DTYPE, NT, BITS>(r, [&](int32_t t, float z) { f(~(uint32_t)t, (u64)(key_of(z) == key)); });
-            });
-            const Whole w = whole_of(m, inv_t, a.n_tokens);
-            u64 sum = 0;
-            if (threadIdx.x == 0) s.n = 0;
-            __syncthreads();
-            for_each<DTYPE, NT, BITS>(r, [&](int32_t t, float z) {
-                sum += w.of(z);
-                if (key_of(z) > key || (key_of(z) == key && (uint32_t)t <= last)) s.list[atomicAdd(&s.n, 1u)] = (u64)key_of(z) << 32 | ~(uint32_t)t;
-            });
-            total = (double)block_sum<NT>(sum, s) / w.scale;
-            n = s.n;
-            sort_list<NT>(s.list, n);
-        }
+        n = 0;
+        if constexpr (DTYPE == TDFA_BF16) n = top_of_counts<NT, R, BITS>(s, row, k, inv_t, &m, &total);
+        if (!n) n = top_by_digits<DTYPE, NT, BITS>(s, r, k, inv_t, &m, &total);
     } else if (n) {
-        list_row<DTYPE, NT, BITS>(s, r, inv_t, &m);
-        total = s.cum[n - 1];
+        list_of<DTYPE, NT, R, BITS>(s, row, [](int32_t, float) { return true; });
+        m = logit_of((uint32_t)(s.sorted[0] >> 32));
+        if (m != -INFINITY) {
+            if (threadIdx.x < 64) sum_list<NT>(s, n, m, inv_t);
+            __syncthreads();
+            total = s.cum[n - 1];
+        }
     }
     const double ln_total = m == -INFINITY ? 0.0 : m == INFINITY ? NAN : log(total);
     for (uint32_t j = threadIdx.x; j < k; j += NT) {
         int32_t id = TDFA_NO_TOKEN;
         float lp = -INFINITY;
-        if (m != -INFINITY && j < n && (uint32_t)(s.list[j] >> 32) > kKeyNegInf) {
-            id = (int32_t)~(uint32_t)s.list[j];
-            lp = (float)(((double)logit_of((uint32_t)(s.list[j] >> 32)) - (double)m) * inv_t - ln_total);
+        if (m != -INFINITY && j < n && (uint32_t)(s.sorted[j] >> 32) > kKeyNegInf) {
+            id = (int32_t)~(uint32_t)s.sorted[j];
+            lp = (float)(((double)logit_of((uint32_t)(s.sorted[j] >> 32)) - (double)m) * inv_t - ln_total);
         }
         a.ids[(uint64_t)i * k + j] = id;
         a.logprobs[(uint64_t)i * k + j] = lp;
@@ -535,10 +999,29 @@ void fill(SelectArgs& x, const LogitRows& a, int64_t from)
     x.temperature = a.temperature;
 }
 
-template <int DTYPE, int NT, bool BITS>
-int draw_rows(const DrawArgs& x, unsigned rows, hipStream_t stream) { return launch(draw_step_kernel<DTYPE, NT, BITS>, dim3(rows), NT, stream, x); }
-template <int DTYPE, int NT, bool BITS>
-int top_rows(const TopArgs& x, unsigned rows, hipStream_t stream) { return launch(top_logprobs_kernel<DTYPE, NT, BITS>, dim3(rows), NT, stream, x); }
+// launch_of(type, threads, groups to a thread, whether there is a constraint) for the shape that rows of n_groups take: in registers as
+// long as they fit, few rows by more threads each.
+template <int DTYPE, bool BITS, typename F>
+int shaped(int64_t rows, int32_t n_groups, F&& launch_of)
+{
+    using std::integral_constant;
+    const integral_constant<int, DTYPE> type;
+    const integral_constant<bool, BITS> bits;
+    const auto go = [&](auto threads, auto groups) { return launch_of(type, threads, groups, bits); };
+    if (n_groups <= 256 * 4) return go(integral_constant<int, 256>(), integral_constant<int, 4>());
+    if (n_groups <= 1024 * 4 && rows <= 256) return go(integral_constant<int, 1024>(), integral_constant<int, 4>());
+    if (n_groups <= 256 * 16) return go(integral_constant<int, 256>(), integral_constant<int, 16>());
+    if (n_groups <= 512 * 16) return go(integral_constant<int, 512>(), integral_constant<int, 16>());
+    if (n_groups <= 1024 * 16) return go(integral_constant<int, 1024>(), integral_constant<int, 16>());
+    return go(integral_constant<int, 1024>(), integral_constant<int, 0>());
+}
+template <typename F>
+int shaped(const LogitRows& a, F&& launch_of)
+{
+    const int32_t n_groups = a.n_tokens / (a.dtype == TDFA_F32 ? 4 : 8);
+    if (a.dtype == TDFA_F32) return a.allow ? shaped<TDFA_F32, true>(a.rows, n_groups, launch_of) : shaped<TDFA_F32, false>(a.rows, n_groups, launch_of);
+    return a.allow ? shaped<TDFA_BF16, true>(a.rows, n_groups, launch_of) : shaped<TDFA_BF16, false>(a.rows, n_groups, launch_of);
+}
 
 }  // namespace
 
@@ -560,8 +1043,10 @@ int launch_draw_step(const LogitRows& a, const DrawRows& d, void*, hipStream_t s
         x.top_k = d.top_k;
         x.top_p = d.top_p;
         x.min_p = d.min_p;
-        if (a.dtype == TDFA_F32) return a.allow ? draw_rows<TDFA_F32, 1024, true>(x, rows, stream) : draw_rows<TDFA_F32, 1024, false>(x, rows, stream);
-        return a.allow ? draw_rows<TDFA_BF16, 1024, true>(x, rows, stream) : draw_rows<TDFA_BF16, 1024, false>(x, rows, stream);
+        return shaped(a, [&](auto type, auto threads, auto groups, auto bits) {
+            constexpr int DTYPE = decltype(type)::value, NT = decltype(threads)::value, R = decltype(groups)::value;
+            return launch(draw_step_kernel<DTYPE, NT, R, decltype(bits)::value>, dim3(rows), NT, stream, x);
+        });
     });
 }
 
@@ -573,8 +1058,10 @@ int launch_top_logprobs(const LogitRows& a, int32_t k, int32_t* ids, float* logp
         x.ids = ids + from * k;
         x.logprobs = logprobs + from * k;
         x.k = k;
-        if (a.dtype == TDFA_F32) return a.allow ? top_rows<TDFA_F32, 1024, true>(x, rows, stream) : top_rows<TDFA_F32, 1024, false>(x, rows, stream);
-        return a.allow ? top_rows<TDFA_BF16, 1024, true>(x, rows, stream) : top_rows<TDFA_BF16, 1024, false>(x, rows, stream);
+        return shaped(a, [&](auto type, auto threads, auto groups, auto bits) {
+            constexpr int DTYPE = decltype(type)::value, NT = decltype(threads)::value, R = decltype(groups)::value;
+            return launch(top_logprobs_kernel<DTYPE, NT, R, decltype(bits)::value>, dim3(rows), NT, stream, x);
+        });
     });
 }
 
