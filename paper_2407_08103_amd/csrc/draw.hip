@@ -58,29 +58,60 @@ struct TopArgs : SelectArgs {
     int32_t k;
 };
 
-// What a row is drawn with.  Every value that the arrays of a call can hold means something.
+// What a row is drawn with, the same in all lanes.  Every value that the arrays of a call can hold means something.
 struct Setting {
-    double inv_t;              // 0: the most likely token
-    double top_p, min_p, u;
+    float t, p, least, number;
     uint32_t top_k;            // 0: no cut
+    __device__ __forceinline__ double inv_t() const { return t > 0.0f ? t == INFINITY ? 1e-300 : 1.0 / (double)t : 0.0; }       // 0: the first token; (next to 0: all weigh 1)
+    __device__ __forceinline__ double top_p() const { return p >= 0.0f ? fminf(p, 1.0f) : p < 0.0f ? 0.0 : 1.0; }
+    __device__ __forceinline__ double min_p() const { return fminf(fmaxf(least, 0.0f), 1.0f); }
+    __device__ __forceinline__ double u() const { return fminf(fmaxf(number, 0.0f), 1.0f); }
 };
 __device__ __forceinline__ Setting setting_of(const DrawArgs& a, uint32_t i)
 {
-    float4 v = {a.temperature, (float)a.top_k, a.top_p, a.min_p};
-    Setting s;
-    s.top_k = (uint32_t)a.top_k;
+    Setting s = {a.temperature, a.top_p, a.min_p, 0.0f, (uint32_t)a.top_k};
     if (a.params) {
-        v = a.params[i];
-        s.top_k = v.y >= 1.0f && v.y < 2147483648.0f ? (uint32_t)v.y : 0u;
+        const float4 v = a.params[i];
+        const float k = shared_by_wave(v.y);
+        s.t = shared_by_wave(v.x);
+        s.p = shared_by_wave(v.z);
+        s.least = shared_by_wave(v.w);
+        s.top_k = k >= 1.0f && k < 2147483648.0f ? (uint32_t)k : 0u;
     }
-    const float u = a.uniforms[i];
-    s.inv_t = v.x > 0.0f ? 1.0 / (double)v.x : 0.0;
-    if (v.x == INFINITY) s.inv_t = 1e-300;                 // (all weights are 1)
-    s.top_p = v.z >= 0.0f ? fminf(v.z, 1.0f) : v.z < 0.0f ? 0.0 : 1.0;
-    s.min_p = fminf(fmaxf(v.w, 0.0f), 1.0f);
-    s.u = fminf(fmaxf(u, 0.0f), 1.0f);
+    s.number = shared_by_wave(a.uniforms[i]);
     return s;
 }
+
+// A barrier for what lies in LDS, the only memory that threads hand one another anything in here: reads of a row stay on their way.
+__device__ __forceinline__ void lds_barrier()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+// What the lanes up to this one hold, added up, by data-parallel primitives; lanes that a step has nothing for add 0.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t lanes_below(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xF, true); }
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double lanes_below(double v)
+{
+    const u64 x = (u64)__double_as_longlong(v);
+    return __longlong_as_double((long long)((u64)lanes_below<CTRL, ROWS>((uint32_t)(x >> 32)) << 32 | lanes_below<CTRL, ROWS>((uint32_t)x)));
+}
+template <typename V>
+__device__ __forceinline__ V wave_upto(V v)
+{
+    v += lanes_below<0x111, 0xF>(v);           // row_shr 1, 2, 4, 8
+    v += lanes_below<0x112, 0xF>(v);
+    v += lanes_below<0x114, 0xF>(v);
+    v += lanes_below<0x118, 0xF>(v);
+    v += lanes_below<0x142, 0xA>(v);           // row_bcast 15 into the second and fourth row
+    v += lanes_below<0x143, 0xC>(v);           // row_bcast 31 into the upper two
+    return v;
+}
+template <typename V>
+__device__ __forceinline__ V wave_before(V upto) { return lanes_below<0x138, 0xF>(upto); }       // wave_shr 1
 
 // The weight of a logit beside the largest, m, which is above -inf.
 __device__ __forceinline__ double weight_of(float z, float m, double inv_t)
@@ -139,18 +170,27 @@ struct Held {
     {
         n_groups = r.n_tokens / G;
         buf = row_buffers<DTYPE>(r.row, r.bits, n_groups);
-        if constexpr (R > 0) {
-            fetch_bits<DTYPE, NT, U, BITS>(buf, 0, b);
-            fetch_groups<DTYPE, NT, U, BITS>(buf, 0, n_groups, x, b);
-        }
+        // (before the groups: what is loaded after them arrives after them)
         const int32_t t = n_groups * G + (int32_t)threadIdx.x;
         has_last = t < r.n_tokens && (!BITS || allowed(r.bits, t));
         last = has_last ? to_f32(r.row[t]) : -INFINITY;
+        if constexpr (R > 0) {
+            fetch_bits<DTYPE, NT, U, BITS>(buf, 0, b);
+            next_group();
+            // in the order in which they are looked at: what comes first is not waited for together with the last
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+                const int32_t g = (int32_t)threadIdx.x + k * NT;
+                if constexpr (BITS && DTYPE == TDFA_F32) b[k] = g < n_groups ? b[k] >> ((g & 1) * 4) & 15u : 0u;
+                x[k] = group_at<false>(buf.x, BITS && b[k] == 0 ? kNowhere : (uint32_t)g * 16u);
+                next_group();
+            }
+        }
     }
     __device__ __forceinline__ uint32_t on_of(int k, int32_t g) const { return BITS ? b[k] : g < n_groups ? kAll : 0u; }
     // f(group, its elements, which of them are allowed) for the groups of this thread; those of a wavefront lie side by side, and one
     // without an allowed token is passed over.
-    template <typename F>
+    template <bool ALL = false, typename F>                 // ALL: none is passed over
     __device__ __forceinline__ void each(F&& f)
     {
         for (int32_t g0 = 0; g0 < (R ? 1 : n_groups); g0 += NT * U) {
@@ -159,7 +199,7 @@ struct Held {
             for (int k = 0; k < U; ++k) {
                 const int32_t g = g0 + (int32_t)threadIdx.x + k * NT;
                 const uint32_t on = on_of(k, g);
-                if (!__ballot(on != 0)) continue;
+                if (!ALL && !__ballot(on != 0)) continue;
                 f(g, x[k], on);
                 next_group();
             }
@@ -181,7 +221,7 @@ struct Shared {
     double cum[kList];
     uint32_t rank[kList];
     double part[NT / 64];
-    uint32_t word[NT / 64];
+    uint32_t word[NT / 64], word2[NT / 64];
     uint32_t n;
     u64 found[2];
     double mass[3];
@@ -194,9 +234,9 @@ __device__ __forceinline__ uint32_t block_sum(uint32_t v, uint32_t (&part)[NT / 
 {
 #pragma unroll
     for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
-    __syncthreads();
+    lds_barrier();
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
-    __syncthreads();
+    lds_barrier();
     v = 0;
     for (int w = 0; w < NT / 64; ++w) v += part[w];
     return v;
@@ -206,9 +246,9 @@ __device__ __forceinline__ uint32_t block_max(uint32_t v, uint32_t (&part)[NT / 
 {
 #pragma unroll
     for (int d = 32; d; d >>= 1) v = max(v, (uint32_t)__shfl_xor(v, d));
-    __syncthreads();
+    lds_barrier();
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
-    __syncthreads();
+    lds_barrier();
     v = 0;
     for (int w = 0; w < NT / 64; ++w) v = max(v, part[w]);
     return v;
@@ -239,7 +279,7 @@ __device__ __forceinline__ void sort_list(Shared<NT>& s, uint32_t n)
     const uint32_t i = threadIdx.x & (size - 1), first = threadIdx.x / size, step = NT / size;
     static_assert(NT >= kList);
     if (threadIdx.x < kList) s.rank[threadIdx.x] = 0;
-    __syncthreads();
+    lds_barrier();
     u64 mine = 0;
     if (i < n) {
         mine = s.list[i];
@@ -247,9 +287,9 @@ __device__ __forceinline__ void sort_list(Shared<NT>& s, uint32_t n)
         for (uint32_t j = first; j < n; j += step) above += s.list[j] > mine ? 1u : 0u;
         if (above) atomicAdd(&s.rank[i], above);
     }
-    __syncthreads();
+    lds_barrier();
     if (first == 0 && i < n) s.sorted[s.rank[i]] = mine;
-    __syncthreads();
+    lds_barrier();
 }
 
 // cum[i] = weights of sorted[0 .. i] added up, n of them.  By one wavefront.
@@ -264,13 +304,7 @@ __device__ __forceinline__ void sum_list(Shared<NT>& s, uint32_t n, float m, dou
         if (from + j < n) mine += weight_of(logit_of((uint32_t)(s.sorted[from + j] >> 32)), m, inv_t);
         w[j] = mine;
     }
-    double upto = mine;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const double other = __shfl_up(upto, d);
-        if ((int)lane >= d) upto += other;
-    }
-    const double below = __shfl_up(upto, 1), before = lane ? below : 0.0;
+    const double before = wave_before(wave_upto(mine));
 #pragma unroll
     for (uint32_t j = 0; j < per; ++j)
         if (from + j < n) s.cum[from + j] = before + w[j];
@@ -307,18 +341,18 @@ __device__ __forceinline__ Drawn draw_of_list(const Shared<NT>& s, uint32_t n, f
         const uint32_t k = key(i);
         return first_where(n, [&](uint32_t j) { return key(j) < k; });
     };
-    if (m == -INFINITY || q.inv_t == 0.0) return {id(0), m == -INFINITY ? -INFINITY : 0.0f};
+    if (m == -INFINITY || q.inv_t() == 0.0) return {id(0), m == -INFINITY ? -INFINITY : 0.0f};
     uint32_t kept = n;
     if (q.top_k && q.top_k < n) kept = end_of(q.top_k - 1);
-    if (q.top_p < 1.0) {
-        const double enough = q.top_p * s.cum[kept - 1];
+    if (q.top_p() < 1.0) {
+        const double enough = q.top_p() * s.cum[kept - 1];
         kept = min(kept, end_of(min(kept - 1, first_where(n, [&](uint32_t i) { return s.cum[i] >= enough; }))));
     }
-    if (q.min_p > 0.0) kept = min(kept, first_where(n, [&](uint32_t i) { return weight_of(logit_of(key(i)), m, q.inv_t) < q.min_p; }));
-    const double total = s.cum[kept - 1], target = q.u * total;
+    if (q.min_p() > 0.0) kept = min(kept, first_where(n, [&](uint32_t i) { return weight_of(logit_of(key(i)), m, q.inv_t()) < q.min_p(); }));
+    const double total = s.cum[kept - 1], target = q.u() * total;
     uint32_t at = first_where(n, [&](uint32_t i) { return s.cum[i] > target; });
     if (at >= kept) at = first_where(n, [&](uint32_t i) { return s.cum[i] >= total; });       // u is 1: the last that weighs anything
-    return {id(at), (float)log(weight_of(logit_of(key(at)), m, q.inv_t) / total)};
+    return {id(at), (float)log(weight_of(logit_of(key(at)), m, q.inv_t()) / total)};
 }
 
 // ---- any number of tokens: thresholds digit by digit -------------------------------------------
@@ -331,13 +365,13 @@ __device__ __forceinline__ uint32_t key_at(Shared<NT>& s, u64 want, u64* before,
     uint32_t prefix = 0, fixed = 0;
     u64 above = 0;
     for (int shift = 24; shift >= 0; shift -= 8) {
-        __syncthreads();
+        lds_barrier();
         for (int i = threadIdx.x; i < 256; i += NT) s.bin[i] = 0;
-        __syncthreads();
+        lds_barrier();
         each([&](uint32_t key, u64 value) {
             if ((key & fixed) == prefix && value) atomicAdd(&s.bin[key >> shift & 255u], value);
         });
-        __syncthreads();
+        lds_barrier();
         if (threadIdx.x < 64) {
             const int lane = threadIdx.x;
             u64 v[4], mine = 0;                            // bins 255 - 4 lane .. 252 - 4 lane
@@ -358,7 +392,7 @@ __device__ __forceinline__ uint32_t key_at(Shared<NT>& s, u64 want, u64* before,
                 s.found[1] = sum;
             }
         }
-        __syncthreads();
+        lds_barrier();
         prefix |= (uint32_t)s.found[0] << shift;
         fixed |= 255u << shift;
         above = s.found[1];
@@ -396,9 +430,9 @@ __device__ __forceinline__ u64 block_sum(u64 v, Shared<NT>& s)
 {
 #pragma unroll
     for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
-    __syncthreads();
+    lds_barrier();
     if ((threadIdx.x & 63) == 0) s.bin[threadIdx.x >> 6] = v;
-    __syncthreads();
+    lds_barrier();
     v = 0;
     for (int w = 0; w < NT / 64; ++w) v += s.bin[w];
     return v;
@@ -406,7 +440,7 @@ __device__ __forceinline__ u64 block_sum(u64 v, Shared<NT>& s)
 
 // The draw from a row of any kind, of which some token is allowed.
 template <int DTYPE, int NT, bool BITS>
-__device__ Drawn draw_by_digits(Shared<NT>& s, const RowOf<DTYPE>& r, const Setting& q)
+__device__ __attribute__((noinline)) Drawn draw_by_digits(Shared<NT>& s, RowOf<DTYPE> r, Setting q)
 {
     uint32_t top = 0;
     for_each<DTYPE, NT, BITS>(r, [&](int32_t, float z) { top = max(top, key_of(z)); });
@@ -415,8 +449,8 @@ __device__ Drawn draw_by_digits(Shared<NT>& s, const RowOf<DTYPE>& r, const Sett
     uint32_t key = top;
     u64 nth = 1, before;
     float lp = m == -INFINITY ? -INFINITY : 0.0f;
-    if (m != -INFINITY && q.inv_t != 0.0) {
-        const Whole w = whole_of(m, q.inv_t, r.n_tokens);
+    if (m != -INFINITY && q.inv_t() != 0.0) {
+        const Whole w = whole_of(m, q.inv_t(), r.n_tokens);
         uint32_t cut = 0;                                  // the smallest key that is kept
         const auto weights = [&](auto&& f) { for_each<DTYPE, NT, BITS>(r, [&](int32_t, float z) { if (key_of(z) >= cut) f(key_of(z), w.of(z)); }); };
         const auto kept_weight = [&]() {
@@ -430,31 +464,34 @@ __device__ Drawn draw_by_digits(Shared<NT>& s, const RowOf<DTYPE>& r, const Sett
             n = block_sum<NT>(n, s);
             if (q.top_k < n) cut = key_at<NT>(s, q.top_k, &before, [&](auto&& f) { for_each<DTYPE, NT, BITS>(r, [&](int32_t, float z) { f(key_of(z), (u64)1); }); });
         }
-        if (q.top_p < 1.0) {
-            const u64 enough = share_of(q.top_p, kept_weight(), true);
+        if (q.top_p() < 1.0) {
+            const u64 enough = share_of(q.top_p(), kept_weight(), true);
             cut = max(cut, enough ? key_at<NT>(s, enough, &before, weights) : top);
         }
-        if (q.min_p > 0.0) {
+        if (q.min_p() > 0.0) {
             uint32_t least = top;
-            for_each<DTYPE, NT, BITS>(r, [&](int32_t, float z) { if (weight_of(z, m, q.inv_t) >= q.min_p) least = min(least, key_of(z)); });
+            for_each<DTYPE, NT, BITS>(r, [&](int32_t, float z) { if (weight_of(z, m, q.inv_t()) >= q.min_p()) least = min(least, key_of(z)); });
             cut = max(cut, ~block_max<NT>(~least, s.word));
         }
-        const u64 total = kept_weight(), target = min(share_of(q.u, total, false), total - 1);
+        const u64 total = kept_weight(), target = min(share_of(q.u(), total, false), total - 1);
         key = key_at<NT>(s, target + 1, &before, weights);
         nth = (target - before) / w.of(logit_of(key)) + 1;
-        lp = (float)log(weight_of(logit_of(key), m, q.inv_t) / ((double)total / w.scale));
+        lp = (float)log(weight_of(logit_of(key), m, q.inv_t()) / ((double)total / w.scale));
     }
     // the nth token of that logit
     const uint32_t id = ~key_at<NT>(s, nth, &before, [&](auto&& f) { for_each<DTYPE, NT, BITS>(r, [&](int32_t t, float z) { f(~(uint32_t)t, (u64)(key_of(z) == key)); }); });
     return {(int32_t)id, lp};
 }
 
-// Takes hold of a row.  How many tokens are allowed; one or two barriers.
+// Takes hold of a row.  How many tokens are allowed; a barrier at least.
 template <int DTYPE, int NT, int R, bool BITS>
 __device__ __forceinline__ uint32_t load_row(Shared<NT>& s, Held<DTYPE, NT, R, BITS>& row, const RowOf<DTYPE>& r)
 {
     row.load(r);
-    if (!BITS) return (uint32_t)r.n_tokens;
+    if (!BITS) {
+        lds_barrier();
+        return (uint32_t)r.n_tokens;
+    }
     if (R == 0) return count_allowed<NT>(r.bits, r.n_tokens, s.word);
     uint32_t n = row.has_last ? 1u : 0u;
 #pragma unroll
@@ -462,30 +499,36 @@ __device__ __forceinline__ uint32_t load_row(Shared<NT>& s, Held<DTYPE, NT, R, B
     return block_sum<NT>(n, s.word);
 }
 
-// The tokens of a row for which wanted(token, logit) holds, at most kList, in order.  How many there are; five barriers.
-template <int DTYPE, int NT, int R, bool BITS, typename F>
-__device__ __forceinline__ uint32_t list_of(Shared<NT>& s, Held<DTYPE, NT, R, BITS>& row, F&& wanted)
+// The tokens of a row for which wanted(token, logit) holds, at most kList, in order.  maybe(a group's elements): whether it may for one of
+// them.  How many there are; five barriers.
+template <int DTYPE, int NT, int R, bool BITS, typename M, typename F>
+__device__ __forceinline__ uint32_t list_of(Shared<NT>& s, Held<DTYPE, NT, R, BITS>& row, M&& maybe, F&& wanted)
 {
     constexpr int G = Elem<DTYPE>::kGroup;
     if (threadIdx.x == 0) s.n = 0;
-    __syncthreads();
+    lds_barrier();
     const auto add = [&](int32_t t, float z) {
         const uint32_t i = atomicAdd(&s.n, 1u);
         if (i < (uint32_t)kList) s.list[i] = (u64)key_of(z) << 32 | ~(uint32_t)t;
     };
     row.each([&](int32_t g, uint4 x, uint32_t on) {
-        float z[G];
-        unpack<DTYPE>(x, z);
-#pragma unroll
-        for (int j = 0; j < G; ++j)
-            if ((on >> j & 1) && wanted(g * G + j, z[j])) add(g * G + j, z[j]);
+        for (uint32_t left = maybe(x) ? on : 0u; left; left &= left - 1) {
+            const int32_t j = __builtin_ctz(left);
+            const float z = element_of<DTYPE>(x, j);
+            if (wanted(g * G + j, z)) add(g * G + j, z);
+        }
     });
     const int32_t behind = row.n_groups * G + (int32_t)threadIdx.x;
     if (row.has_last && wanted(behind, row.last)) add(behind, row.last);
-    __syncthreads();
+    lds_barrier();
     const uint32_t n = min(s.n, (uint32_t)kList);
     sort_list<NT>(s, n);
     return n;
+}
+template <int DTYPE, int NT, int R, bool BITS>
+__device__ __forceinline__ uint32_t list_all(Shared<NT>& s, Held<DTYPE, NT, R, BITS>& row)
+{
+    return list_of<DTYPE, NT, R, BITS>(s, row, [](uint4) { return true; }, [](int32_t, float) { return true; });
 }
 
 // ---- 16-bit logits: how many tokens have each logit ----------------------------------------------
@@ -526,25 +569,28 @@ __device__ __forceinline__ uint32_t counts_of(const Shared<NT>& s, uint32_t stre
     n[0] = hi.w; n[1] = hi.z; n[2] = hi.y; n[3] = hi.x; n[4] = lo.w; n[5] = lo.z; n[6] = lo.y; n[7] = lo.x;
     return (hi.x | hi.y | hi.z | hi.w) | (lo.x | lo.y | lo.z | lo.w);
 }
+// What a thread keeps of its share: the tokens of every bin, of every stretch the weight of the first bin with tokens, and the factor from a
+// weight to the next (the values of a stretch lie equally far from one another).
+template <int NT>
+struct Bins {
+    uint32_t n[kShare<NT>][8];
+    double first[kShare<NT>], factor[kShare<NT>];
+};
 // f(bin, tokens, weight) in the order of the values, for bins with tokens.
 template <int NT, typename F>
-__device__ __forceinline__ void each_bin(const Shared<NT>& s, float m, double inv_t, F&& f)
+__device__ __forceinline__ void each_bin(const Shared<NT>& s, const Bins<NT>& b, float m, double inv_t, F&& f)
 {
+#pragma unroll
     for (uint32_t p = 0; p < kShare<NT>; ++p) {
         const uint32_t o = threadIdx.x * kShare<NT> + p;
-        if (o >= kStretches) return;
-        const uint32_t top = top_of(o);
-        uint32_t n[8];
-        if (counts_of<NT>(s, o, n)) {
-            // the values lie equally far from one another: a weight is a power of one factor, unless that is beyond all reach
-            const double first = (double)value_of(top) - (double)m, step = ((double)value_of(top - 1) - (double)value_of(top)) * inv_t;
-            const bool by_steps = step > -16.0;
-            const double factor = by_steps ? exp(step) : 0.0;
-            double w = by_steps ? exp(first * inv_t) : 0.0;
+        double w = b.first[p];
+        bool begun = false;
 #pragma unroll
-            for (uint32_t j = 0; j < 8; ++j) {
-                if (n[j]) f(top - j, n[j], by_steps && value_of(top - j) != m ? w : weight_of(value_of(top - j), m, inv_t));        // (of the largest: 1)
-                w *= factor;
+        for (uint32_t j = 0; j < 8; ++j) {
+            if (begun) w *= b.factor[p];
+            if (b.n[p][j]) {
+                f(top_of(o) - j, b.n[p][j], w);
+                begun = true;
             }
         }
         if (has_zero(o) && s.count[kZeroBin]) f(kZeroBin, s.count[kZeroBin], weight_of(0.0f, m, inv_t));
@@ -558,15 +604,22 @@ struct Counted {
     float m;                   // the largest logit
     uint32_t n_before, n_upto;
     double before, upto;       // weights up to this thread's bins, and with them
+    double whole;
 };
+
+// Clears the counts, before a barrier.
+template <int NT>
+__device__ __forceinline__ void clear_counts(Shared<NT>& s)
+{
+    for (uint32_t j = threadIdx.x; j < kBins / 4; j += NT) reinterpret_cast<uint4*>(s.count)[j] = make_uint4(0, 0, 0, 0);
+    if (threadIdx.x < kBins % 4) s.count[kBins / 4 * 4 + threadIdx.x] = 0;
+}
 
 // Counts the tokens of a row by their logits, and weighs them.  False: there are logits that the bins do not tell apart and that matter.
 template <int NT, int R, bool BITS>
-__device__ __forceinline__ bool count_row(Shared<NT>& s, Held<TDFA_BF16, NT, R, BITS>& row, double inv_t, Counted& c)
+__device__ __forceinline__ bool count_row(Shared<NT>& s, Held<TDFA_BF16, NT, R, BITS>& row, double inv_t, Bins<NT>& b, Counted& c)
 {
     if (row.n_groups > kCountedGroups) return false;
-    for (uint32_t j = threadIdx.x; j < kBins; j += NT) s.count[j] = 0;
-    __syncthreads();
     row.each([&](int32_t, uint4 x, uint32_t on) {
         float z[8];
         unpack<TDFA_BF16>(x, z);
@@ -576,98 +629,99 @@ __device__ __forceinline__ bool count_row(Shared<NT>& s, Held<TDFA_BF16, NT, R, 
             for (int j = 0; j < 8; ++j) atomicAdd(&s.count[bin_of(z[j])], on >> j & 1u);
     });
     if (row.has_last) atomicAdd(&s.count[bin_of(row.last)], 1u);
-    __syncthreads();
+    lds_barrier();
     if (s.count[kHighBin] | s.count[kZeroBin + 1] | s.count[kZeroBin + 2] | s.count[kZeroBin + 3]) return false;
     if (s.count[kZeroBin]) {                               // NaN counts as -inf, and other numbers than zero have no bin
         if (threadIdx.x < 2) s.at[threadIdx.x] = 0;
-        __syncthreads();
+        lds_barrier();
         uint32_t odd = 0, nans = 0;
         const auto look = [&](float z) {
             nans += z != z ? 1u : 0u;
             odd += z != 0.0f && bin_of(z) == kZeroBin && z == z ? 1u : 0u;
         };
         row.each([&](int32_t, uint4 x, uint32_t on) {
-            float z[8];
-            unpack<TDFA_BF16>(x, z);
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (on >> j & 1) look(z[j]);
+            for (; on; on &= on - 1) look(element_of<TDFA_BF16>(x, __builtin_ctz(on)));
         });
         if (row.has_last) look(row.last);
         if (nans) atomicAdd(&s.at[0], nans);
         if (odd) atomicAdd(&s.at[1], odd);
-        __syncthreads();
+        lds_barrier();
         if (s.at[1]) return false;
         if (threadIdx.x == 0) s.count[kZeroBin] -= s.at[0];
-        __syncthreads();
+        lds_barrier();
     }
     // the largest logit
     uint32_t top = 0;
 #pragma unroll
     for (uint32_t p = 0; p < kShare<NT>; ++p) {
         const uint32_t o = threadIdx.x * kShare<NT> + p;
-        uint32_t n[8];
-        if (top || o >= kStretches) continue;
-        if (counts_of<NT>(s, o, n))
+#pragma unroll
+        for (int j = 0; j < 8; ++j) b.n[p][j] = 0;
+        if (o >= kStretches) continue;
+        uint32_t found = 0;
+        if (counts_of<NT>(s, o, b.n[p]))
 #pragma unroll
             for (int j = 7; j >= 0; --j)
-                if (n[j]) top = top_of(o) - (uint32_t)j;
-        if (!top && has_zero(o) && s.count[kZeroBin]) top = kZeroBin;
+                if (b.n[p][j]) found = top_of(o) - (uint32_t)j;
+        if (has_zero(o) && !found && s.count[kZeroBin]) found = kZeroBin;
+        if (!top) top = found;
     }
-    top = block_max<NT>(top, s.word);
+    // lanes are in the order of the values
+    const u64 some = __ballot(top != 0);
+    top = some ? (uint32_t)__builtin_amdgcn_readlane((int)top, __builtin_ctzll(some)) : 0u;
+    if ((threadIdx.x & 63) == 0) s.word[threadIdx.x >> 6] = top;
+    lds_barrier();
+    top = 0;
+#pragma unroll
+    for (int v = NT / 64 - 1; v >= 0; --v) top = s.word[v] ? s.word[v] : top;
     if (!top) return false;
     c.m = value_of(top);
     // what is not above -2^8 has to weigh next to nothing: less than 2^24 exp(-64) of the whole
     if (s.count[kLowBin] && !((-256.0 - (double)c.m) * inv_t < -64.0) && inv_t != 0.0) return false;
     uint32_t n = 0;
     double w = 0.0;
-    if (inv_t != 0.0)
-        each_bin<NT>(s, c.m, inv_t, [&](uint32_t, uint32_t tokens, double weight) {
+    if (inv_t != 0.0) {
+#pragma unroll
+        for (uint32_t p = 0; p < kShare<NT>; ++p) {
+            uint32_t begin = 8;
+#pragma unroll
+            for (int j = 7; j >= 0; --j)
+                if (b.n[p][j]) begin = (uint32_t)j;
+            b.first[p] = b.factor[p] = 0.0;
+            if (begin == 8) continue;
+            const uint32_t at = top_of(threadIdx.x * kShare<NT> + p);
+            b.first[p] = weight_of(value_of(at - begin), c.m, inv_t);
+            b.factor[p] = exp(((double)value_of(at - 7) - (double)value_of(at - 6)) * inv_t);
+        }
+        each_bin<NT>(s, b, c.m, inv_t, [&](uint32_t, uint32_t tokens, double weight) {
             n += tokens;
             w += (double)tokens * weight;
         });
-    // sums before and up to every thread: what one ends with is to the last bit what the next begins with
-    uint32_t n_sum = n;
-    double sum = w;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const uint32_t n_other = __shfl_up(n_sum, d);
-        const double other = __shfl_up(sum, d);
-        if ((int)(threadIdx.x & 63) >= d) {
-            n_sum += n_other;
-            sum += other;
-        }
     }
-    __syncthreads();
+    // sums before and up to every thread: what one ends with is to the last bit what the next begins with
+    const uint32_t n_sum = wave_upto(n), n_below = wave_before(n_sum);
+    const double sum = wave_upto(w), below = wave_before(sum);
     if ((threadIdx.x & 63) == 63) {
-        s.word[threadIdx.x >> 6] = n_sum;
+        s.word2[threadIdx.x >> 6] = n_sum;
         s.part[threadIdx.x >> 6] = sum;
     }
-    __syncthreads();
+    lds_barrier();
     uint32_t n_base = 0;
-    double base = 0.0;
-    for (uint32_t v = 0; v < threadIdx.x >> 6; ++v) {
-        n_base += s.word[v];
-        base += s.part[v];
+    double base = 0.0, all = 0.0;
+#pragma unroll
+    for (uint32_t v = 0; v < NT / 64; ++v) {               // (in one order, or an interval could begin where none has ended)
+        if (v == threadIdx.x >> 6) base = all;
+        if (v < threadIdx.x >> 6) n_base += s.word2[v];
+        all += s.part[v];
     }
-    const uint32_t n_below = __shfl_up(n_sum, 1);
-    const double below = __shfl_up(sum, 1);
-    c.n_before = threadIdx.x & 63 ? n_base + n_below : n_base;
-    c.before = threadIdx.x & 63 ? base + below : base;
+    c.n_before = n_base + n_below;
+    c.before = base + below;
     c.n_upto = n_base + n_sum;
     c.upto = base + sum;
+    c.whole = all;
     return true;
 }
-// Weights of the whole row.
-template <int NT>
-__device__ __forceinline__ double whole_weight(const Shared<NT>& s)
-{
-    double sum = 0.0;
-    for (int v = 0; v < NT / 64; ++v) sum += s.part[v];
-    return sum;
-}
-
-// The nth (from 0) of the allowed tokens with logit v, by id.  By the whole workgroup; the result is wavefront 0's.
+// The nth (from 0) of the allowed tokens with logit v, by id, in the one thread that holds it; -1 in all others.
 template <int DTYPE, int NT, int R, bool BITS>
 __device__ __forceinline__ int32_t find_nth(Shared<NT>& s, Held<DTYPE, NT, R, BITS>& row, float v, uint32_t nth)
 {
@@ -680,120 +734,127 @@ __device__ __forceinline__ int32_t find_nth(Shared<NT>& s, Held<DTYPE, NT, R, BI
         for (int j = 0; j < G; ++j) found |= (z[j] == v ? 1u : 0u) << j;
         return found & on;
     };
+    // Whether a group has any; 16 bits: two elements at a time, of zero without its sign.
+    const uint32_t bits = DTYPE == TDFA_F32 ? __float_as_uint(v) : (__float_as_uint(v) >> 16) * 0x10001u, sign = v == 0.0f ? (DTYPE == TDFA_F32 ? 0x7FFFFFFFu : 0x7FFF7FFFu) : 0xFFFFFFFFu;
+    const auto maybe = [&](uint4 x) {
+        const uint32_t w[4] = {(x.x ^ bits) & sign, (x.y ^ bits) & sign, (x.z ^ bits) & sign, (x.w ^ bits) & sign};
+        if constexpr (DTYPE == TDFA_F32) {
+            return min(min(w[0], w[1]), min(w[2], w[3])) == 0;
+        } else {
+            typedef unsigned short pair __attribute__((ext_vector_type(2)));
+            const auto p = [&](int j) { return __builtin_bit_cast(pair, w[j]); };
+            const uint32_t m = __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_elementwise_min(p(0), p(1)), __builtin_elementwise_min(p(2), p(3))));
+            return (m & 0xFFFFu) == 0 || m < 0x10000u;
+        }
+    };
     // how many there are in every 64 groups, which a wavefront holds
     const uint32_t lane = threadIdx.x & 63, chunks = (uint32_t)(row.n_groups + 63) / 64;
-    for (uint32_t j = threadIdx.x; j < chunks; j += NT) s.chunk[j] = 0;
-    __syncthreads();
-    row.each([&](int32_t g, uint4 x, uint32_t on) {
-        const uint32_t found = matches(x, on);
-        const u64 any = __ballot(found != 0);
-        if (!any) return;
-        uint32_t n = (uint32_t)__popc(found);
-        if (__ballot(n > 1)) {
+    row.template each<true>([&](int32_t g, uint4 x, uint32_t on) {
+        uint32_t n = 0;
+        if (__ballot(maybe(x))) {
+            const uint32_t found = matches(x, on);
 #pragma unroll
-            for (int d = 32; d; d >>= 1) n += __shfl_xor(n, d);
-        } else {
-            n = (uint32_t)__popcll(any);
+            for (int j = 0; j < G; ++j) n += (uint32_t)__popcll(__ballot(found >> j & 1));
         }
-        if (lane == 0) s.chunk[g >> 6] = n;
+        if (lane == 0 && (uint32_t)g < chunks * 64) s.chunk[g >> 6] = n;
     });
-    __syncthreads();
-    if (threadIdx.x >= 64) return 0;
+    lds_barrier();
+    // every wavefront finds the chunk, and the one that holds it the token
     const uint32_t per = (chunks + 63) / 64;
     uint32_t mine = 0;
     for (uint32_t j = lane * per; j < min(lane * per + per, chunks); ++j) mine += s.chunk[j];
-    uint32_t upto = mine;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const uint32_t other = __shfl_up(upto, d);
-        if ((int)lane >= d) upto += other;
-    }
+    const uint32_t upto = wave_upto(mine);
     const u64 here = __ballot(upto > nth);
-    if (!here) {                                           // behind the whole groups: the tokens of the first lanes
-        const uint32_t left = nth - __shfl(upto, 63);
-        const u64 behind = __ballot(row.has_last && row.last == v), mask = __ballot(row.has_last && row.last == v && (uint32_t)__popcll(behind & ((1ull << lane) - 1)) == left);
-        return row.n_groups * G + (mask ? __builtin_ctzll(mask) : 0);
+    if (!here) {                                           // behind the whole groups: the tokens of the first threads
+        const uint32_t left = nth - (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
+        const bool match = row.has_last && row.last == v;
+        const u64 behind = __ballot(match);
+        return match && (uint32_t)__popcll(behind & ((1ull << lane) - 1)) == left ? row.n_groups * G + (int32_t)threadIdx.x : -1;
     }
     const int src = __builtin_ctzll(here);
     uint32_t chunk = lane * per, left = nth - (upto - mine);
     if ((int)lane == src)
         for (; left >= s.chunk[chunk]; ++chunk) left -= s.chunk[chunk];
-    chunk = __shfl(chunk, src);
-    left = __shfl(left, src);
-    const int32_t g = (int32_t)(chunk * 64 + lane);
-    uint32_t on = (1u << G) - 1u;
-    if constexpr (BITS) {
-        on = __builtin_amdgcn_raw_buffer_load_b8(row.buf.bits, DTYPE == TDFA_F32 ? g >> 1 : g, 0, 0);
-        if (DTYPE == TDFA_F32) on = on >> ((g & 1) * 4) & 15u;
-    }
-    if (g >= row.n_groups) on = 0;
-    uint32_t found = matches(group_at<false>(row.buf.x, (uint32_t)g * 16u), on), n = (uint32_t)__popc(found);
-    upto = n;
+    chunk = (uint32_t)__builtin_amdgcn_readlane((int)chunk, src);
+    left = (uint32_t)__builtin_amdgcn_readlane((int)left, src);
+    int32_t g = -1;
+    uint32_t found = 0;
+    if constexpr (R > 0) {
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const uint32_t other = __shfl_up(upto, d);
-        if ((int)lane >= d) upto += other;
+        for (int k = 0; k < R; ++k)
+            if ((uint32_t)__builtin_amdgcn_readfirstlane((int)threadIdx.x + k * NT) >> 6 == chunk) {
+                g = (int32_t)threadIdx.x + k * NT;
+                found = matches(row.x[k], row.on_of(k, g));
+            }
+    } else if (threadIdx.x < 64) {
+        g = (int32_t)(chunk * 64 + lane);
+        uint32_t on = g < row.n_groups ? row.kAll : 0u;
+        if constexpr (BITS) {
+            const uint32_t byte = __builtin_amdgcn_raw_buffer_load_b8(row.buf.bits, DTYPE == TDFA_F32 ? g >> 1 : g, 0, 0);
+            on &= DTYPE == TDFA_F32 ? byte >> ((g & 1) * 4) : byte;
+        }
+        found = matches(group_at<false>(row.buf.x, (uint32_t)g * 16u), on);
     }
-    const u64 at = __ballot(upto > left);
-    const int owner = at ? __builtin_ctzll(at) : 0;
-    left -= upto - n;                                      // (of the owner's lane)
-    if ((int)lane == owner)
-        for (; left; --left) found &= found - 1;
-    return __shfl(g * G + (found ? __builtin_ctz(found) : 0), owner);
+    if (g < 0) return -1;
+    const uint32_t n = (uint32_t)__popc(found), before = wave_upto(n) - n;
+    if (left < before || left >= before + n) return -1;
+    for (left -= before; left; --left) found &= found - 1;
+    return g * G + __builtin_ctz(found);
 }
 
-// The draw from a row whose tokens have been counted.  By the whole workgroup; the result is wavefront 0's.
+// The draw from a row whose tokens have been counted, in the one thread that holds the token; the others have none.
 template <int NT, int R, bool BITS>
-__device__ __forceinline__ Drawn draw_of_counts(Shared<NT>& s, Held<TDFA_BF16, NT, R, BITS>& row, const Counted& c, const Setting& q)
+__device__ __forceinline__ Drawn draw_of_counts(Shared<NT>& s, Held<TDFA_BF16, NT, R, BITS>& row, const Bins<NT>& b, const Counted& c, const Setting& q)
 {
-    if (q.inv_t == 0.0) return {find_nth<TDFA_BF16>(s, row, c.m, 0), 0.0f};
-    const double whole = whole_weight<NT>(s);
-    if (threadIdx.x == 0) s.mass[0] = s.mass[1] = whole;
-    if (threadIdx.x == 1) s.least = 0;
-    __syncthreads();
+    if (q.inv_t() == 0.0) return {find_nth<TDFA_BF16>(s, row, c.m, 0), 0.0f};
+    double kept = c.whole;
     // Every cut leaves a beginning of the order: what it leaves of the weights, as far as it goes.
     if (q.top_k) {
+        if (threadIdx.x == 0) s.mass[0] = kept;
+        lds_barrier();
         if (c.n_before < q.top_k && q.top_k <= c.n_upto) {
             uint32_t n = c.n_before;
             double sum = c.before;
-            each_bin<NT>(s, c.m, q.inv_t, [&](uint32_t, uint32_t tokens, double w) {
+            each_bin<NT>(s, b, c.m, q.inv_t(), [&](uint32_t, uint32_t tokens, double w) {
                 if (n < q.top_k) sum += (double)tokens * w;
                 n += tokens;
             });
             s.mass[0] = fmin(sum, c.upto);                 // (which is the next thread's beginning, however it has been rounded)
         }
-        __syncthreads();
+        lds_barrier();
+        kept = s.mass[0];
     }
-    double kept = s.mass[0];
-    if (q.top_p < 1.0) {
-        const double enough = fmax(q.top_p * kept, 1e-300);
-        if (c.before < enough && enough <= c.upto) {
+    if (q.top_p() < 1.0 || q.min_p() > 0.0) {
+        const double enough = fmax(q.top_p() * kept, 1e-300);
+        if (threadIdx.x == 0) s.mass[1] = kept;
+        if (threadIdx.x == 1) s.least = 0;
+        lds_barrier();
+        if (q.top_p() < 1.0 && c.before < enough && enough <= c.upto) {
             double sum = c.before;
-            each_bin<NT>(s, c.m, q.inv_t, [&](uint32_t, uint32_t tokens, double w) {
+            each_bin<NT>(s, b, c.m, q.inv_t(), [&](uint32_t, uint32_t tokens, double w) {
                 if (sum < enough) sum += (double)tokens * w;
             });
             s.mass[1] = fmin(sum, c.upto);
         }
+        if (q.min_p() > 0.0) {
+            double sum = c.before, least = 0.0;
+            each_bin<NT>(s, b, c.m, q.inv_t(), [&](uint32_t, uint32_t tokens, double w) {
+                sum += (double)tokens * w;
+                if (w >= q.min_p()) least = sum;
+            });
+            if (least > 0.0) atomicMax(&s.least, (u64)__double_as_longlong(fmin(least, c.upto)));
+        }
+        lds_barrier();
+        kept = fmin(kept, s.mass[1]);
+        if (q.min_p() > 0.0) kept = fmin(kept, __longlong_as_double((long long)s.least));
     }
-    if (q.min_p > 0.0) {
-        double sum = c.before, least = 0.0;
-        each_bin<NT>(s, c.m, q.inv_t, [&](uint32_t, uint32_t tokens, double w) {
-            sum += (double)tokens * w;
-            if (w >= q.min_p) least = sum;
-        });
-        if (least > 0.0) atomicMax(&s.least, (u64)__double_as_longlong(fmin(least, c.upto)));
-    }
-    __syncthreads();
-    kept = fmin(kept, s.mass[1]);
-    if (q.min_p > 0.0) kept = fmin(kept, __longlong_as_double((long long)s.least));
     // the bin up to which the weights come to more than the target, which stays below what is kept
-    const double target = fmin(q.u * kept, __longlong_as_double(__double_as_longlong(kept) - 1));
+    const double target = fmin(q.u() * kept, __longlong_as_double(__double_as_longlong(kept) - 1));
     if (c.before <= target && target < c.upto) {
         double sum = c.before, before = sum, w_at = 1.0;
         uint32_t at = 0, tokens_at = 1;
-        each_bin<NT>(s, c.m, q.inv_t, [&](uint32_t bin, uint32_t tokens, double w) {
-            if (sum > target && at) return;
-            if (w > 0.0 || !at) {
+        each_bin<NT>(s, b, c.m, q.inv_t(), [&](uint32_t bin, uint32_t tokens, double w) {
+            if ((sum <= target && w > 0.0) || !at) {
                 at = bin;
                 tokens_at = tokens;
                 before = sum;
@@ -805,11 +866,12 @@ __device__ __forceinline__ Drawn draw_of_counts(Shared<NT>& s, Held<TDFA_BF16, N
         s.at[1] = (uint32_t)fmin(fmax((target - before) / w_at, 0.0), (double)(tokens_at - 1));
         s.mass[2] = w_at / kept;
     }
-    __syncthreads();
+    lds_barrier();
     const float v = value_of(s.at[0]);
     const uint32_t nth = s.at[1];
     const double share = s.mass[2];
-    return {find_nth<TDFA_BF16>(s, row, v, nth), (float)log(share)};
+    const int32_t token = find_nth<TDFA_BF16>(s, row, v, nth);
+    return {token, token >= 0 ? (float)log(share) : 0.0f};
 }
 
 __device__ __forceinline__ int32_t target_of(const DrawArgs& a, int32_t q, int32_t token)
@@ -839,7 +901,7 @@ __device__ __forceinline__ StateOf state_of(const SelectArgs& a, uint32_t i)
 
 // One workgroup per sequence.
 template <int DTYPE, int NT, int R, bool BITS>
-__global__ void __launch_bounds__(NT, 4) draw_step_kernel(DrawArgs a)
+__global__ void __launch_bounds__(NT, NT == 256 ? 3 : 4) draw_step_kernel(DrawArgs a)
 {
     __shared__ Shared<NT> s;
     const uint32_t i = blockIdx.x;
@@ -847,26 +909,31 @@ __global__ void __launch_bounds__(NT, 4) draw_step_kernel(DrawArgs a)
     const Setting q = setting_of(a, i);
     const RowOf<DTYPE> r = {row_at<DTYPE>(a.logits, i, a.stride16), st.bits, a.n_tokens};
     Held<DTYPE, NT, R, BITS> row;
-    uint32_t n = 0;
-    if (st.valid) n = load_row<DTYPE, NT, R, BITS>(s, row, r);
+    if (DTYPE == TDFA_BF16) clear_counts<NT>(s);
+    const uint32_t n = (uint32_t)__builtin_amdgcn_readfirstlane((int)(st.valid ? load_row<DTYPE, NT, R, BITS>(s, row, r) : 0u));
     Drawn d = {TDFA_NO_TOKEN, 0.0f};
+    bool mine = threadIdx.x == 0;                          // this thread writes the result
     if (n > (uint32_t)kList) {
         bool done = false;
         if constexpr (DTYPE == TDFA_BF16) {
             Counted c;
-            done = count_row<NT, R, BITS>(s, row, q.inv_t, c);
-            if (done) d = draw_of_counts<NT, R, BITS>(s, row, c, q);
+            Bins<NT> b;
+            done = count_row<NT, R, BITS>(s, row, q.inv_t(), b, c);
+            if (done) {
+                d = draw_of_counts<NT, R, BITS>(s, row, b, c, q);
+                mine = d.token >= 0;
+            }
         }
         if (!done) d = draw_by_digits<DTYPE, NT, BITS>(s, r, q);
     } else if (n) {
-        list_of<DTYPE, NT, R, BITS>(s, row, [](int32_t, float) { return true; });
+        list_all<DTYPE, NT, R, BITS>(s, row);
         if (threadIdx.x < 64) {
             const float m = logit_of((uint32_t)(s.sorted[0] >> 32));
-            if (m != -INFINITY) sum_list<NT>(s, n, m, q.inv_t);
+            if (m != -INFINITY) sum_list<NT>(s, n, m, q.inv_t());
             d = draw_of_list<NT>(s, n, m, q);
         }
     }
-    if (threadIdx.x == 0) {
+    if (mine) {
         a.tokens[i] = d.token;
         if (a.targets) a.new_states[i] = !st.valid ? TDFA_DEAD : d.token == TDFA_NO_TOKEN ? st.q : target_of(a, st.q, d.token);
         if (a.logprobs) a.logprobs[i] = d.lp;
@@ -875,7 +942,7 @@ __global__ void __launch_bounds__(NT, 4) draw_step_kernel(DrawArgs a)
 
 // The first k tokens of a row of any kind, in order, in sorted[], and what the row weighs.  How many there are, 0 if all are -inf.
 template <int DTYPE, int NT, bool BITS>
-__device__ uint32_t top_by_digits(Shared<NT>& s, const RowOf<DTYPE>& r, uint32_t k, double inv_t, float* m, double* total)
+__device__ __attribute__((noinline)) uint32_t top_by_digits(Shared<NT>& s, RowOf<DTYPE> r, uint32_t k, double inv_t, float* m, double* total)
 {
     uint32_t top = 0;
     for_each<DTYPE, NT, BITS>(r, [&](int32_t, float z) { top = max(top, key_of(z)); });
@@ -890,7 +957,7 @@ __device__ uint32_t top_by_digits(Shared<NT>& s, const RowOf<DTYPE>& r, uint32_t
     const Whole w = whole_of(*m, inv_t, r.n_tokens);
     u64 sum = 0;
     if (threadIdx.x == 0) s.n = 0;
-    __syncthreads();
+    lds_barrier();
     for_each<DTYPE, NT, BITS>(r, [&](int32_t t, float z) {
         sum += w.of(z);
         if (key_of(z) > key || (key_of(z) == key && (uint32_t)t <= last)) s.list[atomicAdd(&s.n, 1u)] = (u64)key_of(z) << 32 | ~(uint32_t)t;
@@ -906,14 +973,15 @@ template <int NT, int R, bool BITS>
 __device__ __forceinline__ uint32_t top_of_counts(Shared<NT>& s, Held<TDFA_BF16, NT, R, BITS>& row, uint32_t k, double inv_t, float* m, double* total)
 {
     Counted c;
-    if (!count_row<NT, R, BITS>(s, row, inv_t, c)) return 0;
+    Bins<NT> b;
+    if (!count_row<NT, R, BITS>(s, row, inv_t, b, c)) return 0;
     *m = c.m;
-    *total = whole_weight<NT>(s);
+    *total = c.whole;
     if (threadIdx.x == 0) s.at[0] = 0;
-    __syncthreads();
+    lds_barrier();
     if (c.n_before < k && k <= c.n_upto) {
         uint32_t n = c.n_before;
-        each_bin<NT>(s, c.m, inv_t, [&](uint32_t bin, uint32_t tokens, double) {
+        each_bin<NT>(s, b, c.m, inv_t, [&](uint32_t bin, uint32_t tokens, double) {
             if (n < k) {
                 s.at[0] = bin;
                 s.at[1] = n;
@@ -922,24 +990,24 @@ __device__ __forceinline__ uint32_t top_of_counts(Shared<NT>& s, Held<TDFA_BF16,
             n += tokens;
         });
     }
-    __syncthreads();
+    lds_barrier();
     if (!s.at[0]) return 0;                                // fewer than k above -2^8
     const float v = value_of(s.at[0]);
     const uint32_t larger = s.at[1], equal = s.at[2];
     int32_t last = INT32_MAX;
     if (larger + equal > (uint32_t)kList) {                // more than are wanted have that logit: those of the lowest ids
         const int32_t t = find_nth<TDFA_BF16>(s, row, v, k - larger - 1);
-        __syncthreads();
-        if (threadIdx.x == 0) s.at[3] = (uint32_t)t;
-        __syncthreads();
+        if (t >= 0) s.at[3] = (uint32_t)t;
+        lds_barrier();
         last = (int32_t)s.at[3];
     }
-    return list_of<TDFA_BF16, NT, R, BITS>(s, row, [&](int32_t t, float z) { return z > v || (z == v && t <= last); });
+    return list_of<TDFA_BF16, NT, R, BITS>(s, row, [&](uint4 x) { return max_group<TDFA_BF16>(x, -INFINITY) >= v; },
+                                           [&](int32_t t, float z) { return z > v || (z == v && t <= last); });
 }
 
 // One workgroup per row: the k first tokens in order, and their log-probabilities.
 template <int DTYPE, int NT, int R, bool BITS>
-__global__ void __launch_bounds__(NT, 4) top_logprobs_kernel(TopArgs a)
+__global__ void __launch_bounds__(NT, NT == 256 ? 3 : 4) top_logprobs_kernel(TopArgs a)
 {
     __shared__ Shared<NT> s;
     const uint32_t i = blockIdx.x, k = (uint32_t)a.k;
@@ -947,8 +1015,8 @@ __global__ void __launch_bounds__(NT, 4) top_logprobs_kernel(TopArgs a)
     const RowOf<DTYPE> r = {row_at<DTYPE>(a.logits, i, a.stride16), st.bits, a.n_tokens};
     const double inv_t = 1.0 / (double)a.temperature;
     Held<DTYPE, NT, R, BITS> row;
-    uint32_t n = 0;
-    if (st.valid) n = load_row<DTYPE, NT, R, BITS>(s, row, r);
+    if (DTYPE == TDFA_BF16) clear_counts<NT>(s);
+    uint32_t n = (uint32_t)__builtin_amdgcn_readfirstlane((int)(st.valid ? load_row<DTYPE, NT, R, BITS>(s, row, r) : 0u));
     float m = -INFINITY;
     double total = 0.0;
     if (n > (uint32_t)kList) {
@@ -956,11 +1024,11 @@ __global__ void __launch_bounds__(NT, 4) top_logprobs_kernel(TopArgs a)
         if constexpr (DTYPE == TDFA_BF16) n = top_of_counts<NT, R, BITS>(s, row, k, inv_t, &m, &total);
         if (!n) n = top_by_digits<DTYPE, NT, BITS>(s, r, k, inv_t, &m, &total);
     } else if (n) {
-        list_of<DTYPE, NT, R, BITS>(s, row, [](int32_t, float) { return true; });
+        list_all<DTYPE, NT, R, BITS>(s, row);
         m = logit_of((uint32_t)(s.sorted[0] >> 32));
         if (m != -INFINITY) {
             if (threadIdx.x < 64) sum_list<NT>(s, n, m, inv_t);
-            __syncthreads();
+            lds_barrier();
             total = s.cum[n - 1];
         }
     }
@@ -1010,7 +1078,7 @@ int shaped(int64_t rows, int32_t n_groups, F&& launch_of)
     const auto go = [&](auto threads, auto groups) { return launch_of(type, threads, groups, bits); };
     if (n_groups <= 256 * 4) return go(integral_constant<int, 256>(), integral_constant<int, 4>());
     if (n_groups <= 1024 * 4 && rows <= 256) return go(integral_constant<int, 1024>(), integral_constant<int, 4>());
-    if (n_groups <= 256 * 16) return go(integral_constant<int, 256>(), integral_constant<int, 16>());
+    if (n_groups <= 512 * 8) return go(integral_constant<int, 512>(), integral_constant<int, 8>());
     if (n_groups <= 512 * 16) return go(integral_constant<int, 512>(), integral_constant<int, 16>());
     if (n_groups <= 1024 * 16) return go(integral_constant<int, 1024>(), integral_constant<int, 16>());
     return go(integral_constant<int, 1024>(), integral_constant<int, 0>());
