@@ -127,27 +127,21 @@ struct RowOf {
     int32_t n_tokens;
 };
 
-// f(token, logit) for every allowed token of a row, in no order.
+// f(token, logit) for every allowed token of a row, in no order.  (For rows that nothing faster takes: little code.)
 template <int DTYPE, int NT, bool BITS, typename F>
 __device__ __forceinline__ void for_each(const RowOf<DTYPE>& r, F&& f)
 {
-    constexpr int G = Elem<DTYPE>::kGroup, U = 4;
+    constexpr int G = Elem<DTYPE>::kGroup;
     const int32_t n_groups = r.n_tokens / G;
     const RowBuffers buf = row_buffers<DTYPE>(r.row, r.bits, n_groups);
-    for (int32_t g0 = 0; g0 < n_groups; g0 += NT * U) {
-        uint4 x[U];
-        uint32_t b[U];
-        fetch<DTYPE, NT, U, BITS>(buf, g0, n_groups, x, b);
-#pragma unroll
-        for (int k = 0; k < U; ++k) {
-            const int32_t g = g0 + (int32_t)threadIdx.x + k * NT;
-            const uint32_t on = BITS ? b[k] : g < n_groups ? (1u << G) - 1u : 0u;
-            if (!__ballot(on != 0)) continue;
-            float z[G];
-            unpack<DTYPE>(x[k], z);
-#pragma unroll
-            for (int j = 0; j < G; ++j)
-                if (on >> j & 1) f(g * G + j, z[j]);
+    for (int32_t g0 = 0; g0 < n_groups; g0 += NT) {
+        uint4 x[1];
+        uint32_t b[1];
+        fetch<DTYPE, NT, 1, BITS>(buf, g0, n_groups, x, b);
+        const int32_t g = g0 + (int32_t)threadIdx.x;
+        for (uint32_t left = BITS ? b[0] : g < n_groups ? (1u << G) - 1u : 0u; left; left &= left - 1) {
+            const int32_t j = __builtin_ctz(left);
+            f(g * G + j, element_of<DTYPE>(x[0], j));
         }
     }
     const int32_t t = n_groups * G + (int32_t)threadIdx.x;
@@ -157,12 +151,12 @@ __device__ __forceinline__ void for_each(const RowOf<DTYPE>& r, F&& f)
 // The same row as the threads of a workgroup hold it: R > 0 groups each, in registers, or R = 0: read again by every look at it.
 template <int DTYPE, int NT, int R, bool BITS>
 struct Held {
-    static constexpr int G = Elem<DTYPE>::kGroup, U = R ? R : 8;
+    static constexpr int G = Elem<DTYPE>::kGroup, U = R ? R : 8, kAhead = U < 6 ? U : 6;
     static constexpr uint32_t kAll = (1u << G) - 1u;
     RowBuffers buf;
     int32_t n_groups;
     uint4 x[U];
-    uint32_t b[U];
+    uint32_t b[(U + 3) / 4];   // allowed bits, of four groups each
     float last;                // the element behind the whole groups that belongs to this thread
     bool has_last;             // and whether it is allowed
 
@@ -175,30 +169,56 @@ struct Held {
         has_last = t < r.n_tokens && (!BITS || allowed(r.bits, t));
         last = has_last ? to_f32(r.row[t]) : -INFINITY;
         if constexpr (R > 0) {
-            fetch_bits<DTYPE, NT, U, BITS>(buf, 0, b);
+            load_bits(0);
             next_group();
-            // in the order in which they are looked at: what comes first is not waited for together with the last
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) load_group(k);
+        }
+    }
+    __device__ __forceinline__ void load_bits(int32_t g0)
+    {
+        if constexpr (BITS) {
+            uint32_t y[U];
+            fetch_bits<DTYPE, NT, U, BITS>(buf, g0, y);
 #pragma unroll
             for (int k = 0; k < U; ++k) {
-                const int32_t g = (int32_t)threadIdx.x + k * NT;
-                if constexpr (BITS && DTYPE == TDFA_F32) b[k] = g < n_groups ? b[k] >> ((g & 1) * 4) & 15u : 0u;
-                x[k] = group_at<false>(buf.x, BITS && b[k] == 0 ? kNowhere : (uint32_t)g * 16u);
-                next_group();
+                const int32_t g = g0 + (int32_t)threadIdx.x + k * NT;
+                if (DTYPE == TDFA_F32) y[k] = g < n_groups ? y[k] >> ((g & 1) * 4) & 15u : 0u;
+                b[k / 4] = k % 4 ? b[k / 4] | y[k] << (k % 4 * 8) : y[k];
             }
         }
     }
-    __device__ __forceinline__ uint32_t on_of(int k, int32_t g) const { return BITS ? b[k] : g < n_groups ? kAll : 0u; }
+    // Groups are requested in the order in which they are looked at, kAhead of them before the first look, which requests the others: a
+    // wavefront whose requests do not fit the queue waits with all that it has to do.
+    __device__ __forceinline__ void load_group(int k, int32_t g0 = 0)
+    {
+        x[k] = group_at<false>(buf.x, BITS && bits_at(k) == 0 ? kNowhere : (uint32_t)(g0 + (int32_t)threadIdx.x + k * NT) * 16u);
+        next_group();
+    }
+    __device__ __forceinline__ void load_rest()
+    {
+        if constexpr (R > 0)
+#pragma unroll
+            for (int k = kAhead; k < U; ++k) load_group(k);
+    }
+    __device__ __forceinline__ uint32_t bits_at(int k) const { return b[k / 4] >> (k % 4 * 8) & 0xFFu; }
+    __device__ __forceinline__ uint32_t on_of(int k, int32_t g) const { return BITS ? bits_at(k) : g < n_groups ? kAll : 0u; }
     // f(group, its elements, which of them are allowed) for the groups of this thread; those of a wavefront lie side by side, and one
     // without an allowed token is passed over.
-    template <bool ALL = false, typename F>                 // ALL: none is passed over
+    template <bool ALL = false, bool FIRST = false, typename F>                 // ALL: none is passed over
     __device__ __forceinline__ void each(F&& f)
     {
         for (int32_t g0 = 0; g0 < (R ? 1 : n_groups); g0 += NT * U) {
-            if constexpr (R == 0) fetch<DTYPE, NT, U, BITS>(buf, g0, n_groups, x, b);
+            if constexpr (R == 0) {
+                load_bits(g0);
+#pragma unroll
+                for (int k = 0; k < U; ++k) load_group(k, g0);
+            }
 #pragma unroll
             for (int k = 0; k < U; ++k) {
                 const int32_t g = g0 + (int32_t)threadIdx.x + k * NT;
                 const uint32_t on = on_of(k, g);
+                if (FIRST && R > 0 && k + kAhead < U) load_group(k + kAhead);
                 if (!ALL && !__ballot(on != 0)) continue;
                 f(g, x[k], on);
                 next_group();
@@ -440,7 +460,7 @@ __device__ __forceinline__ u64 block_sum(u64 v, Shared<NT>& s)
 
 // The draw from a row of any kind, of which some token is allowed.
 template <int DTYPE, int NT, bool BITS>
-__device__ __attribute__((noinline)) Drawn draw_by_digits(Shared<NT>& s, RowOf<DTYPE> r, Setting q)
+__device__ __forceinline__ Drawn draw_by_digits(Shared<NT>& s, const RowOf<DTYPE>& r, const Setting& q)
 {
     uint32_t top = 0;
     for_each<DTYPE, NT, BITS>(r, [&](int32_t, float z) { top = max(top, key_of(z)); });
@@ -495,7 +515,7 @@ __device__ __forceinline__ uint32_t load_row(Shared<NT>& s, Held<DTYPE, NT, R, B
     if (R == 0) return count_allowed<NT>(r.bits, r.n_tokens, s.word);
     uint32_t n = row.has_last ? 1u : 0u;
 #pragma unroll
-    for (int k = 0; k < (R ? R : 1); ++k) n += (uint32_t)__popc(row.b[k]);
+    for (int k = 0; k < (row.U + 3) / 4; ++k) n += (uint32_t)__popc(row.b[k]);
     return block_sum<NT>(n, s.word);
 }
 
@@ -528,6 +548,7 @@ __device__ __forceinline__ uint32_t list_of(Shared<NT>& s, Held<DTYPE, NT, R, BI
 template <int DTYPE, int NT, int R, bool BITS>
 __device__ __forceinline__ uint32_t list_all(Shared<NT>& s, Held<DTYPE, NT, R, BITS>& row)
 {
+    row.load_rest();
     return list_of<DTYPE, NT, R, BITS>(s, row, [](uint4) { return true; }, [](int32_t, float) { return true; });
 }
 
@@ -569,11 +590,10 @@ __device__ __forceinline__ uint32_t counts_of(const Shared<NT>& s, uint32_t stre
     n[0] = hi.w; n[1] = hi.z; n[2] = hi.y; n[3] = hi.x; n[4] = lo.w; n[5] = lo.z; n[6] = lo.y; n[7] = lo.x;
     return (hi.x | hi.y | hi.z | hi.w) | (lo.x | lo.y | lo.z | lo.w);
 }
-// What a thread keeps of its share: the tokens of every bin, of every stretch the weight of the first bin with tokens, and the factor from a
-// weight to the next (the values of a stretch lie equally far from one another).
+// What a thread keeps of its share: of every stretch the weight of the first bin with tokens, and the factor from a weight to the next (the
+// values of a stretch lie equally far from one another).
 template <int NT>
 struct Bins {
-    uint32_t n[kShare<NT>][8];
     double first[kShare<NT>], factor[kShare<NT>];
 };
 // f(bin, tokens, weight) in the order of the values, for bins with tokens.
@@ -583,14 +603,18 @@ __device__ __forceinline__ void each_bin(const Shared<NT>& s, const Bins<NT>& b,
 #pragma unroll
     for (uint32_t p = 0; p < kShare<NT>; ++p) {
         const uint32_t o = threadIdx.x * kShare<NT> + p;
-        double w = b.first[p];
-        bool begun = false;
+        if (o >= kStretches) return;
+        uint32_t n[8];
+        if (counts_of<NT>(s, o, n)) {
+            double w = b.first[p];
+            bool begun = false;
 #pragma unroll
-        for (uint32_t j = 0; j < 8; ++j) {
-            if (begun) w *= b.factor[p];
-            if (b.n[p][j]) {
-                f(top_of(o) - j, b.n[p][j], w);
-                begun = true;
+            for (uint32_t j = 0; j < 8; ++j) {
+                if (begun) w *= b.factor[p];
+                if (n[j]) {
+                    f(top_of(o) - j, n[j], w);
+                    begun = true;
+                }
             }
         }
         if (has_zero(o) && s.count[kZeroBin]) f(kZeroBin, s.count[kZeroBin], weight_of(0.0f, m, inv_t));
@@ -620,7 +644,7 @@ template <int NT, int R, bool BITS>
 __device__ __forceinline__ bool count_row(Shared<NT>& s, Held<TDFA_BF16, NT, R, BITS>& row, double inv_t, Bins<NT>& b, Counted& c)
 {
     if (row.n_groups > kCountedGroups) return false;
-    row.each([&](int32_t, uint4 x, uint32_t on) {
+    row.template each<false, true>([&](int32_t, uint4 x, uint32_t on) {
         float z[8];
         unpack<TDFA_BF16>(x, z);
         // (a token that is not allowed adds nothing, wherever; a group without any is not in the registers)
@@ -655,14 +679,12 @@ __device__ __forceinline__ bool count_row(Shared<NT>& s, Held<TDFA_BF16, NT, R, 
 #pragma unroll
     for (uint32_t p = 0; p < kShare<NT>; ++p) {
         const uint32_t o = threadIdx.x * kShare<NT> + p;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) b.n[p][j] = 0;
         if (o >= kStretches) continue;
-        uint32_t found = 0;
-        if (counts_of<NT>(s, o, b.n[p]))
+        uint32_t found = 0, n[8];
+        if (counts_of<NT>(s, o, n))
 #pragma unroll
             for (int j = 7; j >= 0; --j)
-                if (b.n[p][j]) found = top_of(o) - (uint32_t)j;
+                if (n[j]) found = top_of(o) - (uint32_t)j;
         if (has_zero(o) && !found && s.count[kZeroBin]) found = kZeroBin;
         if (!top) top = found;
     }
@@ -683,13 +705,14 @@ __device__ __forceinline__ bool count_row(Shared<NT>& s, Held<TDFA_BF16, NT, R, 
     if (inv_t != 0.0) {
 #pragma unroll
         for (uint32_t p = 0; p < kShare<NT>; ++p) {
-            uint32_t begin = 8;
+            const uint32_t o = threadIdx.x * kShare<NT> + p;
+            uint32_t begin = 8, n[8];
+            b.first[p] = b.factor[p] = 0.0;
+            if (o >= kStretches || !counts_of<NT>(s, o, n)) continue;
 #pragma unroll
             for (int j = 7; j >= 0; --j)
-                if (b.n[p][j]) begin = (uint32_t)j;
-            b.first[p] = b.factor[p] = 0.0;
-            if (begin == 8) continue;
-            const uint32_t at = top_of(threadIdx.x * kShare<NT> + p);
+                if (n[j]) begin = (uint32_t)j;
+            const uint32_t at = top_of(o);
             b.first[p] = weight_of(value_of(at - begin), c.m, inv_t);
             b.factor[p] = exp(((double)value_of(at - 7) - (double)value_of(at - 6)) * inv_t);
         }
@@ -942,7 +965,7 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 3 : 4) draw_step_kernel(DrawAr
 
 // The first k tokens of a row of any kind, in order, in sorted[], and what the row weighs.  How many there are, 0 if all are -inf.
 template <int DTYPE, int NT, bool BITS>
-__device__ __attribute__((noinline)) uint32_t top_by_digits(Shared<NT>& s, RowOf<DTYPE> r, uint32_t k, double inv_t, float* m, double* total)
+__device__ __forceinline__ uint32_t top_by_digits(Shared<NT>& s, const RowOf<DTYPE>& r, uint32_t k, double inv_t, float* m, double* total)
 {
     uint32_t top = 0;
     for_each<DTYPE, NT, BITS>(r, [&](int32_t, float z) { top = max(top, key_of(z)); });
