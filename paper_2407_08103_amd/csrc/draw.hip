@@ -110,6 +110,24 @@ __device__ __forceinline__ V wave_upto(V v)
     v += lanes_below<0x143, 0xC>(v);           // row_bcast 31 into the upper two
     return v;
 }
+__device__ __forceinline__ double lane_value(double v, int lane)
+{
+    const u64 x = (u64)__double_as_longlong(v);
+    return __longlong_as_double((long long)((u64)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)x, lane)));
+}
+// The same sums as borders of the lanes' intervals.  The sum of every lane is rounded in an order of its own, so that it may fall from one lane
+// to the next, or rise where a lane adds nothing: a border is the largest sum up to it of a lane that adds something.
+__device__ __forceinline__ double wave_borders(double v)
+{
+    const double sum = wave_upto(v);
+    double top = v > 0.0 ? sum : 0.0;
+    top = fmax(top, lanes_below<0x111, 0xF>(top));
+    top = fmax(top, lanes_below<0x112, 0xF>(top));
+    top = fmax(top, lanes_below<0x114, 0xF>(top));
+    top = fmax(top, lanes_below<0x118, 0xF>(top));
+    top = fmax(top, lanes_below<0x142, 0xA>(top));
+    return fmax(top, lanes_below<0x143, 0xC>(top));
+}
 template <typename V>
 __device__ __forceinline__ V wave_before(V upto) { return lanes_below<0x138, 0xF>(upto); }       // wave_shr 1
 
@@ -631,6 +649,14 @@ struct Counted {
     double whole;
 };
 
+// Of the upper and the lower halves of four words the smallest each.
+__device__ __forceinline__ uint32_t least_of(uint4 w)
+{
+    typedef unsigned short pair __attribute__((ext_vector_type(2)));
+    const auto p = [](uint32_t x) { return __builtin_bit_cast(pair, x); };
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_elementwise_min(p(w.x), p(w.y)), __builtin_elementwise_min(p(w.z), p(w.w))));
+}
+
 // Clears the counts, before a barrier.
 template <int NT>
 __device__ __forceinline__ void clear_counts(Shared<NT>& s)
@@ -664,6 +690,10 @@ __device__ __forceinline__ bool count_row(Shared<NT>& s, Held<TDFA_BF16, NT, R, 
             odd += z != 0.0f && bin_of(z) == kZeroBin && z == z ? 1u : 0u;
         };
         row.each([&](int32_t, uint4 x, uint32_t on) {
+            // magnitudes, those of NaN the largest: next to zero, or NaN?
+            const uint4 w = make_uint4(x.x & 0x7FFF7FFFu, x.y & 0x7FFF7FFFu, x.z & 0x7FFF7FFFu, x.w & 0x7FFF7FFFu);
+            const uint32_t least = least_of(w), most = ~least_of(make_uint4(~w.x, ~w.y, ~w.z, ~w.w));
+            if ((least & 0xFFFFu) > kLowDown && least >> 16 > kLowDown && (most & 0xFFFFu) <= 0x7F80u && most >> 16 <= 0x7F80u) return;
             for (; on; on &= on - 1) look(element_of<TDFA_BF16>(x, __builtin_ctz(on)));
         });
         if (row.has_last) look(row.last);
@@ -674,17 +704,20 @@ __device__ __forceinline__ bool count_row(Shared<NT>& s, Held<TDFA_BF16, NT, R, 
         if (threadIdx.x == 0) s.count[kZeroBin] -= s.at[0];
         lds_barrier();
     }
-    // the largest logit
-    uint32_t top = 0;
+    // the largest logit, and the first bin with tokens of every stretch (8: none)
+    uint32_t top = 0, begin[kShare<NT>];
 #pragma unroll
     for (uint32_t p = 0; p < kShare<NT>; ++p) {
         const uint32_t o = threadIdx.x * kShare<NT> + p;
+        begin[p] = 8;
         if (o >= kStretches) continue;
         uint32_t found = 0, n[8];
-        if (counts_of<NT>(s, o, n))
+        if (counts_of<NT>(s, o, n)) {
 #pragma unroll
             for (int j = 7; j >= 0; --j)
-                if (n[j]) found = top_of(o) - (uint32_t)j;
+                if (n[j]) begin[p] = (uint32_t)j;
+            found = top_of(o) - begin[p];
+        }
         if (has_zero(o) && !found && s.count[kZeroBin]) found = kZeroBin;
         if (!top) top = found;
     }
@@ -705,15 +738,10 @@ __device__ __forceinline__ bool count_row(Shared<NT>& s, Held<TDFA_BF16, NT, R, 
     if (inv_t != 0.0) {
 #pragma unroll
         for (uint32_t p = 0; p < kShare<NT>; ++p) {
-            const uint32_t o = threadIdx.x * kShare<NT> + p;
-            uint32_t begin = 8, n[8];
             b.first[p] = b.factor[p] = 0.0;
-            if (o >= kStretches || !counts_of<NT>(s, o, n)) continue;
-#pragma unroll
-            for (int j = 7; j >= 0; --j)
-                if (n[j]) begin = (uint32_t)j;
-            const uint32_t at = top_of(o);
-            b.first[p] = weight_of(value_of(at - begin), c.m, inv_t);
+            if (begin[p] == 8) continue;
+            const uint32_t at = top_of(threadIdx.x * kShare<NT> + p);
+            b.first[p] = weight_of(value_of(at - begin[p]), c.m, inv_t);
             b.factor[p] = exp(((double)value_of(at - 7) - (double)value_of(at - 6)) * inv_t);
         }
         each_bin<NT>(s, b, c.m, inv_t, [&](uint32_t, uint32_t tokens, double weight) {
@@ -723,25 +751,23 @@ __device__ __forceinline__ bool count_row(Shared<NT>& s, Held<TDFA_BF16, NT, R, 
     }
     // sums before and up to every thread: what one ends with is to the last bit what the next begins with
     const uint32_t n_sum = wave_upto(n), n_below = wave_before(n_sum);
-    const double sum = wave_upto(w), below = wave_before(sum);
+    const double sum = wave_borders(w), below = wave_before(sum);
     if ((threadIdx.x & 63) == 63) {
         s.word2[threadIdx.x >> 6] = n_sum;
         s.part[threadIdx.x >> 6] = sum;
     }
     lds_barrier();
-    uint32_t n_base = 0;
-    double base = 0.0, all = 0.0;
-#pragma unroll
-    for (uint32_t v = 0; v < NT / 64; ++v) {               // (in one order, or an interval could begin where none has ended)
-        if (v == threadIdx.x >> 6) base = all;
-        if (v < threadIdx.x >> 6) n_base += s.word2[v];
-        all += s.part[v];
-    }
+    // The same over the wavefronts; a lane's interval ends at its wavefront's end at most, and exactly there behind the last that adds anything.
+    const uint32_t lane = threadIdx.x & 63, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)threadIdx.x) >> 6;
+    const uint32_t n_waves = wave_upto(lane < NT / 64 ? s.word2[lane] : 0u);
+    const double waves = wave_borders(lane < NT / 64 ? s.part[lane] : 0.0);
+    const double base = wave ? lane_value(waves, (int)wave - 1) : 0.0, end = lane_value(waves, (int)wave), mine = lane_value(sum, 63);
+    const uint32_t n_base = wave ? (uint32_t)__builtin_amdgcn_readlane((int)n_waves, (int)(wave - 1)) : 0u;
     c.n_before = n_base + n_below;
-    c.before = base + below;
     c.n_upto = n_base + n_sum;
-    c.upto = base + sum;
-    c.whole = all;
+    c.before = below == mine ? end : fmin(base + below, end);
+    c.upto = sum == mine ? end : fmin(base + sum, end);
+    c.whole = lane_value(waves, NT / 64 - 1);
     return true;
 }
 // The nth (from 0) of the allowed tokens with logit v, by id, in the one thread that holds it; -1 in all others.
@@ -758,17 +784,17 @@ __device__ __forceinline__ int32_t find_nth(Shared<NT>& s, Held<DTYPE, NT, R, BI
         return found & on;
     };
     // Whether a group has any; 16 bits: two elements at a time, of zero without its sign.
-    const uint32_t bits = DTYPE == TDFA_F32 ? __float_as_uint(v) : (__float_as_uint(v) >> 16) * 0x10001u, sign = v == 0.0f ? (DTYPE == TDFA_F32 ? 0x7FFFFFFFu : 0x7FFF7FFFu) : 0xFFFFFFFFu;
+    const uint32_t bits = (uint32_t)__builtin_amdgcn_readfirstlane((int)(DTYPE == TDFA_F32 ? __float_as_uint(v) : (__float_as_uint(v) >> 16) * 0x10001u));
+    const bool zero = v == 0.0f;
     const auto maybe = [&](uint4 x) {
-        const uint32_t w[4] = {(x.x ^ bits) & sign, (x.y ^ bits) & sign, (x.z ^ bits) & sign, (x.w ^ bits) & sign};
-        if constexpr (DTYPE == TDFA_F32) {
-            return min(min(w[0], w[1]), min(w[2], w[3])) == 0;
-        } else {
-            typedef unsigned short pair __attribute__((ext_vector_type(2)));
-            const auto p = [&](int j) { return __builtin_bit_cast(pair, w[j]); };
-            const uint32_t m = __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_elementwise_min(p(0), p(1)), __builtin_elementwise_min(p(2), p(3))));
-            return (m & 0xFFFFu) == 0 || m < 0x10000u;
+        if (zero) {
+            constexpr uint32_t sign = DTYPE == TDFA_F32 ? 0x7FFFFFFFu : 0x7FFF7FFFu;
+            x = make_uint4(x.x & sign, x.y & sign, x.z & sign, x.w & sign);
         }
+        const uint4 w = make_uint4(x.x ^ bits, x.y ^ bits, x.z ^ bits, x.w ^ bits);
+        if constexpr (DTYPE == TDFA_F32) return min(min(w.x, w.y), min(w.z, w.w)) == 0;
+        const uint32_t m = least_of(w);
+        return (m & 0xFFFFu) == 0 || m < 0x10000u;
     };
     // how many there are in every 64 groups, which a wavefront holds
     const uint32_t lane = threadIdx.x & 63, chunks = (uint32_t)(row.n_groups + 63) / 64;
