@@ -30,7 +30,10 @@ __device__ __forceinline__ uint32_t key_of(float z)
 __device__ __forceinline__ float logit_of(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key & 0x7FFFFFFFu : ~key); }
 constexpr uint32_t kKeyNegInf = 0x007FFFFFu, kKeyPosInf = 0xFF800000u;
 
-constexpr int kList = 256;             // tokens that are put in order in LDS
+// Tokens that are put in order in LDS.  16 bits: what is put in order are few tokens of a row; 32: the tokens of a step (below), which may be
+// some hundreds.
+template <int DTYPE> constexpr uint32_t kList = DTYPE == TDFA_F32 ? 1024 : 256;
+constexpr uint32_t kFew = 256;         // tokens that are put in order without any other look at them
 
 struct SelectArgs {
     const uint32_t* allow;     // or NULL: every token is allowed
@@ -247,22 +250,29 @@ struct Held {
 
 // What the workgroup of a row shares.
 constexpr uint32_t kBins = 11273;       // see bin_of
-template <int NT>
+constexpr uint32_t kSteps = 4096;      // see step_of
+template <int DTYPE, int NT>
 struct Shared {
     union {
         u64 bin[256];          // of one digit
-        alignas(16) uint32_t count[kBins];
+        alignas(16) uint32_t count[DTYPE == TDFA_F32 ? 4 : kBins];
         uint32_t chunk[kBins];
+        struct {
+            u64 weight[DTYPE == TDFA_F32 ? kSteps : 1];
+            uint32_t tokens[DTYPE == TDFA_F32 ? kSteps : 1];
+        } step;
     };
-    u64 list[kList];           // keys above, complements of ids below
-    u64 sorted[kList];
-    double cum[kList];
-    uint32_t rank[kList];
+    union {
+        u64 list[kList<DTYPE>];    // keys above, complements of ids below
+        double cum[kList<DTYPE>];  // of the sorted ones
+    };
+    u64 sorted[kList<DTYPE>];
+    uint32_t rank[kList<DTYPE>];
     double part[NT / 64];
     uint32_t word[NT / 64], word2[NT / 64];
     uint32_t n;
     u64 found[2];
-    double mass[3];
+    double mass[3], end[3];
     u64 least;
     uint32_t at[4];
 };
@@ -309,43 +319,37 @@ __device__ __forceinline__ uint32_t count_allowed(const uint32_t* bits, int32_t 
 // ---- a few tokens: put in order ----------------------------------------------------------------
 
 // list[0 .. n) in order, the largest first, in sorted[]: every entry counts those above it.  n <= kList; three barriers.
-template <int NT>
-__device__ __forceinline__ void sort_list(Shared<NT>& s, uint32_t n)
+template <int DTYPE, int NT>
+__device__ __forceinline__ void sort_list(Shared<DTYPE, NT>& s, uint32_t n)
 {
-    uint32_t size = 64;
-    while (size < n) size <<= 1;
-    const uint32_t i = threadIdx.x & (size - 1), first = threadIdx.x / size, step = NT / size;
-    static_assert(NT >= kList);
-    if (threadIdx.x < kList) s.rank[threadIdx.x] = 0;
+    for (uint32_t i = threadIdx.x; i < n; i += NT) s.rank[i] = 0;
     lds_barrier();
-    u64 mine = 0;
-    if (i < n) {
-        mine = s.list[i];
+    uint32_t size = 64;
+    while (size < n && size < NT) size <<= 1;              // threads side by side, and NT / size of them for one entry
+    const uint32_t first = threadIdx.x / size, step = NT / size;
+    for (uint32_t i = threadIdx.x & (size - 1); i < n; i += size) {
+        const u64 mine = s.list[i];
         uint32_t above = 0;
         for (uint32_t j = first; j < n; j += step) above += s.list[j] > mine ? 1u : 0u;
         if (above) atomicAdd(&s.rank[i], above);
     }
     lds_barrier();
-    if (first == 0 && i < n) s.sorted[s.rank[i]] = mine;
+    for (uint32_t i = threadIdx.x; i < n; i += NT) s.sorted[s.rank[i]] = s.list[i];
     lds_barrier();
 }
 
 // cum[i] = weights of sorted[0 .. i] added up, n of them.  By one wavefront.
-template <int NT>
-__device__ __forceinline__ void sum_list(Shared<NT>& s, uint32_t n, float m, double inv_t)
+template <int DTYPE, int NT>
+__device__ __forceinline__ void sum_list(Shared<DTYPE, NT>& s, uint32_t n, float m, double inv_t)
 {
-    constexpr uint32_t per = kList / 64;
-    const uint32_t lane = threadIdx.x & 63, from = lane * per;
-    double w[per], mine = 0.0;
-#pragma unroll
-    for (uint32_t j = 0; j < per; ++j) {
-        if (from + j < n) mine += weight_of(logit_of((uint32_t)(s.sorted[from + j] >> 32)), m, inv_t);
-        w[j] = mine;
+    const uint32_t per = (n + 63) / 64, from = (threadIdx.x & 63) * per, to = min(from + per, n);
+    double mine = 0.0;
+    for (uint32_t i = from; i < to; ++i) {
+        mine += weight_of(logit_of((uint32_t)(s.sorted[i] >> 32)), m, inv_t);
+        s.cum[i] = mine;
     }
     const double before = wave_before(wave_upto(mine));
-#pragma unroll
-    for (uint32_t j = 0; j < per; ++j)
-        if (from + j < n) s.cum[from + j] = before + w[j];
+    for (uint32_t i = from; i < to; ++i) s.cum[i] += before;
     wave_lds_sync();
 }
 
@@ -370,8 +374,8 @@ struct Drawn {
 };
 
 // The draw from n >= 1 tokens in order with their running sums.  By one wavefront.
-template <int NT>
-__device__ __forceinline__ Drawn draw_of_list(const Shared<NT>& s, uint32_t n, float m, const Setting& q)
+template <int NT, int DTYPE>
+__device__ __forceinline__ Drawn draw_of_list(const Shared<DTYPE, NT>& s, uint32_t n, float m, const Setting& q)
 {
     const auto key = [&](uint32_t i) { return (uint32_t)(s.sorted[i] >> 32); };
     const auto id = [&](uint32_t i) { return (int32_t)~(uint32_t)s.sorted[i]; };
@@ -397,8 +401,8 @@ __device__ __forceinline__ Drawn draw_of_list(const Shared<NT>& s, uint32_t n, f
 
 // Largest key first, values are added up until they reach `want` > 0: the key at which they do, and the sum before it.
 // each(f) calls f(key, value) for the tokens; they add up to `want` at least.  Eight bits of the key by a pass.
-template <int NT, typename E>
-__device__ __forceinline__ uint32_t key_at(Shared<NT>& s, u64 want, u64* before, E&& each)
+template <int NT, int DTYPE, typename E>
+__device__ __forceinline__ uint32_t key_at(Shared<DTYPE, NT>& s, u64 want, u64* before, E&& each)
 {
     uint32_t prefix = 0, fixed = 0;
     u64 above = 0;
@@ -463,8 +467,8 @@ __device__ __forceinline__ Whole whole_of(float m, double inv_t, int32_t n_token
     return {m, inv_t, ldexp(1.0, 62 - (32 - __clz(max(n_tokens, 1))))};
 }
 
-template <int NT>
-__device__ __forceinline__ u64 block_sum(u64 v, Shared<NT>& s)
+template <int NT, int DTYPE>
+__device__ __forceinline__ u64 block_sum(u64 v, Shared<DTYPE, NT>& s)
 {
 #pragma unroll
     for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
@@ -478,7 +482,7 @@ __device__ __forceinline__ u64 block_sum(u64 v, Shared<NT>& s)
 
 // The draw from a row of any kind, of which some token is allowed.
 template <int DTYPE, int NT, bool BITS>
-__device__ __forceinline__ Drawn draw_by_digits(Shared<NT>& s, const RowOf<DTYPE>& r, const Setting& q)
+__device__ __forceinline__ Drawn draw_by_digits(Shared<DTYPE, NT>& s, const RowOf<DTYPE>& r, const Setting& q)
 {
     uint32_t top = 0;
     for_each<DTYPE, NT, BITS>(r, [&](int32_t, float z) { top = max(top, key_of(z)); });
@@ -523,7 +527,7 @@ __device__ __forceinline__ Drawn draw_by_digits(Shared<NT>& s, const RowOf<DTYPE
 
 // Takes hold of a row.  How many tokens are allowed; a barrier at least.
 template <int DTYPE, int NT, int R, bool BITS>
-__device__ __forceinline__ uint32_t load_row(Shared<NT>& s, Held<DTYPE, NT, R, BITS>& row, const RowOf<DTYPE>& r)
+__device__ __forceinline__ uint32_t load_row(Shared<DTYPE, NT>& s, Held<DTYPE, NT, R, BITS>& row, const RowOf<DTYPE>& r)
 {
     row.load(r);
     if (!BITS) {
@@ -537,17 +541,17 @@ __device__ __forceinline__ uint32_t load_row(Shared<NT>& s, Held<DTYPE, NT, R, B
     return block_sum<NT>(n, s.word);
 }
 
-// The tokens of a row for which wanted(token, logit) holds, at most kList, in order.  maybe(a group's elements): whether it may for one of
-// them.  How many there are; five barriers.
+// The tokens of a row for which wanted(token, logit) holds, in order, if there are at most kList.  maybe(a group's elements): whether it may
+// for one of them.  How many there are; two to five barriers.
 template <int DTYPE, int NT, int R, bool BITS, typename M, typename F>
-__device__ __forceinline__ uint32_t list_of(Shared<NT>& s, Held<DTYPE, NT, R, BITS>& row, M&& maybe, F&& wanted)
+__device__ __forceinline__ uint32_t list_of(Shared<DTYPE, NT>& s, Held<DTYPE, NT, R, BITS>& row, M&& maybe, F&& wanted)
 {
     constexpr int G = Elem<DTYPE>::kGroup;
     if (threadIdx.x == 0) s.n = 0;
     lds_barrier();
     const auto add = [&](int32_t t, float z) {
         const uint32_t i = atomicAdd(&s.n, 1u);
-        if (i < (uint32_t)kList) s.list[i] = (u64)key_of(z) << 32 | ~(uint32_t)t;
+        if (i < kList<DTYPE>) s.list[i] = (u64)key_of(z) << 32 | ~(uint32_t)t;
     };
     row.each([&](int32_t g, uint4 x, uint32_t on) {
         for (uint32_t left = maybe(x) ? on : 0u; left; left &= left - 1) {
@@ -559,15 +563,41 @@ __device__ __forceinline__ uint32_t list_of(Shared<NT>& s, Held<DTYPE, NT, R, BI
     const int32_t behind = row.n_groups * G + (int32_t)threadIdx.x;
     if (row.has_last && wanted(behind, row.last)) add(behind, row.last);
     lds_barrier();
-    const uint32_t n = min(s.n, (uint32_t)kList);
-    sort_list<NT>(s, n);
+    const uint32_t n = (uint32_t)__builtin_amdgcn_readfirstlane((int)s.n);
+    if (n <= kList<DTYPE>) sort_list(s, n);
     return n;
 }
 template <int DTYPE, int NT, int R, bool BITS>
-__device__ __forceinline__ uint32_t list_all(Shared<NT>& s, Held<DTYPE, NT, R, BITS>& row)
+__device__ __forceinline__ uint32_t list_all(Shared<DTYPE, NT>& s, Held<DTYPE, NT, R, BITS>& row)
 {
     row.load_rest();
     return list_of<DTYPE, NT, R, BITS>(s, row, [](uint4) { return true; }, [](int32_t, float) { return true; });
+}
+
+// Tokens and weights of the threads before this one and with it, and the weights of all.  What one thread ends with is to the last bit what the
+// next begins with, and a thread whose weights add nothing has an empty interval.  One barrier.
+struct Sums {
+    uint32_t n_before, n_upto;
+    double before, upto, whole;
+};
+template <int NT, int DTYPE>
+__device__ __forceinline__ Sums sums_of(Shared<DTYPE, NT>& s, uint32_t n, double w)
+{
+    const uint32_t n_sum = wave_upto(n), n_below = wave_before(n_sum);
+    const double sum = wave_borders(w), below = wave_before(sum);
+    if ((threadIdx.x & 63) == 63) {
+        s.word2[threadIdx.x >> 6] = n_sum;
+        s.part[threadIdx.x >> 6] = sum;
+    }
+    lds_barrier();
+    // The same over the wavefronts; a lane's interval ends at its wavefront's end at most, and exactly there behind the last that adds anything.
+    const uint32_t lane = threadIdx.x & 63, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)threadIdx.x) >> 6;
+    const uint32_t n_waves = wave_upto(lane < NT / 64 ? s.word2[lane] : 0u);
+    const double waves = wave_borders(lane < NT / 64 ? s.part[lane] : 0.0);
+    const double base = wave ? lane_value(waves, (int)wave - 1) : 0.0, end = lane_value(waves, (int)wave), mine = lane_value(sum, 63);
+    const uint32_t n_base = wave ? (uint32_t)__builtin_amdgcn_readlane((int)n_waves, (int)(wave - 1)) : 0u;
+    return {n_base + n_below, n_base + n_sum, below == mine ? end : fmin(base + below, end), sum == mine ? end : fmin(base + sum, end),
+            lane_value(waves, NT / 64 - 1)};
 }
 
 // ---- 16-bit logits: how many tokens have each logit ----------------------------------------------
@@ -602,7 +632,7 @@ template <int NT> constexpr uint32_t kShare = (kStretches + NT - 1) / NT;
 __device__ __forceinline__ uint32_t top_of(uint32_t stretch) { return kHighBin - 1 - 8 * stretch - (stretch >= kHalf / 8 ? 4 : 0); }
 __device__ __forceinline__ bool has_zero(uint32_t stretch) { return stretch == kHalf / 8 - 1; }
 template <int NT>
-__device__ __forceinline__ uint32_t counts_of(const Shared<NT>& s, uint32_t stretch, uint32_t (&n)[8])       // the largest value's first; whether there are any
+__device__ __forceinline__ uint32_t counts_of(const Shared<TDFA_BF16, NT>& s, uint32_t stretch, uint32_t (&n)[8])       // the largest value's first; whether there are any
 {
     const uint4 hi = *reinterpret_cast<const uint4*>(&s.count[top_of(stretch) - 3]), lo = *reinterpret_cast<const uint4*>(&s.count[top_of(stretch) - 7]);
     n[0] = hi.w; n[1] = hi.z; n[2] = hi.y; n[3] = hi.x; n[4] = lo.w; n[5] = lo.z; n[6] = lo.y; n[7] = lo.x;
@@ -616,7 +646,7 @@ struct Bins {
 };
 // f(bin, tokens, weight) in the order of the values, for bins with tokens.
 template <int NT, typename F>
-__device__ __forceinline__ void each_bin(const Shared<NT>& s, const Bins<NT>& b, float m, double inv_t, F&& f)
+__device__ __forceinline__ void each_bin(const Shared<TDFA_BF16, NT>& s, const Bins<NT>& b, float m, double inv_t, F&& f)
 {
 #pragma unroll
     for (uint32_t p = 0; p < kShare<NT>; ++p) {
@@ -642,11 +672,8 @@ __device__ __forceinline__ void each_bin(const Shared<NT>& s, const Bins<NT>& b,
 constexpr int32_t kCountedGroups = 64 * (int32_t)kBins;      // of longer rows find_nth has no room for the parts
 
 // What the counts tell all threads of a workgroup, and this one of the bins before its own.
-struct Counted {
+struct Counted : Sums {
     float m;                   // the largest logit
-    uint32_t n_before, n_upto;
-    double before, upto;       // weights up to this thread's bins, and with them
-    double whole;
 };
 
 // Of the upper and the lower halves of four words the smallest each.
@@ -659,7 +686,7 @@ __device__ __forceinline__ uint32_t least_of(uint4 w)
 
 // Clears the counts, before a barrier.
 template <int NT>
-__device__ __forceinline__ void clear_counts(Shared<NT>& s)
+__device__ __forceinline__ void clear_counts(Shared<TDFA_BF16, NT>& s)
 {
     for (uint32_t j = threadIdx.x; j < kBins / 4; j += NT) reinterpret_cast<uint4*>(s.count)[j] = make_uint4(0, 0, 0, 0);
     if (threadIdx.x < kBins % 4) s.count[kBins / 4 * 4 + threadIdx.x] = 0;
@@ -667,7 +694,7 @@ __device__ __forceinline__ void clear_counts(Shared<NT>& s)
 
 // Counts the tokens of a row by their logits, and weighs them.  False: there are logits that the bins do not tell apart and that matter.
 template <int NT, int R, bool BITS>
-__device__ __forceinline__ bool count_row(Shared<NT>& s, Held<TDFA_BF16, NT, R, BITS>& row, double inv_t, Bins<NT>& b, Counted& c)
+__device__ __forceinline__ bool count_row(Shared<TDFA_BF16, NT>& s, Held<TDFA_BF16, NT, R, BITS>& row, double inv_t, Bins<NT>& b, Counted& c)
 {
     if (row.n_groups > kCountedGroups) return false;
     row.template each<false, true>([&](int32_t, uint4 x, uint32_t on) {
@@ -749,30 +776,12 @@ __device__ __forceinline__ bool count_row(Shared<NT>& s, Held<TDFA_BF16, NT, R, 
             w += (double)tokens * weight;
         });
     }
-    // sums before and up to every thread: what one ends with is to the last bit what the next begins with
-    const uint32_t n_sum = wave_upto(n), n_below = wave_before(n_sum);
-    const double sum = wave_borders(w), below = wave_before(sum);
-    if ((threadIdx.x & 63) == 63) {
-        s.word2[threadIdx.x >> 6] = n_sum;
-        s.part[threadIdx.x >> 6] = sum;
-    }
-    lds_barrier();
-    // The same over the wavefronts; a lane's interval ends at its wavefront's end at most, and exactly there behind the last that adds anything.
-    const uint32_t lane = threadIdx.x & 63, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)threadIdx.x) >> 6;
-    const uint32_t n_waves = wave_upto(lane < NT / 64 ? s.word2[lane] : 0u);
-    const double waves = wave_borders(lane < NT / 64 ? s.part[lane] : 0.0);
-    const double base = wave ? lane_value(waves, (int)wave - 1) : 0.0, end = lane_value(waves, (int)wave), mine = lane_value(sum, 63);
-    const uint32_t n_base = wave ? (uint32_t)__builtin_amdgcn_readlane((int)n_waves, (int)(wave - 1)) : 0u;
-    c.n_before = n_base + n_below;
-    c.n_upto = n_base + n_sum;
-    c.before = below == mine ? end : fmin(base + below, end);
-    c.upto = sum == mine ? end : fmin(base + sum, end);
-    c.whole = lane_value(waves, NT / 64 - 1);
+    static_cast<Sums&>(c) = sums_of<NT>(s, n, w);
     return true;
 }
 // The nth (from 0) of the allowed tokens with logit v, by id, in the one thread that holds it; -1 in all others.
 template <int DTYPE, int NT, int R, bool BITS>
-__device__ __forceinline__ int32_t find_nth(Shared<NT>& s, Held<DTYPE, NT, R, BITS>& row, float v, uint32_t nth)
+__device__ __forceinline__ int32_t find_nth(Shared<DTYPE, NT>& s, Held<DTYPE, NT, R, BITS>& row, float v, uint32_t nth)
 {
     constexpr int G = Elem<DTYPE>::kGroup;
     const auto matches = [&](uint4 x, uint32_t on) {
@@ -853,7 +862,7 @@ __device__ __forceinline__ int32_t find_nth(Shared<NT>& s, Held<DTYPE, NT, R, BI
 
 // The draw from a row whose tokens have been counted, in the one thread that holds the token; the others have none.
 template <int NT, int R, bool BITS>
-__device__ __forceinline__ Drawn draw_of_counts(Shared<NT>& s, Held<TDFA_BF16, NT, R, BITS>& row, const Bins<NT>& b, const Counted& c, const Setting& q)
+__device__ __forceinline__ Drawn draw_of_counts(Shared<TDFA_BF16, NT>& s, Held<TDFA_BF16, NT, R, BITS>& row, const Bins<NT>& b, const Counted& c, const Setting& q)
 {
     if (q.inv_t() == 0.0) return {find_nth<TDFA_BF16>(s, row, c.m, 0), 0.0f};
     double kept = c.whole;
@@ -923,6 +932,290 @@ __device__ __forceinline__ Drawn draw_of_counts(Shared<NT>& s, Held<TDFA_BF16, N
     return {token, token >= 0 ? (float)log(share) : 0.0f};
 }
 
+// ---- 32-bit logits: tokens by the distance from the largest --------------------------------------
+
+// Logits of 32 bits take too many values for a bin each.  Tokens are told apart by how far they lie below the largest logit, kPerUnit steps to
+// a unit, which is a power of e of the weights; the tokens of the step that a search ends in are put in order.  Weights are added up as
+// whole numbers, each as a part of the largest that its step can have: the sums do not depend on the order in which they are made, and keep their
+// bits however small the weights are.  What lies kSteps or more below weighs less than 10^-22 of the largest and counts as nothing.
+constexpr double kPerUnit = 80.0;
+
+// exp(-x) for 0 <= x <= 1 / 80, by its series, off by 2^-47 of itself.
+__device__ __forceinline__ double exp_near(double x)
+{
+    return fma(x, fma(x, fma(x, fma(x, fma(x, -1.0 / 120.0, 1.0 / 24.0), -1.0 / 6.0), 0.5), -1.0), 1.0);
+}
+
+// The largest logit of a row, by the first look at it.
+template <int NT, int R, bool BITS>
+__device__ __forceinline__ float largest_of(Shared<TDFA_F32, NT>& s, Held<TDFA_F32, NT, R, BITS>& row)
+{
+    float m = row.last;                                    // (NaN: passed over by all of these)
+    m = fmaxf(m, -INFINITY);
+    row.template each<false, true>([&](int32_t, uint4 x, uint32_t on) {
+        x = make_uint4(on & 1 ? x.x : kNegInf<TDFA_F32>, on & 2 ? x.y : kNegInf<TDFA_F32>, on & 4 ? x.z : kNegInf<TDFA_F32>, on & 8 ? x.w : kNegInf<TDFA_F32>);
+        m = max_group<TDFA_F32>(x, m);
+    });
+    m = wave_max(m);
+    if ((threadIdx.x & 63) == 0) s.word[threadIdx.x >> 6] = __float_as_uint(m);
+    for (uint32_t j = threadIdx.x; j < kSteps; j += NT) {
+        s.step.weight[j] = 0;
+        s.step.tokens[j] = 0;
+    }
+    lds_barrier();
+    for (int v = 0; v < NT / 64; ++v) m = fmaxf(m, __uint_as_float(s.word[v]));
+    return shared_by_wave(m);
+}
+
+// The step of a logit (NaN: the last), and how far it lies into it.
+struct Steps {
+    double m, scale;           // steps to a unit of the logits
+    __device__ __forceinline__ uint32_t of(float z, double* into) const
+    {
+        const double y = fmin((m - (double)fmaxf(z, -INFINITY)) * scale, (double)(kSteps - 1));
+        const uint32_t i = (uint32_t)y;
+        *into = y - (double)i;
+        return i;
+    }
+    __device__ __forceinline__ uint32_t of(float z) const
+    {
+        double unused;
+        return of(z, &unused);
+    }
+};
+
+// (A thread has kSteps / NT steps that lie together.)
+template <int NT>
+__device__ __forceinline__ double step_weight(const Shared<TDFA_F32, NT>& s, uint32_t i, double unit) { return (double)s.step.weight[i] * unit; }
+
+// Puts the tokens of a row in steps, and adds up.
+template <int NT, int R, bool BITS>
+__device__ __forceinline__ Sums step_row(Shared<TDFA_F32, NT>& s, Held<TDFA_F32, NT, R, BITS>& row, const Steps& steps, int32_t n_tokens, bool counts)
+{
+    // 2^bits: n_tokens weights stay below 2^62, and one below 2^50
+    const int bits = min(50, 62 - (32 - __clz(n_tokens)));
+    const double one = ldexp(1.0, bits), shift = 0x1p52;
+    const auto add = [&](float z) {
+        double into;
+        const uint32_t i = steps.of(z, &into);
+        // (a sum with 2^52 has the whole number in its lower bits)
+        const u64 w = (u64)__double_as_longlong(fma(exp_near(into * (1.0 / kPerUnit)), one, shift)) & ((1ull << 52) - 1);
+        if (i < kSteps - 1) atomicAdd(&s.step.weight[i], w);
+        if (counts) atomicAdd(&s.step.tokens[i], 1u);
+    };
+    row.each([&](int32_t, uint4 x, uint32_t on) {
+        float z[4];
+        unpack<TDFA_F32>(x, z);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (on >> j & 1) add(z[j]);
+    });
+    if (row.has_last) add(row.last);
+    lds_barrier();
+    constexpr uint32_t P = kSteps / NT;
+    uint32_t n = 0;
+    double w = 0.0, unit = exp(-(double)(threadIdx.x * P) * (1.0 / kPerUnit)) * ldexp(1.0, -bits);
+#pragma unroll
+    for (uint32_t j = 0; j < P; ++j) {
+        if (counts) n += s.step.tokens[threadIdx.x * P + j];
+        w += step_weight<NT>(s, threadIdx.x * P + j, unit);
+        unit *= 0.98757780049388144;                       // exp(-1 / 80)
+    }
+    return sums_of<NT>(s, n, w);
+}
+// f(step, its tokens, its weight) for the steps of this thread in order.
+template <int NT, typename F>
+__device__ __forceinline__ void each_step(const Shared<TDFA_F32, NT>& s, int32_t n_tokens, F&& f)
+{
+    constexpr uint32_t P = kSteps / NT;
+    const int bits = min(50, 62 - (32 - __clz(n_tokens)));
+    double unit = exp(-(double)(threadIdx.x * P) * (1.0 / kPerUnit)) * ldexp(1.0, -bits);
+    for (uint32_t j = 0; j < P; ++j) {
+        f(threadIdx.x * P + j, s.step.tokens[threadIdx.x * P + j], step_weight<NT>(s, threadIdx.x * P + j, unit));
+        unit *= 0.98757780049388144;
+    }
+}
+
+// The draw from a row of 32-bit logits.  By the whole workgroup, the result is thread 0's; false: not to be had in this way.
+template <int NT, int R, bool BITS>
+__device__ __forceinline__ bool draw_of_steps(Shared<TDFA_F32, NT>& s, Held<TDFA_F32, NT, R, BITS>& row, int32_t n_tokens, const Setting& q, Drawn* d)
+{
+    const float m = largest_of<NT, R, BITS>(s, row);
+    if (!(fabsf(m) < INFINITY)) return false;
+    const double inv_t = q.inv_t();
+    const auto key = [&](uint32_t i) { return (uint32_t)(s.sorted[i] >> 32); };
+    const auto reaches = [&](uint4 x) { return max_group<TDFA_F32>(x, -INFINITY); };
+    if (inv_t == 0.0) {
+        const uint32_t n = list_of<TDFA_F32, NT, R, BITS>(s, row, [&](uint4 x) { return reaches(x) == m; }, [&](int32_t, float z) { return z == m; });
+        if (n > kList<TDFA_F32>) return false;
+        *d = {(int32_t)~(uint32_t)s.sorted[0], 0.0f};
+        return true;
+    }
+    const Steps steps = {(double)m, inv_t * kPerUnit};
+    const Sums c = step_row<NT, R, BITS>(s, row, steps, n_tokens, q.top_k != 0);
+    if (threadIdx.x < 2) s.at[threadIdx.x] = kSteps;
+    lds_barrier();
+    double kept = c.whole;
+    // Lists step i and adds up its weights from `base` on; false: too many.
+    const auto look = [&](uint32_t i, double base) {
+        const uint32_t n = list_of<TDFA_F32, NT, R, BITS>(s, row, [&](uint4) { return true; }, [&](int32_t, float z) { return steps.of(z) == i; });
+        if (n == 0 || n > kList<TDFA_F32>) return 0u;
+        if (threadIdx.x < 64) {
+            sum_list(s, n, m, inv_t);
+            for (uint32_t j = threadIdx.x; j < n; j += 64) s.cum[j] += base;
+        }
+        lds_barrier();
+        return n;
+    };
+    const auto behind = [&](uint32_t n, uint32_t i) {      // the tokens that have the i-th one's logit
+        const uint32_t k = key(i);
+        return first_where(n, [&](uint32_t j) { return key(j) < k; });
+    };
+    // Weights up to the first `stay` of a step's n tokens; where that is all of them, up to where the next step begins, however that has been rounded.
+    const auto upto = [&](uint32_t n, uint32_t stay, double end) { return stay == n ? fmin(s.cum[n - 1], end) : s.cum[stay - 1]; };
+    if (q.top_k) {
+        if (c.n_before < q.top_k && q.top_k <= c.n_upto) {
+            uint32_t n = c.n_before;
+            double sum = c.before;
+            each_step<NT>(s, n_tokens, [&](uint32_t i, uint32_t tokens, double w) {
+                if (n < q.top_k && q.top_k <= n + tokens) {
+                    s.at[0] = i;
+                    s.at[2] = q.top_k - n;
+                    s.mass[0] = sum;
+                    s.end[0] = fmin(sum + w, c.upto);
+                }
+                n += tokens;
+                sum += w;
+            });
+        }
+        lds_barrier();
+        const uint32_t i = s.at[0], nth = s.at[2];
+        const double base = s.mass[0];
+        if (i < kSteps - 1) {                              // (a cut in the last step leaves all that weighs anything)
+            const uint32_t n = look(i, base);
+            if (!n) return false;
+            kept = fmin(kept, upto(n, behind(n, min(nth, n) - 1), s.end[0]));
+        }
+    }
+    double cut = kept;
+    if (q.top_p() < 1.0) {
+        const double enough = fmax(q.top_p() * kept, 1e-300);
+        if (c.before < enough && enough <= c.upto) {
+            double sum = c.before;
+            each_step<NT>(s, n_tokens, [&](uint32_t i, uint32_t, double w) {
+                if (w > 0.0 && (s.at[1] == kSteps || sum < enough)) {
+                    s.at[1] = i;
+                    s.mass[1] = sum;
+                    s.end[1] = fmin(sum + w, c.upto);
+                }
+                sum += w;
+            });
+        }
+        lds_barrier();
+        const uint32_t i = s.at[1];
+        const double base = s.mass[1];
+        const uint32_t n = i < kSteps ? look(i, base) : 0u;
+        if (!n) return false;
+        cut = fmin(cut, upto(n, behind(n, min(n - 1, first_where(n, [&](uint32_t j) { return s.cum[j] >= enough; }))), s.end[1]));
+    }
+    // what weighs at least min_p ends in the step of its logarithm
+    if (const uint32_t i = q.min_p() > 0.0 ? (uint32_t)fmin(fmax(-log(q.min_p()), 0.0) * kPerUnit, (double)(kSteps - 1)) : kSteps - 1; i < kSteps - 1) {
+        if (threadIdx.x == i / (kSteps / NT)) {
+            double sum = c.before;
+            each_step<NT>(s, n_tokens, [&](uint32_t j, uint32_t, double w) {
+                if (j == i) {
+                    s.mass[2] = sum;
+                    s.end[2] = fmin(sum + w, c.upto);
+                }
+                sum += w;
+            });
+        }
+        lds_barrier();
+        const double base = s.mass[2];
+        const uint32_t n = list_of<TDFA_F32, NT, R, BITS>(s, row, [&](uint4) { return true; }, [&](int32_t, float z) { return steps.of(z) == i; });
+        if (n > kList<TDFA_F32>) return false;
+        if (threadIdx.x < 64 && n) {
+            sum_list(s, n, m, inv_t);
+            for (uint32_t j = threadIdx.x; j < n; j += 64) s.cum[j] += base;
+        }
+        lds_barrier();
+        const uint32_t stay = first_where(n, [&](uint32_t j) { return weight_of(logit_of(key(j)), m, inv_t) < q.min_p(); });
+        cut = fmin(cut, stay ? upto(n, stay, s.end[2]) : base);
+    }
+    kept = fmin(kept, cut);
+    const double target = fmin(q.u() * kept, __longlong_as_double(__double_as_longlong(kept) - 1));
+    if (threadIdx.x == 0) s.at[3] = kSteps;
+    lds_barrier();
+    if (c.before <= target && target < c.upto) {
+        double sum = c.before;
+        each_step<NT>(s, n_tokens, [&](uint32_t i, uint32_t, double w) {
+            if (w > 0.0 && (s.at[3] == kSteps || sum <= target)) {
+                s.at[3] = i;
+                s.mass[0] = sum;
+            }
+            sum += w;
+        });
+    }
+    lds_barrier();
+    const uint32_t i = s.at[3];
+    const double base = s.mass[0];
+    const uint32_t n = i < kSteps ? look(i, base) : 0u;
+    if (!n) return false;
+    // the last that weighs anything, where roundings leave the target behind all
+    const double end = s.cum[n - 1];
+    uint32_t at = first_where(n, [&](uint32_t j) { return s.cum[j] > target; });
+    if (at >= n) at = first_where(n, [&](uint32_t j) { return s.cum[j] >= end; });
+    *d = {(int32_t)~(uint32_t)s.sorted[at], (float)log(weight_of(logit_of(key(at)), m, inv_t) / kept)};
+    return true;
+}
+
+// The first k tokens of a row of 32-bit logits, in order, in sorted[], and what the row weighs.  How many; 0: not to be had in this way.
+template <int NT, int R, bool BITS>
+__device__ __forceinline__ uint32_t top_of_steps(Shared<TDFA_F32, NT>& s, Held<TDFA_F32, NT, R, BITS>& row, uint32_t k, double inv_t, float* m, double* total)
+{
+    *m = largest_of<NT, R, BITS>(s, row);
+    if (!(fabsf(*m) < INFINITY)) return 0;
+    // Steps of the logits themselves, whatever the temperature, and weights in binary32: only the order has borders.
+    const float top = *m, c2 = (float)(1.44269504088896340736 * inv_t);
+    const auto step = [&](float z) { return (uint32_t)fminf((top - fmaxf(z, -INFINITY)) * (float)kPerUnit, (float)(kSteps - 1)); };
+    float sum = 0.0f;
+    const auto add = [&](float z) {
+        sum += __builtin_amdgcn_exp2f((fmaxf(z, -INFINITY) - top) * c2);
+        atomicAdd(&s.step.tokens[step(z)], 1u);
+    };
+    row.each([&](int32_t, uint4 x, uint32_t on) {
+        float z[4];
+        unpack<TDFA_F32>(x, z);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (on >> j & 1) add(z[j]);
+    });
+    if (row.has_last) add(row.last);
+    lds_barrier();
+    constexpr uint32_t P = kSteps / NT;
+    uint32_t n = 0;
+#pragma unroll
+    for (uint32_t j = 0; j < P; ++j) n += s.step.tokens[threadIdx.x * P + j];
+    const Sums c = sums_of<NT>(s, n, (double)sum);
+    *total = c.whole;
+    if (threadIdx.x == 0) s.at[0] = kSteps;
+    lds_barrier();
+    if (c.n_before < k && k <= c.n_upto) {
+        n = c.n_before;
+        for (uint32_t j = 0; j < P; ++j) {
+            const uint32_t tokens = s.step.tokens[threadIdx.x * P + j];
+            if (n < k && k <= n + tokens) s.at[0] = threadIdx.x * P + j;
+            n += tokens;
+        }
+    }
+    lds_barrier();
+    const uint32_t last = s.at[0];
+    if (last >= kSteps - 1) return 0;
+    n = list_of<TDFA_F32, NT, R, BITS>(s, row, [&](uint4 x) { return step(max_group<TDFA_F32>(x, -INFINITY)) <= last; },
+                                      [&](int32_t, float z) { return step(z) <= last; });
+    return n > kList<TDFA_F32> ? 0u : n;
+}
+
 __device__ __forceinline__ int32_t target_of(const DrawArgs& a, int32_t q, int32_t token)
 {
     if (!a.row_begin) return a.targets[(int64_t)q * a.n_tokens + token];
@@ -950,19 +1243,19 @@ __device__ __forceinline__ StateOf state_of(const SelectArgs& a, uint32_t i)
 
 // One workgroup per sequence.
 template <int DTYPE, int NT, int R, bool BITS>
-__global__ void __launch_bounds__(NT, NT == 256 ? 3 : 4) draw_step_kernel(DrawArgs a)
+__global__ void __launch_bounds__(NT, NT > 256 ? 4 : DTYPE == TDFA_F32 ? 2 : 3) draw_step_kernel(DrawArgs a)
 {
-    __shared__ Shared<NT> s;
+    __shared__ Shared<DTYPE, NT> s;
     const uint32_t i = blockIdx.x;
     const StateOf st = state_of(a, i);
     const Setting q = setting_of(a, i);
     const RowOf<DTYPE> r = {row_at<DTYPE>(a.logits, i, a.stride16), st.bits, a.n_tokens};
     Held<DTYPE, NT, R, BITS> row;
-    if (DTYPE == TDFA_BF16) clear_counts<NT>(s);
+    if constexpr (DTYPE == TDFA_BF16) clear_counts<NT>(s);
     const uint32_t n = (uint32_t)__builtin_amdgcn_readfirstlane((int)(st.valid ? load_row<DTYPE, NT, R, BITS>(s, row, r) : 0u));
     Drawn d = {TDFA_NO_TOKEN, 0.0f};
     bool mine = threadIdx.x == 0;                          // this thread writes the result
-    if (n > (uint32_t)kList) {
+    if (n > kFew) {
         bool done = false;
         if constexpr (DTYPE == TDFA_BF16) {
             Counted c;
@@ -973,12 +1266,13 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 3 : 4) draw_step_kernel(DrawAr
                 mine = d.token >= 0;
             }
         }
+        if constexpr (DTYPE == TDFA_F32) done = draw_of_steps<NT, R, BITS>(s, row, a.n_tokens, q, &d);
         if (!done) d = draw_by_digits<DTYPE, NT, BITS>(s, r, q);
     } else if (n) {
         list_all<DTYPE, NT, R, BITS>(s, row);
         if (threadIdx.x < 64) {
             const float m = logit_of((uint32_t)(s.sorted[0] >> 32));
-            if (m != -INFINITY) sum_list<NT>(s, n, m, q.inv_t());
+            if (m != -INFINITY) sum_list(s, n, m, q.inv_t());
             d = draw_of_list<NT>(s, n, m, q);
         }
     }
@@ -991,7 +1285,7 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 3 : 4) draw_step_kernel(DrawAr
 
 // The first k tokens of a row of any kind, in order, in sorted[], and what the row weighs.  How many there are, 0 if all are -inf.
 template <int DTYPE, int NT, bool BITS>
-__device__ __forceinline__ uint32_t top_by_digits(Shared<NT>& s, const RowOf<DTYPE>& r, uint32_t k, double inv_t, float* m, double* total)
+__device__ __forceinline__ uint32_t top_by_digits(Shared<DTYPE, NT>& s, const RowOf<DTYPE>& r, uint32_t k, double inv_t, float* m, double* total)
 {
     uint32_t top = 0;
     for_each<DTYPE, NT, BITS>(r, [&](int32_t, float z) { top = max(top, key_of(z)); });
@@ -1013,13 +1307,13 @@ __device__ __forceinline__ uint32_t top_by_digits(Shared<NT>& s, const RowOf<DTY
     });
     *total = (double)block_sum<NT>(sum, s) / w.scale;
     const uint32_t n = s.n;
-    sort_list<NT>(s, n);
+    sort_list(s, n);
     return n;
 }
 
 // The same from counts; 0: they do not tell.
 template <int NT, int R, bool BITS>
-__device__ __forceinline__ uint32_t top_of_counts(Shared<NT>& s, Held<TDFA_BF16, NT, R, BITS>& row, uint32_t k, double inv_t, float* m, double* total)
+__device__ __forceinline__ uint32_t top_of_counts(Shared<TDFA_BF16, NT>& s, Held<TDFA_BF16, NT, R, BITS>& row, uint32_t k, double inv_t, float* m, double* total)
 {
     Counted c;
     Bins<NT> b;
@@ -1044,7 +1338,7 @@ __device__ __forceinline__ uint32_t top_of_counts(Shared<NT>& s, Held<TDFA_BF16,
     const float v = value_of(s.at[0]);
     const uint32_t larger = s.at[1], equal = s.at[2];
     int32_t last = INT32_MAX;
-    if (larger + equal > (uint32_t)kList) {                // more than are wanted have that logit: those of the lowest ids
+    if (larger + equal > kList<TDFA_BF16>) {                // more than are wanted have that logit: those of the lowest ids
         const int32_t t = find_nth<TDFA_BF16>(s, row, v, k - larger - 1);
         if (t >= 0) s.at[3] = (uint32_t)t;
         lds_barrier();
@@ -1056,27 +1350,28 @@ __device__ __forceinline__ uint32_t top_of_counts(Shared<NT>& s, Held<TDFA_BF16,
 
 // One workgroup per row: the k first tokens in order, and their log-probabilities.
 template <int DTYPE, int NT, int R, bool BITS>
-__global__ void __launch_bounds__(NT, NT == 256 ? 3 : 4) top_logprobs_kernel(TopArgs a)
+__global__ void __launch_bounds__(NT, NT > 256 ? 4 : DTYPE == TDFA_F32 ? 2 : 3) top_logprobs_kernel(TopArgs a)
 {
-    __shared__ Shared<NT> s;
+    __shared__ Shared<DTYPE, NT> s;
     const uint32_t i = blockIdx.x, k = (uint32_t)a.k;
     const StateOf st = state_of(a, i);
     const RowOf<DTYPE> r = {row_at<DTYPE>(a.logits, i, a.stride16), st.bits, a.n_tokens};
     const double inv_t = 1.0 / (double)a.temperature;
     Held<DTYPE, NT, R, BITS> row;
-    if (DTYPE == TDFA_BF16) clear_counts<NT>(s);
+    if constexpr (DTYPE == TDFA_BF16) clear_counts<NT>(s);
     uint32_t n = (uint32_t)__builtin_amdgcn_readfirstlane((int)(st.valid ? load_row<DTYPE, NT, R, BITS>(s, row, r) : 0u));
     float m = -INFINITY;
     double total = 0.0;
-    if (n > (uint32_t)kList) {
+    if (n > kFew) {
         n = 0;
         if constexpr (DTYPE == TDFA_BF16) n = top_of_counts<NT, R, BITS>(s, row, k, inv_t, &m, &total);
+        else n = top_of_steps<NT, R, BITS>(s, row, k, inv_t, &m, &total);
         if (!n) n = top_by_digits<DTYPE, NT, BITS>(s, r, k, inv_t, &m, &total);
     } else if (n) {
         list_all<DTYPE, NT, R, BITS>(s, row);
         m = logit_of((uint32_t)(s.sorted[0] >> 32));
         if (m != -INFINITY) {
-            if (threadIdx.x < 64) sum_list<NT>(s, n, m, inv_t);
+            if (threadIdx.x < 64) sum_list(s, n, m, inv_t);
             lds_barrier();
             total = s.cum[n - 1];
         }
@@ -1128,8 +1423,13 @@ int shaped(int64_t rows, int32_t n_groups, F&& launch_of)
     if (n_groups <= 256 * 4) return go(integral_constant<int, 256>(), integral_constant<int, 4>());
     if (n_groups <= 1024 * 4 && rows <= 256) return go(integral_constant<int, 1024>(), integral_constant<int, 4>());
     if (n_groups <= 512 * 8) return go(integral_constant<int, 512>(), integral_constant<int, 8>());
-    if (n_groups <= 512 * 16) return go(integral_constant<int, 512>(), integral_constant<int, 16>());
-    if (n_groups <= 1024 * 16) return go(integral_constant<int, 1024>(), integral_constant<int, 16>());
+    if constexpr (DTYPE == TDFA_F32) {
+        // (with more in registers the compiler would keep some in memory)
+        if (n_groups <= 1024 * 8) return go(integral_constant<int, 1024>(), integral_constant<int, 8>());
+    } else {
+        if (n_groups <= 512 * 16) return go(integral_constant<int, 512>(), integral_constant<int, 16>());
+        if (n_groups <= 1024 * 16) return go(integral_constant<int, 1024>(), integral_constant<int, 16>());
+    }
     return go(integral_constant<int, 1024>(), integral_constant<int, 0>());
 }
 template <typename F>
