@@ -67,6 +67,7 @@ struct Shared : Names {
     double part[NT / 64];
     double teacher[kSlots];    // of rows that name a token twice
     uint32_t named[kSlots];
+    float given[kSlots];       // the teacher's values
     float factor;
     int again, active;
     uint2 masks[16];
@@ -121,6 +122,13 @@ __device__ __forceinline__ double block_total(double v, double (&part)[NT / 64])
 #pragma unroll
     for (int w = 1; w < NT / 64; ++w) v += part[w];
     return v;
+}
+
+// A value that is the same in all lanes, in scalar registers: next to a row's elements there are few others.
+__device__ __forceinline__ double uniform(double v)
+{
+    const unsigned long long x = (unsigned long long)__double_as_longlong(v);
+    return __longlong_as_double((long long)((unsigned long long)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)x)));
 }
 
 // A group as it is loaded: its elements are taken out of it where they are used, not kept from one use to the next.
@@ -297,7 +305,10 @@ template <int DTYPE, int NT>
 __device__ __forceinline__ bool enter_slots(Shared<NT>& s, Slot& t, int32_t count)
 {
     clear_names<NT>(s, count);
-    if (threadIdx.x < kSlots) s.named[threadIdx.x] = t.live ? (uint32_t)t.id : kNone;
+    if (threadIdx.x < kSlots) {
+        s.named[threadIdx.x] = t.live ? (uint32_t)t.id : kNone;
+        s.given[threadIdx.x] = t.value;
+    }
     fill_masks(s.masks);
     if (threadIdx.x == 0) s.again = s.active = 0;
     __syncthreads();
@@ -316,23 +327,26 @@ __device__ __forceinline__ bool enter_slots(Shared<NT>& s, Slot& t, int32_t coun
 template <int NT>
 __device__ __forceinline__ void row_numbers(const DistillArgs& a, uint32_t i, const Slot& t, float weight, float ref, double sum, Shared<NT>& s)
 {
-    const double inv_t = 1.0 / (double)a.temperature;
+    const double inv_t = uniform(1.0 / (double)a.temperature);
+    sum = uniform(sum);
     const bool tail = sum != 0.0;                          // (NaN where an allowed logit is +inf, as everything below)
-    const float most = fmaxf(block_reduce<NT, true>(t.live ? t.z : -INFINITY, s.running[0]), tail ? ref : -INFINITY);
-    const double down = ((double)ref - (double)most) * inv_t, mine = t.live ? exp(((double)t.z - (double)most) * inv_t) : 0.0;
-    const double total = (tail ? exp(down) * sum : 0.0) + block_total<NT>(t.owner ? mine : 0.0, s.part);
-    const double ln_total = log(total), lp = ((double)t.z - (double)most) * inv_t - ln_total;
+    const float most = shared_by_wave(fmaxf(block_reduce<NT, true>(t.live ? t.z : -INFINITY, s.running[0]), tail ? ref : -INFINITY));
+    const double down = uniform(((double)ref - (double)most) * inv_t), mine = t.live ? exp(((double)t.z - (double)most) * inv_t) : 0.0;
+    const double total = uniform((tail ? exp(down) * sum : 0.0) + block_total<NT>(t.owner ? mine : 0.0, s.part));
+    const double ln_total = uniform(log(total)), lp = ((double)t.z - (double)most) * inv_t - ln_total;
     const bool counts = t.live && (float)lp != -INFINITY;
+    const float value = counts ? s.given[threadIdx.x] : 0.0f;
     double teacher, mass, rest = 0.0;
     if (a.tail) {
-        teacher = counts ? exp(fmin((double)t.value, 0.0)) : 0.0;
-        mass = block_total<NT>(teacher, s.part);
+        teacher = counts ? exp(fmin((double)value, 0.0)) : 0.0;
+        mass = uniform(block_total<NT>(teacher, s.part));
         if (tail) rest = fmax(1.0 - mass, 0.0);
-        mass += rest;
+        rest = uniform(rest);
+        mass = uniform(mass + rest);
     } else {
-        const float best = block_reduce<NT, true>(counts ? t.value : -INFINITY, s.running[0]);
-        teacher = counts ? exp((double)t.value - (double)best) : 0.0;
-        mass = block_total<NT>(teacher, s.part);
+        const float best = shared_by_wave(block_reduce<NT, true>(counts ? value : -INFINITY, s.running[0]));
+        teacher = counts ? exp((double)value - (double)best) : 0.0;
+        mass = uniform(block_total<NT>(teacher, s.part));
         teacher = mass > 0.0 ? teacher / mass : 0.0;
         mass = mass > 0.0 ? 1.0 : 0.0;
     }
@@ -382,8 +396,15 @@ __global__ void __launch_bounds__(NT, 4) distill_row_kernel(DistillArgs a)
     const int32_t behind = n_groups * G + tid;
     Head h = head_of<DTYPE, BITS>(a, i);
     uint4 x[R];
-    uint32_t b[R];
-    if (h.read) fetch<DTYPE, NT, R, BITS, true>(row_buffers<DTYPE>(row, h.bits, n_groups), 0, n_groups, x, b);
+    uint32_t b[(R + 3) / 4];                               // allowed bits, of four groups each
+    if (h.read) {
+        const RowBuffers buf = row_buffers<DTYPE>(row, h.bits, n_groups);
+        uint32_t y[R];
+        fetch_bits<DTYPE, NT, R, BITS>(buf, 0, y);
+        fetch_groups<DTYPE, NT, R, BITS, true>(buf, 0, n_groups, x, y);
+#pragma unroll
+        for (int k = 0; k < R; ++k) b[k / 4] = k % 4 ? b[k / 4] | y[k] << (k % 4 * 8) : y[k];
+    }
     if (!h.read || !enter_slots<DTYPE, NT>(s, h.slot, n_groups)) {
         no_loss(a, i);
         if (!a.grad) return;
@@ -392,8 +413,8 @@ __global__ void __launch_bounds__(NT, 4) distill_row_kernel(DistillArgs a)
         return;
     }
     const Exponent c(a.temperature);
-    const uint32_t place_behind = behind < a.n_tokens ? find(s, (uint32_t)behind) : kNone;
-    const float last = last_element<DTYPE>(a.n_tokens, row, h.bits, place_behind != kNone ? behind : -1);
+    const auto place_behind = [&]() { return behind < a.n_tokens ? find(s, (uint32_t)behind) : kNone; };
+    const float last = last_element<DTYPE>(a.n_tokens, row, h.bits, place_behind() != kNone ? behind : -1);
     // The tail's sum, and the groups that have something of it (bits of `some`, for the wavefront) or a named token (bits of `names`).
     uint32_t some = 0, names = 0;
     float ref = -INFINITY, sum = NAN;
@@ -402,7 +423,7 @@ __global__ void __launch_bounds__(NT, 4) distill_row_kernel(DistillArgs a)
         const int32_t g = tid + k * NT;
         const uint32_t named = g < n_groups ? named_in(s, g) : 0u;
         names |= (named ? 1u : 0u) << k;
-        const bool any = keep_tail<DTYPE, BITS>(x[k], b[k], g < n_groups, named, s.masks);
+        const bool any = keep_tail<DTYPE, BITS>(x[k], b[k / 4] >> (k % 4 * 8) & 0xFFu, g < n_groups, named, s.masks);
         some |= (any ? 1u : 0u) << k;
         return any;
     };
@@ -448,7 +469,10 @@ __global__ void __launch_bounds__(NT, 4) distill_row_kernel(DistillArgs a)
         set_group(to, g, gradient_group<DTYPE>(s, x[k], some >> k & 1, names >> k & 1 ? named_in(s, g) : 0u, g, q, f, c));
         next_group();
     }
-    if (behind < a.n_tokens) store_rounded(out + behind, place_behind != kNone ? s.value[place_behind] : gradient_of<DTYPE>(last, q, c));
+    if (behind < a.n_tokens) {
+        const uint32_t place = place_behind();
+        store_rounded(out + behind, place != kNone ? s.value[place] : gradient_of<DTYPE>(last, q, c));
+    }
 }
 
 // ---- rows that do not stay in registers: sums by parts, the numbers of the rows, gradients by parts ----------
@@ -627,21 +651,28 @@ __global__ void __launch_bounds__(NT) distill_grad_kernel(PartGradArgs a)
     }
 }
 
+// Groups of the longest rows that stay in registers; with more of them the compiler would keep some in memory, in fp32 sooner.
+constexpr int32_t held_groups(int dtype) { return dtype == TDFA_F32 ? 1024 * 8 : 1024 * 16; }
+
 template <int DTYPE, bool BITS>
 int rows_of(const DistillArgs& x, unsigned rows, hipStream_t stream)
 {
     const int32_t n_groups = x.n_tokens / Elem<DTYPE>::kGroup;
     if (n_groups <= 256 * 4) return launch(distill_row_kernel<DTYPE, 256, 4, BITS>, dim3(rows), 256, stream, x);
-    if (n_groups <= 256 * 16) return launch(distill_row_kernel<DTYPE, 256, 16, BITS>, dim3(rows), 256, stream, x);
-    if (n_groups <= 512 * 16) return launch(distill_row_kernel<DTYPE, 512, 16, BITS>, dim3(rows), 512, stream, x);
-    return launch(distill_row_kernel<DTYPE, 1024, 16, BITS>, dim3(rows), 1024, stream, x);
+    if (n_groups <= 512 * 8) return launch(distill_row_kernel<DTYPE, 512, 8, BITS>, dim3(rows), 512, stream, x);
+    if constexpr (DTYPE == TDFA_F32) {
+        return launch(distill_row_kernel<DTYPE, 1024, 8, BITS>, dim3(rows), 1024, stream, x);
+    } else {
+        if (n_groups <= 512 * 16) return launch(distill_row_kernel<DTYPE, 512, 16, BITS>, dim3(rows), 512, stream, x);
+        return launch(distill_row_kernel<DTYPE, 1024, 16, BITS>, dim3(rows), 1024, stream, x);
+    }
 }
 
 constexpr int kPartThreads = 256, kPartGroups = 8;        // groups in flight per thread of the launches over parts
 constexpr int32_t kPiece = kPartThreads * kPartGroups;
 
 int32_t groups_of(int dtype, int64_t n_tokens) { return (int32_t)(n_tokens / (dtype == TDFA_F32 ? 4 : 8)); }
-bool by_parts(int64_t rows, int32_t n_groups) { return n_groups > kMarks || (rows <= 40 && n_groups > 4096); }
+bool by_parts(int dtype, int64_t rows, int32_t n_groups) { return n_groups > held_groups(dtype) || (rows <= 40 && n_groups > 4096); }
 // Groups to a part of the sums: about 1,024 workgroups, of whole pieces, none of more than kMarks groups.
 int32_t span_of(int64_t rows, int32_t n_groups)
 {
@@ -676,25 +707,22 @@ int parts_of(const DistillArgs& x, int64_t rows, int32_t span, float2* parts, ui
 
 }  // namespace
 
-// The rows' losses; where rows are taken by parts (of 16-bit logits, which have fewer groups, always if of fp32 ones) the slots' and parts' numbers as well.
+// The rows' losses; where rows are taken by parts, of either type, the slots' and parts' numbers as well.
 int64_t distill_workspace(int64_t rows, int64_t n_tokens, int64_t k)
 {
-    int64_t bytes = aligned(8 * rows);
-    const int32_t most = groups_of(TDFA_F32, n_tokens);
-    if (!by_parts(rows, most)) return bytes;
     int64_t parts = 0;
     for (int dtype : {TDFA_F32, TDFA_BF16}) {
         const int32_t n = groups_of(dtype, n_tokens), span = span_of(rows, n);
-        parts = std::max<int64_t>(parts, (n + span - 1) / span);
+        if (by_parts(dtype, rows, n)) parts = std::max<int64_t>(parts, (n + span - 1) / span);
     }
-    return bytes + 16 * rows + aligned(8 * rows * k) + aligned(8 * rows * parts);
+    return aligned(8 * rows) + (parts ? 16 * rows + aligned(8 * rows * k) + aligned(8 * rows * parts) : 0);
 }
 
 int launch_distill_loss(const LogitRows& a, const DistillRows& d, float* loss, void* grad, int64_t grad_stride, void* workspace, hipStream_t stream)
 {
     const int64_t esz = a.dtype == TDFA_F32 ? 4 : 2;
     const int32_t n_groups = groups_of(a.dtype, a.n_tokens), span = span_of(a.rows, n_groups);
-    const bool parted = by_parts(a.rows, n_groups);
+    const bool parted = by_parts(a.dtype, a.rows, n_groups);
     double* work = static_cast<double*>(workspace);
     float4* slopes = reinterpret_cast<float4*>(static_cast<char*>(workspace) + aligned(8 * a.rows));
     uint2* named = reinterpret_cast<uint2*>(slopes + a.rows);

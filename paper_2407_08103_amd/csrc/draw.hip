@@ -1412,7 +1412,11 @@ void fill(SelectArgs& x, const LogitRows& a, int64_t from)
 }
 
 // launch_of(type, threads, groups to a thread, whether there is a constraint) for the shape that rows of n_groups take: in registers as
-// long as they fit, few rows by more threads each.
+// long as they fit, few rows by more threads each.  Where there are several long rows to a compute unit, three of them at a time, each
+// read two or three times, beat one that is held: 128,256 tokens in bf16, draws / lists of 2,048 rows under a constraint 156 -> 119 and
+// 153 -> 118 us, 512 rows 48 -> 45 and 47 -> 44; without one 2,048 rows 174 -> 161 and 167 -> 158, 768 rows 73 -> 75 and 72 -> 68, 512 rows 51.5 ->
+// 51.9 and 49.1 -> 49.9 (workgroups of 1,024 threads, of which one fits: 193 and 189).  Rows of 32,000 by 512 threads with 8 groups each against 256
+// with 16: 300 rows 21 against 26, 1,500 rows 52 against 56.
 template <int DTYPE, bool BITS, typename F>
 int shaped(int64_t rows, int32_t n_groups, F&& launch_of)
 {
@@ -1428,6 +1432,7 @@ int shaped(int64_t rows, int32_t n_groups, F&& launch_of)
         if (n_groups <= 1024 * 8) return go(integral_constant<int, 1024>(), integral_constant<int, 8>());
     } else {
         if (n_groups <= 512 * 16) return go(integral_constant<int, 512>(), integral_constant<int, 16>());
+        if (rows >= (BITS ? 512 : 768)) return go(integral_constant<int, 512>(), integral_constant<int, 0>());
         if (n_groups <= 1024 * 16) return go(integral_constant<int, 1024>(), integral_constant<int, 16>());
     }
     return go(integral_constant<int, 1024>(), integral_constant<int, 0>());
