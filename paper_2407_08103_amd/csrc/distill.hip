@@ -64,10 +64,11 @@ struct Names {
 template <int NT>
 struct Shared : Names {
     float running[2][NT / 64];
-    double part[NT / 64];
-    double teacher[kSlots];    // of rows that name a token twice
-    uint32_t named[kSlots];
-    float given[kSlots];       // the teacher's values
+    // the slots: tokens (kNone: not live), places (the lowest bit: whether the slot owns it), the student's and the teacher's values
+    uint32_t named[kSlots], place[kSlots];
+    float logit[kSlots], given[kSlots];
+    double far[kSlots], teacher[kSlots];       // distances from the largest logit, the teacher's probabilities
+    float top[kSlots / 64];    // the largest live logits
     float factor;
     int again, active;
     uint2 masks[16];
@@ -107,21 +108,6 @@ __device__ __forceinline__ void clear_names(Names& s, int32_t count)
 {
     for (int j = threadIdx.x; j < kHash; j += NT) s.key[j] = kNone;
     for (int j = threadIdx.x; j < (count + 3) / 4; j += NT) s.marks[j] = 0;
-}
-
-// Sum over the workgroup in binary64, in every thread and in one order.  Two barriers.
-template <int NT>
-__device__ __forceinline__ double block_total(double v, double (&part)[NT / 64])
-{
-#pragma unroll
-    for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = part[0];
-#pragma unroll
-    for (int w = 1; w < NT / 64; ++w) v += part[w];
-    return v;
 }
 
 // A value that is the same in all lanes, in scalar registers: next to a row's elements there are few others.
@@ -263,15 +249,12 @@ __device__ __forceinline__ uint4 gradient_group(const Names& s, uint4 x, bool so
     return x;
 }
 
-// The slot of a thread: its token, the teacher's value, the student's logit.
-struct Slot {
+// What a workgroup knows of its row before it reads it, and the slot of this thread.
+struct Head {
     int32_t id;
     float value, z;
-    bool live, owner;          // owner: of the token's place
-    uint32_t place;
-};
-struct Head {
-    Slot slot;
+    uint32_t word;             // the allowed bits with the token's
+    bool named;                // the slot names a token and gives a value
     float weight;
     const uint32_t* bits;
     bool read;                 // the row's logits have to be read
@@ -279,10 +262,10 @@ struct Head {
 template <int DTYPE, bool BITS>
 __device__ __forceinline__ Head head_of(const DistillArgs& a, uint32_t i)
 {
-    Head h = {{-1, 0.0f, -INFINITY, false, false, kNone}, 1.0f, a.allow, true};
+    Head h = {-1, 0.0f, -INFINITY, 0xFFFFFFFFu, false, 1.0f, a.allow, true};
     if ((int)threadIdx.x < a.k) {
-        h.slot.id = a.ids[(uint64_t)i * a.k + threadIdx.x];
-        h.slot.value = a.values[(uint64_t)i * a.k + threadIdx.x];
+        h.id = a.ids[(uint64_t)i * a.k + threadIdx.x];
+        h.value = a.values[(uint64_t)i * a.k + threadIdx.x];
     }
     if (a.weights) h.weight = shared_by_wave(a.weights[i]);
     h.read = h.weight != 0.0f;
@@ -291,83 +274,121 @@ __device__ __forceinline__ Head head_of(const DistillArgs& a, uint32_t i)
         h.read = h.read && q >= 0 && q < a.n_states;
         if (h.read) h.bits = bits_of(a.allow, q, a.n_tokens);
     }
-    Slot& t = h.slot;
-    t.live = h.read && t.id >= 0 && t.id < a.n_tokens && fabsf(t.value) < INFINITY;
-    if (t.live) {
-        t.live = !BITS || allowed(h.bits, t.id);
-        t.z = to_f32(row_at<DTYPE>(a.logits, i, a.stride16)[t.id]);
-        t.live = t.live && t.z > -INFINITY;
+    h.named = h.read && h.id >= 0 && h.id < a.n_tokens && fabsf(h.value) < INFINITY;
+    if (h.named) {                                         // (looked at in enter_slots, when the row is on its way too)
+        if (BITS) h.word = h.bits[h.id >> 5];
+        h.z = to_f32(row_at<DTYPE>(a.logits, i, a.stride16)[h.id]);
     }
     return h;
 }
 // Enters the slots; the marks are for the row's first `count` groups.  False: no slot is live.  Two barriers.
 template <int DTYPE, int NT>
-__device__ __forceinline__ bool enter_slots(Shared<NT>& s, Slot& t, int32_t count)
+__device__ __forceinline__ bool enter_slots(Shared<NT>& s, const Head& h, int32_t count)
 {
     clear_names<NT>(s, count);
-    if (threadIdx.x < kSlots) {
-        s.named[threadIdx.x] = t.live ? (uint32_t)t.id : kNone;
-        s.given[threadIdx.x] = t.value;
-    }
     fill_masks(s.masks);
     if (threadIdx.x == 0) s.again = s.active = 0;
     __syncthreads();
-    if (t.live) {
+    const bool live = h.named && (h.word >> (h.id & 31) & 1) && h.z > -INFINITY;
+    if (threadIdx.x < kSlots) {
+        const float top = wave_max(live ? h.z : -INFINITY);
+        if ((threadIdx.x & 63) == 0) s.top[threadIdx.x >> 6] = top;
+        s.named[threadIdx.x] = live ? (uint32_t)h.id : kNone;
+    }
+    if (live) {
         s.active = 1;
-        t.place = enter(s, (uint32_t)t.id, &t.owner);
-        if (!t.owner) s.again = 1;
-        mark<DTYPE>(s, t.id, 0, count);
+        bool owner;
+        const uint32_t place = enter(s, (uint32_t)h.id, &owner);
+        if (!owner) s.again = 1;
+        mark<DTYPE>(s, h.id, 0, count);
+        s.place[threadIdx.x] = place << 1 | (owner ? 1u : 0u);
+        s.logit[threadIdx.x] = h.z;
+        s.given[threadIdx.x] = h.value;
     }
     __syncthreads();
     return s.active;
 }
+// The largest logit of a live slot.
+template <int NT>
+__device__ __forceinline__ float top_slot(const Shared<NT>& s)
+{
+    float top = s.top[0];
+#pragma unroll
+    for (int w = 1; w < kSlots / 64; ++w) top = fmaxf(top, s.top[w]);
+    return shared_by_wave(top);
+}
+
+// The sum over a wavefront, in binary64 and in one order.
+__device__ __forceinline__ double wave_total(double v) { return lane_value(wave_upto(v), 63); }
 
 // The numbers of a row from its slots and the tail's sum relative to ref, in binary64: the loss, and what the gradients are made
-// of: s.factor, and the value of every owner's place, behind a barrier.
+// of: s.factor, and the value of every owner's place.  By the first wavefront, four slots to a lane, with no barrier but one behind it: by
+// a thread for each slot, with sums over the workgroup, it took 4 us of every row.
 template <int NT>
-__device__ __forceinline__ void row_numbers(const DistillArgs& a, uint32_t i, const Slot& t, float weight, float ref, double sum, Shared<NT>& s)
+__device__ __forceinline__ void row_numbers(const DistillArgs& a, uint32_t i, float weight, float ref, double sum, Shared<NT>& s)
 {
-    const double inv_t = uniform(1.0 / (double)a.temperature);
-    sum = uniform(sum);
-    const bool tail = sum != 0.0;                          // (NaN where an allowed logit is +inf, as everything below)
-    const float most = shared_by_wave(fmaxf(block_reduce<NT, true>(t.live ? t.z : -INFINITY, s.running[0]), tail ? ref : -INFINITY));
-    const double down = uniform(((double)ref - (double)most) * inv_t), mine = t.live ? exp(((double)t.z - (double)most) * inv_t) : 0.0;
-    const double total = uniform((tail ? exp(down) * sum : 0.0) + block_total<NT>(t.owner ? mine : 0.0, s.part));
-    const double ln_total = uniform(log(total)), lp = ((double)t.z - (double)most) * inv_t - ln_total;
-    const bool counts = t.live && (float)lp != -INFINITY;
-    const float value = counts ? s.given[threadIdx.x] : 0.0f;
-    double teacher, mass, rest = 0.0;
-    if (a.tail) {
-        teacher = counts ? exp(fmin((double)value, 0.0)) : 0.0;
-        mass = uniform(block_total<NT>(teacher, s.part));
-        if (tail) rest = fmax(1.0 - mass, 0.0);
-        rest = uniform(rest);
-        mass = uniform(mass + rest);
-    } else {
-        const float best = shared_by_wave(block_reduce<NT, true>(counts ? value : -INFINITY, s.running[0]));
-        teacher = counts ? exp((double)value - (double)best) : 0.0;
-        mass = uniform(block_total<NT>(teacher, s.part));
-        teacher = mass > 0.0 ? teacher / mass : 0.0;
-        mass = mass > 0.0 ? 1.0 : 0.0;
-    }
-    double loss = block_total<NT>(teacher > 0.0 ? teacher * (log(teacher) - lp) : 0.0, s.part);
-    if (rest > 0.0) loss += rest * (log(rest) - (down + log(sum) - ln_total));
-    const double scale = (double)weight * inv_t;
-    if (threadIdx.x == 0) {
-        a.losses[i] = (float)loss;
-        a.work[i] = (double)weight * loss;
-        s.factor = tail ? (float)(scale * (mass * exp(down) / total - rest / sum)) : 0.0f;
-    }
-    if (s.again) {                                         // the slots of one token added up, in their order
-        if (threadIdx.x < kSlots) s.teacher[threadIdx.x] = teacher;
-        __syncthreads();
-        if (t.owner) {
-            teacher = 0.0;
-            for (int j = 0; j < a.k; ++j)
-                if (s.named[j] == (uint32_t)t.id) teacher += s.teacher[j];
+    if (threadIdx.x < 64) {
+        const double inv_t = uniform(1.0 / (double)a.temperature);
+        sum = uniform(sum);
+        const bool tail = sum != 0.0;                      // (NaN where an allowed logit is +inf, as everything below)
+        const float most = shared_by_wave(fmaxf(top_slot(s), tail ? ref : -INFINITY));
+        const double down = uniform(((double)ref - (double)most) * inv_t);
+        const auto each = [&](auto&& f) {                  // f(slot) for the live slots of this lane (what it keeps of them lies in LDS)
+            for (int j = (int)threadIdx.x; j < a.k; j += 64)
+                if (s.named[j] != kNone) f(j);
+        };
+        double part = 0.0;
+        each([&](int j) {
+            const double far = ((double)s.logit[j] - (double)most) * inv_t;
+            s.far[j] = far;
+            if (s.place[j] & 1) part += exp(far);
+        });
+        const double total = uniform((tail ? exp(down) * sum : 0.0) + wave_total(part)), ln_total = uniform(log(total));
+        const auto counts = [&](int j) { return (float)(s.far[j] - ln_total) != -INFINITY; };
+        double mass, rest = 0.0;
+        part = 0.0;
+        if (a.tail) {
+            each([&](int j) { part += s.teacher[j] = counts(j) ? exp(fmin((double)s.given[j], 0.0)) : 0.0; });
+            mass = uniform(wave_total(part));
+            if (tail) rest = uniform(fmax(1.0 - mass, 0.0));
+            mass = uniform(mass + rest);
+        } else {
+            float best = -INFINITY;
+            each([&](int j) {
+                if (counts(j)) best = fmaxf(best, s.given[j]);
+            });
+            best = wave_max(best);
+            each([&](int j) { part += s.teacher[j] = counts(j) ? exp((double)s.given[j] - (double)best) : 0.0; });
+            mass = uniform(wave_total(part));
+            const double share = mass > 0.0 ? 1.0 / mass : 0.0;
+            each([&](int j) { s.teacher[j] *= share; });
+            mass = mass > 0.0 ? 1.0 : 0.0;
         }
+        part = 0.0;
+        each([&](int j) {
+            if (s.teacher[j] > 0.0) part += s.teacher[j] * (log(s.teacher[j]) - (s.far[j] - ln_total));
+        });
+        double loss = wave_total(part);
+        if (rest > 0.0) loss += rest * (log(rest) - (down + log(sum) - ln_total));
+        const double scale = uniform((double)weight * inv_t);
+        if (threadIdx.x == 0) {
+            a.losses[i] = (float)loss;
+            a.work[i] = (double)weight * loss;
+            s.factor = tail ? (float)(scale * (mass * exp(down) / total - rest / sum)) : 0.0f;
+        }
+        wave_lds_sync();
+        const bool again = s.again;
+        each([&](int j) {
+            if (!(s.place[j] & 1)) return;
+            double teacher = s.teacher[j];
+            if (again) {                                   // the slots of one token added up, in their order
+                teacher = 0.0;
+                for (int o = 0; o < a.k; ++o)
+                    if (s.named[o] == s.named[j]) teacher += s.teacher[o];
+            }
+            s.value[s.place[j] >> 1] = (float)(scale * (exp(s.far[j]) / total * mass - teacher));
+        });
     }
-    if (t.owner) s.value[t.place] = (float)(scale * (mine / total * mass - teacher));
     __syncthreads();
 }
 __device__ __forceinline__ void no_loss(const DistillArgs& a, uint32_t i)
@@ -394,7 +415,7 @@ __global__ void __launch_bounds__(NT, 4) distill_row_kernel(DistillArgs a)
     auto* out = row_at<DTYPE>(a.grad, i, a.grad_stride16);
     const __amdgpu_buffer_rsrc_t to = buffer_of(out, (uint32_t)n_groups * 16u);
     const int32_t behind = n_groups * G + tid;
-    Head h = head_of<DTYPE, BITS>(a, i);
+    const Head h = head_of<DTYPE, BITS>(a, i);
     uint4 x[R];
     uint32_t b[(R + 3) / 4];                               // allowed bits, of four groups each
     if (h.read) {
@@ -405,7 +426,7 @@ __global__ void __launch_bounds__(NT, 4) distill_row_kernel(DistillArgs a)
 #pragma unroll
         for (int k = 0; k < R; ++k) b[k / 4] = k % 4 ? b[k / 4] | y[k] << (k % 4 * 8) : y[k];
     }
-    if (!h.read || !enter_slots<DTYPE, NT>(s, h.slot, n_groups)) {
+    if (!h.read || !enter_slots<DTYPE, NT>(s, h, n_groups)) {
         no_loss(a, i);
         if (!a.grad) return;
         for (int32_t g = tid; g < n_groups; g += NT) set_group(to, g, make_uint4(0, 0, 0, 0));
@@ -428,7 +449,7 @@ __global__ void __launch_bounds__(NT, 4) distill_row_kernel(DistillArgs a)
         return any;
     };
     if constexpr (DTYPE == TDFA_BF16) {
-        ref = block_reduce<NT, true>(h.slot.live ? h.slot.z : -INFINITY, s.running[0]);
+        ref = top_slot(s);
         const float nb = offset_of(ref, c.hi);
         float sums[2] = {__builtin_amdgcn_exp2f(fmaf(last, c.hi, nb)), 0.0f};
 #pragma unroll
@@ -458,7 +479,7 @@ __global__ void __launch_bounds__(NT, 4) distill_row_kernel(DistillArgs a)
         if (careful) add_row(std::true_type());
         whole = (double)sum;
     }
-    row_numbers<NT>(a, i, h.slot, h.weight, ref, whole, s);
+    row_numbers<NT>(a, i, h.weight, ref, whole, s);
     if (!a.grad) return;
     some = __builtin_amdgcn_readfirstlane(some);
     const Slope q = {shared_by_wave(s.factor), shared_by_wave(ref), careful};
@@ -572,8 +593,8 @@ __global__ void __launch_bounds__(256) distill_numbers_kernel(NumbersArgs a)
 {
     __shared__ Shared<256> s;
     const uint32_t i = blockIdx.x;
-    Head h = head_of<DTYPE, BITS>(a, i);
-    const bool active = enter_slots<DTYPE, 256>(s, h.slot, 0);
+    const Head h = head_of<DTYPE, BITS>(a, i);
+    const bool active = enter_slots<DTYPE, 256>(s, h, 0);
     float ref = kLowest;
     bool careful = false;
     double sum = 0.0;
@@ -586,13 +607,14 @@ __global__ void __launch_bounds__(256) distill_numbers_kernel(NumbersArgs a)
             careful = careful || !(v.y >= 0.0f);
             if (v.y != 0.0f) sum += fabs((double)v.y) * (v.x == ref ? 1.0 : exp(((double)v.x - (double)ref) * inv_t));
         }
-        row_numbers<256>(a, i, h.slot, h.weight, ref, sum, s);
+        row_numbers<256>(a, i, h.weight, ref, sum, s);
     } else {
         no_loss(a, i);
     }
-    if ((int)threadIdx.x < a.k)
-        a.named[(uint64_t)i * a.k + threadIdx.x] =
-            make_uint2(h.slot.live ? (uint32_t)h.slot.id : kNone, h.slot.live ? __float_as_uint(s.value[h.slot.place]) : 0u);
+    if ((int)threadIdx.x < a.k) {
+        const uint32_t id = s.named[threadIdx.x];
+        a.named[(uint64_t)i * a.k + threadIdx.x] = make_uint2(id, id != kNone ? __float_as_uint(s.value[s.place[threadIdx.x] >> 1]) : 0u);
+    }
     if (threadIdx.x == 0) a.slopes[i] = make_float4(active ? s.factor : 0.0f, ref, careful ? 1.0f : 0.0f, active ? 1.0f : 0.0f);
 }
 

@@ -93,31 +93,6 @@ __device__ __forceinline__ void lds_barrier()
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
-// What the lanes up to this one hold, added up, by data-parallel primitives; lanes that a step has nothing for add 0.
-template <int CTRL, int ROWS>
-__device__ __forceinline__ uint32_t lanes_below(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xF, true); }
-template <int CTRL, int ROWS>
-__device__ __forceinline__ double lanes_below(double v)
-{
-    const u64 x = (u64)__double_as_longlong(v);
-    return __longlong_as_double((long long)((u64)lanes_below<CTRL, ROWS>((uint32_t)(x >> 32)) << 32 | lanes_below<CTRL, ROWS>((uint32_t)x)));
-}
-template <typename V>
-__device__ __forceinline__ V wave_upto(V v)
-{
-    v += lanes_below<0x111, 0xF>(v);           // row_shr 1, 2, 4, 8
-    v += lanes_below<0x112, 0xF>(v);
-    v += lanes_below<0x114, 0xF>(v);
-    v += lanes_below<0x118, 0xF>(v);
-    v += lanes_below<0x142, 0xA>(v);           // row_bcast 15 into the second and fourth row
-    v += lanes_below<0x143, 0xC>(v);           // row_bcast 31 into the upper two
-    return v;
-}
-__device__ __forceinline__ double lane_value(double v, int lane)
-{
-    const u64 x = (u64)__double_as_longlong(v);
-    return __longlong_as_double((long long)((u64)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)x, lane)));
-}
 // The same sums as borders of the lanes' intervals.  The sum of every lane is rounded in an order of its own, so that it may fall from one lane
 // to the next, or rise where a lane adds nothing: a border is the largest sum up to it of a lane that adds something.
 __device__ __forceinline__ double wave_borders(double v)

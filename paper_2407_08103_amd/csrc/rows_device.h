@@ -253,6 +253,31 @@ __device__ __forceinline__ float wave_max(float v)
     v = fmaxf(v, lane_swap<0x140>(v));
     return fmaxf(fmaxf(lane_value(v, 0), lane_value(v, 16)), fmaxf(lane_value(v, 32), lane_value(v, 48)));
 }
+// What the lanes up to this one hold, added up, by data-parallel primitives; lanes that a step has nothing for add 0.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t lanes_below(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xF, true); }
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double lanes_below(double v)
+{
+    const unsigned long long x = (unsigned long long)__double_as_longlong(v);
+    return __longlong_as_double((long long)((unsigned long long)lanes_below<CTRL, ROWS>((uint32_t)(x >> 32)) << 32 | lanes_below<CTRL, ROWS>((uint32_t)x)));
+}
+template <typename V>
+__device__ __forceinline__ V wave_upto(V v)
+{
+    v += lanes_below<0x111, 0xF>(v);           // row_shr 1, 2, 4, 8
+    v += lanes_below<0x112, 0xF>(v);
+    v += lanes_below<0x114, 0xF>(v);
+    v += lanes_below<0x118, 0xF>(v);
+    v += lanes_below<0x142, 0xA>(v);           // row_bcast 15 into the second and fourth row
+    v += lanes_below<0x143, 0xC>(v);           // row_bcast 31 into the upper two
+    return v;
+}
+__device__ __forceinline__ double lane_value(double v, int lane)
+{
+    const unsigned long long x = (unsigned long long)__double_as_longlong(v);
+    return __longlong_as_double((long long)((unsigned long long)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)x, lane)));
+}
 // Sum (MAX: maximum) over the workgroup, in every thread and in one order.  Two barriers.
 template <int NT, bool MAX>
 __device__ __forceinline__ float block_reduce(float v, float (&part)[NT / 64])
