@@ -957,6 +957,24 @@ struct Steps {
         double unused;
         return of(z, &unused);
     }
+    // The logits next to step i: a few units in the last place around it, so that nothing of it is missed.
+    struct Band {
+        float least, most;
+        __device__ __forceinline__ bool any_of(uint4 x) const
+        {
+            float z[4];
+            unpack<TDFA_F32>(x, z);
+            bool any = false;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) any |= z[j] >= least && z[j] <= most;
+            return any;
+        }
+    };
+    __device__ __forceinline__ Band band_of(uint32_t i) const
+    {
+        const float lo = (float)(m - (double)(i + 1) / scale), hi = (float)(m - (double)i / scale);
+        return {shared_by_wave(lo - fabsf(lo) * 0x1p-21f - 1.0e-30f), shared_by_wave(hi + fabsf(hi) * 0x1p-21f + 1.0e-30f)};
+    }
 };
 
 // (A thread has kSteps / NT steps that lie together.)
@@ -1033,7 +1051,8 @@ __device__ __forceinline__ bool draw_of_steps(Shared<TDFA_F32, NT>& s, Held<TDFA
     double kept = c.whole;
     // Lists step i and adds up its weights from `base` on; false: too many.
     const auto look = [&](uint32_t i, double base) {
-        const uint32_t n = list_of<TDFA_F32, NT, R, BITS>(s, row, [&](uint4) { return true; }, [&](int32_t, float z) { return steps.of(z) == i; });
+        const Steps::Band band = steps.band_of(i);
+        const uint32_t n = list_of<TDFA_F32, NT, R, BITS>(s, row, [&](uint4 x) { return band.any_of(x); }, [&](int32_t, float z) { return steps.of(z) == i; });
         if (n == 0 || n > kList<TDFA_F32>) return 0u;
         if (threadIdx.x < 64) {
             sum_list(s, n, m, inv_t);
@@ -1107,7 +1126,8 @@ __device__ __forceinline__ bool draw_of_steps(Shared<TDFA_F32, NT>& s, Held<TDFA
         }
         lds_barrier();
         const double base = s.mass[2];
-        const uint32_t n = list_of<TDFA_F32, NT, R, BITS>(s, row, [&](uint4) { return true; }, [&](int32_t, float z) { return steps.of(z) == i; });
+        const Steps::Band band = steps.band_of(i);
+        const uint32_t n = list_of<TDFA_F32, NT, R, BITS>(s, row, [&](uint4 x) { return band.any_of(x); }, [&](int32_t, float z) { return steps.of(z) == i; });
         if (n > kList<TDFA_F32>) return false;
         if (threadIdx.x < 64 && n) {
             sum_list(s, n, m, inv_t);
@@ -1393,7 +1413,7 @@ void fill(SelectArgs& x, const LogitRows& a, int64_t from)
 // 51.9 and 49.1 -> 49.9 (workgroups of 1,024 threads, of which one fits: 193 and 189).  Rows of 32,000 by 512 threads with 8 groups each against 256
 // with 16: 300 rows 21 against 26, 1,500 rows 52 against 56.
 template <int DTYPE, bool BITS, typename F>
-int shaped(int64_t rows, int32_t n_groups, F&& launch_of)
+int shaped(bool draws, int64_t rows, int32_t n_groups, F&& launch_of)
 {
     using std::integral_constant;
     const integral_constant<int, DTYPE> type;
@@ -1404,6 +1424,7 @@ int shaped(int64_t rows, int32_t n_groups, F&& launch_of)
     if (n_groups <= 512 * 8) return go(integral_constant<int, 512>(), integral_constant<int, 8>());
     if constexpr (DTYPE == TDFA_F32) {
         // (with more in registers the compiler would keep some in memory)
+        if (rows > (BITS ? 448 : 256) && (draws || n_groups <= 1024 * 8)) return go(integral_constant<int, 512>(), integral_constant<int, 0>());
         if (n_groups <= 1024 * 8) return go(integral_constant<int, 1024>(), integral_constant<int, 8>());
     } else {
         if (n_groups <= 512 * 16) return go(integral_constant<int, 512>(), integral_constant<int, 16>());
@@ -1413,11 +1434,11 @@ int shaped(int64_t rows, int32_t n_groups, F&& launch_of)
     return go(integral_constant<int, 1024>(), integral_constant<int, 0>());
 }
 template <typename F>
-int shaped(const LogitRows& a, F&& launch_of)
+int shaped(bool draws, const LogitRows& a, F&& launch_of)
 {
     const int32_t n_groups = a.n_tokens / (a.dtype == TDFA_F32 ? 4 : 8);
-    if (a.dtype == TDFA_F32) return a.allow ? shaped<TDFA_F32, true>(a.rows, n_groups, launch_of) : shaped<TDFA_F32, false>(a.rows, n_groups, launch_of);
-    return a.allow ? shaped<TDFA_BF16, true>(a.rows, n_groups, launch_of) : shaped<TDFA_BF16, false>(a.rows, n_groups, launch_of);
+    if (a.dtype == TDFA_F32) return a.allow ? shaped<TDFA_F32, true>(draws, a.rows, n_groups, launch_of) : shaped<TDFA_F32, false>(draws, a.rows, n_groups, launch_of);
+    return a.allow ? shaped<TDFA_BF16, true>(draws, a.rows, n_groups, launch_of) : shaped<TDFA_BF16, false>(draws, a.rows, n_groups, launch_of);
 }
 
 }  // namespace
@@ -1440,7 +1461,7 @@ int launch_draw_step(const LogitRows& a, const DrawRows& d, void*, hipStream_t s
         x.top_k = d.top_k;
         x.top_p = d.top_p;
         x.min_p = d.min_p;
-        return shaped(a, [&](auto type, auto threads, auto groups, auto bits) {
+        return shaped(true, a, [&](auto type, auto threads, auto groups, auto bits) {
             constexpr int DTYPE = decltype(type)::value, NT = decltype(threads)::value, R = decltype(groups)::value;
             return launch(draw_step_kernel<DTYPE, NT, R, decltype(bits)::value>, dim3(rows), NT, stream, x);
         });
@@ -1455,7 +1476,7 @@ int launch_top_logprobs(const LogitRows& a, int32_t k, int32_t* ids, float* logp
         x.ids = ids + from * k;
         x.logprobs = logprobs + from * k;
         x.k = k;
-        return shaped(a, [&](auto type, auto threads, auto groups, auto bits) {
+        return shaped(false, a, [&](auto type, auto threads, auto groups, auto bits) {
             constexpr int DTYPE = decltype(type)::value, NT = decltype(threads)::value, R = decltype(groups)::value;
             return launch(top_logprobs_kernel<DTYPE, NT, R, decltype(bits)::value>, dim3(rows), NT, stream, x);
         });
