@@ -314,3 +314,60 @@ def test_refusals(T):
         call(wide[:4], None, ids, values, loss, losses, grad_logits=wide[1:])       # over the logits, a row later
     with pytest.raises(T.TdfaError):
         call(x, None, ids, values, loss, losses, workspace=torch.empty(8, dtype=torch.uint8, device="cuda"))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_far_apart(T, dtype):
+    """Rows whose offsets pass 32 bits, of the logits and of the gradient."""
+    import test_gpu_draw as D
+    v, stride = 3001, (1 << 30) + 64
+    far = [torch.empty(2 * stride + 4096, dtype=D.TYPES[dtype], device="cuda").as_strided((3, v), (stride, 1)) for _ in range(2)]
+    near = torch.randn((3, 3008), device="cuda").mul_(2).to(D.TYPES[dtype])[:, :v]
+    far[0].copy_(near)
+    ids, lp = torch.empty((3, 9), dtype=torch.int32, device="cuda"), torch.empty((3, 9), device="cuda")
+    T.top_logprobs(None, near, None, ids, lp, temperature=1.3)
+    got = []
+    for z, g in ((far[0], far[1]), (near, torch.empty((3, 3008), dtype=near.dtype, device="cuda")[:, :v])):
+        loss, losses = torch.empty(1, device="cuda"), torch.empty(3, device="cuda")
+        T.distill_loss(None, z, None, ids, lp, loss, losses, grad_logits=g, tail=True)
+        got.append((loss, losses, g))
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [3, 41, 600])
+@pytest.mark.parametrize("v", [9001, 33001, 70001])
+def test_shapes_agree(T, v, rows, dtype):
+    """Rows by parts and rows in registers give the same to what their sums' orders leave."""
+    r = Rows(T, "peaked", 3, v, dtype, 63)
+    ids, values = slots(r, 60, np.random.default_rng(9))
+    rep = -(-rows // 3)
+    x, q = r.x.repeat(rep, 1)[:rows], r.states.repeat(rep)[:rows].contiguous()
+    i2, v2 = torch.from_numpy(ids).cuda().repeat(rep, 1)[:rows].contiguous(), torch.from_numpy(values).cuda().repeat(rep, 1)[:rows].contiguous()
+    loss, losses, g = torch.empty(1, device="cuda"), torch.empty(rows, device="cuda"), torch.empty_like(x)
+    T.distill_loss(r.table, x[:, :v], q, i2, v2, loss, losses, grad_logits=g[:, :v], tail=True)
+    want, each, want_g = R.loss(r.z, r.on, ids, values, np.ones(3), 1.0, True)
+    for i in range(3):
+        assert abs(float(losses[i]) - each[i]) <= 2.0 ** -18 + abs(each[i]) * 2.0 ** -23
+        got = g[i, :v].double().cpu().numpy()
+        size = np.abs(want_g[i]) + 2 * (upper(r, i, 1.0, ids[i], values[i], True) if r.on[i].any() else 0.0)
+        assert (np.abs(got - want_g[i]) <= HALF[dtype] * np.abs(want_g[i]) + 2.0 ** -18 * size + 2.0 ** -126).all()
+    assert torch.equal(losses, losses[:3].repeat(rep)[:rows])
+    assert torch.equal(g[:, :v], g[:3, :v].repeat(rep, 1)[:rows])
+
+
+def test_two_streams(T):
+    r = [Rows(T, "peaked", 30, 20011, "bf16", 64 + i) for i in range(2)]
+    lists = [[torch.from_numpy(a).cuda() for a in slots(x, 20, np.random.default_rng(i))] for i, x in enumerate(r)]
+    out = [[torch.empty(1, device="cuda"), torch.empty(30, device="cuda"), torch.zeros_like(r[i % 2].x)] for i in range(4)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for k in range(6):
+        for i in range(2):
+            T.distill_loss(r[i].table, r[i].logits, r[i].states, *lists[i], out[i][0], out[i][1], grad_logits=out[i][2][:, :20011], tail=True, stream=streams[i])
+    torch.cuda.synchronize()
+    for i in range(2):
+        T.distill_loss(r[i].table, r[i].logits, r[i].states, *lists[i], out[2 + i][0], out[2 + i][1], grad_logits=out[2 + i][2][:, :20011], tail=True)
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(a, b) for a, b in zip(out[i], out[2 + i]))

@@ -361,3 +361,70 @@ def test_refusals(T):
         T.draw_step(r.table, r.logits[:, :32], r.states, u, t, t.clone())
     with pytest.raises(T.TdfaError):
         T.draw_step(r.table, r.logits, r.states, u, r.states, t)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_far_apart(T, dtype):
+    """Rows whose offsets pass 32 bits, and other strides than the tested ones."""
+    v = 3001
+    stride = (1 << 30) + 64
+    x = torch.empty(2 * stride + 4096, dtype=TYPES[dtype], device="cuda").as_strided((3, v), (stride, 1))
+    near = torch.randn((3, 3008), device="cuda").mul_(2).to(TYPES[dtype])[:, :v]
+    x.copy_(near)
+    u = torch.tensor([0.1, 0.5, 0.9], device="cuda")
+    got = []
+    for z in (x, near):
+        t, lp = torch.empty(3, dtype=torch.int32, device="cuda"), torch.empty(3, device="cuda")
+        ids, top = torch.empty((3, 9), dtype=torch.int32, device="cuda"), torch.empty((3, 9), device="cuda")
+        T.draw_step(None, z, None, u, t, None, top_p=0.9, logprobs=lp)
+        T.top_logprobs(None, z, None, ids, top)
+        got.append((t, lp, ids, top))
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [2, 300, 600, 900])
+@pytest.mark.parametrize("v", [9001, 33001, 66001])
+def test_shapes_agree(T, v, rows, dtype):
+    """A row gives the same whatever the rows around it, which the launch shapes go by."""
+    if v * rows > 40_000_000:
+        pytest.skip("the shapes of fewer tokens cover it")
+    r = Rows(T, "peaked", 6, v, dtype, 60)
+    rep = -(-rows // 6)
+    x = r.x.repeat(rep, 1)[:rows]
+    q = r.states.repeat(rep)[:rows].contiguous()
+    u = torch.from_numpy(r.uniforms()).cuda().repeat(rep)[:rows].contiguous()
+    t, q2, lp = (torch.empty(rows, dtype=d, device="cuda") for d in (torch.int32, torch.int32, torch.float32))
+    ids, top = torch.empty((rows, 33), dtype=torch.int32, device="cuda"), torch.empty((rows, 33), device="cuda")
+    for s in (dict(temperature=0.8, top_p=0.9), dict(top_k=900, min_p=0.001)):
+        T.draw_step(r.table, x[:, :v], q, u, t, q2, logprobs=lp, **s)
+        for i in range(min(6, rows)):
+            want = R.draw(r.z[i], r.on[i], float(u[i]), s.get("temperature", 1.0), s.get("top_k", 0), s.get("top_p", 1.0), s.get("min_p", 0.0))
+            assert int(t[i]) in want and close(float(lp[i]), want[int(t[i])])
+        for a in (t, q2, lp):
+            assert torch.equal(a, a[:6].repeat(rep)[:rows])
+    T.top_logprobs(r.table, x[:, :v], q, ids, top)
+    assert torch.equal(ids, ids[:6].repeat(rep, 1)[:rows]) and torch.equal(top, top[:6].repeat(rep, 1)[:rows])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("temperature", [1e-3, 0.02, 30.0, 1e4, 1e30])
+def test_draw_temperatures(T, dtype, temperature):
+    r = Rows(T, "open", 12, 5003, dtype, 61, table=None)
+    for s in (dict(), dict(top_p=0.5), dict(top_k=3), dict(min_p=0.3)):
+        check_draw(T, r, r.uniforms(), temperature=temperature, **s)
+    if temperature > 1e-4:
+        check_top(T, r, 10, temperature)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_top_k_ends_in_ties(T, dtype):
+    """More tokens share the k-th logit than fit the list: those of the lowest ids, and a draw among all of them."""
+    r = Rows(T, "open", 4, 7001, dtype, 62, table=None)
+    r.x[:, 100:5100] = 3.0
+    r.x[:, 50] = 9.0
+    r.z = r.logits.double().cpu().numpy()
+    for k in (1, 2, 40, 256):
+        check_top(T, r, k)
+    for s in (dict(top_k=2), dict(top_k=5000, top_p=0.7), dict(min_p=0.001)):
+        check_draw(T, r, r.uniforms(), **s)
