@@ -445,7 +445,8 @@ TDFA_API int64_t tdfa_select_workspace_bytes(int32_t rows, int32_t n_tokens);
  *     tokens[i] = the first t of N, in the order of the tokens, up to which (t included) the weights of N add up to more than
  *                 u times their sum;   new_states[i] = delta_T[q][tokens[i]];   logprobs[i] = ln(w_t / the sum of N).
  * So u = 0 gives the most likely token, and tokens with equal logits are cut together or not at all.  A number within 2^-40 or so of the border
- * between two tokens may give either, always the same one for the same arguments.
+ * between two tokens may give either, and a top_p or min_p as near to what ends a cut may leave the tokens of one logit more or less: always the same for
+ * the same arguments.
  * If A is empty: tokens[i] = TDFA_NO_TOKEN, new_states[i] = q, logprobs[i] = 0.  If q is no row of the table: TDFA_NO_TOKEN,
  * TDFA_DEAD and 0.  If m is -inf: the lowest id in A, with a log-probability of -inf.
  *   uniforms_dev   : device, float [rows], 0 .. 1 (less counts as 0, as NaN does, and more as 1; at 1 the last token of N is drawn, or

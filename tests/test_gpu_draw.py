@@ -428,3 +428,25 @@ def test_top_k_ends_in_ties(T, dtype):
         check_top(T, r, k)
     for s in (dict(top_k=2), dict(top_k=5000, top_p=0.7), dict(min_p=0.001)):
         check_draw(T, r, r.uniforms(), **s)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("temperature", [1e-40, 1e-30, 1e30, 3e38])
+def test_top_temperatures_at_the_ends(T, dtype, temperature):
+    """Next to no temperature: all of the probability is the largest logit's; a huge one: every token has the same, logits that differ by more
+    than binary32 reaches excepted."""
+    r = Rows(T, "open", 3, 5003, dtype, 63, table=None)
+    r.x[:, 77], r.x[:, 78], r.x[2, 79] = 20.0, 19.0, -3.0e38
+    ids, lp = (torch.empty((3, 5), dtype=t, device="cuda") for t in (torch.int32, torch.float32))
+    T.top_logprobs(None, r.logits, None, ids, lp, temperature=temperature)
+    ids, lp = ids.cpu().numpy(), lp.cpu().numpy()
+    assert (ids[:, :2] == [77, 78]).all()
+    if temperature < 1:
+        assert (lp[:, 0] == 0).all()
+        t = float(np.float32(temperature))
+        assert np.allclose(lp[:, 1], np.float32(-1 / t) if 1 / t < 3.4e38 else -np.inf, rtol=1e-6)
+    else:
+        far = 1.0 if temperature == 1e30 else 1.0 - np.exp(-3.0e38 / 3e38)
+        want = -np.log(np.array([5003, 5003, 5003 - far]))[:, None]
+        # the rounding of the result, and of 5,003 weights next to 1 and their sum by threads: a few units in the last place
+        assert np.abs(lp - want).max() <= 1e-6 * 8.6
