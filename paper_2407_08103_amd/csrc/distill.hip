@@ -440,9 +440,9 @@ __device__ __forceinline__ void no_loss(const DistillArgs& a, uint32_t i)
 // One workgroup per row, of at most NT R groups, which stay in registers between the sum and the gradient.  16 bits: the sum is relative to the
 // largest logit that is named, so that terms are added as they arrive; where that does not do, and in fp32, whose gradients would show what
 // exponents lose far from the largest logit, relative to a running maximum.
-// What bounds it: the memory where there are many rows, 4,096 rows of 128,256 tokens in bf16 348 us for 1.05 GB written and 0.4 GB
-// of groups with an allowed token read (4.1 TB/s; a large copy runs at 4.7), 1,024 rows without a constraint 113 us (4.6); few rows, the chain of slots, row, sums, numbers (by one wavefront, in binary64) and
-// gradients: 24 rows of 32,000 11 us, and 2 to 4 for the sum of their losses.  (A workgroup per row that reads it twice: 1,222, 323 and 28 us a call.)
+// What bounds it: the memory where there are many rows, 4,096 rows of 128,256 tokens in bf16 350 us for 1.05 GB written and 0.4 GB
+// of groups with an allowed token read (4.1 TB/s; a large copy runs at 4.7), 1,024 rows without a constraint 116 us (4.5); few rows, the chain of slots, row, sums, numbers (by one wavefront, in binary64) and
+// gradients: 24 rows of 32,000 10 us, and 2 for the sum of their losses.  (A workgroup per row that reads it twice: 1,222, 323 and 28 us a call.)
 template <int DTYPE, int NT, int R, bool BITS>
 __global__ void __launch_bounds__(NT, 4) distill_row_kernel(DistillArgs a)
 {
