@@ -935,13 +935,14 @@ __device__ __forceinline__ float largest_of(Shared<TDFA_F32, NT>& s, Held<TDFA_F
         m = max_group<TDFA_F32>(x, m);
     });
     m = wave_max(m);
-    if ((threadIdx.x & 63) == 0) s.word[threadIdx.x >> 6] = __float_as_uint(m);
+    // (not in s.word: a wavefront without a token is here while others read there how many the row has)
+    if ((threadIdx.x & 63) == 0) s.word2[threadIdx.x >> 6] = __float_as_uint(m);
     for (uint32_t j = threadIdx.x; j < kSteps; j += NT) {
         s.step.weight[j] = 0;
         s.step.tokens[j] = 0;
     }
     lds_barrier();
-    for (int v = 0; v < NT / 64; ++v) m = fmaxf(m, __uint_as_float(s.word[v]));
+    for (int v = 0; v < NT / 64; ++v) m = fmaxf(m, __uint_as_float(s.word2[v]));
     return shared_by_wave(m);
 }
 
