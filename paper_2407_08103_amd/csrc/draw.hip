@@ -1041,10 +1041,10 @@ __device__ __forceinline__ bool draw_of_steps(Shared<TDFA_F32, NT>& s, Held<TDFA
     if (!(fabsf(m) < INFINITY)) return false;
     const double inv_t = q.inv_t();
     const auto key = [&](uint32_t i) { return (uint32_t)(s.sorted[i] >> 32); };
-    const auto reaches = [&](uint4 x) { return max_group<TDFA_F32>(x, -INFINITY); };
     if (inv_t == 0.0) {
-        const uint32_t n = list_of<TDFA_F32, NT, R, BITS>(s, row, [&](uint4 x) { return reaches(x) == m; }, [&](int32_t, float z) { return z == m; });
-        if (n > kList<TDFA_F32>) return false;
+        // (a group may hold larger logits too, of tokens that are not allowed)
+        const uint32_t n = list_of<TDFA_F32, NT, R, BITS>(s, row, [&](uint4 x) { return max_group<TDFA_F32>(x, -INFINITY) >= m; }, [&](int32_t, float z) { return z == m; });
+        if (n == 0 || n > kList<TDFA_F32>) return false;
         *d = {(int32_t)~(uint32_t)s.sorted[0], 0.0f};
         return true;
     }

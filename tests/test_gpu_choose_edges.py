@@ -58,3 +58,34 @@ def test_few_wavefronts_have_a_token(T, v, dtype):
         check_draw(T, r, r.uniforms(), temperature=0.8, top_p=0.9)
         check_draw(T, r, r.uniforms(), top_k=20, min_p=0.01)
         check_top(T, r, 30)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("v,copies", [(3001, 1), (9001, 1), (33001, 1), (33001, 60), (66001, 1), (66001, 60)])
+@pytest.mark.parametrize("beside", [50.0, 3.0e38, np.inf, np.nan])
+def test_larger_logits_that_are_not_allowed(T, beside, v, copies, dtype):
+    """The first token of a row has logits above its own in its group of 16 bytes, of tokens that the constraint does not allow; and ties: the lowest id of
+    the largest allowed logit is in such a group or not."""
+    n = 8
+    rng = np.random.default_rng([v, 2])
+    on = rng.random((n, v)) < 0.6
+    z = rng.normal(0, 2, (n, v))
+    want = np.zeros(n, dtype=np.int64)
+    for i in range(n):
+        at = [0, 1, 3, v // 8 * 8 + (v % 8 - 1), v // 2, v // 3, v // 16 * 8 + 5, v // 4 * 4 - 1][i]
+        z[i, at], on[i, at], want[i] = 20.0, True, at
+        for other in {at ^ 1, at ^ 2, at ^ 3} - {at}:
+            if other < v:
+                z[i, other], on[i, other] = beside, False
+        if i % 2 and at + 100 < v:
+            z[i, at + 100], on[i, at + 100] = 20.0, True              # a tie behind it
+    r = Given(T, z, on, dtype)
+    for s in (dict(temperature=0.0), dict(top_k=1), dict(temperature=0.7, top_p=0.9), dict(min_p=0.2)):
+        check_draw(T, r, r.uniforms(), **s)
+    # the same rows in a batch of as many as take other launch shapes
+    x, q = r.x.repeat(copies, 1)[:, :v], r.states.repeat(copies)
+    tokens, after = (torch.full((n * copies,), -7, dtype=torch.int32, device="cuda") for _ in range(2))
+    T.draw_step(r.table, x, q, torch.rand(n * copies, device="cuda"), tokens, after, temperature=0.0)
+    assert np.array_equal(tokens.cpu().numpy(), np.tile(want, copies))
+    assert np.array_equal(after.cpu().numpy(), np.tile(r.delta[np.arange(n), want], copies))
+    check_top(T, r, 5)
