@@ -541,7 +541,7 @@ __global__ void __launch_bounds__(NT, 4) distill_row_kernel(DistillArgs a)
 // ---- rows that do not stay in registers: sums by parts, the numbers of the rows, gradients by parts ----------
 
 struct PartArgs : DistillArgs {
-    float2* parts;             // [rows][n_parts]: the largest logit of the tail in the part, and the sum relative to it, below 0 if it was taken with care
+    float2* parts;             // [rows][n_parts]: the largest logit of the tail in the part, and the sum relative to it, with its sign set if it was taken with care
     int32_t n_parts, span;     // groups to a part
 };
 struct NumbersArgs : DistillArgs {
@@ -627,7 +627,7 @@ __global__ void __launch_bounds__(NT) distill_part_kernel(PartArgs a)
     add_part(std::false_type());
     const bool careful = !(sum < INFINITY);
     if (careful) add_part(std::true_type());
-    if (tid == 0) a.parts[blockIdx.x] = make_float2(m, careful ? -sum : sum);
+    if (tid == 0) a.parts[blockIdx.x] = make_float2(m, __uint_as_float(__float_as_uint(sum) | (careful ? 0x80000000u : 0u)));
 }
 
 // One workgroup per row: its numbers from its slots and the sums of its parts.
@@ -647,7 +647,7 @@ __global__ void __launch_bounds__(256) distill_numbers_kernel(NumbersArgs a)
             if (a.parts[(uint64_t)i * a.n_parts + p].y != 0.0f) ref = fmaxf(ref, a.parts[(uint64_t)i * a.n_parts + p].x);
         for (int32_t p = 0; p < a.n_parts; ++p) {
             const float2 v = a.parts[(uint64_t)i * a.n_parts + p];
-            careful = careful || !(v.y >= 0.0f);
+            careful = careful || __float_as_uint(v.y) >> 31;               // (also of a sum of 0, where the part has nothing but NaN)
             if (v.y != 0.0f) sum += fabs((double)v.y) * (v.x == ref ? 1.0 : exp(((double)v.x - (double)ref) * inv_t));
         }
         slot_numbers(a, s);

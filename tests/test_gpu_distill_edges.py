@@ -1,0 +1,59 @@
+"""Distillation where a row's tail, its slots or its weight lie at an edge of how the loss and its gradient are worked out."""
+import numpy as np
+import pytest
+import torch
+
+import distill_ref as R
+from test_gpu_choose_edges import Given
+from test_gpu_distill import HALF, Rows, check, run
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def T():
+    import paper_2407_08103_amd as T
+    assert torch.cuda.is_available()
+    return T
+
+
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kind", ["special", "none", "infinite", "zeros", "wide", "ties"])
+def test_kinds_of_long_rows(T, kind, dtype, tail):
+    """Rows that are taken by parts, of values that are no ordinary text."""
+    for v, table in ((33001, "owned"), (140003, None), (140003, "packed")):
+        r = Rows(T, kind, 6, v, dtype, 71, table=table)
+        check(T, r, dtype, 20, 0.8, tail)
+        check(T, r, dtype, 200, 1.7, tail, grad="in place")
+
+
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("v", [9001, 33001, 140003])
+def test_nan_alone_in_a_part(T, v, dtype, tail):
+    """Few tokens are allowed, and what is allowed besides the named ones is NaN or -inf, in all of the row or in a stretch of it: it counts as -inf, and its
+    gradient is 0."""
+    n, k = 6, 4
+    rng = np.random.default_rng([v, 3])
+    on = np.zeros((n, v), dtype=bool)
+    z = rng.normal(0, 2, (n, v))
+    named = np.array([5, 6, v // 2 + 1, v - 1])
+    on[:, named] = True
+    at = [[100], [v - 2], [100, 101, v // 3], [v // 2, v // 2 + 2, v // 4], [100, v // 3], [100, v - 2]]
+    for i in range(n):
+        on[i, at[i]] = True
+        z[i, at[i]] = np.nan
+    z[4, v // 3] = -np.inf
+    on[5, 2000], z[5, 2000] = True, 1.0                      # one token of the tail that counts, elsewhere
+    r = Given(T, z, on, dtype)
+    ids = np.tile(named.astype(np.int32), (n, 1))
+    values = np.log(np.tile(np.float32([0.4, 0.3, 0.1, 0.1]), (n, 1)))
+    for grad in ("new", "in place"):
+        _, losses, g = run(T, r, ids, values, None, 0.9, tail, grad)
+        for i in range(n):
+            l, want = R.row(r.z[i], r.on[i], ids[i], values[i], 0.9, tail)
+            assert abs(losses[i] - l) <= 2.0 ** -18 + abs(l) * 2.0 ** -23, (i, losses[i], l)
+            assert (g[i, at[i]] == 0).all(), (i, g[i, at[i]])
+            # two terms of at most 1 / temperature each, off by 2^-18 of themselves, and a rounding
+            assert (np.abs(g[i] - want) <= HALF[dtype] * np.abs(want) + 2.0 ** -18 * 2 / 0.9).all(), i
