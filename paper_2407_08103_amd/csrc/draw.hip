@@ -961,7 +961,8 @@ struct Steps {
         double unused;
         return of(z, &unused);
     }
-    // The logits next to step i: a few units in the last place around it, so that nothing of it is missed.
+    // The logits next to step i: so far around it that nothing of it is missed.  A distance from m and its step are rounded to 53 bits, and so is a
+    // border: each is off by 2^-51 or less of the distance, however near to 0 the border itself lies, and by 2^-24 of the border in binary32.
     struct Band {
         float least, most;
         __device__ __forceinline__ bool any_of(uint4 x) const
@@ -976,8 +977,9 @@ struct Steps {
     };
     __device__ __forceinline__ Band band_of(uint32_t i) const
     {
-        const float lo = (float)(m - (double)(i + 1) / scale), hi = (float)(m - (double)i / scale);
-        return {shared_by_wave(lo - fabsf(lo) * 0x1p-21f - 1.0e-30f), shared_by_wave(hi + fabsf(hi) * 0x1p-21f + 1.0e-30f)};
+        const double end = (double)(i + 1) / scale;
+        const float lo = (float)(m - end), hi = (float)(m - (double)i / scale), around = (float)(end * 0x1p-45) + 1.0e-30f;
+        return {shared_by_wave(lo - fabsf(lo) * 0x1p-21f - around), shared_by_wave(hi + fabsf(hi) * 0x1p-21f + around)};
     }
 };
 

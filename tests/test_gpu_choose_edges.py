@@ -89,3 +89,28 @@ def test_larger_logits_that_are_not_allowed(T, beside, v, copies, dtype):
     assert np.array_equal(tokens.cpu().numpy(), np.tile(want, copies))
     assert np.array_equal(after.cpu().numpy(), np.tile(r.delta[np.arange(n), want], copies))
     check_top(T, r, 5)
+
+
+@pytest.mark.parametrize("table", [False, True])
+@pytest.mark.parametrize("temperature,largest", [(1.5, 3.0), (1.5, 0.1875), (0.75, 20.25), (0.75, 24.0), (0.4, 3.2), (0.4, 0.2), (1.0, 2.5), (0.25, 6.0), (2.0, 12.0),
+                                                 (1.25, 5.0), (0.5, 0.5)])
+def test_zeros_at_a_border(T, temperature, largest, table):
+    """Many logits of exactly 0, or next to it, where the distance of the largest logit from 0 is a whole number of 80ths of the temperature or so: tokens that share out
+    a search are found however near its end they lie."""
+    n, v = 48, 4001
+    rng = np.random.default_rng([int(largest * 1000), 5])
+    z = np.minimum(rng.normal(0, 2, (n, v)), largest * 0.99)
+    z[rng.random((n, v)) < 0.2] = 0.0
+    tiny = (rng.random((n, v)) < 0.02)
+    z[tiny] = (rng.choice([-1.0, 1.0], (n, v)) * 10.0 ** rng.uniform(-30, -14, (n, v)))[tiny]
+    z[np.arange(n), rng.integers(0, v, n)] = largest
+    on = None
+    if table:
+        on = (rng.random((n, v)) < 0.7) | (z == largest)
+    r = Given(T, z, on, "f32")
+    zeros = [int(np.count_nonzero(r.on[i] & (r.z[i] > 0))) for i in range(n)]
+    u = np.linspace(0.0, 0.9999, n).astype(np.float32)
+    far = np.exp(-np.float64(np.float32(largest)) / np.float64(np.float32(temperature)))
+    for s in (dict(), dict(top_k=zeros[0] + 5), dict(top_k=zeros[n // 2] + 60, top_p=0.95), dict(min_p=float(far * 0.999)), dict(min_p=float(far * 0.999), top_p=0.9), dict(top_p=0.6)):
+        for i in range(2):
+            check_draw(T, r, np.roll(u, i), temperature=temperature, **s)
