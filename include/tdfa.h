@@ -430,7 +430,7 @@ TDFA_API int tdfa_sample_noise(int32_t batch, int32_t n_tokens, uint64_t seed, u
  * Row i has logits l, allowed set A (of states[i]), the largest logit m in A, and weights w_t = exp((l_t - m) / T) in A.
  * NaN counts as -inf and -0 as +0, and a logit outside A has no effect whatever it is.  Tokens are in the order of their
  * logits, the largest first, and of their ids among equal logits.  Where m is +inf the tokens that have it weigh 1 and
- * all others nothing.  Weights and their sums are held in 64 bits.
+ * all others nothing.  Weights and their sums are held in 64 bits, but for the weights of lists of 32-bit logits, which are of 32 bits.
  * What a call writes must not overlap anything else that it reads or writes, but for new_states in place of states.
  * The calls enqueue on `stream` and return, allocate nothing and may be captured into a graph.  Results depend on the arguments
  * only, not on the order in which anything runs.  Errors: INVALID_ARG, DEVICE. */
@@ -470,6 +470,8 @@ TDFA_API int tdfa_draw_step(const tdfa_table *table, const void *logits_dev, int
 /* The k first tokens of A with a logit above -inf, in the order of the tokens, and their log-probabilities
  *     lp = (l_t - m) / T - ln(the sum over A of w)
  * which are those that tdfa_token_logprobs gives (NaN where m is +inf).  Places that are left over get TDFA_NO_TOKEN and -inf.
+ * They are off by a rounding and 2^-39, and with 32-bit logits by what the weights of the tokens below m add to it: each may be off by (1 + |x|) 2^-22 of itself, for
+ * a weight of 2^x, so that the logarithm of the sum is off by 2^-20 or so where the probability is spread over many tokens, and by 2^-17 of lp where one has nearly all of it.
  *   k            : 1 .. TDFA_TOP_MAX.
  *   temperature  : > 0, finite.
  *   ids_dev      : device, int32 [rows][k], written.

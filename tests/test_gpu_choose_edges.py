@@ -114,3 +114,31 @@ def test_zeros_at_a_border(T, temperature, largest, table):
     for s in (dict(), dict(top_k=zeros[0] + 5), dict(top_k=zeros[n // 2] + 60, top_p=0.95), dict(min_p=float(far * 0.999)), dict(min_p=float(far * 0.999), top_p=0.9), dict(top_p=0.6)):
         for i in range(2):
             check_draw(T, r, np.roll(u, i), temperature=temperature, **s)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("v", [300, 4099, 33001, 262147])
+def test_lists_keep_their_bits(T, v, dtype):
+    """Log-probabilities as near to the definition as weights and sums of 64 bits and one rounding leave them: where the largest token has nearly all of the probability,
+    its logarithm is what all the others add up to.  With 32-bit logits and more than 256 allowed tokens a weight 2^x below the largest, which is 1, may be off: its exponent is a
+    difference, times a constant that was rounded, each off by 2^-24 of itself, ln 2 * 3 * 2^-24 |x| of the weight, and the exponential by 2^-23."""
+    n = 10
+    rng = np.random.default_rng([v, 6])
+    z = rng.normal(0, 2, (n, v))
+    on = rng.random((n, v)) < 0.7
+    at = rng.integers(0, v, n)
+    z[np.arange(n), at] = rng.uniform(5, 45, n)
+    on[np.arange(n), at] = True
+    z[0] = rng.normal(0, 0.1, v)
+    for r in (Given(T, z, on, dtype), Given(T, z, None, dtype)):
+        for k, t in ((1, 1.0), (40, 0.7), (256, 1.9)):
+            ids, lp = torch.empty((n, k), dtype=torch.int32, device="cuda"), torch.empty((n, k), device="cuda")
+            T.top_logprobs(r.table, r.logits, r.states, ids, lp, temperature=t)
+            for i in range(n):
+                want, want_lp = R.top(r.z[i], r.on[i], k, float(np.float32(t)))
+                assert np.array_equal(ids[i].cpu().numpy(), want), i
+                lost = 0.0
+                if dtype == "f32" and np.count_nonzero(r.on[i]) > 256:
+                    x = (r.z[i][r.on[i]] - r.z[i][r.on[i]].max()) / float(np.float32(t)) / np.log(2)
+                    lost = np.sum(np.where(x < 0, 2.0 ** x * (1 + 3 / 2 * np.log(2) * -x) * 2.0 ** -23, 0.0)) / np.sum(2.0 ** x)
+                assert all(close(a, b) or abs(a - b) <= lost + 2.0 ** -39 + abs(b) * 2.0 ** -23 for a, b in zip(lp[i].cpu().numpy(), want_lp)), (i, k, lp[i], want_lp)
