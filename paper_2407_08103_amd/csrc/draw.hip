@@ -431,18 +431,28 @@ __device__ __forceinline__ u64 share_of(double x, u64 y, bool up)
     return (u64)((p + (up ? ((unsigned __int128)1 << shift) - 1 : 0)) >> shift);
 }
 
-// Weights as whole numbers, so that their sums do not depend on the order in which they are added: 2^bits times the weight, where
-// n_tokens of them stay below 2^62.
+// Weights as whole numbers, so that their sums do not depend on the order in which they are added: times the power of two with which
+// those of the whole row, `sum` in all, stay below 2^62.  So n weights are off by n 2^-62 of the row's at most, however small each of them is.  (A cut leaves the larger
+// ones: of n tokens with weights w in all it leaves k with k w / n at least, whose own are off by (k + n) 2^-62 of what it leaves.)
 struct Whole {
     float m;
     double inv_t, scale;
     __device__ __forceinline__ u64 of(float z) const { return (u64)(weight_of(z, m, inv_t) * scale + 0.5); }
 };
-__device__ __forceinline__ Whole whole_of(float m, double inv_t, int32_t n_tokens)
-{
-    return {m, inv_t, ldexp(1.0, 62 - (32 - __clz(max(n_tokens, 1))))};
-}
+__device__ __forceinline__ Whole whole_of(float m, double inv_t, double sum) { return {m, inv_t, ldexp(1.0, 61 - ilogb(sum))}; }
 
+// The sum over the workgroup, in every thread and in one order.
+template <int NT>
+__device__ __forceinline__ double block_sum(double v, double (&part)[NT / 64])
+{
+    v = lane_value(wave_upto(v), 63);
+    lds_barrier();
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+    lds_barrier();
+    v = 0.0;
+    for (int w = 0; w < NT / 64; ++w) v += part[w];
+    return v;
+}
 template <int NT, int DTYPE>
 __device__ __forceinline__ u64 block_sum(u64 v, Shared<DTYPE, NT>& s)
 {
@@ -468,7 +478,9 @@ __device__ __forceinline__ Drawn draw_by_digits(Shared<DTYPE, NT>& s, const RowO
     u64 nth = 1, before;
     float lp = m == -INFINITY ? -INFINITY : 0.0f;
     if (m != -INFINITY && q.inv_t() != 0.0) {
-        const Whole w = whole_of(m, q.inv_t(), r.n_tokens);
+        double sum = 0.0;
+        for_each<DTYPE, NT, BITS>(r, [&](int32_t, float z) { sum += weight_of(z, m, q.inv_t()); });
+        const Whole w = whole_of(m, q.inv_t(), block_sum<NT>(sum, s.part));
         uint32_t cut = 0;                                  // the smallest key that is kept
         const auto weights = [&](auto&& f) { for_each<DTYPE, NT, BITS>(r, [&](int32_t, float z) { if (key_of(z) >= cut) f(key_of(z), w.of(z)); }); };
         const auto kept_weight = [&]() {
@@ -1308,15 +1320,14 @@ __device__ __forceinline__ uint32_t top_by_digits(Shared<DTYPE, NT>& s, const Ro
     const uint32_t last = ~key_at<NT>(s, k - larger, &unused, [&](auto&& f) {
         for_each<DTYPE, NT, BITS>(r, [&](int32_t t, float z) { f(~(uint32_t)t, (u64)(key_of(z) == key)); });
     });
-    const Whole w = whole_of(*m, inv_t, r.n_tokens);
-    u64 sum = 0;
+    double sum = 0.0;
     if (threadIdx.x == 0) s.n = 0;
     lds_barrier();
     for_each<DTYPE, NT, BITS>(r, [&](int32_t t, float z) {
-        sum += w.of(z);
+        sum += weight_of(z, *m, inv_t);
         if (key_of(z) > key || (key_of(z) == key && (uint32_t)t <= last)) s.list[atomicAdd(&s.n, 1u)] = (u64)key_of(z) << 32 | ~(uint32_t)t;
     });
-    *total = (double)block_sum<NT>(sum, s) / w.scale;
+    *total = block_sum<NT>(sum, s.part);
     const uint32_t n = s.n;
     sort_list(s, n);
     return n;

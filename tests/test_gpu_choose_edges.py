@@ -142,3 +142,37 @@ def test_lists_keep_their_bits(T, v, dtype):
                     x = (r.z[i][r.on[i]] - r.z[i][r.on[i]].max()) / float(np.float32(t)) / np.log(2)
                     lost = np.sum(np.where(x < 0, 2.0 ** x * (1 + 3 / 2 * np.log(2) * -x) * 2.0 ** -23, 0.0)) / np.sum(2.0 ** x)
                 assert all(close(a, b) or abs(a - b) <= lost + 2.0 ** -39 + abs(b) * 2.0 ** -23 for a, b in zip(lp[i].cpu().numpy(), want_lp)), (i, k, lp[i], want_lp)
+
+
+def draw_long(z, allow, u, temperature, top_k=0, top_p=1.0):
+    """draw_ref.draw with sums of 64-bit mantissas: one by one, 2^22 weights of 2^-41 beside one of 1 are off by 2^-31 of it with 53."""
+    temperature, top_p, u = (float(np.float32(x)) for x in (temperature, top_p, u))
+    ids, x = R.ordered(z, allow)
+    w = R.weights(x, temperature).astype(np.longdouble)
+    w = w[:R.kept(x, w, top_k, top_p, 0.0)]
+    upto = np.cumsum(w)
+    total, last = upto[-1], int(np.flatnonzero(w)[-1])
+    lo, hi = (min(int(np.searchsorted(upto, np.longdouble(u) * total + e * total, side="right")), last) for e in (-R.BORDER, R.BORDER))
+    return {int(ids[i]): float(np.log(w[i] / total)) for i in range(lo, hi + 1)}
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("v", [131077, (1 << 22) + 3])
+def test_many_tokens_of_next_to_no_weight(T, v, dtype):
+    """Tokens that weigh less than a rounding of the largest's weight each, but more than 2^-40 of the whole together: numbers next to 1 draw them."""
+    n = 12
+    each = -32.1 if v < 1 << 20 else -28.2                      # their weights are 2^-46.3 and 2^-40.7
+    z = np.full((n, v), 400.0 + 10.0 * np.floor(each * 5) / 5)
+    z[np.arange(n), np.arange(n) * 977] = 400.0
+    z[:, 5::1001] = 400.0 - 620.0
+    r = Given(T, z, None, dtype)
+    u = np.float32(1.0 - 2.0 ** -np.linspace(18, 24, n))
+    u[:2] = 1.0
+    tokens, lp = torch.empty(n, dtype=torch.int32, device="cuda"), torch.empty(n, device="cuda")
+    for s in (dict(), dict(top_k=v - 7), dict(top_p=1.0 - 2.0 ** -24)):
+        T.draw_step(None, r.logits, None, torch.from_numpy(u).cuda(), tokens, None, temperature=10.0, logprobs=lp, **s)
+        for i in range(n):
+            want = draw_long(r.z[i], r.on[i], u[i], 10.0, **s)
+            assert int(tokens[i]) in want, (i, s, u[i], tokens[i], want)
+            assert close(float(lp[i]), want[int(tokens[i])]), (i, s, lp[i], want)
+    check_top(T, r, 3, 10.0)
