@@ -338,6 +338,15 @@ template <int NT>
 __device__ __forceinline__ void slot_numbers(const DistillArgs& a, Shared<NT>& s)
 {
     if (threadIdx.x >= 64) return;
+    if (s.again) {
+        // Which of a token's slots came first is chance: the first of them owns it, so that sums over owners have one order.
+        each_slot(a, s, [&](int j) {
+            uint32_t owner = 1;
+            for (int o = 0; o < j; ++o)
+                if (s.named[o] == s.named[j]) owner = 0;
+            s.place[j] = (s.place[j] & ~1u) | owner;
+        });
+    }
     const double inv_t = uniform(1.0 / (double)a.temperature), top = (double)top_slot(s);
     float best = -INFINITY;
     if (!a.tail) each_slot(a, s, [&](int j) { best = fmaxf(best, s.given[j]); });

@@ -57,3 +57,21 @@ def test_nan_alone_in_a_part(T, v, dtype, tail):
             assert (g[i, at[i]] == 0).all(), (i, g[i, at[i]])
             # two terms of at most 1 / temperature each, off by 2^-18 of themselves, and a rounding
             assert (np.abs(g[i] - want) <= HALF[dtype] * np.abs(want) + 2.0 ** -18 * 2 / 0.9).all(), i
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("v", [3001, 33001])
+def test_repeated_tokens_always_give_the_same(T, v, dtype):
+    """Slots of one token far from one another, of a student that is its teacher: what is left of the loss is the sums' last bits, and shows the order in which they are made."""
+    n, k = 30, 256
+    rng = np.random.default_rng([v, 4])
+    z = rng.normal(0, 2, (n, v))
+    r = Given(T, z, None, dtype)
+    ids = np.stack([rng.permutation(np.concatenate([rng.choice(v, 64, replace=False)] * 4)) for _ in range(n)]).astype(np.int32)
+    lp = r.z - np.log(np.exp(r.z).sum(1, keepdims=True))
+    values = (np.take_along_axis(lp, ids.astype(np.int64), 1) - np.log(4.0)).astype(np.float32)
+    for tail in (False, True):
+        first = run(T, r, ids, values, None, 1.0, tail)
+        for _ in range(20):
+            again = run(T, r, ids, values, None, 1.0, tail)
+            assert first[0] == again[0] and np.array_equal(first[1], again[1]) and np.array_equal(first[2], again[2])
