@@ -70,7 +70,7 @@ struct Shared : Names {
     double far[kSlots], teacher[kSlots];       // exponentials relative to the largest of them, the teacher's probabilities
     struct { double part, mass, dot, low; } early;      // the sums of both, of q (ln q - ln of the exponential), and the lowest ln of one
     float top[kSlots / 64];    // the largest live logits
-    float factor;
+    double factor;
     int again, active;
     uint2 masks[16];
 };
@@ -193,10 +193,12 @@ __device__ __forceinline__ float join_running(float& m, float sum, const Exponen
 
 // What a row's gradients are made of: those of the tail are factor exp((z - ref) c).
 struct Slope {
-    float factor, ref;
+    float factor, log;         // log2 of |factor|, which may be beyond binary32
+    float ref;
     bool careful;              // there is a NaN among the tail's logits, or something beyond the reach of binary32
 };
-// 16 bits: |factor| in the exponent, which saves a product and a difference for each element and is off by 2^-14 or so of itself, beside a
+// 16 bits: |factor| is in the exponent.  The largest of the tail may lie far above ref, and a factor that binary32 does not hold be that of gradients
+// that it does.  Without the difference from ref as well it saves a product and a difference for each element and is off by 2^-14 or so of itself, beside a
 // rounding by up to 2^-8.
 struct Fold {
     float at;                  // NaN: not to be taken
@@ -205,13 +207,15 @@ struct Fold {
 __device__ __forceinline__ Fold fold_of(const Slope& q, const Exponent& c)
 {
     const float nb = -(q.ref * c.hi);
-    const bool folds = !q.careful && fabsf(nb) < 1024.0f && q.factor != 0.0f;
-    return {shared_by_wave(folds ? nb + __builtin_amdgcn_logf(fabsf(q.factor)) : __uint_as_float(0x7FC00000u)), q.factor < 0.0f ? 0x80008000u : 0u};
+    const bool folds = !q.careful && fabsf(nb) < 1024.0f;
+    return {shared_by_wave(folds ? nb + q.log : __uint_as_float(0x7FC00000u)), __float_as_uint(q.factor) >> 31 ? 0x80008000u : 0u};
 }
 template <int DTYPE>
 __device__ __forceinline__ float gradient_of(float z, const Slope& q, const Exponent& c)
 {
-    return q.factor * c.of((q.careful ? fmaxf(z, -INFINITY) : z) - q.ref);
+    const float x = (q.careful ? fmaxf(z, -INFINITY) : z) - q.ref;
+    if constexpr (DTYPE == TDFA_BF16) return copysignf(__builtin_amdgcn_exp2f(fmaf(x, c.hi, fmaf(x, c.lo, q.log))), q.factor);
+    return q.factor * c.of(x);
 }
 // y in place of element j of a group.
 template <int DTYPE>
@@ -421,7 +425,7 @@ __device__ __forceinline__ void row_numbers(const DistillArgs& a, uint32_t i, fl
         if (threadIdx.x == 0) {
             a.losses[i] = (float)loss;
             a.work[i] = (double)weight * loss;
-            s.factor = tail ? (float)(scale * (mass * exp(down) / total - rest / sum)) : 0.0f;
+            s.factor = tail ? scale * (mass * exp(down) / total - rest / sum) : 0.0;
         }
         wave_lds_sync();
         const bool again = s.again;
@@ -533,7 +537,9 @@ __global__ void __launch_bounds__(NT, 4) distill_row_kernel(DistillArgs a)
     row_numbers<NT>(a, i, h.weight, ref, whole, s);
     if (!a.grad) return;
     some = __builtin_amdgcn_readfirstlane(some);
-    const Slope q = {shared_by_wave(s.factor), shared_by_wave(ref), careful};
+    const double factor = s.factor;
+    const Slope q = {shared_by_wave((float)factor), shared_by_wave(__builtin_amdgcn_logf((float)fabs(__builtin_amdgcn_frexp_mant(factor))) + (float)__builtin_amdgcn_frexp_exp(factor)),
+                     shared_by_wave(ref), careful};
     const Fold f = fold_of(q, c);
 #pragma unroll
     for (int k = 0; k < R; ++k) {
@@ -542,8 +548,9 @@ __global__ void __launch_bounds__(NT, 4) distill_row_kernel(DistillArgs a)
         next_group();
     }
     if (behind < a.n_tokens) {
+        // (read again, not kept in a register in between)
         const uint32_t place = place_behind();
-        store_rounded(out + behind, place != kNone ? s.value[place] : gradient_of<DTYPE>(last, q, c));
+        store_rounded(out + behind, place != kNone ? s.value[place] : gradient_of<DTYPE>(last_element<DTYPE>(a.n_tokens, row, h.bits, -1), q, c));
     }
 }
 
@@ -668,7 +675,7 @@ __global__ void __launch_bounds__(256) distill_numbers_kernel(NumbersArgs a)
         const uint32_t id = s.named[threadIdx.x];
         a.named[(uint64_t)i * a.k + threadIdx.x] = make_uint2(id, id != kNone ? __float_as_uint(s.value[s.place[threadIdx.x] >> 1]) : 0u);
     }
-    if (threadIdx.x == 0) a.slopes[i] = make_float4(active ? s.factor : 0.0f, ref, careful ? 1.0f : 0.0f, active ? 1.0f : 0.0f);
+    if (threadIdx.x == 0) a.slopes[i] = make_float4(active ? (float)s.factor : 0.0f, ref, careful ? 1.0f : 0.0f, active ? 1.0f : 0.0f);
 }
 
 // Gradients of NT U groups of a row, the last part with the elements behind the whole groups.  Bound by the memory: the same rows 58 us, 307 MB
@@ -710,7 +717,7 @@ __global__ void __launch_bounds__(NT) distill_grad_kernel(PartGradArgs a)
     }
     __syncthreads();
     const Exponent c(a.temperature);
-    const Slope q = {shared_by_wave(v.x), shared_by_wave(v.y), __builtin_amdgcn_readfirstlane(v.z != 0.0f) != 0};
+    const Slope q = {shared_by_wave(v.x), shared_by_wave(__builtin_amdgcn_logf(fabsf(v.x))), shared_by_wave(v.y), __builtin_amdgcn_readfirstlane(v.z != 0.0f) != 0};
     const Fold f = fold_of(q, c);
 #pragma unroll
     for (int k = 0; k < U; ++k) {

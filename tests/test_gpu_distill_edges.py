@@ -75,3 +75,29 @@ def test_repeated_tokens_always_give_the_same(T, v, dtype):
         for _ in range(20):
             again = run(T, r, ids, values, None, 1.0, tail)
             assert first[0] == again[0] and np.array_equal(first[1], again[1]) and np.array_equal(first[2], again[2])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("temperature,near", [(1.0, 0.0), (1.0, -30.0), (0.02, 21.0)])
+@pytest.mark.parametrize("v", [3001, 9001, 33001])
+def test_small_weights_of_unlikely_lists(T, v, temperature, near, dtype):
+    """A student that finds the listed tokens e^-50 times as likely as others, in a row of little weight: the gradients are small, and there."""
+    n = 6
+    rng = np.random.default_rng([v, 8])
+    z = near + rng.normal(0, 2, (n, v)) * temperature
+    ids = np.stack([rng.choice(v, 5, replace=False) for _ in range(n)]).astype(np.int32)
+    for i in range(n):
+        z[i, ids[i]] = near + temperature * (2.0 * rng.random(5) - 58.0)
+    r = Given(T, z, None, dtype)
+    values = np.log(np.tile(np.float32([0.3, 0.1, 0.05, 0.03, 0.02]), (n, 1)))
+    weights = np.float32(10.0) ** np.float32([-8, -11, -13, -15, -20, -28])
+    for tail in (False, True):
+        _, losses, g = run(T, r, ids, values, weights, temperature, tail)
+        for i in range(n):
+            l, want = R.row(r.z[i], r.on[i], ids[i], values[i], temperature, tail)
+            assert abs(losses[i] - l) <= 2.0 ** -18 + abs(l) * 2.0 ** -23
+            w = float(weights[i])
+            x = np.exp((r.z[i] - r.z[i].max()) / float(np.float32(temperature)))
+            size = np.abs(want) + 2.0 / temperature * x / x.sum()               # (the tail holds nearly all of it)
+            bad = np.abs(g[i] - w * want) > w * (HALF[dtype] * np.abs(want) + 2.0 ** -18 * size) + 2.0 ** -126
+            assert not bad.any(), (i, tail, np.flatnonzero(bad)[:4], g[i][bad][:4], (w * want)[bad][:4])
