@@ -578,7 +578,8 @@ def draw_step(table: Table | None, logits: torch.Tensor, states: torch.Tensor | 
     vectors = (_vector(params, "params", torch.float32, 4 * rows, dev, True), _vector(tokens, "tokens", torch.int32, rows, dev),
                _vector(new_states, "new_states", torch.int32, rows, dev, table is None), _vector(logprobs, "logprobs", torch.float32, rows, dev, True))
     ws, n, _held = _workspace_of(lib().tdfa_select_workspace_bytes(rows, a[4]), workspace, logits, stream)
-    _check(lib().tdfa_draw_step(*a, _vector(uniforms, "uniforms", torch.float32, rows, dev), float(temperature), int(top_k), float(top_p),
+    top_k = max(-1, min(int(top_k), 2 ** 31 - 1))               # (any number of tokens and more is no cut; ctypes would take it modulo 2^32)
+    _check(lib().tdfa_draw_step(*a, _vector(uniforms, "uniforms", torch.float32, rows, dev), float(temperature), top_k, float(top_p),
                                 float(min_p), *vectors, ws, n, _stream(stream)))
 
 

@@ -176,3 +176,17 @@ def test_many_tokens_of_next_to_no_weight(T, v, dtype):
             assert int(tokens[i]) in want, (i, s, u[i], tokens[i], want)
             assert close(float(lp[i]), want[int(tokens[i])]), (i, s, lp[i], want)
     check_top(T, r, 3, 10.0)
+
+
+def test_top_k_of_any_size(T):
+    """A top_k beyond 32 bits cuts nothing off, and below 0 it is refused, whatever it is modulo 2^32."""
+    r = Rows(T, "open", 30, 3001, "f32", 91, table=None)
+    u = torch.from_numpy(r.uniforms()).cuda()
+    want, got = torch.empty(30, dtype=torch.int32, device="cuda"), torch.empty(30, dtype=torch.int32, device="cuda")
+    T.draw_step(None, r.logits, None, u, want, None)
+    for k in (3001, 2 ** 31 - 1, 2 ** 31, 2 ** 32 + 1, 2 ** 63 + 2, 10 ** 30):
+        T.draw_step(None, r.logits, None, u, got, None, top_k=k)
+        assert torch.equal(got, want), k
+    for k in (-1, -2 ** 31, 1 - 2 ** 32, -2 ** 32, -10 ** 30):
+        with pytest.raises(T.TdfaError):
+            T.draw_step(None, r.logits, None, u, got, None, top_k=k)
