@@ -1229,7 +1229,7 @@ __device__ __forceinline__ uint32_t top_of_steps(Shared<TDFA_F32, NT>& s, Held<T
     lds_barrier();
     const uint32_t last = s.at[0];
     if (last >= kSteps - 1) return 0;
-    n = list_of<TDFA_F32, NT, R, BITS>(s, row, [&](uint4 x) { return step(max_group<TDFA_F32>(x, -INFINITY)) <= last; },
+    n = list_of<TDFA_F32, NT, R, BITS>(s, row, [&](uint4 x) { return step(fminf(max_group<TDFA_F32>(x, -INFINITY), top)) <= last; },     // (or above, if it is not allowed)
                                       [&](int32_t, float z) { return step(z) <= last; });
     return n > kList<TDFA_F32> ? 0u : n;
 }

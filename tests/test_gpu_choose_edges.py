@@ -190,3 +190,19 @@ def test_top_k_of_any_size(T):
     for k in (-1, -2 ** 31, 1 - 2 ** 32, -2 ** 32, -10 ** 30):
         with pytest.raises(T.TdfaError):
             T.draw_step(None, r.logits, None, u, got, None, top_k=k)
+
+
+@pytest.mark.parametrize("beside", [2.0, 3.0e38, np.inf])
+def test_lists_beside_larger_logits_that_are_not_allowed(T, beside):
+    """The first tokens have a larger logit each in its group of 16 bytes that the constraint does not allow: its distance below the largest is no step."""
+    n, v = 6, 9004
+    rng = np.random.default_rng(12)
+    z = rng.normal(-3, 1, (n, v))
+    on = rng.random((n, v)) < 0.6
+    for i in range(n):
+        at = rng.choice(v // 4, 40, replace=False) * 4 + rng.integers(0, 4, 40)
+        z[i, at], on[i, at] = 1.0 - np.arange(40) / 64, True
+        z[i, at ^ 1], on[i, at ^ 1] = beside, False
+    r = Given(T, z, on, "f32")
+    for k in (1, 40, 200):
+        check_top(T, r, k)
