@@ -206,3 +206,48 @@ def test_lists_beside_larger_logits_that_are_not_allowed(T, beside):
     r = Given(T, z, on, "f32")
     for k in (1, 40, 200):
         check_top(T, r, k)
+
+
+@pytest.mark.parametrize("table", [None, "owned"])
+@pytest.mark.parametrize("dtype,v,rows", [("bf16", 66001, 800), ("bf16", 131081, 770), ("f32", 17003, 470), ("f32", 33003, 470), ("f32", 70001, 470)])
+def test_many_long_rows(T, dtype, v, rows, table):
+    """Shapes of launches that many rows take, with a constraint and without one: a row gives the same wherever it lies, what the definition says."""
+    r = Rows(T, "peaked", 5, v, dtype, 92, table=table)
+    rep = -(-rows // 5)
+    x, q = r.x.repeat(rep, 1)[:rows], None if table is None else r.states.repeat(rep)[:rows].contiguous()
+    u = torch.from_numpy(r.uniforms()).cuda()
+    t, lp, ids, top = (torch.empty(s, dtype=d, device="cuda") for s, d in ((rows, torch.int32), (rows, torch.float32), ((rows, 33), torch.int32), ((rows, 33), torch.float32)))
+    after = None if table is None else torch.empty_like(t)
+    for s in (dict(temperature=0.8, top_p=0.9), dict(top_k=900, min_p=0.001), dict(temperature=0.0)):
+        T.draw_step(r.table, x[:, :v], q, u.repeat(rep)[:rows].contiguous(), t, after, logprobs=lp, **s)
+        for i in range(5):
+            want = R.draw(r.z[i], r.on[i], float(u[i]), s.get("temperature", 1.0), s.get("top_k", 0), s.get("top_p", 1.0), s.get("min_p", 0.0))
+            assert int(t[i]) in want and close(float(lp[i]), want[int(t[i])]), (i, s)
+            assert after is None or int(after[i]) == r.after(int(t[i]), i), (i, s)
+        for a in (t, lp, after):
+            assert a is None or torch.equal(a, a[:5].repeat(rep)[:rows])
+    T.top_logprobs(r.table, x[:, :v], q, ids, top)
+    assert torch.equal(ids, ids[:5].repeat(rep, 1)[:rows]) and torch.equal(top, top[:5].repeat(rep, 1)[:rows])
+    check_top(T, r, 33)
+    for i in range(5):
+        assert np.array_equal(ids[i].cpu().numpy(), R.top(r.z[i], r.on[i], 33, 1.0)[0])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_more_rows_than_a_launch(T, dtype):
+    n, v = (1 << 21) + 77, 9
+    x = torch.randn((n, 16), generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").to(TYPES[dtype])
+    u = torch.rand(n, generator=torch.Generator(device="cuda").manual_seed(2), device="cuda")
+    t, lp = torch.empty(n, dtype=torch.int32, device="cuda"), torch.empty(n, device="cuda")
+    ids, top = torch.empty((n, 2), dtype=torch.int32, device="cuda"), torch.empty((n, 2), device="cuda")
+    T.draw_step(None, x[:, :v], None, u, t, None, logprobs=lp)
+    T.top_logprobs(None, x[:, :v], None, ids, top)
+    want = torch.log_softmax(x[:, :v].double(), 1)
+    # a rounding, and 2^-20 for weights of 32 bits
+    assert (lp - want.gather(1, t.long()[:, None])[:, 0]).abs().max() <= 2.0 ** -19
+    value, order = torch.sort(x[:, :v].float(), dim=1, descending=True, stable=True)
+    assert torch.equal(ids.long(), order[:, :2]) and (top - want.gather(1, order[:, :2])).abs().max() <= 2.0 ** -19
+    upto = torch.cumsum(want.gather(1, order).exp(), 1)
+    at = (order == t.long()[:, None]).to(torch.int8).argmax(1, keepdim=True)
+    last, before = upto.gather(1, at)[:, 0], torch.where(at > 0, upto.gather(1, (at - 1).clamp(min=0)), 0.0)[:, 0]
+    assert ((before - 2.0 ** -39 <= u) & (u <= last + 2.0 ** -39)).all()

@@ -101,3 +101,27 @@ def test_small_weights_of_unlikely_lists(T, v, temperature, near, dtype):
             size = np.abs(want) + 2.0 / temperature * x / x.sum()               # (the tail holds nearly all of it)
             bad = np.abs(g[i] - w * want) > w * (HALF[dtype] * np.abs(want) + 2.0 ** -18 * size) + 2.0 ** -126
             assert not bad.any(), (i, tail, np.flatnonzero(bad)[:4], g[i][bad][:4], (w * want)[bad][:4])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_more_rows_than_a_launch(T, dtype):
+    """One value of d loss / d logits and of the loss for every row of 2^21 and some."""
+    n, v, k = (1 << 21) + 77, 9, 2
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.randn((n, 16), generator=g, device="cuda").to(torch.bfloat16 if dtype == "bf16" else torch.float32)
+    ids = torch.randint(0, v, (n, k), generator=g, device="cuda", dtype=torch.int32)
+    ids[:, 1] = (ids[:, 0] + 1 + ids[:, 1] % (v - 1)) % v
+    values = torch.log(torch.rand((n, k), generator=g, device="cuda") * 0.5)
+    loss, losses, grad = torch.empty(1, device="cuda"), torch.empty(n, device="cuda"), torch.full_like(x, 7.0)
+    T.distill_loss(None, x[:, :v], None, ids, values, loss, losses, grad_logits=grad[:, :v], tail=True)
+    lp, q = torch.log_softmax(x[:, :v].double(), 1), values.double().exp()
+    rest = 1.0 - q.sum(1)
+    named = torch.zeros_like(lp).scatter_(1, ids.long(), 1.0)
+    p_tail = (lp.exp() * (1.0 - named)).sum(1)
+    each = (q * (values.double() - lp.gather(1, ids.long()))).sum(1) + torch.xlogy(rest, rest) - rest * p_tail.log()
+    want = lp.exp() - torch.zeros_like(lp).scatter_(1, ids.long(), q) - (1.0 - named) * lp.exp() * (rest / p_tail)[:, None]
+    # as in the other tests of the loss: 2^-18 of the sums and of the gradients' terms, below 2 each, and roundings
+    assert ((losses - each).abs() <= 2.0 ** -18 + each.abs() * 2.0 ** -23).all()
+    assert abs(float(loss) - float(each.sum())) <= n * 2.0 ** -18 + float(each.sum()) * 2.0 ** -23
+    assert ((grad[:, :v].double() - want).abs() <= HALF[dtype] * want.abs() + 2.0 ** -18 * 2).all()
+    assert (grad[:, v:] == 7.0).all()
