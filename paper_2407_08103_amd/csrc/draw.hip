@@ -314,7 +314,7 @@ __device__ __forceinline__ void sort_list(Shared<DTYPE, NT>& s, uint32_t n)
     lds_barrier();
 }
 
-// cum[i] = weights of sorted[0 .. i] added up, n of them.  By one wavefront.
+// cum[i] = weights of sorted[0 .. i] added up, n of them; it never falls, and does not rise at a token that weighs nothing.  By one wavefront.
 template <int DTYPE, int NT>
 __device__ __forceinline__ void sum_list(Shared<DTYPE, NT>& s, uint32_t n, float m, double inv_t)
 {
@@ -324,8 +324,8 @@ __device__ __forceinline__ void sum_list(Shared<DTYPE, NT>& s, uint32_t n, float
         mine += weight_of(logit_of((uint32_t)(s.sorted[i] >> 32)), m, inv_t);
         s.cum[i] = mine;
     }
-    const double before = wave_before(wave_upto(mine));
-    for (uint32_t i = from; i < to; ++i) s.cum[i] += before;
+    const double end = wave_borders(mine), before = wave_before(end);
+    for (uint32_t i = from; i < to; ++i) s.cum[i] = s.cum[i] == mine ? end : fmin(before + s.cum[i], end);
     wave_lds_sync();
 }
 

@@ -251,3 +251,19 @@ def test_more_rows_than_a_launch(T, dtype):
     at = (order == t.long()[:, None]).to(torch.int8).argmax(1, keepdim=True)
     last, before = upto.gather(1, at)[:, 0], torch.where(at > 0, upto.gather(1, (at - 1).clamp(min=0)), 0.0)[:, 0]
     assert ((before - 2.0 ** -39 <= u) & (u <= last + 2.0 ** -39)).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("v", [30, 89, 201, 256, 3001])
+def test_tokens_of_no_weight_are_not_drawn(T, v, dtype):
+    """Many logits so low that their weights are 0 in 64 bits: the number 1 draws the last token that has one."""
+    n = 150
+    rng = np.random.default_rng([v, 9])
+    z = rng.normal(0, 3, (n, v))
+    z[rng.random((n, v)) < 0.5] = -1.0e4
+    z[:, 1] = 2.0
+    on = None if v <= 256 else (rng.random((n, v)) < 200 / v) | (np.arange(v) == 1)
+    r = Given(T, z, on, dtype)
+    for temperature in (0.7, 0.5, 1.3):
+        for u in (1.0, 1.0 - 2.0 ** -24):
+            check_draw(T, r, np.full(n, u, dtype=np.float32), temperature=temperature)
