@@ -110,10 +110,18 @@ __device__ __forceinline__ double wave_borders(double v)
 template <typename V>
 __device__ __forceinline__ V wave_before(V upto) { return lanes_below<0x138, 0xF>(upto); }       // wave_shr 1
 
+// A product that is rounded by itself.  A cut and the draw add up the same weights and have to find the same sums: as part of a fused product and sum, in one
+// of them and not in the other, the draw with 1 went past the cut.
+__device__ __forceinline__ double product(double x, double y)
+{
+#pragma clang fp contract(off)
+    return x * y;
+}
+
 // The weight of a logit beside the largest, m, which is above -inf.
 __device__ __forceinline__ double weight_of(float z, float m, double inv_t)
 {
-    return z == m ? 1.0 : z > -INFINITY ? exp(((double)z - (double)m) * inv_t) : 0.0;
+    return z == m ? 1.0 : z > -INFINITY ? exp(product((double)z - (double)m, inv_t)) : 0.0;
 }
 
 // A row and its allowed bits.
@@ -764,7 +772,7 @@ __device__ __forceinline__ bool count_row(Shared<TDFA_BF16, NT>& s, Held<TDFA_BF
         }
         each_bin<NT>(s, b, c.m, inv_t, [&](uint32_t, uint32_t tokens, double weight) {
             n += tokens;
-            w += (double)tokens * weight;
+            w += product((double)tokens, weight);
         });
     }
     static_cast<Sums&>(c) = sums_of<NT>(s, n, w);
@@ -865,7 +873,7 @@ __device__ __forceinline__ Drawn draw_of_counts(Shared<TDFA_BF16, NT>& s, Held<T
             uint32_t n = c.n_before;
             double sum = c.before;
             each_bin<NT>(s, b, c.m, q.inv_t(), [&](uint32_t, uint32_t tokens, double w) {
-                if (n < q.top_k) sum += (double)tokens * w;
+                if (n < q.top_k) sum += product((double)tokens, w);
                 n += tokens;
             });
             s.mass[0] = fmin(sum, c.upto);                 // (which is the next thread's beginning, however it has been rounded)
@@ -881,14 +889,14 @@ __device__ __forceinline__ Drawn draw_of_counts(Shared<TDFA_BF16, NT>& s, Held<T
         if (q.top_p() < 1.0 && c.before < enough && enough <= c.upto) {
             double sum = c.before;
             each_bin<NT>(s, b, c.m, q.inv_t(), [&](uint32_t, uint32_t tokens, double w) {
-                if (sum < enough) sum += (double)tokens * w;
+                if (sum < enough) sum += product((double)tokens, w);
             });
             s.mass[1] = fmin(sum, c.upto);
         }
         if (q.min_p() > 0.0) {
             double sum = c.before, least = 0.0;
             each_bin<NT>(s, b, c.m, q.inv_t(), [&](uint32_t, uint32_t tokens, double w) {
-                sum += (double)tokens * w;
+                sum += product((double)tokens, w);
                 if (w >= q.min_p()) least = sum;
             });
             if (least > 0.0) atomicMax(&s.least, (u64)__double_as_longlong(fmin(least, c.upto)));
@@ -909,7 +917,7 @@ __device__ __forceinline__ Drawn draw_of_counts(Shared<TDFA_BF16, NT>& s, Held<T
                 before = sum;
                 w_at = w;
             }
-            sum += (double)tokens * w;
+            sum += product((double)tokens, w);
         });
         s.at[0] = at;
         s.at[1] = (uint32_t)fmin(fmax((target - before) / w_at, 0.0), (double)(tokens_at - 1));
@@ -998,7 +1006,7 @@ struct Steps {
 
 // (A thread has kSteps / NT steps that lie together.)
 template <int NT>
-__device__ __forceinline__ double step_weight(const Shared<TDFA_F32, NT>& s, uint32_t i, double unit) { return (double)s.step.weight[i] * unit; }
+__device__ __forceinline__ double step_weight(const Shared<TDFA_F32, NT>& s, uint32_t i, double unit) { return product((double)s.step.weight[i], unit); }
 
 // Puts the tokens of a row in steps, and adds up.  An LDS atomic of 64 bits for each token, and one of 32 where a cut by number needs counts.
 template <int NT, int R, bool BITS>
@@ -1084,8 +1092,8 @@ __device__ __forceinline__ bool draw_of_steps(Shared<TDFA_F32, NT>& s, Held<TDFA
         const uint32_t k = key(i);
         return first_where(n, [&](uint32_t j) { return key(j) < k; });
     };
-    // Weights up to the first `stay` of a step's n tokens; where that is all of them, up to where the next step begins, however that has been rounded.
-    const auto upto = [&](uint32_t n, uint32_t stay, double end) { return stay == n ? fmin(s.cum[n - 1], end) : s.cum[stay - 1]; };
+    // Weights up to the first `stay` of a step's tokens, no more than up to where the next step begins, however that has been rounded.
+    const auto upto = [&](uint32_t stay, double end) { return fmin(s.cum[stay - 1], end); };
     if (q.top_k) {
         if (c.n_before < q.top_k && q.top_k <= c.n_upto) {
             uint32_t n = c.n_before;
@@ -1107,7 +1115,7 @@ __device__ __forceinline__ bool draw_of_steps(Shared<TDFA_F32, NT>& s, Held<TDFA
         if (i < kSteps - 1) {                              // (a cut in the last step leaves all that weighs anything)
             const uint32_t n = look(i, base);
             if (!n) return false;
-            kept = fmin(kept, upto(n, behind(n, min(nth, n) - 1), s.end[0]));
+            kept = fmin(kept, upto(behind(n, min(nth, n) - 1), s.end[0]));
         }
     }
     double cut = kept;
@@ -1129,7 +1137,7 @@ __device__ __forceinline__ bool draw_of_steps(Shared<TDFA_F32, NT>& s, Held<TDFA
         const double base = s.mass[1];
         const uint32_t n = i < kSteps ? look(i, base) : 0u;
         if (!n) return false;
-        cut = fmin(cut, upto(n, behind(n, min(n - 1, first_where(n, [&](uint32_t j) { return s.cum[j] >= enough; }))), s.end[1]));
+        cut = fmin(cut, upto(behind(n, min(n - 1, first_where(n, [&](uint32_t j) { return s.cum[j] >= enough; }))), s.end[1]));
     }
     // what weighs at least min_p ends in the step of its logarithm
     if (const uint32_t i = q.min_p() > 0.0 ? (uint32_t)fmin(fmax(-log(q.min_p()), 0.0) * kPerUnit, (double)(kSteps - 1)) : kSteps - 1; i < kSteps - 1) {
@@ -1137,7 +1145,7 @@ __device__ __forceinline__ bool draw_of_steps(Shared<TDFA_F32, NT>& s, Held<TDFA
             double sum = c.before;
             each_step<NT>(s, n_tokens, [&](uint32_t j, uint32_t, double w) {
                 if (j == i) {
-                    s.mass[2] = sum;
+                    s.mass[2] = fmin(sum, c.upto);         // (as the next thread's steps begin)
                     s.end[2] = fmin(sum + w, c.upto);
                 }
                 sum += w;
@@ -1154,7 +1162,7 @@ __device__ __forceinline__ bool draw_of_steps(Shared<TDFA_F32, NT>& s, Held<TDFA
         }
         lds_barrier();
         const uint32_t stay = first_where(n, [&](uint32_t j) { return weight_of(logit_of(key(j)), m, inv_t) < q.min_p(); });
-        cut = fmin(cut, stay ? upto(n, stay, s.end[2]) : base);
+        cut = fmin(cut, stay ? upto(stay, s.end[2]) : base);
     }
     kept = fmin(kept, cut);
     const double target = fmin(q.u() * kept, __longlong_as_double(__double_as_longlong(kept) - 1));

@@ -267,3 +267,22 @@ def test_tokens_of_no_weight_are_not_drawn(T, v, dtype):
     for temperature in (0.7, 0.5, 1.3):
         for u in (1.0, 1.0 - 2.0 ** -24):
             check_draw(T, r, np.full(n, u, dtype=np.float32), temperature=temperature)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("v", [200, 2873, 9001])
+@pytest.mark.parametrize("kind", ["open", "grid", "upcast"])
+def test_the_last_token_of_what_is_left(T, kind, v, dtype):
+    """The number 1 draws the last token that the cuts leave, and none behind it, however the sums up to there were rounded."""
+    n = 60
+    rng = np.random.default_rng([v, 10])
+    z = rng.normal(0, 3, (n, v))
+    if kind == "grid":
+        z = np.round(z * 16) / 16
+    elif kind == "upcast":
+        z = torch.from_numpy(z).bfloat16().double().numpy()
+    r = Given(T, z, None, dtype)
+    u = np.float32([1.0, 1.0, 1.0 - 2.0 ** -24] * (n // 3))
+    for s in (dict(temperature=2.0, top_k=v // 2, min_p=0.05), dict(temperature=5.0, top_k=v // 3, top_p=0.95), dict(temperature=5.0, top_k=v // 3, top_p=0.9),
+              dict(temperature=0.9, top_p=0.8), dict(top_p=0.9, min_p=0.01), dict(temperature=1.5, top_k=50, top_p=0.97, min_p=0.02), dict(min_p=0.3), dict(top_k=20)):
+        check_draw(T, r, u, **s)
