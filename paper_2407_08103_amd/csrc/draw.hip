@@ -1272,7 +1272,7 @@ __device__ __forceinline__ StateOf state_of(const SelectArgs& a, uint32_t i)
 // sums.  What bounds it: one row, its chain of phases on one compute unit (bf16, 128,256 tokens, no constraint: 19 us, of which 9 to 12 until all
 // tokens are counted, 4 for weights and their sums, 3 for the token among those of its logit); many rows, LDS atomics, one for each token, eight
 // to a group of 16 bytes: 1,000 such rows 84 to 88 us, 2.9 to 3.1 TB/s.  fp32, 300 rows of 32,003 with three cuts: 53 to 55 us, 6 for the largest logit, 13 for
-// the steps, 4 to 6 for each of up to four steps that are put in order.  (Thresholds digit by digit instead, nine looks at a row or more: 470, 2,110 and 389 us.)
+// the steps, 4 to 6 for each of up to four steps that are put in order.  (Thresholds digit by digit instead, ten looks at a row or more: 434, 1,900 and 373 us.)
 template <int DTYPE, int NT, int R, bool BITS>
 __global__ void __launch_bounds__(NT, NT > 256 ? 4 : DTYPE == TDFA_F32 ? 2 : 3) draw_step_kernel(DrawArgs a)
 {
@@ -1380,7 +1380,7 @@ __device__ __forceinline__ uint32_t top_of_counts(Shared<TDFA_BF16, NT>& s, Held
 
 // One workgroup per row: the k first tokens in order, and their log-probabilities.  The same counts or steps give the logit that k tokens reach; those
 // that do are put in order.  Bounds as for a draw: one row of 128,256 tokens in bf16 19 us, 2,048 rows under a constraint 130 to 136 (212 MB of groups with an
-// allowed token, 292 MB read), 500 fp32 rows of 32,000 with 200 tokens listed 36.  (By digits: 221, 1,315 and 145 us.)
+// allowed token, 292 MB read), 500 fp32 rows of 32,000 with 200 tokens listed 37.  (By digits: 195, 1,290 and 190 us.)
 template <int DTYPE, int NT, int R, bool BITS>
 __global__ void __launch_bounds__(NT, NT > 256 ? 4 : DTYPE == TDFA_F32 ? 2 : 3) top_logprobs_kernel(TopArgs a)
 {
